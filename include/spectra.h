@@ -301,6 +301,121 @@ spectra_status spectra_decode_step_static(const spectra_codec* ck, const spectra
                                           int32_t n_kv_heads, float softmax_scale, float* out, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Paged caches: the records of many sequences in pools of pages under one page map.
+ *
+ * A pool holds one layer's and tensor's records: n_pages pages of page_tokens slots (a
+ * multiple of 64), each page the records of those slots for every KV head in turn, in the
+ * tiles of the file header:
+ *   pool[(((page*H + kv)*(page_tokens/64) + tile)*W + w)*64 + slot%64], H = KV heads.
+ * The codec of a pool has one stream per KV head, shared by all sequences (a basis fitted
+ * once, e.g. by spectra_fit_weights). One map serves any number of pools (all layers).
+ *
+ * The map lives on the device, so that serving loops need no synchronisation and can be
+ * captured in graphs. Row r is a sequence: lens[r] slots, in the pages table[r][0 ..
+ * ceil(lens[r] / page_tokens)); what the table holds beyond is ignored (the calls below leave
+ * -1 where they drop a page). refs[p] counts the table entries, of any row, that name page p
+ * (a caller that holds on to a page in another way adds to it); 0 means free. An empty map is
+ * lens and refs 0. A map's calls run in stream order; two of them, or one and an append, must
+ * not overlap on one map.
+ *
+ * The lists of a call (rows, parents, children, counts, keep: int32, at most 1024 entries) and
+ * its results are device arrays. What they hold is checked on the device: an entry that cannot
+ * be served gets -1 and changes nothing, and no list, table, length or count can make a call
+ * touch memory outside the map and the pools.
+ * ------------------------------------------------------------------------- */
+typedef struct {
+  int64_t n_pages;     /* pages of every pool, < 2^31 - 1 */
+  int32_t page_tokens; /* slots of a page, a multiple of 64 */
+  int32_t rows;        /* sequences, <= 65535 */
+  int32_t row_pages;   /* entries of a table row; row_pages * page_tokens < 2^31 */
+  int32_t reserved;
+  int32_t* table;      /* device [rows][row_pages] */
+  int32_t* lens;       /* device [rows] */
+  int32_t* refs;       /* device [n_pages]; unused by append and attention */
+} spectra_pages;
+
+typedef struct {
+  uint32_t* base;     /* device, 16-byte aligned */
+  int64_t page_words; /* words of a page: page_tokens * KV heads * W, for any geometry's records */
+} spectra_pool;
+
+/* Words of a pool for the codec's records (n_pages * page_tokens * n_streams * W). Host only. */
+int64_t spectra_paged_pool_words(const spectra_pages* m, const spectra_codec* c);
+
+/* Workspace of pages_extend and pages_compact (device, 256-byte aligned). Host only. */
+size_t spectra_pages_workspace_bytes(const spectra_pages* m);
+
+/* Room for counts[i] more tokens in row rows[i]: new pages where the row's own do not reach
+ * (the lowest free ones, in list order), and, where the last page is partly filled and has other
+ * owners, a copy of it in every pool in its place (the last owner keeps the page). lens[rows[i]]
+ * grows by counts[i] and ends[i] is the new length. ends[i] = -1 and nothing changed: a row out
+ * of range or listed before, a negative count, more slots than the row has; and, from the first
+ * entry for which too few pages are free, every entry that needs a page or shares its last page
+ * with an entry before it. Asynchronous. */
+spectra_status spectra_pages_extend(const spectra_pages* m, const int32_t* rows, const int32_t* counts, int32_t n,
+                                    const spectra_pool* pools, int32_t n_pools, int32_t* ends, void* workspace,
+                                    size_t ws_bytes, void* stream);
+
+/* Row children[i] becomes a copy of row parents[i] that shares its pages; ends[i] is its length.
+ * ends[i] = -1 and nothing changed: a row out of range, a child that is not empty, is listed
+ * before, or a parent that is listed as a child. No records are copied: pages_extend does that
+ * before a shared page is written. Asynchronous. */
+spectra_status spectra_pages_fork(const spectra_pages* m, const int32_t* parents, const int32_t* children, int32_t n,
+                                  int32_t* ends, void* stream);
+
+/* Row rows[i] keeps its first keep[i] slots (none with keep NULL or negative; all where it has no
+ * more): the pages behind them leave the row, and are free once no row holds them. A row listed
+ * again keeps the fewest listed. Rows out of range are passed over. Asynchronous. */
+spectra_status spectra_pages_truncate(const spectra_pages* m, const int32_t* rows, const int32_t* keep, int32_t n,
+                                      void* stream);
+
+/* The used pages move to the front of every pool: with U of them, the k-th used page at or past
+ * U takes the place of the k-th free page before U, in the pools, the table and the counts.
+ * moved (device, n_pages + 1): every page's place afterwards, then U. Asynchronous. */
+spectra_status spectra_pages_compact(const spectra_pages* m, const spectra_pool* pools, int32_t n_pools,
+                                     int32_t* moved, void* workspace, size_t ws_bytes, void* stream);
+
+/* Encode of the new tokens of `batch` sequences into their pages. Sequence b is map row rows[b]
+ * (row b with rows NULL) and has ends[b] slots (lens of its row with ends NULL), its new tokens
+ * included; those are rows cu_new[b] .. cu_new[b + 1] of k and v (cu_new: device, batch + 1
+ * entries that do not fall, cut to [0, n_new]) and go to its last slots. k[t*k_token_stride +
+ * kv*k_head_stride + c], v alike, kv < n_streams of the codecs, strides multiples of 16 bytes.
+ * The records are those of spectra_encode for the same rows. Written are only those slots, so
+ * pages must not be shared there (spectra_pages_extend). Not written: tokens before slot 0 (a
+ * sequence with ends[b] = -1 gets none), and those whose page is out of range. Asynchronous. */
+spectra_status spectra_paged_encode(const spectra_pages* m, const spectra_codec* ck, const spectra_codec* cv,
+                                    uint32_t* pool_k, uint32_t* pool_v, const int32_t* rows, const int32_t* ends,
+                                    const int32_t* cu_new, int32_t batch, int64_t n_new, const void* k,
+                                    int64_t k_token_stride, int64_t k_head_stride, const void* v, int64_t v_token_stride,
+                                    int64_t v_head_stride, spectra_dtype dt, void* stream);
+
+/* Causal attention of the new tokens over their sequences' pages, in the latent space (App. E).
+ * Sequences, ends and cu_new as in spectra_paged_encode; q[t*q_token_stride + h*q_head_stride + c],
+ * query head h reads KV head h / (n_q_heads / n_streams), at most 16 query heads each. New token i
+ * of the n of a sequence with L slots sees slots t <= L - n + i:
+ *   out[t][h] = sum_t' softmax_t'(scale q . k_hat_t') v_hat_t'      (contiguous, dtype out_dt),
+ *   lse[t][h] = ln sum_t' exp(scale q . k_hat_t')   (fp32, or NULL), for merging with attention
+ * over other tokens. A token that sees no slot gets zeros and -inf. Rows of no sequence are left
+ * as they were; so are those of sequences with more than max_new new tokens or max_tokens slots
+ * (the call's bounds, by which the work is split). Slots past a sequence's end are never read
+ * into a result; a page out of range counts as a page of zero records; in records, NaN or
+ * infinite metadata counts as 0 (such tokens' codes are unspecified anyway).
+ * out_dt fp32: the error is that of fp32 sums (about 1e-6 of the result). bf16: operands are
+ * rounded to fp16, which stays below the output's rounding; lse is then good to about 1e-3.
+ * Coefficients are held in fp16 parts: those beyond 65504 are taken as 65504, and of those below
+ * 2^-14 absolute errors of 2^-25 remain. softmax_scale <= 0 selects 1/sqrt(128). Workspace:
+ * device, spectra_paged_attention_workspace_bytes, 256-byte aligned. Asynchronous. */
+size_t spectra_paged_attention_workspace_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv_heads,
+                                               int32_t max_new, int64_t max_tokens);
+spectra_status spectra_paged_attention(const spectra_pages* m, const spectra_codec* ck, const spectra_codec* cv,
+                                       const uint32_t* pool_k, const uint32_t* pool_v, const int32_t* rows,
+                                       const int32_t* ends, const int32_t* cu_new, int32_t batch, int64_t n_new,
+                                       int32_t max_new, int64_t max_tokens, const void* q, spectra_dtype q_dt,
+                                       int64_t q_token_stride, int64_t q_head_stride, int32_t n_q_heads,
+                                       float softmax_scale, void* out, spectra_dtype out_dt, float* lse,
+                                       void* workspace, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Host-side pieces of the fit, exported so they can be checked without a GPU.
  * ------------------------------------------------------------------------- */
 

@@ -15,3 +15,8 @@ from .codec import (  # noqa: F401
     spectra_split_budget, spectra_unpack_codes, spectra_layer_attention_workspace_bytes,
     spectra_layer_decode_attention,
 )
+from .paged import (  # noqa: F401
+    PagedCache,
+    spectra_paged_attention, spectra_paged_attention_workspace_bytes, spectra_paged_encode, spectra_pages_compact,
+    spectra_pages_extend, spectra_pages_fork, spectra_pages_truncate, spectra_pages_workspace_bytes,
+)

@@ -33,10 +33,22 @@ class spectra_codec(ctypes.Structure):
                 ("var", ctypes.c_void_p), ("bits", ctypes.c_void_p), ("lscale", ctypes.c_void_p)]
 
 
+class spectra_pages(ctypes.Structure):
+    _fields_ = [("n_pages", ctypes.c_int64), ("page_tokens", ctypes.c_int32), ("rows", ctypes.c_int32),
+                ("row_pages", ctypes.c_int32), ("reserved", ctypes.c_int32), ("table", ctypes.c_void_p),
+                ("lens", ctypes.c_void_p), ("refs", ctypes.c_void_p)]
+
+
+class spectra_pool(ctypes.Structure):
+    _fields_ = [("base", ctypes.c_void_p), ("page_words", ctypes.c_int64)]
+
+
 _P = ctypes.c_void_p
 _I32, _I64, _F32, _SZ = ctypes.c_int32, ctypes.c_int64, ctypes.c_float, ctypes.c_size_t
 _PP = ctypes.POINTER(spectra_params)
 _PC = ctypes.POINTER(spectra_codec)
+_PM = ctypes.POINTER(spectra_pages)
+_PL = ctypes.POINTER(spectra_pool)
 
 _SIGNATURES = {
     "spectra_codec_init": (_I32, [_PC, _PP, _I64]),
@@ -62,6 +74,17 @@ _SIGNATURES = {
                                    _P, _P, _SZ, _P]),
     "spectra_decode_step_static": (_I32, [_PC, _PC, _P, _P, _I64, _I64, _P, _P, _I32, _P, _I32, _I32, _I32, _I32,
                                           _F32, _P, _P]),
+    "spectra_paged_pool_words": (_I64, [_PM, _PC]),
+    "spectra_pages_workspace_bytes": (_SZ, [_PM]),
+    "spectra_pages_extend": (_I32, [_PM, _P, _P, _I32, _PL, _I32, _P, _P, _SZ, _P]),
+    "spectra_pages_fork": (_I32, [_PM, _P, _P, _I32, _P, _P]),
+    "spectra_pages_truncate": (_I32, [_PM, _P, _P, _I32, _P]),
+    "spectra_pages_compact": (_I32, [_PM, _PL, _I32, _P, _P, _SZ, _P]),
+    "spectra_paged_encode": (_I32, [_PM, _PC, _PC, _P, _P, _P, _P, _P, _I32, _I64, _P, _I64, _I64, _P, _I64, _I64,
+                                    _I32, _P]),
+    "spectra_paged_attention_workspace_bytes": (_SZ, [_I32, _I64, _I32, _I32, _I32, _I64]),
+    "spectra_paged_attention": (_I32, [_PM, _PC, _PC, _P, _P, _P, _P, _P, _I32, _I64, _I32, _I64, _P, _I32, _I64, _I64,
+                                       _I32, _F32, _P, _I32, _P, _P, _SZ, _P]),
     "spectra_allocate_bits": (_I32, [_P, _PP, _P]),
     "spectra_eigh_host": (_I32, [_P, _I32, _P, _P]),
     "spectra_fit_from_moments_host": (_I32, [_PP, _I64, _P, _P, _P, _P, _P, _P]),

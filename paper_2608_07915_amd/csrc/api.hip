@@ -7,6 +7,7 @@
 #include <thread>
 #include <vector>
 
+#include "api_common.hpp"
 #include "host_common.hpp"
 #include "kernels.hpp"
 #include "splits.hpp"
@@ -23,33 +24,6 @@ namespace {
 
 constexpr int kD = 128;
 constexpr int64_t kMoments = (int64_t)kD * kD + kD;  // gram + column sums per stream
-
-spectra_status hip_fail(hipError_t e, const char* what) {
-  return fail(SPECTRA_EHIP, "%s: %s", what, hipGetErrorString(e));
-}
-
-bool aligned(const void* p, size_t a) { return ((uintptr_t)p % a) == 0; }
-
-spectra_status check_codec(const spectra_codec* c, const char* name, bool layer_ok = false) {
-  if (!c) return fail(SPECTRA_EINVAL, "%s: null codec", name);
-  spectra_status st = check_params_gpu(c->p);
-  if (st != SPECTRA_OK) return st;
-  if (!layer_ok && layer_geometry(c->p))
-    return fail(SPECTRA_EUNSUPPORTED, "%s: the per-layer geometry (head_dim %d, group_size 64) supports fit, encode and decode only",
-                name, c->p.head_dim);
-  if (c->record_words != record_words(c->p))
-    return fail(SPECTRA_EINVAL, "%s: record_words %d does not match the parameters (%d); call spectra_codec_init",
-                name, c->record_words, record_words(c->p));
-  if (c->n_streams <= 0 || c->n_streams > 65535)
-    return fail(SPECTRA_EINVAL, "%s: n_streams=%lld out of range [1, 65535]", name, (long long)c->n_streams);
-  if (!c->basis || !c->mean || !c->var || !c->bits) return fail(SPECTRA_EINVAL, "%s: null codec array", name);
-  if (c->lscale && !layer_geometry(c->p))
-    return fail(SPECTRA_EUNSUPPORTED, "%s: the square-root latent split (lscale) runs in the per-layer geometry only", name);
-  if (c->lscale && !aligned(c->lscale, 4)) return fail(SPECTRA_EINVAL, "%s: lscale must be 4-byte aligned", name);
-  if (!aligned(c->basis, 16) || !aligned(c->mean, 4) || !aligned(c->var, 4) || !aligned(c->bits, 4))
-    return fail(SPECTRA_EINVAL, "%s: basis must be 16-byte aligned, the other codec arrays 4-byte aligned", name);
-  return SPECTRA_OK;
-}
 
 spectra_status check_slots(int64_t t0, int64_t n, int64_t t_cap) {
   if (t_cap <= 0 || t_cap % 64 != 0) return fail(SPECTRA_EINVAL, "t_capacity=%lld must be a positive multiple of 64", (long long)t_cap);
@@ -70,8 +44,6 @@ spectra_status check_input(const void* x, spectra_dtype dt, int64_t stream_strid
   if (n_streams > 1 && stream_stride == 0) return fail(SPECTRA_EINVAL, "stream_stride is 0 for several streams");
   return SPECTRA_OK;
 }
-
-size_t round256(size_t b) { return (b + 255) / 256 * 256; }
 
 void moments_layout(int64_t n_streams, int64_t n_tokens, int32_t* n_chunks, int64_t* chunk_tokens) {
   int64_t want = (1024 + n_streams - 1) / n_streams;

@@ -14,7 +14,8 @@ typedef __attribute__((__vector_size__(8 * sizeof(_Float16)))) _Float16 f16x8;
 // serve both; OR-ing in the exponent of 1024 and subtracting 1024 + 2^(B-1) (both
 // exact) gives the two as fp16 integers centered on 0. About 1.6 instructions per code
 // against 2.5 for single extraction and conversion. Element 2i + e of codes_f16(k) is code
-// 4k + i + 16e: the other operand of a product is laid out to match.
+// 4k + i + 16e: the other operand of a product is laid out to match. CENTERED = false
+// subtracts 1024 alone: the codes themselves.
 // ---------------------------------------------------------------------------
 template <int B>
 __device__ __forceinline__ void join_halves(const uint32_t (&w)[8], uint32_t (&Z)[8]) {
@@ -24,10 +25,10 @@ __device__ __forceinline__ void join_halves(const uint32_t (&w)[8], uint32_t (&Z
     Z[i] = __builtin_amdgcn_perm(w[(i + B) >> 1], w[i >> 1], sel);
   }
 }
-template <int B>
+template <int B, bool CENTERED = true>
 __device__ __forceinline__ f16x8 codes_f16(const uint32_t (&Z)[8], int k, uint32_t magic) {
   constexpr uint32_t M = (1u << B) - 1u, MM = M | (M << 16);
-  const _Float16 off = (_Float16)(1024.0f + (float)(1 << (B - 1)));
+  const _Float16 off = (_Float16)(1024.0f + (CENTERED ? (float)(1 << (B - 1)) : 0.0f));
   u32x4 r;
 #pragma unroll
   for (int i = 0; i < 4; ++i) {

@@ -1,0 +1,539 @@
+// Attention of new tokens over the pages of a packed cache, in the latent space (App. E).
+//
+//   row (i, h) of a sequence: new token i of n, query head h; it sees slots t <= L - n + i
+//   q'  = scale * log2(e) * q V_K
+//   S   = q' . c_hat_K(t)                     (the constant q' . m_K cancels in the softmax)
+//   p   = exp2(S - m), l = sum p, a = sum p c_hat_V(t)   in one pass, m the running maximum
+//   out = (a / l + m_V) V_V^T
+//
+// A workgroup takes 256 rows of one KV head (new tokens x query heads on it), a wavefront 32.
+// Products are transposed, slots or coefficients as MFMA rows and the query rows as columns, so
+// a lane keeps one query row from q to the output and every product's result registers are the
+// next product's column operand as they stand: nothing of q', p or a passes through LDS, and
+// the softmax needs one exchange between the halves of a wavefront. Which K index of a product
+// stands for which coefficient or slot is free as long as both operands agree.
+//
+// Records are turned into fp16 coefficients once per workgroup: a lane holds one slot's words of
+// a kept group, makes z + s code by packed fp16 multiply-adds (z, s and code are exact in fp16,
+// so this rounds once) and writes the 32 values as four 16-byte pieces into LDS. Keys and values
+// have one layout, [group][slot][32 places], pieces XOR-swizzled by the slot so that 16-byte
+// reads of 16 neighbouring slots fall on distinct banks; values are read transposed
+// (ds_read_b64_tr_b16: four slots of a coefficient per lane).
+//
+// With 16-bit outputs the operands are single fp16 numbers (p between 2^-26 and 8 of the
+// running maximum in the normal range). With fp32 outputs q', p and the coefficients are two
+// fp16 parts each and a product is three (relative error about 2^-21).
+#include "attn_common.hpp"
+#include "code_operands.hpp"
+#include "encode_dev.hpp"
+#include "paged_dev.hpp"
+
+namespace spectra_dev {
+
+constexpr int CA_NW = 8;               // wavefronts of a workgroup
+constexpr int CA_ROWS = 32 * CA_NW;    // query rows of a workgroup
+constexpr int CA_TILE = TILE * 64;     // bytes of a slot tile: 64 slots x 32 fp16
+constexpr float CA_SLACK = 3.0f;       // log2: the running maximum moves when passed by more
+constexpr float CA_LIFT = 12.0f;       // log2: weights are kept 2^12 above their share
+constexpr float LN2 = 0.69314718055994531f;
+constexpr float CA_LO = 2048.0f;       // the second fp16 part of a number is scaled by 2^11
+
+// LDS byte of 16-byte piece `piece` of slot `t` in a slot tile.
+__device__ __forceinline__ int piece_at(int t, int piece) { return t * 64 + ((piece ^ ((t >> 2) & 3)) << 4); }
+
+// A token's metadata word of a b-bit group, made finite: NaN or infinite scales count as 0, and
+// the scale is lowered where z + s (2^b - 1) would pass fp16's largest number.
+__device__ __forceinline__ uint32_t finite_meta(uint32_t m, int b) {
+  if ((m & 0x7C00u) == 0x7C00u || (m & 0x7C000000u) == 0x7C000000u) return 0u;
+  const float s = h2f(m), z = h2f(m >> 16), top = (float)((1 << b) - 1);
+  if (__builtin_fabsf(__builtin_fmaf(s, top, z)) > 65504.0f)
+    m = (m & 0xFFFF0000u) | f2h_sat((__builtin_copysignf(65472.0f, s) - z) / top);
+  return m;
+}
+
+// One slot's group as fp16 coefficients z + s code into its LDS row (parts: the low parts'
+// tiles are `lo` bytes further).
+template <int B, bool PRECISE>
+__device__ __forceinline__ void write_coefficients(const uint32_t (&w)[8], uint32_t meta, uint8_t* tile, int t, int lo,
+                                                   uint32_t magic) {
+  uint32_t Z[8];
+  join_halves<B>(w, Z);
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const f16x8 c = codes_f16<B, false>(Z, k, magic);
+    const _Float16 s = __builtin_bit_cast(_Float16, (uint16_t)meta), z = __builtin_bit_cast(_Float16, (uint16_t)(meta >> 16));
+    if constexpr (!PRECISE) {
+      u32x4 r;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        r[i] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(f16x2{s, s}, f16x2{c[2 * i], c[2 * i + 1]}, f16x2{z, z}));
+      *reinterpret_cast<u32x4*>(tile + piece_at(t, k)) = r;
+    } else {
+      u32x4 rh, rl;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const f32x2 x = f32x2{__builtin_fmaf((float)s, (float)c[2 * i], (float)z), __builtin_fmaf((float)s, (float)c[2 * i + 1], (float)z)};
+        const f16x2 hi = __builtin_convertvector(x, f16x2);
+        const f32x2 d = f32x2{(x[0] - (float)hi[0]) * CA_LO, (x[1] - (float)hi[1]) * CA_LO};
+        rh[i] = __builtin_bit_cast(uint32_t, hi);
+        rl[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(d, f16x2));
+      }
+      *reinterpret_cast<u32x4*>(tile + piece_at(t, k)) = rh;
+      *reinterpret_cast<u32x4*>(tile + lo + piece_at(t, k)) = rl;
+    }
+  }
+}
+
+typedef short s16x4 __attribute__((ext_vector_type(4)));
+typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
+__device__ __forceinline__ u32x2 read_transposed(const uint8_t* p) {
+  return __builtin_bit_cast(u32x2, __builtin_amdgcn_ds_read_tr16_b64_v4i16((lds_s16x4*)p));
+}
+__device__ __forceinline__ f16x8 as_f16x8(u32x4 v) { return __builtin_bit_cast(f16x8, v); }
+__device__ __forceinline__ f32x16 mfma_f16(f16x8 a, f16x8 b, f32x16 c) {
+  return __builtin_amdgcn_mfma_f32_32x32x16_f16(a, b, c, 0, 0, 0);
+}
+__device__ __forceinline__ f32x16 zero16() {
+  f32x16 z;
+#pragma unroll
+  for (int i = 0; i < 16; ++i) z[i] = 0.0f;
+  return z;
+}
+// Eight fp32 numbers as NP bf16 parts.
+template <int NP>
+__device__ __forceinline__ void split8(const float (&v)[8], bf16x8 (&p)[NP]) {
+  uint32_t a[NP][8];
+#pragma unroll
+  for (int i = 0; i < 8; ++i) {
+    float r = v[i];
+#pragma unroll
+    for (int q = 0; q < NP; ++q) {
+      a[q][i] = f2bf(r);
+      r -= bf2f(a[q][i]);
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < NP; ++q)
+    p[q] = as_bf16x8(u32x4{pack2(a[q][0], a[q][1]), pack2(a[q][2], a[q][3]), pack2(a[q][4], a[q][5]), pack2(a[q][6], a[q][7])});
+}
+
+__device__ __forceinline__ float query_at(const PagedAttnArgs& a, int64_t i) {
+  return a.q_f32 ? reinterpret_cast<const float*>(a.q)[i] : bf2f(reinterpret_cast<const uint16_t*>(a.q)[i]);
+}
+
+// Which sequence a unit of R rows belongs to: sequence b has ceil(n_b n_qh / R) of them. The
+// same in every thread; false when there is none. s: LDS. Sequences past the call's bounds
+// have none: their rows are left as they were.
+__device__ __forceinline__ bool attended(const PagedAttnArgs& a, const PagedSeq& q) {
+  return q.n <= a.max_new && q.len <= a.max_tokens;
+}
+struct FindScratch {
+  int64_t part[CA_NW];
+  int64_t total;
+  int32_t b, tile;
+};
+__device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int R, int64_t unit, FindScratch& s, int& b, int64_t& tile) {
+  const PagedCache& c = a.c;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  if (tid == 0) s.b = -1;
+  int64_t base = 0;
+  for (int b0 = 0; b0 < c.batch; b0 += 64 * CA_NW) {
+    int64_t mine = 0;
+    if (b0 + tid < c.batch) {
+      const PagedSeq q = paged_seq(c, b0 + tid);
+      if (attended(a, q)) mine = (q.n * a.n_qh + R - 1) / R;
+    }
+    int64_t v = mine;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t u = __shfl_up(v, o);
+      if (lane >= o) v += u;
+    }
+    __syncthreads();
+    if (lane == 63) s.part[wave] = v;
+    __syncthreads();
+    int64_t before = base;
+    for (int w = 0; w < wave; ++w) before += s.part[w];
+    const int64_t lo = before + v - mine;
+    if (unit >= lo && unit < lo + mine) {
+      s.b = b0 + tid;
+      s.tile = (int32_t)(unit - lo);
+    }
+    if (tid == 64 * CA_NW - 1) s.total = before + v;
+    __syncthreads();
+    if (s.b >= 0) break;
+    base = s.total;
+  }
+  b = __builtin_amdgcn_readfirstlane(s.b);
+  tile = __builtin_amdgcn_readfirstlane(s.tile);
+  return b >= 0;
+}
+
+template <bool PRECISE>
+__global__ __launch_bounds__(64 * CA_NW, 2) void paged_chunk_kernel(PagedAttnArgs a) {
+  constexpr int KT = PRECISE ? 1 : 2;       // slot tiles of a step
+  constexpr int UNITS = KT * 2 * NG / CA_NW;  // group tiles that a wavefront unpacks in a step
+  constexpr int NP = PRECISE ? 3 : 2;       // bf16 parts of the bases (and of fp32 queries)
+  extern __shared__ __attribute__((aligned(16))) uint8_t tiles[];
+  __shared__ FindScratch find_s;
+  const int kv = (int)(blockIdx.x % (unsigned)a.c.n_kv);
+  const int tid = threadIdx.x, lane = tid & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const int h = lane >> 5, col = lane & 31;
+  int b;
+  int64_t tile;
+  if (!find_unit(a, CA_ROWS, blockIdx.x / (unsigned)a.c.n_kv, find_s, b, tile)) return;
+  const PagedSeq seq = paged_seq(a.c, b);
+  const int n_rows = (int)(seq.n * a.n_qh);
+  const int row0 = (int)tile * CA_ROWS + 32 * wave;
+  // rows past the sequence's last compute that row again and store nothing
+  const int row = row0 + col, rowc = row < n_rows ? row : n_rows - 1;
+  const int tok = rowc / a.n_qh, head = kv * a.n_qh + (rowc - tok * a.n_qh);
+  const int past = (int)(seq.len - seq.n) + 1;  // slots that row (0, .) sees
+  auto limit_of = [&](int r) {
+    const int l = past + (r < n_rows ? r : n_rows - 1) / a.n_qh;
+    return l < 0 ? 0 : l;
+  };
+  const int lim = past + tok < 0 ? 0 : past + tok;
+  const int lim_first = __builtin_amdgcn_readfirstlane(limit_of(row0)), lim_last = __builtin_amdgcn_readfirstlane(limit_of(row0 + 31));
+  const int lim_wg = __builtin_amdgcn_readfirstlane(limit_of((int)tile * CA_ROWS + CA_ROWS - 1));
+
+  Kept Kk = read_kept(a.bits_k + kv * NG), Kv = read_kept(a.bits_v + kv * NG);
+  if (!Kk.ok || Kk.used > a.Wk) Kk.n = 0;  // width table inconsistent with the record
+  if (!Kv.ok || Kv.used > a.Wv) Kv.n = 0;
+  const int ns = Kk.n + Kv.n;
+  const int lo_off = KT * ns * CA_TILE;  // the low parts' tiles
+
+  // ---- q' as column operands: element e of piece 2s + h of slot sl is the lane's row's q' of
+  // code 4 (2s + h) + e / 2 + 16 (e % 2), scaled by 2^E into [2^8, 2^9) ----
+  f16x8 qb[NG][2], ql[PRECISE ? NG : 1][2];
+  float unscale;
+  {
+    const int64_t qoff = (seq.first + tok) * a.q_token_stride + head * a.q_head_stride + 8 * h;
+    f32x16 acc[NG];
+    float most = 0.0f;
+    const int i = 4 * (col >> 3) + (col & 3), hh = (col >> 2) & 1;  // MFMA row col is register i of lane half hh
+    const int code = 4 * (2 * (i >> 3) + hh) + ((i & 7) >> 1) + 16 * (i & 1);
+#pragma unroll
+    for (int sl = 0; sl < NG; ++sl) {
+      acc[sl] = zero16();
+      if (sl >= Kk.n) continue;
+      const float* V = a.basis_k + (int64_t)kv * D * D + (8 * h) * D + G * Kk.grp[sl] + code;
+#pragma unroll 1
+      for (int k = 0; k < 8; ++k) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = V[(16 * k + e) * D];
+        bf16x8 vp[NP];
+        split8<NP>(v, vp);
+        if (a.q_f32) {
+          const f32x4* qp = reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.q) + qoff + 16 * k);
+          const f32x4 q0 = qp[0], q1 = qp[1];
+          const float qv[8] = {q0[0], q0[1], q0[2], q0[3], q1[0], q1[1], q1[2], q1[3]};
+          bf16x8 qq[NP];
+          split8<NP>(qv, qq);
+#pragma unroll
+          for (int x = 0; x < NP; ++x)
+#pragma unroll
+            for (int y = 0; x + y < NP; ++y)
+              acc[sl] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vp[x], qq[y], acc[sl], 0, 0, 0);
+        } else {
+          const bf16x8 qq = as_bf16x8(*reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.q) + qoff + 16 * k));
+#pragma unroll
+          for (int x = 0; x < NP; ++x) acc[sl] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vp[x], qq, acc[sl], 0, 0, 0);
+        }
+      }
+#pragma unroll
+      for (int j = 0; j < 16; ++j) {
+        acc[sl][j] *= a.scale_log2;
+        most = __builtin_fmaxf(most, __builtin_fabsf(acc[sl][j]));
+      }
+    }
+    most = __builtin_fmaxf(most, other_half(most));
+    const int E = 9 - scale_exponent(most);
+    unscale = __builtin_ldexpf(1.0f, -E);
+    const float up = __builtin_ldexpf(1.0f, E);
+#pragma unroll
+    for (int sl = 0; sl < NG; ++sl)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        u32x4 rh, rl;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x2 x = f32x2{acc[sl][8 * s + 2 * j] * up, acc[sl][8 * s + 2 * j + 1] * up};
+          const f16x2 hi = __builtin_convertvector(x, f16x2);
+          rh[j] = __builtin_bit_cast(uint32_t, hi);
+          if constexpr (PRECISE)
+            rl[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
+                                                     f32x2{(x[0] - (float)hi[0]) * CA_LO, (x[1] - (float)hi[1]) * CA_LO}, f16x2));
+        }
+        qb[sl][s] = as_f16x8(rh);
+        if constexpr (PRECISE) ql[sl][s] = as_f16x8(rl);
+      }
+  }
+
+  // ---- the wavefront's group tiles of a step: words in registers one step ahead ----
+  uint32_t words[UNITS][8], meta[UNITS];
+  auto load_step = [&](int j) {
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+      const int unit = wave + CA_NW * u;
+      meta[u] = 0u;
+#pragma unroll
+      for (int i = 0; i < 8; ++i) words[u][i] = 0u;
+      if (unit >= KT * ns) continue;
+      const int tl = unit >= ns ? 1 : 0, si = unit - tl * ns, jt = j * KT + tl;
+      if (jt * TILE >= lim_wg) continue;
+      const bool val = si >= Kk.n;
+      const int sl = val ? si - Kk.n : si;
+      const int bits = val ? pick4(Kv.bits, sl) : pick4(Kk.bits, sl), pay = val ? pick4(Kv.pay, sl) : pick4(Kk.pay, sl);
+      const uint32_t* rec = paged_tile(a.c, val ? a.pool_v : a.pool_k, val ? a.Wv : a.Wk, seq.row, jt, kv);
+      if (!rec) continue;  // a page outside the pool: zeros
+      rec += lane;
+      if (jt * TILE + lane < seq.len) meta[u] = finite_meta(rec[sl * TILE], bits);
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < bits) words[u][i] = rec[(pay + i) * TILE];
+    }
+  };
+  uint32_t magic = 0x64006400u;  // exponent of 1024 in both halves, in a VGPR
+  asm volatile("" : "+v"(magic));
+
+  f32x16 acc[NG];
+#pragma unroll
+  for (int sl = 0; sl < NG; ++sl) acc[sl] = zero16();
+  float m_run = -__builtin_inff(), l_run = 0.0f;
+  const int n_steps = (lim_wg + KT * TILE - 1) / (KT * TILE);
+  if (n_steps > 0) load_step(0);
+#pragma unroll 1
+  for (int j = 0; j < n_steps; ++j) {
+    __syncthreads();  // every wavefront is done with the last step's tiles
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+      const int unit = wave + CA_NW * u;
+      if (unit >= KT * ns) continue;
+      const int tl = unit >= ns ? 1 : 0, si = unit - tl * ns;
+      const int bits = si >= Kk.n ? pick4(Kv.bits, si - Kk.n) : pick4(Kk.bits, si);
+      with_bits(bits, [&](auto bc) {
+        write_coefficients<decltype(bc)::value, PRECISE>(words[u], meta[u], tiles + unit * CA_TILE, lane, lo_off, magic);
+      });
+    }
+    if (j + 1 < n_steps) load_step(j + 1);
+    __syncthreads();  // the step's tiles are in LDS
+    const int t0 = j * KT * TILE;
+    if (t0 >= lim_last) continue;
+    f32x16 S[2 * KT];
+#pragma unroll
+    for (int k = 0; k < 2 * KT; ++k) {
+      S[k] = zero16();
+      f32x16 lo = zero16();
+#pragma unroll
+      for (int sl = 0; sl < NG; ++sl) {
+        if (sl >= Kk.n) continue;
+#pragma unroll
+        for (int s = 0; s < 2; ++s) {
+          const uint8_t* p = tiles + ((k >> 1) * ns + sl) * CA_TILE + piece_at(32 * (k & 1) + col, 2 * s + h);
+          const f16x8 kh = as_f16x8(*reinterpret_cast<const u32x4*>(p));
+          S[k] = mfma_f16(kh, qb[sl][s], S[k]);
+          if constexpr (PRECISE) {
+            const f16x8 kl = as_f16x8(*reinterpret_cast<const u32x4*>(p + lo_off));
+            lo = mfma_f16(kh, ql[sl][s], lo);
+            lo = mfma_f16(kl, qb[sl][s], lo);
+          }
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < 16; ++i) {
+        if constexpr (PRECISE) S[k][i] = __builtin_fmaf(lo[i], 1.0f / CA_LO, S[k][i]);
+        S[k][i] *= unscale;
+      }
+    }
+    if (t0 + KT * TILE > lim_first) {  // some row of the wavefront does not see the whole step
+#pragma unroll
+      for (int k = 0; k < 2 * KT; ++k)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          const int t = t0 + 32 * k + 8 * (i >> 2) + 4 * h + (i & 3);
+          S[k][i] = t < lim ? S[k][i] : -__builtin_inff();
+        }
+    }
+    float top = S[0][0];
+#pragma unroll
+    for (int k = 0; k < 2 * KT; ++k)
+#pragma unroll
+      for (int i = 0; i < 16; ++i) top = __builtin_fmaxf(top, S[k][i]);
+    top = __builtin_fmaxf(top, other_half(top));
+    if (__any(top > m_run + CA_SLACK)) {
+      const float mn = __builtin_fmaxf(m_run, top);
+      const float f = m_run == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m_run - mn);
+      l_run *= f;
+#pragma unroll
+      for (int sl = 0; sl < NG; ++sl)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[sl][i] *= f;
+      m_run = mn;
+    }
+    const float ref = (m_run == -__builtin_inff() ? 0.0f : m_run) - CA_LIFT;
+    f32x16 lo[PRECISE ? NG : 1];
+    if constexpr (PRECISE) {
+#pragma unroll
+      for (int sl = 0; sl < NG; ++sl) lo[sl] = zero16();
+    }
+#pragma unroll
+    for (int k = 0; k < 2 * KT; ++k)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) {
+        u32x4 rh, rl;
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          const f32x2 p = f32x2{__builtin_amdgcn_exp2f(S[k][8 * s + 2 * i] - ref), __builtin_amdgcn_exp2f(S[k][8 * s + 2 * i + 1] - ref)};
+          l_run += p[0] + p[1];
+          const f16x2 hi = __builtin_convertvector(p, f16x2);
+          rh[i] = __builtin_bit_cast(uint32_t, hi);
+          if constexpr (PRECISE)
+            rl[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
+                                                     f32x2{(p[0] - (float)hi[0]) * CA_LO, (p[1] - (float)hi[1]) * CA_LO}, f16x2));
+        }
+        const f16x8 ph = as_f16x8(rh);
+        // value rows: slots 16 s + 4 h + (0..3) and 8 further, as p's registers have them
+        const int t = 32 * (k & 1) + 16 * s + 4 * h + ((lane & 15) >> 2);
+        const int piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
+#pragma unroll
+        for (int sl = 0; sl < NG; ++sl) {
+          if (sl >= Kv.n) continue;
+          const uint8_t* vt = tiles + ((k >> 1) * ns + Kk.n + sl) * CA_TILE + 8 * (lane & 1);
+          const u32x2 x0 = read_transposed(vt + piece_at(t, piece)), x1 = read_transposed(vt + piece_at(t + 8, piece));
+          const f16x8 vh = as_f16x8(u32x4{x0[0], x0[1], x1[0], x1[1]});
+          acc[sl] = mfma_f16(vh, ph, acc[sl]);
+          if constexpr (PRECISE) {
+            const u32x2 y0 = read_transposed(vt + lo_off + piece_at(t, piece)), y1 = read_transposed(vt + lo_off + piece_at(t + 8, piece));
+            lo[sl] = mfma_f16(as_f16x8(u32x4{y0[0], y0[1], y1[0], y1[1]}), ph, lo[sl]);
+            lo[sl] = mfma_f16(vh, as_f16x8(rl), lo[sl]);
+          }
+        }
+      }
+    if constexpr (PRECISE) {
+#pragma unroll
+      for (int sl = 0; sl < NG; ++sl)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[sl][i] = __builtin_fmaf(lo[sl][i], 1.0f / CA_LO, acc[sl][i]);
+    }
+  }
+
+  // ---- out = (a / l + m_V) V_V^T: the coefficients as column operand in bf16 parts ----
+  const float l = l_run + other_half(l_run);
+  const bool seen = l > 0.0f || !(l == l);
+  const float inv = 1.0f / l;
+  const float* Vv = a.basis_v + (int64_t)kv * D * D;
+  f32x16 out[4];
+#pragma unroll
+  for (int cb = 0; cb < 4; ++cb) out[cb] = zero16();
+  const int i0 = 4 * (col >> 3) + (col & 3), h0 = (col >> 2) & 1;
+  const int chan = 16 * h0 + i0;  // MFMA row col of a 32-channel block: then a lane half has 16 neighbouring channels
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    int sl = -1;
+#pragma unroll
+    for (int x = 0; x < NG; ++x) sl = (x < Kv.n && Kv.grp[x] == g) ? x : sl;
+    f32x16 av = zero16();
+#pragma unroll
+    for (int x = 0; x < NG; ++x)
+      if (x == sl) av = acc[x];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      float cf[8];
+      int at[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int place = 16 * s + 8 * (e >> 2) + 4 * h + (e & 3);  // of register 8 s + e
+        at[e] = G * g + 4 * (place >> 3) + ((place & 7) >> 1) + 16 * (place & 1);
+        cf[e] = (sl >= 0 ? av[8 * s + e] * inv : 0.0f) + a.mean_v[kv * D + at[e]];
+      }
+      bf16x8 cp[NP];
+      split8<NP>(cf, cp);
+#pragma unroll
+      for (int cb = 0; cb < 4; ++cb) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = Vv[(32 * cb + chan) * D + at[e]];
+        bf16x8 vp[NP];
+        split8<NP>(v, vp);
+#pragma unroll
+        for (int x = 0; x < NP; ++x)
+#pragma unroll
+          for (int y = 0; x + y < NP; ++y)
+            out[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vp[x], cp[y], out[cb], 0, 0, 0);
+      }
+    }
+  }
+  if (row >= n_rows) return;
+  const int64_t o = ((seq.first + tok) * a.n_q_heads + head) * D + 16 * h;
+#pragma unroll
+  for (int cb = 0; cb < 4; ++cb) {
+    if (a.out_f32) {
+      float* op = reinterpret_cast<float*>(a.out) + o + 32 * cb;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(op + 4 * i) = seen ? f32x4{out[cb][4 * i], out[cb][4 * i + 1], out[cb][4 * i + 2], out[cb][4 * i + 3]}
+                                                     : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    } else {
+      uint32_t* op = reinterpret_cast<uint32_t*>(reinterpret_cast<uint16_t*>(a.out) + o + 32 * cb);
+      uint32_t w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        w[i] = seen ? __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{out[cb][2 * i], out[cb][2 * i + 1]}, bf16x2)) : 0u;
+      *reinterpret_cast<u32x4*>(op) = u32x4{w[0], w[1], w[2], w[3]};
+      *reinterpret_cast<u32x4*>(op + 4) = u32x4{w[4], w[5], w[6], w[7]};
+    }
+  }
+  if (a.lse != nullptr && h == 0) {
+    const int64_t qo = (seq.first + tok) * a.q_token_stride + head * a.q_head_stride;
+    float s = 0.0f;
+    for (int c = 0; c < D; ++c) s = __builtin_fmaf(query_at(a, qo + c), a.lse_u[kv * D + c], s);
+    a.lse[(seq.first + tok) * a.n_q_heads + head] =
+        seen ? __builtin_fmaf(__builtin_amdgcn_logf(l) + (m_run - CA_LIFT), LN2, s) : -__builtin_inff();
+  }
+}
+
+// ---------------------------------------------------------------------------
+// u = scale V_K m_K of each KV head: q . u is the part of the log-sum-exp that the softmax does
+// not need.
+// ---------------------------------------------------------------------------
+__global__ __launch_bounds__(256) void paged_lse_kernel(PagedAttnArgs a) {
+  const int kv = blockIdx.x, ch = threadIdx.x >> 1, half = threadIdx.x & 1;
+  const float* v = a.basis_k + ((int64_t)kv * D + ch) * D + 64 * half;
+  const float* m = a.mean_k + kv * D + 64 * half;
+  float s = 0.0f;
+#pragma unroll 16
+  for (int j = 0; j < 64; ++j) s = __builtin_fmaf(v[j], m[j], s);
+  s += __shfl_xor(s, 1);
+  if (half == 0) a.lse_u[kv * D + ch] = s * (a.scale_log2 * LN2);
+}
+
+}  // namespace spectra_dev
+
+namespace spectra {
+using namespace spectra_dev;
+
+size_t paged_attention_ws_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv, int32_t max_new,
+                                int64_t max_tokens) {
+  return (size_t)n_kv * D * sizeof(float);
+}
+
+hipError_t launch_paged_attention(const PagedAttnArgs& args, void* workspace, hipStream_t st) {
+  PagedAttnArgs a = args;
+  a.lse_u = reinterpret_cast<float*>(workspace);
+  if (a.lse != nullptr) hipLaunchKernelGGL(paged_lse_kernel, dim3(a.c.n_kv), dim3(256), 0, st, a);
+  const int64_t per_seq = ((int64_t)a.max_new * a.n_qh + CA_ROWS - 1) / CA_ROWS;
+  int64_t units = a.c.n_new * a.n_qh / CA_ROWS + a.c.batch;
+  if (units > per_seq * a.c.batch) units = per_seq * a.c.batch;
+  const int groups = (a.Wk / 2 < NG ? a.Wk / 2 : NG) + (a.Wv / 2 < NG ? a.Wv / 2 : NG);  // a kept group takes two words
+  const dim3 grid((unsigned)(units * a.c.n_kv));
+  if (a.out_f32)
+    hipLaunchKernelGGL((paged_chunk_kernel<true>), grid, dim3(64 * CA_NW), 2 * groups * CA_TILE, st, a);
+  else
+    hipLaunchKernelGGL((paged_chunk_kernel<false>), grid, dim3(64 * CA_NW), 2 * groups * CA_TILE, st, a);
+  return hipGetLastError();
+}
+
+}  // namespace spectra
