@@ -226,7 +226,8 @@ spectra_status spectra_layer_decode_attention(const spectra_codec* ck, const spe
  * computed as q' = scale q V_K once, scores over the kept key coefficients
  * (the constant q' . m_K cancels in the softmax), value accumulation over the
  * kept value coefficients, then one inverse rotation (a + m_V) V_V^T.
- * softmax_scale <= 0 selects 1/sqrt(d). n_q_heads / n_kv_heads <= 16;
+ * softmax_scale <= 0 selects 1/sqrt(d). n_q_heads / n_kv_heads <= 16 (12 where keys' and
+ * values' min(W, 36) come to more than 67 words together: the tiles must fit the LDS);
  * t_capacity * record_words < 2^31 for both codecs.
  * Workspace: device, spectra_attention_workspace_bytes bytes (never fewer for more
  * tokens: one taken for the longest cache serves every shorter one). Asynchronous.
@@ -404,7 +405,8 @@ spectra_status spectra_paged_encode(const spectra_pages* m, const spectra_codec*
  * rounded to fp16, which stays below the output's rounding; lse is then good to about 1e-3.
  * Coefficients are held in fp16 parts: those beyond 65504 are taken as 65504, and of those below
  * 2^-14 absolute errors of 2^-25 remain. softmax_scale <= 0 selects 1/sqrt(128). Workspace:
- * device, spectra_paged_attention_workspace_bytes, 256-byte aligned. Asynchronous. */
+ * device, 256-byte aligned, spectra_paged_attention_workspace_bytes (never fewer for larger counts:
+ * one taken for the largest call serves every smaller one of as many heads). Asynchronous. */
 size_t spectra_paged_attention_workspace_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv_heads,
                                                int32_t max_new, int64_t max_tokens);
 spectra_status spectra_paged_attention(const spectra_pages* m, const spectra_codec* ck, const spectra_codec* cv,

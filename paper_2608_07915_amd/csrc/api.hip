@@ -401,6 +401,8 @@ static spectra_status prepare_attention(const char* name, const spectra_codec* c
   if (batch <= 0 || n_kv_heads <= 0 || n_q_heads <= 0 || n_q_heads % n_kv_heads != 0)
     return fail(SPECTRA_EINVAL, "%s: need batch > 0 and n_q_heads a positive multiple of n_kv_heads", name);
   if (n_q_heads / n_kv_heads > 16) return fail(SPECTRA_EUNSUPPORTED, "%s: more than 16 query heads per kv head", name);
+  if (n_q_heads / n_kv_heads > scan_rows(ck->record_words, cv->record_words))
+    return fail(SPECTRA_EUNSUPPORTED, "%s: more than 12 query heads per kv head with records this wide", name);
   if (batch > 65535 || n_kv_heads > 65535) return fail(SPECTRA_EINVAL, "%s: batch or n_kv_heads too large", name);
   if ((int64_t)batch * n_kv_heads > ck->n_streams || (int64_t)batch * n_kv_heads > cv->n_streams)
     return fail(SPECTRA_EINVAL, "%s: batch * n_kv_heads exceeds the codec's streams", name);

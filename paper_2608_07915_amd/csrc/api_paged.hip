@@ -5,6 +5,7 @@
 
 #include "api_common.hpp"
 #include "paged.hpp"
+#include "splits.hpp"
 
 using namespace spectra;
 using spectra_dev::PagedAttnArgs;
@@ -17,6 +18,7 @@ using spectra_dev::PoolList;
 namespace {
 
 constexpr int64_t kMaxBatch = 16384;
+constexpr int64_t kMost = (int64_t)1 << 31;  // slots, rows: counted in 32 bits
 
 spectra_status check_map(const spectra_pages* m, const char* name, bool with_refs) {
   if (!m) return fail(SPECTRA_EINVAL, "%s: null page map", name);
@@ -211,8 +213,9 @@ spectra_status spectra_paged_encode(const spectra_pages* m, const spectra_codec*
 
 size_t spectra_paged_attention_workspace_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv_heads,
                                                int32_t max_new, int64_t max_tokens) {
-  if (batch <= 0 || n_new <= 0 || n_kv_heads <= 0 || n_q_heads <= 0 || n_q_heads % n_kv_heads || max_new <= 0 || max_tokens <= 0) return 0;
-  return round256(paged_attention_ws_bytes(batch, n_new, n_q_heads, n_kv_heads, max_new, max_tokens));
+  if (batch <= 0 || batch > kMaxBatch || n_new <= 0 || n_new >= kMost || max_new <= 0 || max_tokens <= 0 || max_tokens >= kMost) return 0;
+  if (n_kv_heads <= 0 || n_kv_heads > 65535 || n_q_heads <= 0 || n_q_heads % n_kv_heads || n_q_heads / n_kv_heads > 16) return 0;
+  return paged_workspace_bytes(batch, n_new, n_q_heads, n_kv_heads, max_new, max_tokens);
 }
 
 spectra_status spectra_paged_attention(const spectra_pages* m, const spectra_codec* ck, const spectra_codec* cv,
@@ -228,9 +231,9 @@ spectra_status spectra_paged_attention(const spectra_pages* m, const spectra_cod
   if (n_q_heads <= 0 || n_q_heads % a.c.n_kv != 0)
     return fail(SPECTRA_EINVAL, "%s: n_q_heads=%d must be a positive multiple of the codecs' %d KV heads", name, n_q_heads, a.c.n_kv);
   if (n_q_heads / a.c.n_kv > 16) return fail(SPECTRA_EUNSUPPORTED, "%s: more than 16 query heads per KV head", name);
-  if (max_new < 0 || max_tokens < 0 || (int64_t)max_new * n_q_heads >= ((int64_t)1 << 31))
+  if (max_new < 0 || max_tokens < 0 || max_tokens >= kMost || (int64_t)max_new * n_q_heads >= kMost)
     return fail(SPECTRA_EINVAL, "%s: max_new=%d or max_tokens=%lld out of range", name, max_new, (long long)max_tokens);
-  if (n_new * n_q_heads >= ((int64_t)1 << 31)) return fail(SPECTRA_EINVAL, "%s: n_new * n_q_heads must stay below 2^31", name);
+  if (n_new * n_q_heads >= kMost || (int64_t)batch * 16 * n_q_heads >= kMost) return fail(SPECTRA_EINVAL, "%s: n_new * n_q_heads and 16 * batch * n_q_heads must stay below 2^31", name);
   if (!(softmax_scale == softmax_scale) || std::isinf(softmax_scale)) return fail(SPECTRA_EINVAL, "%s: softmax_scale not finite", name);
   if (out_dt != SPECTRA_F32 && out_dt != SPECTRA_BF16) return fail(SPECTRA_EINVAL, "%s: output dtype %d not supported", name, (int)out_dt);
   if (batch == 0 || n_new == 0 || max_new == 0 || max_tokens == 0) return SPECTRA_OK;

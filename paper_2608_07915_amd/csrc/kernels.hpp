@@ -109,6 +109,9 @@ hipError_t launch_gram(const spectra_dev::GramArgs& a, bool f32_input, hipStream
 // Decode-step attention; with a.app_k != nullptr the new token of every stream is
 // appended first (the decode step).
 hipError_t launch_attention(const spectra_dev::AttnArgs& a, hipStream_t st);
+// Query heads per KV head that its LDS holds beside records of Wk and Wv words: 16, or 12
+// beside wide ones (more than 67 used words in all).
+int scan_rows(int Wk, int Wv);
 // Merge of the chunk partials in a.partial into a.out (+ m_V, inverse value rotation).
 hipError_t launch_combine(const spectra_dev::AttnArgs& a, hipStream_t st);
 // Attention with rotary position embeddings (Mode A keys, latent values), then the

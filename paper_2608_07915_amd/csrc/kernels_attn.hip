@@ -33,6 +33,7 @@
 #include "kernels.hpp"
 #include "splits.hpp"
 #include "kplan.hpp"
+#include "paged_dev.hpp"
 
 namespace spectra_dev {
 
@@ -114,18 +115,18 @@ __host__ __device__ constexpr int qprep_scratch_bytes(int nq) {
   return (5 * 4 * nq * D) * 4 + (int)sizeof(KGather);
 }
 
-// `issue_more` is called once the loads this step needs are in flight (the caller
-// puts its own, later-needed loads behind them).
-template <int NQ, typename F>
-__device__ __forceinline__ float prepare_query(const AttnArgs& a, int s, int b, int kv, int tid, uint8_t* scratch,
+// `row_at(h)` is the element of a.q at which row h < nqh starts; `issue_more` is called
+// once the loads this step needs are in flight (the caller puts its own, later-needed
+// loads behind them).
+template <int NQ, typename R, typename F>
+__device__ __forceinline__ float prepare_query(const AttnArgs& a, int s, int nqh, int tid, uint8_t* scratch,
                                                uint32_t* __restrict__ qa_s, float* __restrict__ qbar_s, float* red_s,
-                                               F&& issue_more) {
+                                               R&& row_at, F&& issue_more) {
   constexpr int NH = 4 * NQ;
   constexpr int QPT = (NH * D) / 256;  // q values per thread
   float(*qs)[D] = reinterpret_cast<float(*)[D]>(scratch);                          // [NH][D]: q, then q'
   float(*part)[NH][D] = reinterpret_cast<float(*)[NH][D]>(scratch + NH * D * 4);  // [4][NH][D]
   KField(*gat)[KM_MAX][4] = reinterpret_cast<KField(*)[KM_MAX][4]>(scratch + 5 * NH * D * 4);  // [8][m][k]
-  const int nqh = a.n_qh;
   const uint32_t bwk = *reinterpret_cast<const uint32_t*>(a.bits_k + (int64_t)s * NG);
   // Only the kept groups' q' are needed. Columns 0..63 (groups 0 and 1, kept in the
   // common case: widths fall with the variance) are requested before the width
@@ -142,7 +143,7 @@ __device__ __forceinline__ float prepare_query(const AttnArgs& a, int s, int b, 
     const int e = tid + 256 * i, h = e >> 7, c = e & 127;
     qv[i] = 0.0f;
     if (h < nqh) {
-      const int64_t qi = ((int64_t)b * a.n_q_heads + kv * nqh + h) * D + c;
+      const int64_t qi = row_at(h) + c;
       qv[i] = a.q_f32 ? reinterpret_cast<const float*>(a.q)[qi] : bf2f(reinterpret_cast<const uint16_t*>(a.q)[qi]);
     }
   }
@@ -248,9 +249,19 @@ __host__ __device__ constexpr int attn_static_lds(int nq) {
   return nq * QA_QUAD * 4 + 16 * 4 * 4 + WAVES * 4 * nq * (2 + NG) * 4 + WAVES * 4 + 64;
 }
 
+// Record words that are staged without prefetch: no record uses more than four metadata words
+// and four groups of 8 bits, whatever its budget.
+constexpr int USED_MOST = NG + NG * G * 8 / 32;
+__host__ __device__ constexpr int staged_words(int W) { return W < USED_MOST ? W : USED_MOST; }
+
 // Bytes of LDS holding the softmax-weight rows of all wavefronts: per wave and kept
 // slot, 2*NH rows (hi parts of the NH heads, then lo parts) of 64 bf16 tokens.
 __host__ __device__ constexpr int attn_wt_bytes(int nq) { return WAVES * NG * (8 * nq) * WROW * 2; }
+
+// All of it, for tiles of `words` staged words per token.
+constexpr int LDS_MOST = 160 * 1024;
+constexpr int attn_lds(int nq, int words) { return WAVES * words * TROW * 4 + attn_wt_bytes(nq) + attn_static_lds(nq); }
+static_assert(attn_lds(3, 2 * USED_MOST) <= LDS_MOST && attn_lds(4, 32) <= LDS_MOST, "up to 12 rows always fit, 16 with prefetched records");
 
 // ---------------------------------------------------------------------------
 // Score contributions of one kept key slot of width B for the lane's token:
@@ -304,11 +315,11 @@ __device__ __forceinline__ void score_slot(const uint32_t* __restrict__ kt, int 
 // ---------------------------------------------------------------------------
 // Merge of the four wavefronts' online-softmax states of one scan workgroup in LDS
 // and the chunk's partial (m, l, zero-point sums per group, value sums per
-// coefficient) for every query head of the KV head. smem: the tile buffers, free
+// coefficient) for every query row (nqh of them). smem: the tile buffers, free
 // once every wave has left its tile loop.
 // ---------------------------------------------------------------------------
-template <int NQ>
-__device__ __forceinline__ void write_chunk_partial(const AttnArgs& a, int b, int kv, int chunk, int tid, int wave,
+template <int NQ, typename R>
+__device__ __forceinline__ void write_chunk_partial(const AttnArgs& a, int nqh, R&& partial_row, int chunk, int tid, int wave,
                                                     int lane, int kq, int col, bool ok, const Kept& Kv,
                                                     const float (&m_run)[4 * NQ], const float (&l_run)[4 * NQ],
                                                     const float (&zacc)[4 * NQ][NG], const f32x4 (&vacc)[NG][2],
@@ -316,7 +327,6 @@ __device__ __forceinline__ void write_chunk_partial(const AttnArgs& a, int b, in
   constexpr int NH = 4 * NQ;
   constexpr bool STACK = NQ <= 2;
   __shared__ float mst[WAVES][NH], lst[WAVES][NH], zst[WAVES][NH][NG];
-  const int nqh = a.n_qh;
 #pragma unroll
   for (int h = 0; h < NH; ++h) {
     const float l = wave_sum_lane63(l_run[h]);
@@ -358,7 +368,6 @@ __device__ __forceinline__ void write_chunk_partial(const AttnArgs& a, int b, in
   for (int sl = 0; sl < NG; ++sl)
     if (sl < Kv.n) kept_groups |= 1u << Kv.grp[sl];
   __syncthreads();
-  float* part = a.partial + ((int64_t)b * a.n_q_heads + kv * nqh) * a.n_chunks * PART + (int64_t)chunk * PART;
   for (int e = tid; e < nqh * D; e += 256) {
     const int h = e >> 7, j = e & 127;
     const bool kept = (kept_groups >> (j >> 5)) & 1u;
@@ -376,7 +385,7 @@ __device__ __forceinline__ void write_chunk_partial(const AttnArgs& a, int b, in
       l += f * lst[w][h];
       if (j < NG) z += f * zst[w][h][j];
     }
-    float* ph = part + (int64_t)h * a.n_chunks * PART;
+    float* ph = a.partial + (partial_row(h) * a.n_chunks + chunk) * PART;  // row h's partial of this chunk
     ph[8 + j] = acc;
     if (j == 0) {
       ph[0] = M;
@@ -386,8 +395,12 @@ __device__ __forceinline__ void write_chunk_partial(const AttnArgs& a, int b, in
   }
 }
 
-template <int NQ, int PK, int PV, bool EXACT>
-__global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
+// PAGED: the tiles lie in pages (p: the paged call), the codec's streams are the KV heads
+// whatever the sequence, the rows are a sequence's new tokens times the query heads on the KV
+// head (row h = token h / n_qh, head h % n_qh; at most 4 NQ), each with a limit of its own,
+// and chunks come tiles_per_chunk at a time without a last one apart.
+template <int NQ, int PK, int PV, bool EXACT, bool PAGED>
+__device__ __forceinline__ void attn_scan(const AttnArgs& a, const PagedAttnArgs& p) {
   constexpr int NH = 4 * NQ;
   constexpr bool STACK = NQ <= 2;  // 2*NH <= 16: hi and lo weight rows share one MFMA
   extern __shared__ __attribute__((aligned(16))) uint32_t smem[];
@@ -405,12 +418,24 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     b = gid / a.n_kv_heads;
   }
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
-  const int s = b * a.n_kv_heads + kv;
-  const int nqh = a.n_qh;
+  PagedSeq seq{};
+  if constexpr (PAGED) {
+    seq = paged_seq(p.c, b);
+    if (!scanned(p, seq)) return;  // the rows of longer sequences are the other kernel's
+    if ((int64_t)chunk * a.tiles_per_chunk * TILE >= seq.len) return;  // nor does a sequence have chunks past its end
+  }
+  const int s = PAGED ? kv : b * a.n_kv_heads + kv;
+  const int nqh = PAGED ? (int)seq.n * a.n_qh : a.n_qh;
+  const int64_t n_tokens = PAGED ? seq.len : a.n_tokens;
+  int limit[PAGED ? NH : 1];  // slots that a row sees
+  if constexpr (PAGED) {
+#pragma unroll
+    for (int h = 0; h < NH; ++h) limit[h] = h < nqh ? (int)(seq.len - seq.n) + 1 + h / a.n_qh : 0;
+  }
   const int Wk = a.Wk, Wv = a.Wv;
   // ---- per-wave streaming over this chunk's tiles ----
   static_assert((PK > 0) == (PV > 0), "prefetch both tensors or neither");
-  const int wk_rows = PK > 0 ? PK : Wk, wv_rows = PV > 0 ? PV : Wv;  // staged words per token
+  const int wk_rows = PK > 0 ? PK : staged_words(Wk), wv_rows = PV > 0 ? PV : staged_words(Wv);  // per token
   const int wpw = wk_rows + wv_rows;
   uint32_t* kt = smem + wave * wpw * TROW;
   uint32_t* vt = kt + wk_rows * TROW;
@@ -419,11 +444,11 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   const int64_t vbase = (int64_t)s * a.t_cap * Wv;
   // chunk c < n_chunks - 1 holds tiles [c * tpc, (c + 1) * tpc) of all but the last
   // tile; the last chunk holds the last tile alone
-  const int64_t n_tiles = (a.n_tokens + 63) >> 6;
-  const bool last_chunk = chunk == a.n_chunks - 1;
+  const int64_t n_tiles = (n_tokens + 63) >> 6;
+  const bool last_chunk = !PAGED && chunk == a.n_chunks - 1;
   const int64_t tile_begin = last_chunk ? n_tiles - 1 : (int64_t)chunk * a.tiles_per_chunk;
   int64_t tile_end = last_chunk ? n_tiles : tile_begin + a.tiles_per_chunk;
-  if (!last_chunk && tile_end > n_tiles - 1) tile_end = n_tiles - 1;
+  if (!last_chunk && tile_end > n_tiles - (PAGED ? 0 : 1)) tile_end = n_tiles - (PAGED ? 0 : 1);
 
   float m_run[NH], l_run[NH], zacc[NH][NG];
 #pragma unroll
@@ -449,9 +474,28 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   // tokens past n_tokens are never weighted (their value metadata is zeroed)
   const uint32_t* kps = a.packed_k + kbase;
   const uint32_t* vps = a.packed_v + vbase;
+  // PAGED: the page of the next tile to load is read a tile ahead; a page outside the pool is
+  // read as page 0 with all metadata taken as zero
+  const int tpp = PAGED ? p.c.page_tokens >> 6 : 1;
+  int next_page = 0;
+  bool loaded_ok = true, tile_ok = true;  // of the tile in flight, of the staged one
+  auto look_up = [&](int64_t t2) {
+    if constexpr (PAGED)
+      next_page = t2 < tile_end ? p.c.table[(int64_t)seq.row * p.c.row_pages + (int)t2 / tpp] : 0;
+  };
   auto load_tile = [&](int64_t tt) {
-    const uint32_t ko = (uint32_t)tt * (uint32_t)(64 * Wk) + (uint32_t)lane;
-    const uint32_t vo = (uint32_t)tt * (uint32_t)(64 * Wv) + (uint32_t)lane;
+    uint32_t ko, vo;
+    if constexpr (PAGED) {
+      loaded_ok = next_page >= 0 && next_page < p.c.n_pages;
+      const int64_t at = ((int64_t)(loaded_ok ? next_page : 0) * a.n_kv_heads + kv) * tpp + (int)tt % tpp;
+      kps = a.packed_k + at * (64 * Wk);
+      vps = a.packed_v + at * (64 * Wv);
+      ko = vo = (uint32_t)lane;
+      look_up(tt + WAVES);
+    } else {
+      ko = (uint32_t)tt * (uint32_t)(64 * Wk) + (uint32_t)lane;
+      vo = (uint32_t)tt * (uint32_t)(64 * Wv) + (uint32_t)lane;
+    }
     if constexpr (EXACT) {  // Wk == PK, Wv == PV: no clamping, word offsets are immediates
       const uint32_t* kp = kps + ko;
       const uint32_t* vp = vps + vo;
@@ -469,10 +513,11 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     }
   };
   int64_t tt = tile_begin + wave;
+  look_up(tt);
 
   // In a decode step the workgroup of the last chunk (the last tile) first appends
   // the new token of its stream (and makes the records visible to its own loads).
-  if (a.app_k != nullptr && last_chunk) {
+  if (!PAGED && a.app_k != nullptr && last_chunk) {
     if (a.app_f32)
       append_token<true>(a, s, tid, reinterpret_cast<uint8_t*>(smem));
     else
@@ -486,8 +531,16 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   // its loads ----
   __shared__ float red_s[WAVES];
   __shared__ float e2_s;
-  const float E2q = prepare_query<NQ>(a, s, b, kv, tid, reinterpret_cast<uint8_t*>(smem), qa_s, qbar_s, red_s, [&] {
-    if (tt < tile_end) load_tile(tt);
+  const auto row_at = [&](int h) -> int64_t {
+    if constexpr (PAGED) {
+      const int tok = h / a.n_qh;
+      return (seq.first + tok) * p.q_token_stride + (kv * a.n_qh + h - tok * a.n_qh) * p.q_head_stride;
+    } else {
+      return ((int64_t)b * a.n_q_heads + kv * nqh + h) * D;
+    }
+  };
+  const float E2q = prepare_query<NQ>(a, s, nqh, tid, reinterpret_cast<uint8_t*>(smem), qa_s, qbar_s, red_s, row_at, [&] {
+    if (PK > 0 && tt < tile_end) load_tile(tt);
   });
   const Kept Kk = read_kept(a.bits_k + (int64_t)s * NG);
   const Kept Kv = read_kept(a.bits_v + (int64_t)s * NG);
@@ -522,8 +575,10 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     kvv.used = __builtin_amdgcn_readfirstlane(kvv.used);
     asm volatile("" : "+s"(kk.n), "+s"(kvv.n), "+s"(kvv.used));
     const int64_t t = tt * 64 + lane;
-    const bool valid = t < a.n_tokens;
+    const bool valid = t < n_tokens;
     // stage this tile's words in LDS (lane = token), then prefetch the next tile
+    if constexpr (PAGED && PK == 0) load_tile(tt);  // its addresses
+    tile_ok = loaded_ok;
     if constexpr (PK > 0) {
 #pragma unroll
       for (int w = 0; w < (PK > PV ? PK : PV); ++w) {
@@ -532,8 +587,8 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
       }
       if (tt + WAVES < tile_end) load_tile(tt + WAVES);
     } else {
-      const uint32_t ko = (uint32_t)tt * (uint32_t)(64 * Wk) + (uint32_t)lane;
-      const uint32_t vo = (uint32_t)tt * (uint32_t)(64 * Wv) + (uint32_t)lane;
+      const uint32_t ko = (PAGED ? 0u : (uint32_t)tt * (uint32_t)(64 * Wk)) + (uint32_t)lane;
+      const uint32_t vo = (PAGED ? 0u : (uint32_t)tt * (uint32_t)(64 * Wv)) + (uint32_t)lane;
       for (int w = 0; w < kk.used; ++w) kt[w * TROW + lane] = (kps + 64 * w)[ko];
       for (int w = 0; w < kvv.used; ++w) vt[w * TROW + lane] = (vps + 64 * w)[vo];
     }
@@ -547,7 +602,8 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     for (int sl = 0; sl < NG; ++sl) {
       if (sl >= kk.n) continue;
       const int g = kk.grp[sl];
-      const uint32_t meta = kt[sl * TROW + lane];
+      uint32_t meta = kt[sl * TROW + lane];
+      if constexpr (PAGED) meta = tile_ok ? finite_or_zero(meta) : 0u;
       f32x4 dh[NQ], dl[NQ];
 #pragma unroll
       for (int q = 0; q < NQ; ++q) dh[q] = dl[q] = f32x4{0.f, 0.f, 0.f, 0.f};
@@ -578,7 +634,10 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     bool over = false;
 #pragma unroll
     for (int h = 0; h < NH; ++h) {
-      x[h] = (valid && h < nqh) ? sc[h] : -__builtin_inff();
+      if constexpr (PAGED)
+        x[h] = (int)t < limit[h] ? sc[h] : -__builtin_inff();
+      else
+        x[h] = (valid && h < nqh) ? sc[h] : -__builtin_inff();
       over = over || x[h] > m_run[h] + RESCALE_SLACK;
     }
     if (__any(over)) {  // rare after the first tile: one branch for all heads
@@ -614,7 +673,8 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     for (int sl = 0; sl < NG; ++sl) {
       if (sl >= kvv.n) continue;
       // tokens past n_tokens hold whatever the cache holds there: zero their metadata
-      const uint32_t meta = valid ? vt[sl * TROW + lane] : 0u;
+      uint32_t meta = valid ? vt[sl * TROW + lane] : 0u;
+      if constexpr (PAGED) meta = tile_ok ? finite_or_zero(meta) : 0u;
       const float sv = h2f(meta), zv = h2f(meta >> 16);
       uint16_t* ws = wt + sl * 2 * NH * WROW;  // rows: hi of heads 0..NH-1, then lo
 #pragma unroll
@@ -683,7 +743,26 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
     __builtin_amdgcn_wave_barrier();
   }
 
-  write_chunk_partial<NQ>(a, b, kv, chunk, tid, wave, lane, kq, col, ok, Kv, m_run, l_run, zacc, vacc, smem);
+  const auto partial_row = [&](int h) -> int64_t {
+    if constexpr (PAGED) {
+      const int tok = h / a.n_qh;
+      return ((int64_t)b * p.scan_tokens + tok) * a.n_q_heads + kv * a.n_qh + h - tok * a.n_qh;
+    } else {
+      return (int64_t)b * a.n_q_heads + kv * nqh + h;
+    }
+  };
+  write_chunk_partial<NQ>(a, nqh, partial_row, chunk, tid, wave, lane, kq, col, ok, Kv, m_run, l_run, zacc, vacc, smem);
+}
+
+template <int NQ, int PK, int PV, bool EXACT>
+__global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
+  attn_scan<NQ, PK, PV, EXACT, false>(a, PagedAttnArgs{});
+}
+
+// Sequences with few new rows: a decode step's single tokens, a few speculative ones.
+template <int NQ, int PK, int PV, bool EXACT>
+__global__ __launch_bounds__(256, 2) void paged_scan_kernel(AttnArgs a, PagedAttnArgs p) {
+  attn_scan<NQ, PK, PV, EXACT, true>(a, p);
 }
 
 // ---------------------------------------------------------------------------
@@ -693,15 +772,18 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
 // chunk, merged with a running maximum in batches of CB chunks); the group
 // states are then merged in LDS.
 // ---------------------------------------------------------------------------
-__global__ __launch_bounds__(1024) void combine_kernel(AttnArgs a) {
+// combine_row: nch partials from ph, value stream s; store(i, out_i) takes the row's channels,
+// stats(m, l) in one thread the overall maximum (log2 domain) and sum. With EMPTY, a row without
+// weights gets zeros.
+template <bool EMPTY, typename Store, typename Stats>
+__device__ __forceinline__ void combine_row(const AttnArgs& a, const float* __restrict__ ph, int nch, int s, Store&& store,
+                                            Stats&& stats) {
   constexpr int CB = 12;  // 8 x 12 = 96 chunks per round: one round of loads for ~768 scan workgroups over 8 heads
   __shared__ float accs[8][D];
   __shared__ float chat[D];
   __shared__ float gm[8], gl[8];
-  const int hq = blockIdx.x, b = blockIdx.y, tid = threadIdx.x;
+  const int tid = threadIdx.x;
   const int j = tid & 127, grp = tid >> 7;
-  const int kv = hq / a.n_qh;
-  const int s = b * a.n_kv_heads + kv;
   // rotation operands: output row i = tid / 8, coefficients 16 (tid % 8) .. + 15
   const int ri = tid >> 3, rpart = tid & 7;
   const f32x4* Vr = reinterpret_cast<const f32x4*>(a.basis_v + (int64_t)s * D * D + (int64_t)ri * D + 16 * rpart);
@@ -709,8 +791,6 @@ __global__ __launch_bounds__(1024) void combine_kernel(AttnArgs a) {
   const float mv = tid < D ? a.mean_v[(int64_t)s * D + tid] : 0.0f;
   const uint32_t bw = *reinterpret_cast<const uint32_t*>(a.bits_v + (int64_t)s * NG);
 
-  const float* ph = a.partial + ((int64_t)b * a.n_q_heads + hq) * a.n_chunks * PART;
-  const int nch = a.n_chunks;
   const int g = j >> 5;
   float M = -__builtin_inff(), L = 0.0f, A = 0.0f;
   for (int c0 = grp; c0 < nch; c0 += 8 * CB) {
@@ -761,6 +841,10 @@ __global__ __launch_bounds__(1024) void combine_kernel(AttnArgs a) {
     }
     const bool kept = ((bw >> (8 * (tid >> 5))) & 0xFFu) != 0u;
     chat[tid] = (kept ? sacc / sl : 0.0f) + mv;
+    if constexpr (EMPTY) {
+      if (sl == 0.0f) chat[tid] = 0.0f;
+    }
+    if (tid == 0) stats(Mx, sl);
   }
   __syncthreads();
   // out_i = sum_j chat_j V[i][j]: eight lanes per output row, 16 contiguous j each
@@ -776,7 +860,40 @@ __global__ __launch_bounds__(1024) void combine_kernel(AttnArgs a) {
   o += __shfl_xor(o, 1);
   o += __shfl_xor(o, 2);
   o += __shfl_xor(o, 4);
-  if (rpart == 0) a.out[((int64_t)b * a.n_q_heads + hq) * D + ri] = o;
+  if (rpart == 0) store(ri, o);
+}
+
+__global__ __launch_bounds__(1024) void combine_kernel(AttnArgs a) {
+  const int hq = blockIdx.x, b = blockIdx.y;
+  const int64_t row = (int64_t)b * a.n_q_heads + hq;
+  combine_row<false>(a, a.partial + row * a.n_chunks * PART, a.n_chunks, b * a.n_kv_heads + hq / a.n_qh,
+                     [&](int i, float o) { a.out[row * D + i] = o; }, [](float, float) {});
+}
+
+// The same for the rows of scanned sequences: workgroup = (sequence, token, query head).
+__global__ __launch_bounds__(1024) void paged_combine_kernel(AttnArgs a, PagedAttnArgs p) {
+  const int hq = blockIdx.x % (unsigned)a.n_q_heads, at = blockIdx.x / (unsigned)a.n_q_heads;
+  const int b = at / p.scan_tokens, tok = at % p.scan_tokens;
+  const PagedSeq seq = paged_seq(p.c, b);
+  if (!scanned(p, seq) || tok >= seq.n) return;
+  const int64_t per = (int64_t)a.tiles_per_chunk * TILE;  // slots of a chunk
+  const int nch = (int)((seq.len + per - 1) / per);
+  const int64_t row = (seq.first + tok) * a.n_q_heads + hq;
+  combine_row<true>(
+      a, a.partial + ((int64_t)at * a.n_q_heads + hq) * a.n_chunks * PART, nch, hq / a.n_qh,
+      [&](int i, float o) {
+        if (p.out_f32)
+          reinterpret_cast<float*>(p.out)[row * D + i] = o;
+        else
+          reinterpret_cast<__bf16*>(p.out)[row * D + i] = (__bf16)o;
+      },
+      [&](float m, float l) {
+        if (p.lse == nullptr) return;
+        const int64_t qo = (seq.first + tok) * p.q_token_stride + hq * p.q_head_stride;
+        float u = 0.0f;
+        for (int c = 0; c < D; ++c) u = __builtin_fmaf(query_at(p, qo + c), p.lse_u[hq / a.n_qh * D + c], u);
+        p.lse[row] = l == 0.0f ? -__builtin_inff() : __builtin_fmaf(__builtin_amdgcn_logf(l) + m, LN2, u);
+      });
 }
 
 }  // namespace spectra_dev
@@ -793,8 +910,8 @@ size_t attention_call_bytes(int32_t batch, int32_t n_q_heads, int32_t n_kv_heads
 }
 
 template <int NQ, int PK, int PV, bool EXACT>
-static int32_t launch_nq_pw(const AttnArgs& a, hipStream_t st) {
-  const int wpw = PK > 0 ? PK + PV : a.Wk + a.Wv;
+static Split launch_nq_pw(const AttnArgs& a, const PagedAttnArgs* p, hipStream_t st) {
+  const int wpw = PK > 0 ? PK + PV : staged_words(a.Wk) + staged_words(a.Wv);
   size_t tiles = (size_t)WAVES * wpw * TROW * 4 + (size_t)attn_wt_bytes(NQ);
   size_t merge = (size_t)WAVES * (NQ <= 2 ? 8 * NQ : 4 * NQ) * AROW * 4;  // per-wave value sums
   size_t lds = tiles > merge ? tiles : merge;
@@ -807,14 +924,19 @@ static int32_t launch_nq_pw(const AttnArgs& a, hipStream_t st) {
   // head quad and at most 24 prefetched words, two for the others; and its 160 KB of LDS
   // (that of a call without an append: a decode step has the same split)
   constexpr int REGS = NQ == 1 && PK + PV <= 24 ? 3 : 2;
-  const int fit = (int)(160 * 1024 / (lds + attn_static_lds(NQ)));
+  const int fit = (int)(LDS_MOST / (lds + attn_static_lds(NQ)));
   if (a.app_k && (size_t)append_stage_bytes(a.app_f32 != 0) > lds) lds = append_stage_bytes(a.app_f32 != 0);
-  const Split split = scan_split(groups, (a.n_tokens + 63) / 64, fit < 1 ? 1 : fit < REGS ? fit : REGS, NQ * (a.Wk + a.Wv));
+  const int per_cu = fit < 1 ? 1 : fit < REGS ? fit : REGS;
+  const Split split = p ? paged_scan_split(groups, (a.n_tokens + 63) / 64, per_cu)
+                        : scan_split(groups, (a.n_tokens + 63) / 64, per_cu, NQ * (a.Wk + a.Wv));
   g.tiles_per_chunk = split.tiles_per_chunk;
   g.n_chunks = split.n_chunks;
   const dim3 grid = g.group_major ? dim3(g.n_chunks * a.n_kv_heads * a.batch, 1, 1) : dim3(g.n_chunks, a.n_kv_heads, a.batch);
-  hipLaunchKernelGGL((attn_kernel<NQ, PK, PV, EXACT>), grid, dim3(256), lds, st, g);
-  return g.n_chunks;
+  if (p)
+    hipLaunchKernelGGL((paged_scan_kernel<NQ, PK, PV, EXACT>), grid, dim3(256), lds, st, g, *p);
+  else
+    hipLaunchKernelGGL((attn_kernel<NQ, PK, PV, EXACT>), grid, dim3(256), lds, st, g);
+  return split;
 }
 
 // Prefetch shapes. Up to eight query heads per KV head, records of unequal width
@@ -822,24 +944,26 @@ static int32_t launch_nq_pw(const AttnArgs& a, hipStream_t st) {
 // or three quarters to the keys), otherwise (8, 16) or (16, 8); at most 24
 // prefetch registers keep three wavefronts per SIMD.
 template <int NQ>
-static int32_t launch_nq(const AttnArgs& a, hipStream_t st) {
+static Split launch_nq(const AttnArgs& a, const PagedAttnArgs* p, hipStream_t st) {
   const int wk = a.Wk, wv = a.Wv;
   if constexpr (NQ <= 2) {
-    if (wk == 4 && wv == 12) return launch_nq_pw<NQ, 4, 12, true>(a, st);
-    if (wk == 12 && wv == 4) return launch_nq_pw<NQ, 12, 4, true>(a, st);
-    if (wk <= 8 && wv > 8 && wv <= 16) return launch_nq_pw<NQ, 8, 16, false>(a, st);
-    if (wv <= 8 && wk > 8 && wk <= 16) return launch_nq_pw<NQ, 16, 8, false>(a, st);
+    if (wk == 4 && wv == 12) return launch_nq_pw<NQ, 4, 12, true>(a, p, st);
+    if (wk == 12 && wv == 4) return launch_nq_pw<NQ, 12, 4, true>(a, p, st);
+    if (wk <= 8 && wv > 8 && wv <= 16) return launch_nq_pw<NQ, 8, 16, false>(a, p, st);
+    if (wv <= 8 && wk > 8 && wk <= 16) return launch_nq_pw<NQ, 16, 8, false>(a, p, st);
   }
   if (wk == 8 && wv == 8)
-    return launch_nq_pw<NQ, 8, 8, true>(a, st);
+    return launch_nq_pw<NQ, 8, 8, true>(a, p, st);
   if (wk <= 8 && wv <= 8)
-    return launch_nq_pw<NQ, 8, 8, false>(a, st);
+    return launch_nq_pw<NQ, 8, 8, false>(a, p, st);
   if (wk == 16 && wv == 16)
-    return launch_nq_pw<NQ, 16, 16, true>(a, st);
+    return launch_nq_pw<NQ, 16, 16, true>(a, p, st);
   if (wk <= 16 && wv <= 16)
-    return launch_nq_pw<NQ, 16, 16, false>(a, st);
-  return launch_nq_pw<NQ, 0, 0, false>(a, st);
+    return launch_nq_pw<NQ, 16, 16, false>(a, p, st);
+  return launch_nq_pw<NQ, 0, 0, false>(a, p, st);
 }
+
+int scan_rows(int Wk, int Wv) { return attn_lds(4, staged_words(Wk) + staged_words(Wv)) <= LDS_MOST ? 16 : 12; }
 
 hipError_t launch_combine(const AttnArgs& a, hipStream_t st) {
   hipLaunchKernelGGL(combine_kernel, dim3(a.n_q_heads, a.batch), dim3(1024), 0, st, a);
@@ -851,13 +975,49 @@ hipError_t launch_combine(const AttnArgs& a, hipStream_t st) {
 hipError_t launch_attention(const AttnArgs& a, hipStream_t st) {
   AttnArgs g = a;
   switch ((a.n_qh + 3) / 4) {
-    case 1: g.n_chunks = launch_nq<1>(a, st); break;
-    case 2: g.n_chunks = launch_nq<2>(a, st); break;
-    case 3: g.n_chunks = launch_nq<3>(a, st); break;
-    default: g.n_chunks = launch_nq<4>(a, st); break;
+    case 1: g.n_chunks = launch_nq<1>(a, nullptr, st).n_chunks; break;
+    case 2: g.n_chunks = launch_nq<2>(a, nullptr, st).n_chunks; break;
+    case 3: g.n_chunks = launch_nq<3>(a, nullptr, st).n_chunks; break;
+    default: g.n_chunks = launch_nq<4>(a, nullptr, st).n_chunks; break;
   }
   const hipError_t e = hipGetLastError();
   return e == hipSuccess ? launch_combine(g, st) : e;
+}
+
+static_assert(PART * sizeof(float) == SCAN_PART_BYTES, "workspace of a scanned row");
+
+// The sequences of a paged call with at most p.scan_tokens new tokens.
+hipError_t launch_paged_scan(const PagedAttnArgs& p, float* partial, hipStream_t st) {
+  AttnArgs a{};
+  a.packed_k = p.pool_k;
+  a.packed_v = p.pool_v;
+  a.n_tokens = p.max_tokens;
+  a.basis_k = p.basis_k;
+  a.basis_v = p.basis_v;
+  a.mean_v = p.mean_v;
+  a.bits_k = p.bits_k;
+  a.bits_v = p.bits_v;
+  a.q = p.q;
+  a.q_f32 = p.q_f32;
+  a.batch = p.c.batch;
+  a.n_q_heads = p.n_q_heads;
+  a.n_kv_heads = p.c.n_kv;
+  a.n_qh = p.n_qh;
+  a.Wk = p.Wk;
+  a.Wv = p.Wv;
+  a.scale_log2 = p.scale_log2;
+  a.partial = partial;
+  Split split{};
+  switch ((p.scan_tokens * p.n_qh + 3) / 4) {
+    case 1: split = launch_nq<1>(a, &p, st); break;
+    case 2: split = launch_nq<2>(a, &p, st); break;
+    case 3: split = launch_nq<3>(a, &p, st); break;
+    default: split = launch_nq<4>(a, &p, st); break;
+  }
+  a.tiles_per_chunk = split.tiles_per_chunk;
+  a.n_chunks = split.n_chunks;
+  hipLaunchKernelGGL(paged_combine_kernel, dim3((unsigned)(a.n_q_heads * p.c.batch * p.scan_tokens)), dim3(1024), 0, st, a, p);
+  return hipGetLastError();
 }
 
 }  // namespace spectra

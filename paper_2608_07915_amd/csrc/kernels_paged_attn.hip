@@ -26,7 +26,9 @@
 #include "attn_common.hpp"
 #include "code_operands.hpp"
 #include "encode_dev.hpp"
+#include "kernels.hpp"
 #include "paged_dev.hpp"
+#include "splits.hpp"
 
 namespace spectra_dev {
 
@@ -35,7 +37,6 @@ constexpr int CA_ROWS = 32 * CA_NW;    // query rows of a workgroup
 constexpr int CA_TILE = TILE * 64;     // bytes of a slot tile: 64 slots x 32 fp16
 constexpr float CA_SLACK = 3.0f;       // log2: the running maximum moves when passed by more
 constexpr float CA_LIFT = 12.0f;       // log2: weights are kept 2^12 above their share
-constexpr float LN2 = 0.69314718055994531f;
 constexpr float CA_LO = 2048.0f;       // the second fp16 part of a number is scaled by 2^11
 
 // LDS byte of 16-byte piece `piece` of slot `t` in a slot tile.
@@ -117,31 +118,25 @@ __device__ __forceinline__ void split8(const float (&v)[8], bf16x8 (&p)[NP]) {
     p[q] = as_bf16x8(u32x4{pack2(a[q][0], a[q][1]), pack2(a[q][2], a[q][3]), pack2(a[q][4], a[q][5]), pack2(a[q][6], a[q][7])});
 }
 
-__device__ __forceinline__ float query_at(const PagedAttnArgs& a, int64_t i) {
-  return a.q_f32 ? reinterpret_cast<const float*>(a.q)[i] : bf2f(reinterpret_cast<const uint16_t*>(a.q)[i]);
-}
-
-// Which sequence a unit of R rows belongs to: sequence b has ceil(n_b n_qh / R) of them. The
-// same in every thread; false when there is none. s: LDS. Sequences past the call's bounds
-// have none: their rows are left as they were.
-__device__ __forceinline__ bool attended(const PagedAttnArgs& a, const PagedSeq& q) {
-  return q.n <= a.max_new && q.len <= a.max_tokens;
-}
+// Which sequence a unit of CA_ROWS rows belongs to: sequence b has ceil(n_b n_qh / CA_ROWS) of
+// them, but none where the scan takes it or it is past the call's bounds. The same in every
+// thread of a workgroup of NW wavefronts; false when there is none. s: LDS.
 struct FindScratch {
   int64_t part[CA_NW];
   int64_t total;
   int32_t b, tile;
 };
-__device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int R, int64_t unit, FindScratch& s, int& b, int64_t& tile) {
+template <int NW>
+__device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int64_t unit, FindScratch& s, int& b, int64_t& tile) {
   const PagedCache& c = a.c;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   if (tid == 0) s.b = -1;
   int64_t base = 0;
-  for (int b0 = 0; b0 < c.batch; b0 += 64 * CA_NW) {
+  for (int b0 = 0; b0 < c.batch; b0 += 64 * NW) {
     int64_t mine = 0;
     if (b0 + tid < c.batch) {
       const PagedSeq q = paged_seq(c, b0 + tid);
-      if (attended(a, q)) mine = (q.n * a.n_qh + R - 1) / R;
+      if (attended(a, q) && !scanned(a, q)) mine = (q.n * a.n_qh + CA_ROWS - 1) / CA_ROWS;
     }
     int64_t v = mine;
 #pragma unroll
@@ -159,7 +154,7 @@ __device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int R, int64_t
       s.b = b0 + tid;
       s.tile = (int32_t)(unit - lo);
     }
-    if (tid == 64 * CA_NW - 1) s.total = before + v;
+    if (tid == 64 * NW - 1) s.total = before + v;
     __syncthreads();
     if (s.b >= 0) break;
     base = s.total;
@@ -167,6 +162,119 @@ __device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int R, int64_t
   b = __builtin_amdgcn_readfirstlane(s.b);
   tile = __builtin_amdgcn_readfirstlane(s.tile);
   return b >= 0;
+}
+
+// The 32 rows of a wavefront: row = new token x query heads on the KV head + query head. Rows
+// past the sequence's last repeat that one and are not stored.
+struct Rows {
+  int tok, head;      // of the lane's row
+  bool live;
+  int lim;            // slots that it sees
+  int lim_first, lim_last, lim_unit;  // the wavefront's first row, its last, the unit's last
+};
+__device__ __forceinline__ Rows rows_of(const PagedAttnArgs& a, const PagedSeq& seq, int64_t tile, int wave, int col) {
+  const int n_rows = (int)(seq.n * a.n_qh), past = (int)(seq.len - seq.n) + 1;  // slots that token 0 sees
+  const int row0 = (int)tile * CA_ROWS + 32 * wave, row = row0 + col;
+  auto limit = [&](int r) {
+    const int l = past + (r < n_rows ? r : n_rows - 1) / a.n_qh;
+    return l < 0 ? 0 : l;
+  };
+  Rows x;
+  x.live = row < n_rows;
+  const int rc = x.live ? row : n_rows - 1;
+  x.tok = rc / a.n_qh;
+  x.head = rc - x.tok * a.n_qh;
+  x.lim = past + x.tok < 0 ? 0 : past + x.tok;
+  x.lim_first = __builtin_amdgcn_readfirstlane(limit(row0));
+  x.lim_last = __builtin_amdgcn_readfirstlane(limit(row0 + 31));
+  x.lim_unit = __builtin_amdgcn_readfirstlane(limit((int)tile * CA_ROWS + CA_ROWS - 1));
+  return x;
+}
+
+// Parts that a unit seeing lim slots has, and where a wavefront's results of one lie: 16 floats
+// per value group and lane, then m and l.
+__device__ __forceinline__ int parts_of(const PagedAttnArgs& a, int lim) { return (int)((lim + a.part_slots - 1) / a.part_slots); }
+__device__ __forceinline__ int64_t part_at(const PagedAttnArgs& a, int64_t unit, int kv, int part, int wave) {
+  return (((unit * a.c.n_kv + kv) * a.parts + part) * CA_NW + wave) * ((16 * NG + 2) * 64);
+}
+
+// out = (a / l + m_V) V_V^T of a wavefront's 32 rows, the coefficients as column operand, and
+// both sides in NP bf16 parts; stores the rows and their log-sum-exp. m, l: of the lane's row.
+template <int NP>
+__device__ __forceinline__ void finish_rows(const PagedAttnArgs& a, const PagedSeq& seq, const Rows& r, int kv, const Kept& Kv,
+                                            const f32x16 (&acc)[NG], float m, float l, int lane) {
+  const int h = lane >> 5, col = lane & 31;
+  const bool seen = l > 0.0f || !(l == l);
+  const float inv = 1.0f / l;
+  const float* Vv = a.basis_v + (int64_t)kv * D * D;
+  f32x16 out[4];
+#pragma unroll
+  for (int cb = 0; cb < 4; ++cb) out[cb] = zero16();
+  const int i0 = 4 * (col >> 3) + (col & 3), h0 = (col >> 2) & 1;
+  const int chan = 16 * h0 + i0;  // MFMA row col of a 32-channel block: then a lane half has 16 neighbouring channels
+#pragma unroll
+  for (int g = 0; g < NG; ++g) {
+    int sl = -1;
+#pragma unroll
+    for (int x = 0; x < NG; ++x) sl = (x < Kv.n && Kv.grp[x] == g) ? x : sl;
+    f32x16 av = zero16();
+#pragma unroll
+    for (int x = 0; x < NG; ++x)
+      if (x == sl) av = acc[x];
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      float cf[8];
+      int at[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        const int place = 16 * s + 8 * (e >> 2) + 4 * h + (e & 3);  // of register 8 s + e
+        at[e] = G * g + 4 * (place >> 3) + ((place & 7) >> 1) + 16 * (place & 1);
+        cf[e] = (sl >= 0 ? av[8 * s + e] * inv : 0.0f) + a.mean_v[kv * D + at[e]];
+      }
+      bf16x8 cp[NP];
+      split8<NP>(cf, cp);
+#pragma unroll
+      for (int cb = 0; cb < 4; ++cb) {
+        float v[8];
+#pragma unroll
+        for (int e = 0; e < 8; ++e) v[e] = Vv[(32 * cb + chan) * D + at[e]];
+        bf16x8 vp[NP];
+        split8<NP>(v, vp);
+#pragma unroll
+        for (int x = 0; x < NP; ++x)
+#pragma unroll
+          for (int y = 0; x + y < NP; ++y)
+            out[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vp[x], cp[y], out[cb], 0, 0, 0);
+      }
+    }
+  }
+  if (!r.live) return;
+  const int64_t o = ((seq.first + r.tok) * a.n_q_heads + kv * a.n_qh + r.head) * D + 16 * h;
+#pragma unroll
+  for (int cb = 0; cb < 4; ++cb) {
+    if (a.out_f32) {
+      float* op = reinterpret_cast<float*>(a.out) + o + 32 * cb;
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        *reinterpret_cast<f32x4*>(op + 4 * i) = seen ? f32x4{out[cb][4 * i], out[cb][4 * i + 1], out[cb][4 * i + 2], out[cb][4 * i + 3]}
+                                                     : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    } else {
+      uint32_t* op = reinterpret_cast<uint32_t*>(reinterpret_cast<uint16_t*>(a.out) + o + 32 * cb);
+      uint32_t w[8];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        w[i] = seen ? __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{out[cb][2 * i], out[cb][2 * i + 1]}, bf16x2)) : 0u;
+      *reinterpret_cast<u32x4*>(op) = u32x4{w[0], w[1], w[2], w[3]};
+      *reinterpret_cast<u32x4*>(op + 4) = u32x4{w[4], w[5], w[6], w[7]};
+    }
+  }
+  if (a.lse != nullptr && h == 0) {
+    const int64_t qo = (seq.first + r.tok) * a.q_token_stride + (kv * a.n_qh + r.head) * a.q_head_stride;
+    float s = 0.0f;
+    for (int c = 0; c < D; ++c) s = __builtin_fmaf(query_at(a, qo + c), a.lse_u[kv * D + c], s);
+    a.lse[(seq.first + r.tok) * a.n_q_heads + kv * a.n_qh + r.head] =
+        seen ? __builtin_fmaf(__builtin_amdgcn_logf(l) + (m - CA_LIFT), LN2, s) : -__builtin_inff();
+  }
 }
 
 template <bool PRECISE>
@@ -180,23 +288,18 @@ __global__ __launch_bounds__(64 * CA_NW, 2) void paged_chunk_kernel(PagedAttnArg
   const int tid = threadIdx.x, lane = tid & 63;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   const int h = lane >> 5, col = lane & 31;
+  const int64_t unit = blockIdx.x / (unsigned)a.c.n_kv;
+  const int part = blockIdx.y;
   int b;
   int64_t tile;
-  if (!find_unit(a, CA_ROWS, blockIdx.x / (unsigned)a.c.n_kv, find_s, b, tile)) return;
+  if (!find_unit<CA_NW>(a, unit, find_s, b, tile)) return;
   const PagedSeq seq = paged_seq(a.c, b);
-  const int n_rows = (int)(seq.n * a.n_qh);
-  const int row0 = (int)tile * CA_ROWS + 32 * wave;
-  // rows past the sequence's last compute that row again and store nothing
-  const int row = row0 + col, rowc = row < n_rows ? row : n_rows - 1;
-  const int tok = rowc / a.n_qh, head = kv * a.n_qh + (rowc - tok * a.n_qh);
-  const int past = (int)(seq.len - seq.n) + 1;  // slots that row (0, .) sees
-  auto limit_of = [&](int r) {
-    const int l = past + (r < n_rows ? r : n_rows - 1) / a.n_qh;
-    return l < 0 ? 0 : l;
-  };
-  const int lim = past + tok < 0 ? 0 : past + tok;
-  const int lim_first = __builtin_amdgcn_readfirstlane(limit_of(row0)), lim_last = __builtin_amdgcn_readfirstlane(limit_of(row0 + 31));
-  const int lim_wg = __builtin_amdgcn_readfirstlane(limit_of((int)tile * CA_ROWS + CA_ROWS - 1));
+  const Rows rows = rows_of(a, seq, tile, wave, col);
+  // the part's slots: those of a unit end at its last row's
+  const int n_parts = parts_of(a, rows.lim_unit);
+  if (part > 0 && part >= n_parts) return;
+  const int from = (int)(part * a.part_slots);
+  const int to = rows.lim_unit < from + a.part_slots ? rows.lim_unit : (int)(from + a.part_slots);
 
   Kept Kk = read_kept(a.bits_k + kv * NG), Kv = read_kept(a.bits_v + kv * NG);
   if (!Kk.ok || Kk.used > a.Wk) Kk.n = 0;  // width table inconsistent with the record
@@ -209,7 +312,7 @@ __global__ __launch_bounds__(64 * CA_NW, 2) void paged_chunk_kernel(PagedAttnArg
   f16x8 qb[NG][2], ql[PRECISE ? NG : 1][2];
   float unscale;
   {
-    const int64_t qoff = (seq.first + tok) * a.q_token_stride + head * a.q_head_stride + 8 * h;
+    const int64_t qoff = (seq.first + rows.tok) * a.q_token_stride + (kv * a.n_qh + rows.head) * a.q_head_stride + 8 * h;
     f32x16 acc[NG];
     float most = 0.0f;
     const int i = 4 * (col >> 3) + (col & 3), hh = (col >> 2) & 1;  // MFMA row col is register i of lane half hh
@@ -277,13 +380,13 @@ __global__ __launch_bounds__(64 * CA_NW, 2) void paged_chunk_kernel(PagedAttnArg
   auto load_step = [&](int j) {
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
-      const int unit = wave + CA_NW * u;
+      const int u1 = wave + CA_NW * u;
       meta[u] = 0u;
 #pragma unroll
       for (int i = 0; i < 8; ++i) words[u][i] = 0u;
-      if (unit >= KT * ns) continue;
-      const int tl = unit >= ns ? 1 : 0, si = unit - tl * ns, jt = j * KT + tl;
-      if (jt * TILE >= lim_wg) continue;
+      if (u1 >= KT * ns) continue;
+      const int tl = u1 >= ns ? 1 : 0, si = u1 - tl * ns, jt = from / TILE + j * KT + tl;
+      if (jt * TILE >= to) continue;
       const bool val = si >= Kk.n;
       const int sl = val ? si - Kk.n : si;
       const int bits = val ? pick4(Kv.bits, sl) : pick4(Kk.bits, sl), pay = val ? pick4(Kv.pay, sl) : pick4(Kk.pay, sl);
@@ -303,25 +406,25 @@ __global__ __launch_bounds__(64 * CA_NW, 2) void paged_chunk_kernel(PagedAttnArg
 #pragma unroll
   for (int sl = 0; sl < NG; ++sl) acc[sl] = zero16();
   float m_run = -__builtin_inff(), l_run = 0.0f;
-  const int n_steps = (lim_wg + KT * TILE - 1) / (KT * TILE);
+  const int n_steps = (to - from + KT * TILE - 1) / (KT * TILE);
   if (n_steps > 0) load_step(0);
 #pragma unroll 1
   for (int j = 0; j < n_steps; ++j) {
     __syncthreads();  // every wavefront is done with the last step's tiles
 #pragma unroll
     for (int u = 0; u < UNITS; ++u) {
-      const int unit = wave + CA_NW * u;
-      if (unit >= KT * ns) continue;
-      const int tl = unit >= ns ? 1 : 0, si = unit - tl * ns;
+      const int u1 = wave + CA_NW * u;
+      if (u1 >= KT * ns) continue;
+      const int tl = u1 >= ns ? 1 : 0, si = u1 - tl * ns;
       const int bits = si >= Kk.n ? pick4(Kv.bits, si - Kk.n) : pick4(Kk.bits, si);
       with_bits(bits, [&](auto bc) {
-        write_coefficients<decltype(bc)::value, PRECISE>(words[u], meta[u], tiles + unit * CA_TILE, lane, lo_off, magic);
+        write_coefficients<decltype(bc)::value, PRECISE>(words[u], meta[u], tiles + u1 * CA_TILE, lane, lo_off, magic);
       });
     }
     if (j + 1 < n_steps) load_step(j + 1);
     __syncthreads();  // the step's tiles are in LDS
-    const int t0 = j * KT * TILE;
-    if (t0 >= lim_last) continue;
+    const int t0 = from + j * KT * TILE;
+    if (t0 >= rows.lim_last) continue;
     f32x16 S[2 * KT];
 #pragma unroll
     for (int k = 0; k < 2 * KT; ++k) {
@@ -348,13 +451,13 @@ __global__ __launch_bounds__(64 * CA_NW, 2) void paged_chunk_kernel(PagedAttnArg
         S[k][i] *= unscale;
       }
     }
-    if (t0 + KT * TILE > lim_first) {  // some row of the wavefront does not see the whole step
+    if (t0 + KT * TILE > rows.lim_first) {  // some row of the wavefront does not see the whole step
 #pragma unroll
       for (int k = 0; k < 2 * KT; ++k)
 #pragma unroll
         for (int i = 0; i < 16; ++i) {
           const int t = t0 + 32 * k + 8 * (i >> 2) + 4 * h + (i & 3);
-          S[k][i] = t < lim ? S[k][i] : -__builtin_inff();
+          S[k][i] = t < rows.lim ? S[k][i] : -__builtin_inff();
         }
     }
     float top = S[0][0];
@@ -420,79 +523,55 @@ __global__ __launch_bounds__(64 * CA_NW, 2) void paged_chunk_kernel(PagedAttnArg
     }
   }
 
-  // ---- out = (a / l + m_V) V_V^T: the coefficients as column operand in bf16 parts ----
   const float l = l_run + other_half(l_run);
-  const bool seen = l > 0.0f || !(l == l);
-  const float inv = 1.0f / l;
-  const float* Vv = a.basis_v + (int64_t)kv * D * D;
-  f32x16 out[4];
+  if (n_parts > 1) {
+    float* p = a.partial + part_at(a, unit, kv, part, wave) + lane;
 #pragma unroll
-  for (int cb = 0; cb < 4; ++cb) out[cb] = zero16();
-  const int i0 = 4 * (col >> 3) + (col & 3), h0 = (col >> 2) & 1;
-  const int chan = 16 * h0 + i0;  // MFMA row col of a 32-channel block: then a lane half has 16 neighbouring channels
+    for (int sl = 0; sl < NG; ++sl)
+      if (sl < Kv.n)
 #pragma unroll
-  for (int g = 0; g < NG; ++g) {
-    int sl = -1;
-#pragma unroll
-    for (int x = 0; x < NG; ++x) sl = (x < Kv.n && Kv.grp[x] == g) ? x : sl;
-    f32x16 av = zero16();
-#pragma unroll
-    for (int x = 0; x < NG; ++x)
-      if (x == sl) av = acc[x];
-#pragma unroll
-    for (int s = 0; s < 2; ++s) {
-      float cf[8];
-      int at[8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        const int place = 16 * s + 8 * (e >> 2) + 4 * h + (e & 3);  // of register 8 s + e
-        at[e] = G * g + 4 * (place >> 3) + ((place & 7) >> 1) + 16 * (place & 1);
-        cf[e] = (sl >= 0 ? av[8 * s + e] * inv : 0.0f) + a.mean_v[kv * D + at[e]];
-      }
-      bf16x8 cp[NP];
-      split8<NP>(cf, cp);
-#pragma unroll
-      for (int cb = 0; cb < 4; ++cb) {
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = Vv[(32 * cb + chan) * D + at[e]];
-        bf16x8 vp[NP];
-        split8<NP>(v, vp);
-#pragma unroll
-        for (int x = 0; x < NP; ++x)
-#pragma unroll
-          for (int y = 0; x + y < NP; ++y)
-            out[cb] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vp[x], cp[y], out[cb], 0, 0, 0);
-      }
-    }
+        for (int i = 0; i < 16; ++i) p[(16 * sl + i) * 64] = acc[sl][i];
+    p[16 * NG * 64] = m_run;
+    p[(16 * NG + 1) * 64] = l;
+    return;
   }
-  if (row >= n_rows) return;
-  const int64_t o = ((seq.first + tok) * a.n_q_heads + head) * D + 16 * h;
+  finish_rows<NP>(a, seq, rows, kv, Kv, acc, m_run, l, lane);
+}
+
+// ---------------------------------------------------------------------------
+// Join of a unit's parts: a wavefront per 32 rows, on registers as the parts left them.
+// ---------------------------------------------------------------------------
+template <bool PRECISE>
+__global__ __launch_bounds__(64) void paged_join_kernel(PagedAttnArgs a) {
+  __shared__ FindScratch find_s;
+  const int kv = (int)(blockIdx.x % (unsigned)a.c.n_kv), wave = blockIdx.y, lane = threadIdx.x;
+  const int64_t unit = blockIdx.x / (unsigned)a.c.n_kv;
+  int b;
+  int64_t tile;
+  if (!find_unit<1>(a, unit, find_s, b, tile)) return;
+  const PagedSeq seq = paged_seq(a.c, b);
+  const Rows rows = rows_of(a, seq, tile, wave, lane & 31);
+  const int n_parts = parts_of(a, rows.lim_unit);
+  if (n_parts <= 1) return;  // done by the part itself
+  Kept Kv = read_kept(a.bits_v + kv * NG);
+  if (!Kv.ok || Kv.used > a.Wv) Kv.n = 0;
+  float m = -__builtin_inff(), l = 0.0f;
+  const int ml = 16 * NG * 64 + lane;
+  for (int i = 0; i < n_parts; ++i) m = __builtin_fmaxf(m, a.partial[part_at(a, unit, kv, i, wave) + ml]);
+  f32x16 acc[NG];
 #pragma unroll
-  for (int cb = 0; cb < 4; ++cb) {
-    if (a.out_f32) {
-      float* op = reinterpret_cast<float*>(a.out) + o + 32 * cb;
+  for (int sl = 0; sl < NG; ++sl) acc[sl] = zero16();
+  for (int i = 0; i < n_parts; ++i) {
+    const float* p = a.partial + part_at(a, unit, kv, i, wave);
+    const float mi = p[ml], f = mi == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(mi - m);
+    l = __builtin_fmaf(f, p[ml + 64], l);
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        *reinterpret_cast<f32x4*>(op + 4 * i) = seen ? f32x4{out[cb][4 * i], out[cb][4 * i + 1], out[cb][4 * i + 2], out[cb][4 * i + 3]}
-                                                     : f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-    } else {
-      uint32_t* op = reinterpret_cast<uint32_t*>(reinterpret_cast<uint16_t*>(a.out) + o + 32 * cb);
-      uint32_t w[8];
+    for (int sl = 0; sl < NG; ++sl)
+      if (sl < Kv.n)
 #pragma unroll
-      for (int i = 0; i < 8; ++i)
-        w[i] = seen ? __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{out[cb][2 * i], out[cb][2 * i + 1]}, bf16x2)) : 0u;
-      *reinterpret_cast<u32x4*>(op) = u32x4{w[0], w[1], w[2], w[3]};
-      *reinterpret_cast<u32x4*>(op + 4) = u32x4{w[4], w[5], w[6], w[7]};
-    }
+        for (int j = 0; j < 16; ++j) acc[sl][j] = __builtin_fmaf(f, p[(16 * sl + j) * 64 + lane], acc[sl][j]);
   }
-  if (a.lse != nullptr && h == 0) {
-    const int64_t qo = (seq.first + tok) * a.q_token_stride + head * a.q_head_stride;
-    float s = 0.0f;
-    for (int c = 0; c < D; ++c) s = __builtin_fmaf(query_at(a, qo + c), a.lse_u[kv * D + c], s);
-    a.lse[(seq.first + tok) * a.n_q_heads + head] =
-        seen ? __builtin_fmaf(__builtin_amdgcn_logf(l) + (m_run - CA_LIFT), LN2, s) : -__builtin_inff();
-  }
+  finish_rows<PRECISE ? 3 : 2>(a, seq, rows, kv, Kv, acc, m, l, lane);
 }
 
 // ---------------------------------------------------------------------------
@@ -515,25 +594,36 @@ __global__ __launch_bounds__(256) void paged_lse_kernel(PagedAttnArgs a) {
 namespace spectra {
 using namespace spectra_dev;
 
-size_t paged_attention_ws_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv, int32_t max_new,
-                                int64_t max_tokens) {
-  return (size_t)n_kv * D * sizeof(float);
-}
+static_assert(PAGED_STEP % (2 * TILE) == 0, "whole steps in a part");
+
+static_assert(CA_ROWS == PAGED_ROWS && CA_NW * (16 * NG + 2) * 64 * sizeof(float) == PAGED_PART_BYTES, "workspace of a part");
 
 hipError_t launch_paged_attention(const PagedAttnArgs& args, void* workspace, hipStream_t st) {
   PagedAttnArgs a = args;
-  a.lse_u = reinterpret_cast<float*>(workspace);
+  const PagedPlan p = paged_plan(a.c.batch, a.c.n_new, a.n_q_heads, a.c.n_kv, a.max_new, a.max_tokens,
+                                 scan_rows(a.Wk, a.Wv));
+  char* ws = static_cast<char*>(workspace);
+  a.lse_u = reinterpret_cast<float*>(ws);
+  a.scan_tokens = p.scan_tokens;
+  a.part_slots = p.split.slots;
+  a.parts = p.split.parts;
+  a.partial = reinterpret_cast<float*>(ws + p.part_at);
   if (a.lse != nullptr) hipLaunchKernelGGL(paged_lse_kernel, dim3(a.c.n_kv), dim3(256), 0, st, a);
-  const int64_t per_seq = ((int64_t)a.max_new * a.n_qh + CA_ROWS - 1) / CA_ROWS;
-  int64_t units = a.c.n_new * a.n_qh / CA_ROWS + a.c.batch;
-  if (units > per_seq * a.c.batch) units = per_seq * a.c.batch;
-  const int groups = (a.Wk / 2 < NG ? a.Wk / 2 : NG) + (a.Wv / 2 < NG ? a.Wv / 2 : NG);  // a kept group takes two words
-  const dim3 grid((unsigned)(units * a.c.n_kv));
-  if (a.out_f32)
-    hipLaunchKernelGGL((paged_chunk_kernel<true>), grid, dim3(64 * CA_NW), 2 * groups * CA_TILE, st, a);
-  else
-    hipLaunchKernelGGL((paged_chunk_kernel<false>), grid, dim3(64 * CA_NW), 2 * groups * CA_TILE, st, a);
-  return hipGetLastError();
+  hipError_t e = hipSuccess;
+  if (p.units > 0) {
+    const int groups = (a.Wk / 2 < NG ? a.Wk / 2 : NG) + (a.Wv / 2 < NG ? a.Wv / 2 : NG);  // a kept group takes two words
+    const dim3 grid((unsigned)(p.units * a.c.n_kv), (unsigned)p.split.parts), join((unsigned)(p.units * a.c.n_kv), CA_NW);
+    if (a.out_f32) {
+      hipLaunchKernelGGL((paged_chunk_kernel<true>), grid, dim3(64 * CA_NW), 2 * groups * CA_TILE, st, a);
+      if (p.split.parts > 1) hipLaunchKernelGGL((paged_join_kernel<true>), join, dim3(64), 0, st, a);
+    } else {
+      hipLaunchKernelGGL((paged_chunk_kernel<false>), grid, dim3(64 * CA_NW), 2 * groups * CA_TILE, st, a);
+      if (p.split.parts > 1) hipLaunchKernelGGL((paged_join_kernel<false>), join, dim3(64), 0, st, a);
+    }
+    e = hipGetLastError();
+  }
+  if (e == hipSuccess && p.scan_tokens > 0) e = launch_paged_scan(a, reinterpret_cast<float*>(ws + p.scan_at), st);
+  return e;
 }
 
 }  // namespace spectra

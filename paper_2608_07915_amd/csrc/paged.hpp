@@ -70,12 +70,17 @@ struct PagedAttnArgs {
   int32_t q_f32, out_f32;
   int32_t n_q_heads, n_qh;
   int32_t max_new;
+  int32_t scan_tokens;  // sequences with at most so many new tokens are the scan kernel's
   int32_t Wk, Wv;
   int64_t max_tokens;
   float scale_log2;  // softmax scale * log2(e)
   void* out;         // [n_new][n_q_heads][128]
   float* lse;        // [n_new][n_q_heads] or null
   float* lse_u;      // workspace: scale V_K m_K of each KV head
+  // chunk kernel: the slots of a part, parts, and their results (joined when a unit has several)
+  int64_t part_slots;
+  int32_t parts;
+  float* partial;
 };
 
 }  // namespace spectra_dev
@@ -93,7 +98,7 @@ hipError_t launch_pages_compact(const spectra_dev::PageMap& m, int32_t* moved, c
 hipError_t launch_page_copies(const spectra_dev::PoolList& pools, const spectra_dev::PageMoves& mv, int64_t most_moves,
                               hipStream_t st);
 hipError_t launch_paged_encode(const spectra_dev::PagedEncodeArgs& a, bool f32_input, hipStream_t st);
-size_t paged_attention_ws_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv, int32_t max_new,
-                                int64_t max_tokens);
+// Sequences of at most a.scan_tokens new tokens (a.scan_tokens * n_qh <= scan_rows), partials in `partial`.
+hipError_t launch_paged_scan(const spectra_dev::PagedAttnArgs& a, float* partial, hipStream_t st);
 hipError_t launch_paged_attention(const spectra_dev::PagedAttnArgs& a, void* workspace, hipStream_t st);
 }  // namespace spectra

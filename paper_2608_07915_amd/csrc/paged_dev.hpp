@@ -42,4 +42,24 @@ __device__ __forceinline__ Word* paged_tile(const PagedCache& c, Word* pool, int
   return pool + (((int64_t)page * c.n_kv + kv) * tpp + (tile - at * tpp)) * (int64_t)(TILE * W);
 }
 
+// Sequences past the call's bounds are left out, their rows as they were.
+__device__ __forceinline__ bool attended(const PagedAttnArgs& a, const PagedSeq& s) {
+  return s.n <= a.max_new && s.len <= a.max_tokens;
+}
+// Few new tokens: the scan's; the others are the chunk kernel's.
+__device__ __forceinline__ bool scanned(const PagedAttnArgs& a, const PagedSeq& s) {
+  return s.n > 0 && s.n <= a.scan_tokens && attended(a, s);
+}
+
+__device__ __forceinline__ float query_at(const PagedAttnArgs& a, int64_t i) {
+  return a.q_f32 ? reinterpret_cast<const float*>(a.q)[i] : bf2f(reinterpret_cast<const uint16_t*>(a.q)[i]);
+}
+
+// A metadata word, 0 where its scale or zero point is NaN or infinite.
+__device__ __forceinline__ uint32_t finite_or_zero(uint32_t m) {
+  return (m & 0x7C00u) == 0x7C00u || (m & 0x7C000000u) == 0x7C000000u ? 0u : m;
+}
+
+constexpr float LN2 = 0.69314718055994531f;
+
 }  // namespace spectra_dev

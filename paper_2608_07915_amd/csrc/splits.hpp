@@ -206,4 +206,100 @@ inline RopeSplit rope_split(int64_t groups, int n_qh, int words, int64_t n_tiles
   return RopeSplit{RopeKernel::EIGHT, rope_chunks(groups, n_tiles, 1, 1)};
 }
 
+// ---------------------------------------------------------------------------
+// Paged attention
+// ---------------------------------------------------------------------------
+// Scan of sequences with few new tokens: chunks of whole steps of four wavefronts for at most
+// one round of workgroups over all sequences at the longest length.
+inline int64_t paged_scan_wanted(int64_t groups, int per_cu) {
+  const int64_t n = N_CU * per_cu / groups;
+  return n < 1 ? 1 : n;
+}
+inline Split paged_scan_split(int64_t groups, int64_t n_tiles, int per_cu) {
+  int64_t tpc = ceil_div(n_tiles, paged_scan_wanted(groups, per_cu));
+  if (tpc < 2 * SCAN_WAVES) tpc = 2 * SCAN_WAVES;
+  return split_tiles(n_tiles, ceil_div(tpc, SCAN_WAVES) * SCAN_WAVES);
+}
+// The most chunks that any cache of up to n_tiles tiles is split into.
+inline int64_t paged_scan_chunks(int64_t groups, int64_t n_tiles) {
+  const int64_t most = ceil_div(n_tiles, 2 * SCAN_WAVES), want = paged_scan_wanted(groups, 3);
+  return most < want ? most : want;
+}
+
+// Workgroups of 256 rows, of which a CU holds one, take a step of 128 slots at a time. With
+// fewer of them than CUs, or a last round that leaves many idle, the slots are split: as many
+// ways as end soonest, a step counted one, a workgroup's start and the join of its parts eight.
+struct ChunkSplit {
+  int64_t slots;  // of a part, whole steps
+  int32_t parts;
+};
+constexpr int64_t PAGED_STEP = 128;
+inline ChunkSplit paged_chunk_split(int64_t groups, int64_t max_tokens) {
+  const int64_t steps = ceil_div(max_tokens, PAGED_STEP);
+  int64_t best = 1, best_cost = 0;
+  for (int64_t n = 1; n <= 64 && n <= steps && (n == 1 || n * groups <= 2 * N_CU); ++n) {
+    const int64_t cost = ceil_div(groups * n, N_CU) * (ceil_div(steps, n) + 8) + (n > 1 ? 8 + n / 4 : 0);
+    if (n == 1 || cost < best_cost) {
+      best = n;
+      best_cost = cost;
+    }
+  }
+  const int64_t each = ceil_div(steps, best);
+  return ChunkSplit{each * PAGED_STEP, (int32_t)ceil_div(steps, each)};
+}
+
+// How a call's work is laid out, from what the host knows of it: `batch` sequences of n_new new
+// tokens in all, none with more than max_new or longer than max_tokens. scan_rows: rows that the
+// scan takes of a sequence and KV head (12 or 16, by the records' width).
+constexpr int32_t PAGED_ROWS = 256;                      // query rows of a chunk workgroup
+constexpr size_t PAGED_PART_BYTES = 8 * (16 * 4 + 2) * 64 * 4;  // results of one of its parts
+constexpr size_t SCAN_PART_BYTES = 136 * 4;              // of a scanned row's chunk
+struct PagedPlan {
+  int32_t scan_tokens;  // sequences of at most so many new tokens are scanned (0: none)
+  int64_t units;        // of PAGED_ROWS rows, for the others (0: none)
+  ChunkSplit split;
+  size_t scan_at, part_at, bytes;  // workspace: lse terms, then the scan's partials, then the parts
+};
+inline size_t paged_round(size_t b) { return (b + 255) / 256 * 256; }
+inline int64_t paged_units(int32_t batch, int64_t n_new, int32_t n_qh, int32_t max_new) {
+  const int64_t all = n_new * n_qh / PAGED_ROWS + batch, most = ceil_div((int64_t)max_new * n_qh, PAGED_ROWS) * batch;
+  return all < most ? all : most;
+}
+inline PagedPlan paged_plan(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv, int32_t max_new, int64_t max_tokens,
+                            int32_t scan_rows) {
+  PagedPlan p{};
+  const int32_t n_qh = n_q_heads / n_kv, few = scan_rows / n_qh;
+  // the scan takes sequences of few rows; none where every sequence has max_new
+  p.scan_tokens = max_new <= few ? max_new : (n_new < (int64_t)batch * max_new ? few : 0);
+  p.split = ChunkSplit{max_tokens, 1};
+  if (max_new > p.scan_tokens) {
+    p.units = paged_units(batch, n_new, n_qh, max_new);
+    p.split = paged_chunk_split(p.units * n_kv, max_tokens);
+  }
+  p.scan_at = paged_round((size_t)n_kv * 128 * sizeof(float));
+  p.part_at = p.scan_at;
+  if (p.scan_tokens > 0)
+    p.part_at += paged_round((size_t)batch * p.scan_tokens * n_q_heads * SCAN_PART_BYTES *
+                             (size_t)paged_scan_chunks((int64_t)batch * n_kv, ceil_div(max_tokens, 64)));
+  p.bytes = p.part_at + (p.split.parts > 1 ? (size_t)(p.units * n_kv * p.split.parts) * PAGED_PART_BYTES : 0);
+  return p;
+}
+// What any call with at most these counts needs, so that a workspace taken for the largest
+// serves every smaller one.
+inline size_t paged_workspace_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv, int32_t max_new, int64_t max_tokens) {
+  const int32_t n_qh = n_q_heads / n_kv, few = 16 / n_qh;
+  const int64_t groups = (int64_t)batch * n_kv, tiles = ceil_div(max_tokens, 64), steps = ceil_div(max_tokens, PAGED_STEP);
+  int64_t scan = groups * ceil_div(tiles, 2 * SCAN_WAVES);  // chunks of all sequences
+  const int64_t round = groups > 3 * N_CU ? groups : 3 * N_CU;
+  if (scan > round) scan = round;
+  size_t b = paged_round((size_t)n_kv * 128 * sizeof(float)) +
+             paged_round((size_t)(scan * n_qh * (max_new < few ? max_new : few)) * SCAN_PART_BYTES);
+  if (max_new > 12 / n_qh) {
+    int64_t parts = paged_units(batch, n_new, n_qh, max_new) * n_kv * (steps < 64 ? steps : 64);
+    if (parts > 2 * N_CU) parts = 2 * N_CU;
+    b += (size_t)parts * PAGED_PART_BYTES;
+  }
+  return b;
+}
+
 }  // namespace spectra

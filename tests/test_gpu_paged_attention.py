@@ -75,6 +75,8 @@ class Case:
                                                       softmax_scale or default_scale())
                 bf16 = out.dtype == torch.bfloat16
                 tol = allowed(want, swing, most, max(L, 1), bf16, not bf16)
+                if n * self.n_qh <= 16:
+                    tol = tol + 2.0 ** -16 * swing  # few rows: softmax weights are two bf16 parts (2^-17)
                 off = np.abs(got[at:at + n, hs] - want)
                 assert (off <= tol).all(), (b, h, float((off / np.maximum(tol, 1e-300)).max()))
                 worst = max(worst, float((off / np.maximum(tol, 1e-300)).max(initial=0.0)))
