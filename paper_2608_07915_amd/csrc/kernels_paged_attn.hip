@@ -45,7 +45,7 @@ __device__ __forceinline__ int piece_at(int t, int piece) { return t * 64 + ((pi
 // A token's metadata word of a b-bit group, made finite: NaN or infinite scales count as 0, and
 // the scale is lowered where z + s (2^b - 1) would pass fp16's largest number.
 __device__ __forceinline__ uint32_t finite_meta(uint32_t m, int b) {
-  if ((m & 0x7C00u) == 0x7C00u || (m & 0x7C000000u) == 0x7C000000u) return 0u;
+  m = finite_or_zero(m);
   const float s = h2f(m), z = h2f(m >> 16), top = (float)((1 << b) - 1);
   if (__builtin_fabsf(__builtin_fmaf(s, top, z)) > 65504.0f)
     m = (m & 0xFFFF0000u) | f2h_sat((__builtin_copysignf(65472.0f, s) - z) / top);
@@ -85,6 +85,7 @@ __device__ __forceinline__ void write_coefficients(const uint32_t (&w)[8], uint3
   }
 }
 
+typedef __fp16 h16x2 __attribute__((ext_vector_type(2)));
 typedef short s16x4 __attribute__((ext_vector_type(4)));
 typedef __attribute__((address_space(3))) s16x4 lds_s16x4;
 __device__ __forceinline__ u32x2 read_transposed(const uint8_t* p) {
@@ -164,17 +165,17 @@ __device__ __forceinline__ bool find_unit(const PagedAttnArgs& a, int64_t unit, 
   return b >= 0;
 }
 
-// The 32 rows of a wavefront: row = new token x query heads on the KV head + query head. Rows
-// past the sequence's last repeat that one and are not stored.
+// Row block `block` of a unit: 32 rows, row = new token x query heads on the KV head + query head.
+// Rows past the sequence's last repeat that one and are not stored.
 struct Rows {
-  int tok, head;      // of the lane's row
+  int tok, head;  // of the lane's row
   bool live;
-  int lim;            // slots that it sees
-  int lim_first, lim_last, lim_unit;  // the wavefront's first row, its last, the unit's last
+  int lim;        // slots that it sees
+  int lim_first, lim_last, lim_unit;  // that the block's first row sees, its last, the unit's last
 };
-__device__ __forceinline__ Rows rows_of(const PagedAttnArgs& a, const PagedSeq& seq, int64_t tile, int wave, int col) {
+__device__ __forceinline__ Rows rows_of(const PagedAttnArgs& a, const PagedSeq& seq, int64_t tile, int block, int col) {
   const int n_rows = (int)(seq.n * a.n_qh), past = (int)(seq.len - seq.n) + 1;  // slots that token 0 sees
-  const int row0 = (int)tile * CA_ROWS + 32 * wave, row = row0 + col;
+  const int row0 = (int)tile * CA_ROWS + 32 * block, row = row0 + col;
   auto limit = [&](int r) {
     const int l = past + (r < n_rows ? r : n_rows - 1) / a.n_qh;
     return l < 0 ? 0 : l;
@@ -191,18 +192,18 @@ __device__ __forceinline__ Rows rows_of(const PagedAttnArgs& a, const PagedSeq& 
   return x;
 }
 
-// Parts that a unit seeing lim slots has, and where a wavefront's results of one lie: 16 floats
+// Parts that a unit seeing lim slots has, and where a row block's results of one lie: 16 floats
 // per value group and lane, then m and l.
 __device__ __forceinline__ int parts_of(const PagedAttnArgs& a, int lim) { return (int)((lim + a.part_slots - 1) / a.part_slots); }
-__device__ __forceinline__ int64_t part_at(const PagedAttnArgs& a, int64_t unit, int kv, int part, int wave) {
-  return (((unit * a.c.n_kv + kv) * a.parts + part) * CA_NW + wave) * ((16 * NG + 2) * 64);
+__device__ __forceinline__ int64_t part_at(const PagedAttnArgs& a, int64_t unit, int kv, int part, int block) {
+  return (((unit * a.c.n_kv + kv) * a.parts + part) * CA_NW + block) * ((16 * NG + 2) * 64);
 }
 
 // out = (a / l + m_V) V_V^T of a wavefront's 32 rows, the coefficients as column operand, and
 // both sides in NP bf16 parts; stores the rows and their log-sum-exp. m, l: of the lane's row.
-template <int NP>
+template <int NP, int N>
 __device__ __forceinline__ void finish_rows(const PagedAttnArgs& a, const PagedSeq& seq, const Rows& r, int kv, const Kept& Kv,
-                                            const f32x16 (&acc)[NG], float m, float l, int lane) {
+                                            const f32x16 (&acc)[N], float m, float l, int lane) {
   const int h = lane >> 5, col = lane & 31;
   const bool seen = l > 0.0f || !(l == l);
   const float inv = 1.0f / l;
@@ -216,10 +217,10 @@ __device__ __forceinline__ void finish_rows(const PagedAttnArgs& a, const PagedS
   for (int g = 0; g < NG; ++g) {
     int sl = -1;
 #pragma unroll
-    for (int x = 0; x < NG; ++x) sl = (x < Kv.n && Kv.grp[x] == g) ? x : sl;
+    for (int x = 0; x < N; ++x) sl = (x < Kv.n && Kv.grp[x] == g) ? x : sl;
     f32x16 av = zero16();
 #pragma unroll
-    for (int x = 0; x < NG; ++x)
+    for (int x = 0; x < N; ++x)
       if (x == sl) av = acc[x];
 #pragma unroll
     for (int s = 0; s < 2; ++s) {
@@ -273,269 +274,505 @@ __device__ __forceinline__ void finish_rows(const PagedAttnArgs& a, const PagedS
     float s = 0.0f;
     for (int c = 0; c < D; ++c) s = __builtin_fmaf(query_at(a, qo + c), a.lse_u[kv * D + c], s);
     a.lse[(seq.first + r.tok) * a.n_q_heads + kv * a.n_qh + r.head] =
-        seen ? __builtin_fmaf(__builtin_amdgcn_logf(l) + (m - CA_LIFT), LN2, s) : -__builtin_inff();
+        seen ? __builtin_fmaf(__builtin_amdgcn_logf(l) + m, LN2, s) : -__builtin_inff();
   }
 }
 
+// ---------------------------------------------------------------------------
+// A workgroup's group tiles: 64 slots of a kept group each, KT slot tiles of NK key and NV value
+// groups a step, shared out over the wavefronts. A lane has one slot's words in registers, loaded
+// a step before they are written to LDS, its page read another step ahead. Key tiles begin KOFF
+// slots later than value tiles (see chunk_steps).
+// ---------------------------------------------------------------------------
+template <int NK, int NV, int KT, int KOFF>
+struct GroupTiles {
+  static constexpr int NS = NK + NV, N = KT * NS, UNITS = (N + CA_NW - 1) / CA_NW;
+  uint32_t words[UNITS][8], meta[UNITS];
+  int page[UNITS], in_page[UNITS];  // of the slot to load next: its page, and its record's place in it
+  int idx[UNITS], off[UNITS];       // of the slot to look up next: page index and slot in the page
+  int bits[UNITS], pay[UNITS], slot[UNITS], first[UNITS];  // uniform; 0 bits: no such group, zeros
+  bool val[UNITS];
+  int64_t page_words[2];
+  const uint32_t* base[2];
+
+  __device__ __forceinline__ void init(const PagedAttnArgs& a, int kv, const Kept& Kk, const Kept& Kv, int wave) {
+    base[0] = a.pool_k + (int64_t)kv * a.c.page_tokens * a.Wk;
+    base[1] = a.pool_v + (int64_t)kv * a.c.page_tokens * a.Wv;
+    page_words[0] = (int64_t)a.c.n_kv * a.c.page_tokens * a.Wk;
+    page_words[1] = (int64_t)a.c.n_kv * a.c.page_tokens * a.Wv;
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+      const int x = wave + CA_NW * u, si = x % NS;
+      val[u] = si >= NK;
+      slot[u] = val[u] ? si - NK : si;
+      first[u] = x / NS * TILE + (val[u] ? 0 : KOFF);
+      bits[u] = val[u] ? pick4(Kv.bits, slot[u]) : pick4(Kk.bits, slot[u]);
+      pay[u] = val[u] ? pick4(Kv.pay, slot[u]) : pick4(Kk.pay, slot[u]);
+      if (x >= N || slot[u] >= (val[u] ? Kv.n : Kk.n)) bits[u] = 0;
+      page[u] = -1;
+      in_page[u] = 0;
+    }
+  }
+  // The pages of the step whose slots begin at t0 (any t0, by division: where a walk begins).
+  __device__ __forceinline__ void look_up_at(const PagedAttnArgs& a, int row, int t0, int from, int to, int lane) {
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+      const int t = t0 + first[u] + lane;
+      idx[u] = (t < 0 ? 0 : t) / a.c.page_tokens;
+      off[u] = t - idx[u] * a.c.page_tokens;
+    }
+    look_up(a, row, t0, from, to, lane);
+  }
+  // The same, and the walk goes on by a step.
+  __device__ __forceinline__ void look_up(const PagedAttnArgs& a, int row, int t0, int from, int to, int lane) {
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+      const int t = t0 + first[u] + lane;
+      page[u] = -1;
+      if (bits[u] != 0 && t >= from && t < to) page[u] = a.c.table[(int64_t)row * a.c.row_pages + idx[u]];
+      in_page[u] = (off[u] & -TILE) * (val[u] ? a.Wv : a.Wk) + (off[u] & (TILE - 1));
+      off[u] += KT * TILE;
+#pragma unroll
+      for (int i = 0; i < KT; ++i) {  // a page has at least one tile
+        const bool next = off[u] >= a.c.page_tokens;
+        off[u] -= next ? a.c.page_tokens : 0;
+        idx[u] += next ? 1 : 0;
+      }
+    }
+  }
+  // The words of the step looked up last; slots without a page of the pool: zeros (metadata 0).
+  __device__ __forceinline__ void load(const PagedAttnArgs& a) {
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+      meta[u] = 0u;
+      if (page[u] < 0 || page[u] >= a.c.n_pages) continue;
+      const uint32_t* rec = (val[u] ? base[1] : base[0]) + (int64_t)page[u] * (val[u] ? page_words[1] : page_words[0]) + in_page[u];
+      meta[u] = rec[slot[u] * TILE];
+#pragma unroll
+      for (int i = 0; i < 8; ++i)
+        if (i < bits[u]) words[u][i] = rec[(pay[u] + i) * TILE];
+    }
+  }
+  // The loaded step's coefficients into the buffer `buf` (low parts: lo bytes further).
+  template <bool PRECISE>
+  __device__ __forceinline__ void write(uint8_t* buf, int lo, int wave, int lane, uint32_t magic) {
+#pragma unroll
+    for (int u = 0; u < UNITS; ++u) {
+      if (wave + CA_NW * u >= N) continue;
+      uint8_t* tile = buf + (wave + CA_NW * u) * CA_TILE;
+      if (bits[u] == 0) {
+        const u32x4 z = u32x4{0u, 0u, 0u, 0u};
+#pragma unroll
+        for (int k = 0; k < (PRECISE ? 8 : 4); ++k) *reinterpret_cast<u32x4*>(tile + (k >> 2) * lo + piece_at(lane, k & 3)) = z;
+      }
+      const uint32_t m = finite_meta(meta[u], bits[u]);
+      with_bits(bits[u], [&](auto bc) __attribute__((always_inline)) { write_coefficients<decltype(bc)::value, PRECISE>(words[u], m, tile, lane, lo, magic); });
+    }
+  }
+};
+
+// The slots [from, to) of a pass over a workgroup's rows; lim: slots that the lane's row sees,
+// lim_first and lim_last: the wavefront's first row and its last.
+struct Pass {
+  int row;  // of the table
+  int from, to, lim_first, lim_last;
+};
+
+// A lane's row in a row block: the result of a pass.
+struct RowSum {
+  float m, l;  // reference of the weights (log2; -inf: none), their sum over the lane's slots
+};
+
+__device__ __forceinline__ float max16(const f32x16& S) {
+  float top = __builtin_fmaxf(S[0], S[1]);
+#pragma unroll
+  for (int i = 2; i < 16; ++i) top = __builtin_fmaxf(top, S[i]);
+  return top;
+}
+
+// Value operand of 32 slots (block k of a slot tile), transposed: K element 8 h + e of product s is
+// slot 16 s + 8 (e / 4) + 4 h + e % 4, as the weights' registers have them.
+__device__ __forceinline__ f16x8 value_operand(const uint8_t* tile, int k, int s, int lane) {
+  const int piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1), t = 32 * k + 16 * s + 4 * (lane >> 5) + ((lane & 15) >> 2);
+  const uint8_t* p = tile + 8 * (lane & 1);
+  const u32x2 x0 = read_transposed(p + piece_at(t, piece)), x1 = read_transposed(p + piece_at(t + 8, piece));
+  return as_f16x8(u32x4{x0[0], x0[1], x1[0], x1[1]});
+}
+__device__ __forceinline__ f16x8 key_operand(const uint8_t* tile, int k, int s, int h, int col) {
+  return as_f16x8(*reinterpret_cast<const u32x4*>(tile + piece_at(32 * k + col, 2 * s + h)));
+}
+
+// ---------------------------------------------------------------------------
+// 16-bit outputs. A wavefront has 32 rows and goes 32 slots at a time; all counts are compile-time,
+// so a block is straight-line code (with the groups counted at run time a 4096-token chunk over 32k
+// slots took 2.7 ms). Weights are exp2(S - ref); the reference moves only when a score passes it by
+// CA_SLACK, in all rows at once, which after the first block is rare.
+// The score products of the next block run among the exponentials and value products of this one;
+// as keys are then wanted a block earlier than values, key tiles begin 32 slots later.
+// Two buffers of tiles, one barrier a step of two slot tiles. Two wavefronts on a SIMD: three or
+// four of them without the lead, so with fewer registers, came to the same rate a row.
+// Bound by the vector unit and the matrix cores together: per 32 rows and 32 slots, 16 exponentials,
+// 16 differences, 8 maxima, 8 conversions and 8 sums, and 8 to 16 matrix instructions; making the
+// coefficients takes a fifth of the time (4096 rows of four heads a KV head over 32k slots, two
+// groups: 1.47 ms, 1.17 without it).
+// ---------------------------------------------------------------------------
+template <int NK, int NV>
+__device__ __forceinline__ void chunk_steps(const PagedAttnArgs& a, int kv, const Kept& Kk, const Kept& Kv, const Pass& pass, int lim,
+                                            uint8_t* tiles, int wave, int lane, const f16x8 (&qb)[NK][2], f32x16 (&acc)[NV],
+                                            RowSum& sum) {
+  constexpr int KT = 2, NS = NK + NV, BUF = KT * NS * CA_TILE, STEP = KT * TILE;
+  const int h = lane >> 5, col = lane & 31;
+  uint32_t magic = 0x64006400u;  // exponent of 1024 in both halves, in a VGPR
+  asm volatile("" : "+v"(magic));
+  float ref = 0.0f, l = 0.0f;  // the reference less CA_LIFT
+  const int n_steps = (pass.to - pass.from + STEP - 1) / STEP;
+  auto scores = [&](const uint8_t* tile, int k) {
+    f16x8 ko[NK][2];
+#pragma unroll
+    for (int sl = 0; sl < NK; ++sl)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) ko[sl][s] = key_operand(tile + sl * CA_TILE, k, s, h, col);
+    f32x16 S = zero16();
+#pragma unroll
+    for (int sl = 0; sl < NK; ++sl)
+#pragma unroll
+      for (int s = 0; s < 2; ++s) S = mfma_f16(ko[sl][s], qb[sl][s], S);
+    return S;
+  };
+  // The scores of the block at slot t0 are there: what a row does not see weighs nothing; the
+  // reference moves.
+  auto settle = [&](f32x16& S, int t0, bool begin) {
+    if (t0 + 32 > pass.lim_first) {
+      int left = lim - t0 - 4 * h;
+      asm volatile("" : "+v"(left));  // a branch: as selects this took two instructions a score in every block
+#pragma unroll
+      for (int i = 0; i < 16; ++i) S[i] = 8 * (i >> 2) + (i & 3) < left ? S[i] : -__builtin_inff();
+    }
+    float top = max16(S) - (CA_LIFT + CA_SLACK);
+    if (begin) {  // the row's largest score so far (none: left at 0)
+      top = __builtin_fmaxf(top, other_half(top));
+      ref = top == -__builtin_inff() ? 0.0f : top + CA_SLACK;
+    } else if (__any(top > ref)) {
+      top = __builtin_fmaxf(top, other_half(top));
+      const float d = top > ref ? top + CA_SLACK - ref : 0.0f, f = __builtin_amdgcn_exp2f(-d);
+      l *= f;
+      ref += d;
+#pragma unroll
+      for (int sl = 0; sl < NV; ++sl)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) acc[sl][i] *= f;
+    }
+  };
+  auto values = [&](const f16x8 (&vo)[NV][2], const f32x16& S) {
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      u32x4 w;
+#pragma unroll
+      for (int x = 0; x < 4; ++x) {
+        const f32x2 e = f32x2{__builtin_amdgcn_exp2f(S[8 * s + 2 * x] - ref), __builtin_amdgcn_exp2f(S[8 * s + 2 * x + 1] - ref)};
+        const f16x2 r = __builtin_convertvector(e, f16x2);
+        w[x] = __builtin_bit_cast(uint32_t, r);
+        // the sum of the rounded weights, two a time
+        l = __builtin_amdgcn_fdot2(__builtin_bit_cast(h16x2, r), h16x2{(__fp16)1.0f, (__fp16)1.0f}, l, false);
+      }
+#pragma unroll
+      for (int sl = 0; sl < NV; ++sl) acc[sl] = mfma_f16(vo[sl][s], as_f16x8(w), acc[sl]);
+    }
+  };
+  if (n_steps > 0) {
+    GroupTiles<NK, NV, KT, 32> g;
+    g.init(a, kv, Kk, Kv, wave);
+    // step -1 holds the first 32 keys, in the last half of its last key tile
+    g.look_up_at(a, pass.row, pass.from - STEP, pass.from, pass.to, lane);
+    g.load(a);
+    g.template write<false>(tiles + BUF, 0, wave, lane, magic);
+    g.look_up_at(a, pass.row, pass.from, pass.from, pass.to, lane);
+    g.load(a);
+    g.look_up(a, pass.row, pass.from + STEP, pass.from, pass.to, lane);
+    g.template write<false>(tiles, 0, wave, lane, magic);
+    g.load(a);
+    g.look_up(a, pass.row, pass.from + 2 * STEP, pass.from, pass.to, lane);
+    __syncthreads();
+    f32x16 S[2];
+    S[0] = scores(tiles + BUF + (KT - 1) * NS * CA_TILE, 1);
+    settle(S[0], pass.from, true);
+    __syncthreads();
+#pragma unroll 1
+    for (int j = 0; j < n_steps; ++j) {
+      const int t0 = pass.from + j * STEP;
+      if (j + 1 < n_steps) {
+        g.template write<false>(tiles + ((j + 1) & 1) * BUF, 0, wave, lane, magic);
+        g.load(a);
+        g.look_up(a, pass.row, t0 + 3 * STEP, pass.from, pass.to, lane);
+      }
+      if (t0 < pass.lim_last) {
+        const uint8_t* buf = tiles + (j & 1) * BUF;
+#pragma unroll
+        for (int i = 0; i < 2 * KT; ++i) {
+          const uint8_t* tile = buf + (i >> 1) * NS * CA_TILE;
+          f16x8 vo[NV][2];
+#pragma unroll
+          for (int sl = 0; sl < NV; ++sl)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) vo[sl][s] = value_operand(tile + (NK + sl) * CA_TILE, i & 1, s, lane);
+          f32x16& next = S[(i + 1) & 1];
+          next = scores(tile, i & 1);
+          values(vo, S[i & 1]);
+          settle(next, t0 + 32 * i + 32, false);
+        }
+      }
+      __syncthreads();  // the next step's tiles are written, this one's are free
+    }
+  }
+  sum = RowSum{l == 0.0f ? -__builtin_inff() : ref, l};
+}
+
+// ---------------------------------------------------------------------------
+// fp32 outputs: every factor in two fp16 parts, every product three matrix instructions; scores
+// carry the row's scale 2^E (unscale = 2^-E). Steps of 64 slots, the rest as above.
+// ---------------------------------------------------------------------------
+template <int NK, int NV>
+__device__ __forceinline__ void chunk_steps_precise(const PagedAttnArgs& a, int kv, const Kept& Kk, const Kept& Kv, const Pass& pass,
+                                                    int lim, float unscale, uint8_t* tiles, int wave, int lane,
+                                                    const f16x8 (&qb)[NK][2], const f16x8 (&ql)[NK][2], f32x16 (&acc)[NV], RowSum& sum) {
+  constexpr int NS = NK + NV, LO = NS * CA_TILE, BUF = 2 * LO;
+  const int h = lane >> 5, col = lane & 31;
+  uint32_t magic = 0x64006400u;
+  asm volatile("" : "+v"(magic));
+  float m_run = -__builtin_inff(), l_run = 0.0f;
+  const int n_steps = (pass.to - pass.from + TILE - 1) / TILE;
+  if (n_steps > 0) {
+    GroupTiles<NK, NV, 1, 0> g;
+    g.init(a, kv, Kk, Kv, wave);
+    g.look_up_at(a, pass.row, pass.from, pass.from, pass.to, lane);
+    g.load(a);
+    g.look_up(a, pass.row, pass.from + TILE, pass.from, pass.to, lane);
+    g.template write<true>(tiles, LO, wave, lane, magic);
+    g.load(a);
+    g.look_up(a, pass.row, pass.from + 2 * TILE, pass.from, pass.to, lane);
+    __syncthreads();
+#pragma unroll 1
+    for (int j = 0; j < n_steps; ++j) {
+      const int t0 = pass.from + j * TILE;
+      if (j + 1 < n_steps) {
+        g.template write<true>(tiles + ((j + 1) & 1) * BUF, LO, wave, lane, magic);
+        g.load(a);
+        g.look_up(a, pass.row, t0 + 3 * TILE, pass.from, pass.to, lane);
+      }
+      if (t0 < pass.lim_last) {
+        const uint8_t* buf = tiles + (j & 1) * BUF;
+        f32x16 S[2];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+          S[k] = zero16();
+          f32x16 lo = zero16();
+#pragma unroll
+          for (int sl = 0; sl < NK; ++sl)
+#pragma unroll
+            for (int s = 0; s < 2; ++s) {
+              const f16x8 kh = key_operand(buf + sl * CA_TILE, k, s, h, col), kl = key_operand(buf + LO + sl * CA_TILE, k, s, h, col);
+              S[k] = mfma_f16(kh, qb[sl][s], S[k]);
+              lo = mfma_f16(kh, ql[sl][s], lo);
+              lo = mfma_f16(kl, qb[sl][s], lo);
+            }
+#pragma unroll
+          for (int i = 0; i < 16; ++i) S[k][i] = __builtin_fmaf(lo[i], 1.0f / CA_LO, S[k][i]);
+        }
+        if (t0 + TILE > pass.lim_first) {  // some row of the wavefront does not see the whole step
+          int left = lim - t0 - 4 * h;
+          asm volatile("" : "+v"(left));
+#pragma unroll
+          for (int k = 0; k < 2; ++k)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) S[k][i] = 32 * k + 8 * (i >> 2) + (i & 3) < left ? S[k][i] : -__builtin_inff();
+        }
+        float top = __builtin_fmaxf(max16(S[0]), max16(S[1]));
+        top = __builtin_fmaxf(top, other_half(top)) * unscale;
+        if (__any(top > m_run + CA_SLACK)) {
+          const float mn = __builtin_fmaxf(m_run, top);
+          const float f = m_run == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m_run - mn);
+          l_run *= f;
+#pragma unroll
+          for (int sl = 0; sl < NV; ++sl)
+#pragma unroll
+            for (int i = 0; i < 16; ++i) acc[sl][i] *= f;
+          m_run = mn;
+        }
+        const float lift = CA_LIFT - (m_run == -__builtin_inff() ? 0.0f : m_run);
+        f32x16 lo[NV];
+#pragma unroll
+        for (int sl = 0; sl < NV; ++sl) lo[sl] = zero16();
+#pragma unroll
+        for (int k = 0; k < 2; ++k)
+#pragma unroll
+          for (int s = 0; s < 2; ++s) {
+            u32x4 rh, rl;
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const f32x2 p = f32x2{__builtin_amdgcn_exp2f(__builtin_fmaf(S[k][8 * s + 2 * i], unscale, lift)),
+                                    __builtin_amdgcn_exp2f(__builtin_fmaf(S[k][8 * s + 2 * i + 1], unscale, lift))};
+              l_run += p[0] + p[1];
+              const f16x2 hi = __builtin_convertvector(p, f16x2);
+              rh[i] = __builtin_bit_cast(uint32_t, hi);
+              rl[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
+                                                       f32x2{(p[0] - (float)hi[0]) * CA_LO, (p[1] - (float)hi[1]) * CA_LO}, f16x2));
+            }
+#pragma unroll
+            for (int sl = 0; sl < NV; ++sl) {
+              const uint8_t* vt = buf + (NK + sl) * CA_TILE;
+              const f16x8 vh = value_operand(vt, k, s, lane), vl = value_operand(vt + LO, k, s, lane);
+              acc[sl] = mfma_f16(vh, as_f16x8(rh), acc[sl]);
+              lo[sl] = mfma_f16(vl, as_f16x8(rh), lo[sl]);
+              lo[sl] = mfma_f16(vh, as_f16x8(rl), lo[sl]);
+            }
+          }
+#pragma unroll
+        for (int sl = 0; sl < NV; ++sl)
+#pragma unroll
+          for (int i = 0; i < 16; ++i) acc[sl][i] = __builtin_fmaf(lo[sl][i], 1.0f / CA_LO, acc[sl][i]);
+      }
+      __syncthreads();  // the next step's tiles are written, this one's are free
+    }
+  }
+  sum = RowSum{m_run == -__builtin_inff() ? m_run : m_run - CA_LIFT, l_run};
+}
+
+// q' of a row block as column operands: element e of piece 2s + h of slot sl is the lane's row's
+// q' of code 4 (2s + h) + e / 2 + 16 (e % 2). With parts, scaled by 2^E into [2^8, 2^9) and the low
+// parts in ql; returns 2^-E.
+template <bool PRECISE, int N>
+__device__ __forceinline__ float rotate_queries(const PagedAttnArgs& a, const PagedSeq& seq, const Rows& rows, int kv, const Kept& Kk,
+                                                int lane, f16x8 (&qb)[N][2], f16x8 (&ql)[PRECISE ? N : 1][2]) {
+  constexpr int NP = PRECISE ? 3 : 2;  // bf16 parts of the basis (and of fp32 queries)
+  const int h = lane >> 5, col = lane & 31;
+  const int64_t qoff = (seq.first + rows.tok) * a.q_token_stride + (kv * a.n_qh + rows.head) * a.q_head_stride + 8 * h;
+  f32x16 acc[N];
+  float most = 0.0f;
+  const int i = 4 * (col >> 3) + (col & 3), hh = (col >> 2) & 1;  // MFMA row col is register i of lane half hh
+  const int code = 4 * (2 * (i >> 3) + hh) + ((i & 7) >> 1) + 16 * (i & 1);
+#pragma unroll
+  for (int sl = 0; sl < N; ++sl) {
+    acc[sl] = zero16();
+    if (sl >= Kk.n) continue;
+    const float* V = a.basis_k + (int64_t)kv * D * D + (8 * h) * D + G * Kk.grp[sl] + code;
+#pragma unroll 1
+    for (int k = 0; k < 8; ++k) {
+      float v[8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) v[e] = V[(16 * k + e) * D];
+      bf16x8 vp[NP];
+      split8<NP>(v, vp);
+      if (a.q_f32) {
+        const f32x4* qp = reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.q) + qoff + 16 * k);
+        const f32x4 q0 = qp[0], q1 = qp[1];
+        const float qv[8] = {q0[0], q0[1], q0[2], q0[3], q1[0], q1[1], q1[2], q1[3]};
+        bf16x8 qq[NP];
+        split8<NP>(qv, qq);
+#pragma unroll
+        for (int x = 0; x < NP; ++x)
+#pragma unroll
+          for (int y = 0; x + y < NP; ++y)
+            acc[sl] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vp[x], qq[y], acc[sl], 0, 0, 0);
+      } else {
+        const bf16x8 qq = as_bf16x8(*reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.q) + qoff + 16 * k));
+#pragma unroll
+        for (int x = 0; x < NP; ++x) acc[sl] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vp[x], qq, acc[sl], 0, 0, 0);
+      }
+    }
+#pragma unroll
+    for (int j = 0; j < 16; ++j) {
+      acc[sl][j] *= a.scale_log2;
+      most = __builtin_fmaxf(most, __builtin_fabsf(acc[sl][j]));
+    }
+  }
+  float up = 1.0f;
+  if constexpr (PRECISE) {
+    most = __builtin_fmaxf(most, other_half(most));
+    up = __builtin_ldexpf(1.0f, 9 - scale_exponent(most));
+  }
+#pragma unroll
+  for (int sl = 0; sl < N; ++sl)
+#pragma unroll
+    for (int s = 0; s < 2; ++s) {
+      u32x4 rh, rl;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        f32x2 x = f32x2{acc[sl][8 * s + 2 * j] * up, acc[sl][8 * s + 2 * j + 1] * up};
+        if constexpr (!PRECISE) x = f32x2{__builtin_amdgcn_fmed3f(x[0], -65504.0f, 65504.0f), __builtin_amdgcn_fmed3f(x[1], -65504.0f, 65504.0f)};
+        const f16x2 hi = __builtin_convertvector(x, f16x2);
+        rh[j] = __builtin_bit_cast(uint32_t, hi);
+        rl[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{(x[0] - (float)hi[0]) * CA_LO, (x[1] - (float)hi[1]) * CA_LO}, f16x2));
+      }
+      qb[sl][s] = as_f16x8(rh);
+      if constexpr (PRECISE) ql[sl][s] = as_f16x8(rl);
+    }
+  return 1.0f / up;
+}
+
+// What a wavefront does, for N groups of each kind (missing ones are zeros).
+template <bool PRECISE, int N>
+__device__ __forceinline__ void chunk_rows(const PagedAttnArgs& a, const PagedSeq& seq, int kv, const Kept& Kk, const Kept& Kv,
+                                           int64_t unit, int64_t tile, int part, int wave, int lane, uint8_t* tiles) {
+  const Rows rows = rows_of(a, seq, tile, wave, lane & 31);
+  // the part's slots: those of a unit end at its last row's
+  const int n_parts = parts_of(a, rows.lim_unit);
+  if (part > 0 && part >= n_parts) return;
+  Pass pass;
+  pass.row = seq.row;
+  pass.from = (int)(part * a.part_slots);
+  pass.to = rows.lim_unit < pass.from + a.part_slots ? rows.lim_unit : (int)(pass.from + a.part_slots);
+  pass.lim_first = rows.lim_first;
+  pass.lim_last = rows.lim_last;
+
+  f16x8 qb[N][2], ql[PRECISE ? N : 1][2];
+  const float unscale = rotate_queries<PRECISE, N>(a, seq, rows, kv, Kk, lane, qb, ql);
+  f32x16 acc[N];
+#pragma unroll
+  for (int sl = 0; sl < N; ++sl) acc[sl] = zero16();
+  RowSum sum;
+  if constexpr (PRECISE)
+    chunk_steps_precise<N, N>(a, kv, Kk, Kv, pass, rows.lim, unscale, tiles, wave, lane, qb, ql, acc, sum);
+  else
+    chunk_steps<N, N>(a, kv, Kk, Kv, pass, rows.lim, tiles, wave, lane, qb, acc, sum);
+  const float m = __builtin_fmaxf(sum.m, other_half(sum.m)), l = sum.l + other_half(sum.l);
+  if (n_parts > 1) {
+    float* p = a.partial + part_at(a, unit, kv, part, wave) + lane;
+#pragma unroll
+    for (int sl = 0; sl < N; ++sl)
+      if (sl < Kv.n)
+#pragma unroll
+        for (int i = 0; i < 16; ++i) p[(16 * sl + i) * 64] = acc[sl][i];
+    p[16 * NG * 64] = l == 0.0f ? -__builtin_inff() : m;
+    p[(16 * NG + 1) * 64] = l;
+    return;
+  }
+  finish_rows<PRECISE ? 3 : 2, N>(a, seq, rows, kv, Kv, acc, m, l, lane);
+}
+
+// Workgroup = (unit of 256 rows, KV head; part of the slots). The counts of kept groups lie on the
+// device and differ from head to head: their cases share nothing but the scalars, so that each
+// has its own registers (with preparation and output outside the switch, the products of two
+// groups ran at the widest case's; as kernels of their own, the heads of one waited for the others').
 template <bool PRECISE>
 __global__ __launch_bounds__(64 * CA_NW, 2) void paged_chunk_kernel(PagedAttnArgs a) {
-  constexpr int KT = PRECISE ? 1 : 2;       // slot tiles of a step
-  constexpr int UNITS = KT * 2 * NG / CA_NW;  // group tiles that a wavefront unpacks in a step
-  constexpr int NP = PRECISE ? 3 : 2;       // bf16 parts of the bases (and of fp32 queries)
   extern __shared__ __attribute__((aligned(16))) uint8_t tiles[];
   __shared__ FindScratch find_s;
   const int kv = (int)(blockIdx.x % (unsigned)a.c.n_kv);
-  const int tid = threadIdx.x, lane = tid & 63;
-  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  const int h = lane >> 5, col = lane & 31;
+  const int lane = threadIdx.x & 63;
+  const int wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int64_t unit = blockIdx.x / (unsigned)a.c.n_kv;
-  const int part = blockIdx.y;
   int b;
   int64_t tile;
   if (!find_unit<CA_NW>(a, unit, find_s, b, tile)) return;
   const PagedSeq seq = paged_seq(a.c, b);
-  const Rows rows = rows_of(a, seq, tile, wave, col);
-  // the part's slots: those of a unit end at its last row's
-  const int n_parts = parts_of(a, rows.lim_unit);
-  if (part > 0 && part >= n_parts) return;
-  const int from = (int)(part * a.part_slots);
-  const int to = rows.lim_unit < from + a.part_slots ? rows.lim_unit : (int)(from + a.part_slots);
-
   Kept Kk = read_kept(a.bits_k + kv * NG), Kv = read_kept(a.bits_v + kv * NG);
   if (!Kk.ok || Kk.used > a.Wk) Kk.n = 0;  // width table inconsistent with the record
   if (!Kv.ok || Kv.used > a.Wv) Kv.n = 0;
-  const int ns = Kk.n + Kv.n;
-  const int lo_off = KT * ns * CA_TILE;  // the low parts' tiles
-
-  // ---- q' as column operands: element e of piece 2s + h of slot sl is the lane's row's q' of
-  // code 4 (2s + h) + e / 2 + 16 (e % 2), scaled by 2^E into [2^8, 2^9) ----
-  f16x8 qb[NG][2], ql[PRECISE ? NG : 1][2];
-  float unscale;
-  {
-    const int64_t qoff = (seq.first + rows.tok) * a.q_token_stride + (kv * a.n_qh + rows.head) * a.q_head_stride + 8 * h;
-    f32x16 acc[NG];
-    float most = 0.0f;
-    const int i = 4 * (col >> 3) + (col & 3), hh = (col >> 2) & 1;  // MFMA row col is register i of lane half hh
-    const int code = 4 * (2 * (i >> 3) + hh) + ((i & 7) >> 1) + 16 * (i & 1);
-#pragma unroll
-    for (int sl = 0; sl < NG; ++sl) {
-      acc[sl] = zero16();
-      if (sl >= Kk.n) continue;
-      const float* V = a.basis_k + (int64_t)kv * D * D + (8 * h) * D + G * Kk.grp[sl] + code;
-#pragma unroll 1
-      for (int k = 0; k < 8; ++k) {
-        float v[8];
-#pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = V[(16 * k + e) * D];
-        bf16x8 vp[NP];
-        split8<NP>(v, vp);
-        if (a.q_f32) {
-          const f32x4* qp = reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.q) + qoff + 16 * k);
-          const f32x4 q0 = qp[0], q1 = qp[1];
-          const float qv[8] = {q0[0], q0[1], q0[2], q0[3], q1[0], q1[1], q1[2], q1[3]};
-          bf16x8 qq[NP];
-          split8<NP>(qv, qq);
-#pragma unroll
-          for (int x = 0; x < NP; ++x)
-#pragma unroll
-            for (int y = 0; x + y < NP; ++y)
-              acc[sl] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vp[x], qq[y], acc[sl], 0, 0, 0);
-        } else {
-          const bf16x8 qq = as_bf16x8(*reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.q) + qoff + 16 * k));
-#pragma unroll
-          for (int x = 0; x < NP; ++x) acc[sl] = __builtin_amdgcn_mfma_f32_32x32x16_bf16(vp[x], qq, acc[sl], 0, 0, 0);
-        }
-      }
-#pragma unroll
-      for (int j = 0; j < 16; ++j) {
-        acc[sl][j] *= a.scale_log2;
-        most = __builtin_fmaxf(most, __builtin_fabsf(acc[sl][j]));
-      }
-    }
-    most = __builtin_fmaxf(most, other_half(most));
-    const int E = 9 - scale_exponent(most);
-    unscale = __builtin_ldexpf(1.0f, -E);
-    const float up = __builtin_ldexpf(1.0f, E);
-#pragma unroll
-    for (int sl = 0; sl < NG; ++sl)
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        u32x4 rh, rl;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const f32x2 x = f32x2{acc[sl][8 * s + 2 * j] * up, acc[sl][8 * s + 2 * j + 1] * up};
-          const f16x2 hi = __builtin_convertvector(x, f16x2);
-          rh[j] = __builtin_bit_cast(uint32_t, hi);
-          if constexpr (PRECISE)
-            rl[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
-                                                     f32x2{(x[0] - (float)hi[0]) * CA_LO, (x[1] - (float)hi[1]) * CA_LO}, f16x2));
-        }
-        qb[sl][s] = as_f16x8(rh);
-        if constexpr (PRECISE) ql[sl][s] = as_f16x8(rl);
-      }
+  switch (Kk.n > Kv.n ? Kk.n : Kv.n) {
+    case 4: chunk_rows<PRECISE, 4>(a, seq, kv, Kk, Kv, unit, tile, blockIdx.y, wave, lane, tiles); break;
+    case 3: chunk_rows<PRECISE, 3>(a, seq, kv, Kk, Kv, unit, tile, blockIdx.y, wave, lane, tiles); break;
+    default: chunk_rows<PRECISE, 2>(a, seq, kv, Kk, Kv, unit, tile, blockIdx.y, wave, lane, tiles);
   }
-
-  // ---- the wavefront's group tiles of a step: words in registers one step ahead ----
-  uint32_t words[UNITS][8], meta[UNITS];
-  auto load_step = [&](int j) {
-#pragma unroll
-    for (int u = 0; u < UNITS; ++u) {
-      const int u1 = wave + CA_NW * u;
-      meta[u] = 0u;
-#pragma unroll
-      for (int i = 0; i < 8; ++i) words[u][i] = 0u;
-      if (u1 >= KT * ns) continue;
-      const int tl = u1 >= ns ? 1 : 0, si = u1 - tl * ns, jt = from / TILE + j * KT + tl;
-      if (jt * TILE >= to) continue;
-      const bool val = si >= Kk.n;
-      const int sl = val ? si - Kk.n : si;
-      const int bits = val ? pick4(Kv.bits, sl) : pick4(Kk.bits, sl), pay = val ? pick4(Kv.pay, sl) : pick4(Kk.pay, sl);
-      const uint32_t* rec = paged_tile(a.c, val ? a.pool_v : a.pool_k, val ? a.Wv : a.Wk, seq.row, jt, kv);
-      if (!rec) continue;  // a page outside the pool: zeros
-      rec += lane;
-      if (jt * TILE + lane < seq.len) meta[u] = finite_meta(rec[sl * TILE], bits);
-#pragma unroll
-      for (int i = 0; i < 8; ++i)
-        if (i < bits) words[u][i] = rec[(pay + i) * TILE];
-    }
-  };
-  uint32_t magic = 0x64006400u;  // exponent of 1024 in both halves, in a VGPR
-  asm volatile("" : "+v"(magic));
-
-  f32x16 acc[NG];
-#pragma unroll
-  for (int sl = 0; sl < NG; ++sl) acc[sl] = zero16();
-  float m_run = -__builtin_inff(), l_run = 0.0f;
-  const int n_steps = (to - from + KT * TILE - 1) / (KT * TILE);
-  if (n_steps > 0) load_step(0);
-#pragma unroll 1
-  for (int j = 0; j < n_steps; ++j) {
-    __syncthreads();  // every wavefront is done with the last step's tiles
-#pragma unroll
-    for (int u = 0; u < UNITS; ++u) {
-      const int u1 = wave + CA_NW * u;
-      if (u1 >= KT * ns) continue;
-      const int tl = u1 >= ns ? 1 : 0, si = u1 - tl * ns;
-      const int bits = si >= Kk.n ? pick4(Kv.bits, si - Kk.n) : pick4(Kk.bits, si);
-      with_bits(bits, [&](auto bc) {
-        write_coefficients<decltype(bc)::value, PRECISE>(words[u], meta[u], tiles + u1 * CA_TILE, lane, lo_off, magic);
-      });
-    }
-    if (j + 1 < n_steps) load_step(j + 1);
-    __syncthreads();  // the step's tiles are in LDS
-    const int t0 = from + j * KT * TILE;
-    if (t0 >= rows.lim_last) continue;
-    f32x16 S[2 * KT];
-#pragma unroll
-    for (int k = 0; k < 2 * KT; ++k) {
-      S[k] = zero16();
-      f32x16 lo = zero16();
-#pragma unroll
-      for (int sl = 0; sl < NG; ++sl) {
-        if (sl >= Kk.n) continue;
-#pragma unroll
-        for (int s = 0; s < 2; ++s) {
-          const uint8_t* p = tiles + ((k >> 1) * ns + sl) * CA_TILE + piece_at(32 * (k & 1) + col, 2 * s + h);
-          const f16x8 kh = as_f16x8(*reinterpret_cast<const u32x4*>(p));
-          S[k] = mfma_f16(kh, qb[sl][s], S[k]);
-          if constexpr (PRECISE) {
-            const f16x8 kl = as_f16x8(*reinterpret_cast<const u32x4*>(p + lo_off));
-            lo = mfma_f16(kh, ql[sl][s], lo);
-            lo = mfma_f16(kl, qb[sl][s], lo);
-          }
-        }
-      }
-#pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        if constexpr (PRECISE) S[k][i] = __builtin_fmaf(lo[i], 1.0f / CA_LO, S[k][i]);
-        S[k][i] *= unscale;
-      }
-    }
-    if (t0 + KT * TILE > rows.lim_first) {  // some row of the wavefront does not see the whole step
-#pragma unroll
-      for (int k = 0; k < 2 * KT; ++k)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) {
-          const int t = t0 + 32 * k + 8 * (i >> 2) + 4 * h + (i & 3);
-          S[k][i] = t < rows.lim ? S[k][i] : -__builtin_inff();
-        }
-    }
-    float top = S[0][0];
-#pragma unroll
-    for (int k = 0; k < 2 * KT; ++k)
-#pragma unroll
-      for (int i = 0; i < 16; ++i) top = __builtin_fmaxf(top, S[k][i]);
-    top = __builtin_fmaxf(top, other_half(top));
-    if (__any(top > m_run + CA_SLACK)) {
-      const float mn = __builtin_fmaxf(m_run, top);
-      const float f = m_run == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m_run - mn);
-      l_run *= f;
-#pragma unroll
-      for (int sl = 0; sl < NG; ++sl)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[sl][i] *= f;
-      m_run = mn;
-    }
-    const float ref = (m_run == -__builtin_inff() ? 0.0f : m_run) - CA_LIFT;
-    f32x16 lo[PRECISE ? NG : 1];
-    if constexpr (PRECISE) {
-#pragma unroll
-      for (int sl = 0; sl < NG; ++sl) lo[sl] = zero16();
-    }
-#pragma unroll
-    for (int k = 0; k < 2 * KT; ++k)
-#pragma unroll
-      for (int s = 0; s < 2; ++s) {
-        u32x4 rh, rl;
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          const f32x2 p = f32x2{__builtin_amdgcn_exp2f(S[k][8 * s + 2 * i] - ref), __builtin_amdgcn_exp2f(S[k][8 * s + 2 * i + 1] - ref)};
-          l_run += p[0] + p[1];
-          const f16x2 hi = __builtin_convertvector(p, f16x2);
-          rh[i] = __builtin_bit_cast(uint32_t, hi);
-          if constexpr (PRECISE)
-            rl[i] = __builtin_bit_cast(uint32_t, __builtin_convertvector(
-                                                     f32x2{(p[0] - (float)hi[0]) * CA_LO, (p[1] - (float)hi[1]) * CA_LO}, f16x2));
-        }
-        const f16x8 ph = as_f16x8(rh);
-        // value rows: slots 16 s + 4 h + (0..3) and 8 further, as p's registers have them
-        const int t = 32 * (k & 1) + 16 * s + 4 * h + ((lane & 15) >> 2);
-        const int piece = 2 * ((lane >> 4) & 1) + ((lane & 3) >> 1);
-#pragma unroll
-        for (int sl = 0; sl < NG; ++sl) {
-          if (sl >= Kv.n) continue;
-          const uint8_t* vt = tiles + ((k >> 1) * ns + Kk.n + sl) * CA_TILE + 8 * (lane & 1);
-          const u32x2 x0 = read_transposed(vt + piece_at(t, piece)), x1 = read_transposed(vt + piece_at(t + 8, piece));
-          const f16x8 vh = as_f16x8(u32x4{x0[0], x0[1], x1[0], x1[1]});
-          acc[sl] = mfma_f16(vh, ph, acc[sl]);
-          if constexpr (PRECISE) {
-            const u32x2 y0 = read_transposed(vt + lo_off + piece_at(t, piece)), y1 = read_transposed(vt + lo_off + piece_at(t + 8, piece));
-            lo[sl] = mfma_f16(as_f16x8(u32x4{y0[0], y0[1], y1[0], y1[1]}), ph, lo[sl]);
-            lo[sl] = mfma_f16(vh, as_f16x8(rl), lo[sl]);
-          }
-        }
-      }
-    if constexpr (PRECISE) {
-#pragma unroll
-      for (int sl = 0; sl < NG; ++sl)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) acc[sl][i] = __builtin_fmaf(lo[sl][i], 1.0f / CA_LO, acc[sl][i]);
-    }
-  }
-
-  const float l = l_run + other_half(l_run);
-  if (n_parts > 1) {
-    float* p = a.partial + part_at(a, unit, kv, part, wave) + lane;
-#pragma unroll
-    for (int sl = 0; sl < NG; ++sl)
-      if (sl < Kv.n)
-#pragma unroll
-        for (int i = 0; i < 16; ++i) p[(16 * sl + i) * 64] = acc[sl][i];
-    p[16 * NG * 64] = m_run;
-    p[(16 * NG + 1) * 64] = l;
-    return;
-  }
-  finish_rows<NP>(a, seq, rows, kv, Kv, acc, m_run, l, lane);
 }
 
 // ---------------------------------------------------------------------------
@@ -544,25 +781,25 @@ __global__ __launch_bounds__(64 * CA_NW, 2) void paged_chunk_kernel(PagedAttnArg
 template <bool PRECISE>
 __global__ __launch_bounds__(64) void paged_join_kernel(PagedAttnArgs a) {
   __shared__ FindScratch find_s;
-  const int kv = (int)(blockIdx.x % (unsigned)a.c.n_kv), wave = blockIdx.y, lane = threadIdx.x;
+  const int kv = (int)(blockIdx.x % (unsigned)a.c.n_kv), block = blockIdx.y, lane = threadIdx.x;
   const int64_t unit = blockIdx.x / (unsigned)a.c.n_kv;
   int b;
   int64_t tile;
   if (!find_unit<1>(a, unit, find_s, b, tile)) return;
   const PagedSeq seq = paged_seq(a.c, b);
-  const Rows rows = rows_of(a, seq, tile, wave, lane & 31);
+  const Rows rows = rows_of(a, seq, tile, block, lane & 31);
   const int n_parts = parts_of(a, rows.lim_unit);
   if (n_parts <= 1) return;  // done by the part itself
   Kept Kv = read_kept(a.bits_v + kv * NG);
   if (!Kv.ok || Kv.used > a.Wv) Kv.n = 0;
   float m = -__builtin_inff(), l = 0.0f;
   const int ml = 16 * NG * 64 + lane;
-  for (int i = 0; i < n_parts; ++i) m = __builtin_fmaxf(m, a.partial[part_at(a, unit, kv, i, wave) + ml]);
+  for (int i = 0; i < n_parts; ++i) m = __builtin_fmaxf(m, a.partial[part_at(a, unit, kv, i, block) + ml]);
   f32x16 acc[NG];
 #pragma unroll
   for (int sl = 0; sl < NG; ++sl) acc[sl] = zero16();
   for (int i = 0; i < n_parts; ++i) {
-    const float* p = a.partial + part_at(a, unit, kv, i, wave);
+    const float* p = a.partial + part_at(a, unit, kv, i, block);
     const float mi = p[ml], f = mi == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(mi - m);
     l = __builtin_fmaf(f, p[ml + 64], l);
 #pragma unroll
@@ -571,7 +808,7 @@ __global__ __launch_bounds__(64) void paged_join_kernel(PagedAttnArgs a) {
 #pragma unroll
         for (int j = 0; j < 16; ++j) acc[sl][j] = __builtin_fmaf(f, p[(16 * sl + j) * 64 + lane], acc[sl][j]);
   }
-  finish_rows<PRECISE ? 3 : 2>(a, seq, rows, kv, Kv, acc, m, l, lane);
+  finish_rows<PRECISE ? 3 : 2, NG>(a, seq, rows, kv, Kv, acc, m, l, lane);
 }
 
 // ---------------------------------------------------------------------------
@@ -611,14 +848,19 @@ hipError_t launch_paged_attention(const PagedAttnArgs& args, void* workspace, hi
   if (a.lse != nullptr) hipLaunchKernelGGL(paged_lse_kernel, dim3(a.c.n_kv), dim3(256), 0, st, a);
   hipError_t e = hipSuccess;
   if (p.units > 0) {
-    const int groups = (a.Wk / 2 < NG ? a.Wk / 2 : NG) + (a.Wv / 2 < NG ? a.Wv / 2 : NG);  // a kept group takes two words
+    // a kept group takes two words at least; two buffers of two slot tiles, or of one in two parts
+    auto groups = [](int W) { return W < 6 ? 2 : W / 2 < NG ? W / 2 : NG; };
+    const int lds = 2 * 2 * 2 * (groups(a.Wk) > groups(a.Wv) ? groups(a.Wk) : groups(a.Wv)) * CA_TILE;
     const dim3 grid((unsigned)(p.units * a.c.n_kv), (unsigned)p.split.parts), join((unsigned)(p.units * a.c.n_kv), CA_NW);
-    if (a.out_f32) {
-      hipLaunchKernelGGL((paged_chunk_kernel<true>), grid, dim3(64 * CA_NW), 2 * groups * CA_TILE, st, a);
-      if (p.split.parts > 1) hipLaunchKernelGGL((paged_join_kernel<true>), join, dim3(64), 0, st, a);
-    } else {
-      hipLaunchKernelGGL((paged_chunk_kernel<false>), grid, dim3(64 * CA_NW), 2 * groups * CA_TILE, st, a);
-      if (p.split.parts > 1) hipLaunchKernelGGL((paged_join_kernel<false>), join, dim3(64), 0, st, a);
+    if (a.out_f32)
+      hipLaunchKernelGGL((paged_chunk_kernel<true>), grid, dim3(64 * CA_NW), lds, st, a);
+    else
+      hipLaunchKernelGGL((paged_chunk_kernel<false>), grid, dim3(64 * CA_NW), lds, st, a);
+    if (p.split.parts > 1) {
+      if (a.out_f32)
+        hipLaunchKernelGGL((paged_join_kernel<true>), join, dim3(64), 0, st, a);
+      else
+        hipLaunchKernelGGL((paged_join_kernel<false>), join, dim3(64), 0, st, a);
     }
     e = hipGetLastError();
   }
