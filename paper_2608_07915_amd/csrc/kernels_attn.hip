@@ -319,7 +319,7 @@ __device__ __forceinline__ void score_slot(const uint32_t* __restrict__ kt, int 
 // once every wave has left its tile loop.
 // ---------------------------------------------------------------------------
 template <int NQ, typename R>
-__device__ __forceinline__ void write_chunk_partial(const AttnArgs& a, int nqh, R&& partial_row, int chunk, int tid, int wave,
+__device__ __forceinline__ void write_chunk_partial(const AttnArgs& a, int nqh, R&& partial_at, int tid, int wave,
                                                     int lane, int kq, int col, bool ok, const Kept& Kv,
                                                     const float (&m_run)[4 * NQ], const float (&l_run)[4 * NQ],
                                                     const float (&zacc)[4 * NQ][NG], const f32x4 (&vacc)[NG][2],
@@ -385,7 +385,7 @@ __device__ __forceinline__ void write_chunk_partial(const AttnArgs& a, int nqh, 
       l += f * lst[w][h];
       if (j < NG) z += f * zst[w][h][j];
     }
-    float* ph = a.partial + (partial_row(h) * a.n_chunks + chunk) * PART;  // row h's partial of this chunk
+    float* ph = a.partial + partial_at(h) * PART;  // row h's partial of this chunk
     ph[8 + j] = acc;
     if (j == 0) {
       ph[0] = M;
@@ -411,7 +411,7 @@ __device__ __forceinline__ void attn_scan(const AttnArgs& a, const PagedAttnArgs
   // (dispatched round-robin over the XCDs) every chunk of a (sequence, kv head) runs on
   // the same XCD and its L2 serves that head's key basis to all of them
   int chunk = blockIdx.x, kv = blockIdx.y, b = blockIdx.z;
-  if (a.group_major) {
+  if (!PAGED && a.group_major) {
     const int ngr = a.n_kv_heads * a.batch, gid = (int)(blockIdx.x % (unsigned)ngr);
     chunk = (int)(blockIdx.x / (unsigned)ngr);
     kv = gid % a.n_kv_heads;
@@ -419,10 +419,22 @@ __device__ __forceinline__ void attn_scan(const AttnArgs& a, const PagedAttnArgs
   }
   const int tid = threadIdx.x, wave = tid >> 6, lane = tid & 63;
   PagedSeq seq{};
+  int item = 0, tiles_per_chunk = a.tiles_per_chunk;
   if constexpr (PAGED) {
+    // workgroup i = item * KV heads + KV head: a head's chunks on one XCD
+    kv = (int)(blockIdx.x % (unsigned)a.n_kv_heads);
+    item = (int)(blockIdx.x / (unsigned)a.n_kv_heads);
+    __shared__ ScanScratch place_s;
+    const ScanPlace at = scan_place(p, item, place_s);
+    if (at.b < 0) return;
+    b = at.b;
+    if (at.chunk == 0 && kv == 0 && threadIdx.x == 0) {  // for the combine
+      p.scan_plan[2 * b] = item;
+      p.scan_plan[2 * b + 1] = at.n_chunks;
+    }
+    chunk = at.chunk;
+    tiles_per_chunk = at.tiles_per_chunk;
     seq = paged_seq(p.c, b);
-    if (!scanned(p, seq)) return;  // the rows of longer sequences are the other kernel's
-    if ((int64_t)chunk * a.tiles_per_chunk * TILE >= seq.len) return;  // nor does a sequence have chunks past its end
   }
   const int s = PAGED ? kv : b * a.n_kv_heads + kv;
   const int nqh = PAGED ? (int)seq.n * a.n_qh : a.n_qh;
@@ -446,8 +458,8 @@ __device__ __forceinline__ void attn_scan(const AttnArgs& a, const PagedAttnArgs
   // tile; the last chunk holds the last tile alone
   const int64_t n_tiles = (n_tokens + 63) >> 6;
   const bool last_chunk = !PAGED && chunk == a.n_chunks - 1;
-  const int64_t tile_begin = last_chunk ? n_tiles - 1 : (int64_t)chunk * a.tiles_per_chunk;
-  int64_t tile_end = last_chunk ? n_tiles : tile_begin + a.tiles_per_chunk;
+  const int64_t tile_begin = last_chunk ? n_tiles - 1 : (int64_t)chunk * tiles_per_chunk;
+  int64_t tile_end = last_chunk ? n_tiles : tile_begin + tiles_per_chunk;
   if (!last_chunk && tile_end > n_tiles - (PAGED ? 0 : 1)) tile_end = n_tiles - (PAGED ? 0 : 1);
 
   float m_run[NH], l_run[NH], zacc[NH][NG];
@@ -743,15 +755,13 @@ __device__ __forceinline__ void attn_scan(const AttnArgs& a, const PagedAttnArgs
     __builtin_amdgcn_wave_barrier();
   }
 
-  const auto partial_row = [&](int h) -> int64_t {
-    if constexpr (PAGED) {
-      const int tok = h / a.n_qh;
-      return ((int64_t)b * p.scan_tokens + tok) * a.n_q_heads + kv * a.n_qh + h - tok * a.n_qh;
-    } else {
-      return (int64_t)b * a.n_q_heads + kv * nqh + h;
-    }
+  const auto partial_at = [&](int h) -> int64_t {
+    if constexpr (PAGED)
+      return ((int64_t)item * a.n_kv_heads + kv) * (p.scan_tokens * a.n_qh) + h;
+    else
+      return ((int64_t)b * a.n_q_heads + kv * nqh + h) * a.n_chunks + chunk;
   };
-  write_chunk_partial<NQ>(a, nqh, partial_row, chunk, tid, wave, lane, kq, col, ok, Kv, m_run, l_run, zacc, vacc, smem);
+  write_chunk_partial<NQ>(a, nqh, partial_at, tid, wave, lane, kq, col, ok, Kv, m_run, l_run, zacc, vacc, smem);
 }
 
 template <int NQ, int PK, int PV, bool EXACT>
@@ -772,11 +782,11 @@ __global__ __launch_bounds__(256, 2) void paged_scan_kernel(AttnArgs a, PagedAtt
 // chunk, merged with a running maximum in batches of CB chunks); the group
 // states are then merged in LDS.
 // ---------------------------------------------------------------------------
-// combine_row: nch partials from ph, value stream s; store(i, out_i) takes the row's channels,
+// combine_row: nch partials from ph on, `step` floats apart, value stream s; store(i, out_i) takes the row's channels,
 // stats(m, l) in one thread the overall maximum (log2 domain) and sum. With EMPTY, a row without
 // weights gets zeros.
 template <bool EMPTY, typename Store, typename Stats>
-__device__ __forceinline__ void combine_row(const AttnArgs& a, const float* __restrict__ ph, int nch, int s, Store&& store,
+__device__ __forceinline__ void combine_row(const AttnArgs& a, const float* __restrict__ ph, int64_t step, int nch, int s, Store&& store,
                                             Stats&& stats) {
   constexpr int CB = 12;  // 8 x 12 = 96 chunks per round: one round of loads for ~768 scan workgroups over 8 heads
   __shared__ float accs[8][D];
@@ -798,7 +808,7 @@ __device__ __forceinline__ void combine_row(const AttnArgs& a, const float* __re
 #pragma unroll
     for (int k = 0; k < CB; ++k) {
       const int c = c0 + 8 * k;
-      const float* pc = ph + (int64_t)(c < nch ? c : grp) * PART;
+      const float* pc = ph + (c < nch ? c : grp) * step;
       m[k] = c < nch ? pc[0] : -__builtin_inff();
       l[k] = pc[1];
       z[k] = pc[2 + g];
@@ -866,34 +876,106 @@ __device__ __forceinline__ void combine_row(const AttnArgs& a, const float* __re
 __global__ __launch_bounds__(1024) void combine_kernel(AttnArgs a) {
   const int hq = blockIdx.x, b = blockIdx.y;
   const int64_t row = (int64_t)b * a.n_q_heads + hq;
-  combine_row<false>(a, a.partial + row * a.n_chunks * PART, a.n_chunks, b * a.n_kv_heads + hq / a.n_qh,
+  combine_row<false>(a, a.partial + row * a.n_chunks * PART, PART, a.n_chunks, b * a.n_kv_heads + hq / a.n_qh,
                      [&](int i, float o) { a.out[row * D + i] = o; }, [](float, float) {});
 }
 
-// The same for the rows of scanned sequences: workgroup = (sequence, token, query head).
+// The rows of scanned sequences. Few rows in all (ROWS = 1): a workgroup per row, as above, its
+// chunks merged by eight thread groups. More rows than the card holds such workgroups: a workgroup
+// per (sequence, token, KV head), with a thread group for each of ROWS = 8 query heads and the
+// basis read once for them (48 sequences of seven heads on each of four KV heads: 22 us by 1344
+// workgroups of one row, 9 by 192).
+template <int ROWS>
 __global__ __launch_bounds__(1024) void paged_combine_kernel(AttnArgs a, PagedAttnArgs p) {
-  const int hq = blockIdx.x % (unsigned)a.n_q_heads, at = blockIdx.x / (unsigned)a.n_q_heads;
+  const int per = ROWS == 1 ? a.n_q_heads : a.n_kv_heads;  // workgroups of a token
+  const int at = blockIdx.x / (unsigned)per, which = blockIdx.x % (unsigned)per;
   const int b = at / p.scan_tokens, tok = at % p.scan_tokens;
   const PagedSeq seq = paged_seq(p.c, b);
   if (!scanned(p, seq) || tok >= seq.n) return;
-  const int64_t per = (int64_t)a.tiles_per_chunk * TILE;  // slots of a chunk
-  const int nch = (int)((seq.len + per - 1) / per);
-  const int64_t row = (seq.first + tok) * a.n_q_heads + hq;
-  combine_row<true>(
-      a, a.partial + ((int64_t)at * a.n_q_heads + hq) * a.n_chunks * PART, nch, hq / a.n_qh,
-      [&](int i, float o) {
-        if (p.out_f32)
-          reinterpret_cast<float*>(p.out)[row * D + i] = o;
-        else
-          reinterpret_cast<__bf16*>(p.out)[row * D + i] = (__bf16)o;
-      },
-      [&](float m, float l) {
-        if (p.lse == nullptr) return;
-        const int64_t qo = (seq.first + tok) * p.q_token_stride + hq * p.q_head_stride;
-        float u = 0.0f;
-        for (int c = 0; c < D; ++c) u = __builtin_fmaf(query_at(p, qo + c), p.lse_u[hq / a.n_qh * D + c], u);
-        p.lse[row] = l == 0.0f ? -__builtin_inff() : __builtin_fmaf(__builtin_amdgcn_logf(l) + m, LN2, u);
-      });
+  const int kv = ROWS == 1 ? which / a.n_qh : which;
+  const int item0 = seq.len > 0 ? p.scan_plan[2 * b] : 0, n_items = seq.len > 0 ? p.scan_plan[2 * b + 1] : 0;
+  const int rows = p.scan_tokens * a.n_qh;  // partials of an item and KV head
+  const int64_t step = (int64_t)a.n_kv_heads * rows * PART;
+  const float* first = a.partial + (((int64_t)item0 * a.n_kv_heads + kv) * rows + tok * a.n_qh) * PART;  // of the KV head's first row
+  auto store = [&](int hq, int i, float o) {
+    const int64_t at_row = ((seq.first + tok) * a.n_q_heads + hq) * D + i;
+    if (p.out_f32)
+      reinterpret_cast<float*>(p.out)[at_row] = o;
+    else
+      reinterpret_cast<__bf16*>(p.out)[at_row] = (__bf16)o;
+  };
+  auto write_lse = [&](int hq, float m, float l) {
+    if (p.lse == nullptr) return;
+    const int64_t qo = (seq.first + tok) * p.q_token_stride + hq * p.q_head_stride;
+    float u = 0.0f;
+    for (int c = 0; c < D; ++c) u = __builtin_fmaf(query_at(p, qo + c), p.lse_u[kv * D + c], u);
+    p.lse[(seq.first + tok) * a.n_q_heads + hq] = l == 0.0f ? -__builtin_inff() : __builtin_fmaf(__builtin_amdgcn_logf(l) + m, LN2, u);
+  };
+  if constexpr (ROWS == 1) {
+    combine_row<true>(a, first + (which - kv * a.n_qh) * PART, step, n_items, kv, [&](int i, float o) { store(which, i, o); },
+                      [&](float m, float l) { write_lse(which, m, l); });
+  } else {
+    __shared__ float chat[ROWS][D];
+    const int tid = threadIdx.x, j = tid & 127, r = tid >> 7;
+    const int ri = tid >> 3, rpart = tid & 7;
+    const f32x4* Vr = reinterpret_cast<const f32x4*>(a.basis_v + (int64_t)kv * D * D + (int64_t)ri * D + 16 * rpart);
+    const f32x4 v0 = Vr[0], v1 = Vr[1], v2 = Vr[2], v3 = Vr[3];
+    const float mv = a.mean_v[(int64_t)kv * D + j];
+    const bool kept = a.bits_v[kv * NG + (j >> 5)] != 0;
+    for (int h0 = 0; h0 < a.n_qh; h0 += ROWS) {
+      const int h = h0 + r;
+      if (h < a.n_qh) {
+        const float* ph = first + h * PART;
+        float M = -__builtin_inff(), L = 0.0f, A = 0.0f;
+        constexpr int CB = 4;
+        for (int c0 = 0; c0 < n_items; c0 += CB) {
+          float m[CB], l[CB], x[CB];
+#pragma unroll
+          for (int k = 0; k < CB; ++k) {
+            const float* pc = ph + (c0 + k < n_items ? c0 + k : c0) * step;
+            m[k] = c0 + k < n_items ? pc[0] : -__builtin_inff();
+            l[k] = pc[1];
+            x[k] = pc[2 + (j >> 5)] + pc[8 + j];
+          }
+          float mb = M;
+#pragma unroll
+          for (int k = 0; k < CB; ++k) mb = __builtin_fmaxf(mb, m[k]);
+          if (mb != -__builtin_inff()) {
+            const float f = M == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(M - mb);
+            L *= f;
+            A *= f;
+#pragma unroll
+            for (int k = 0; k < CB; ++k) {
+              const float w = m[k] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m[k] - mb);
+              L = __builtin_fmaf(w, l[k], L);
+              A = __builtin_fmaf(w, x[k], A);
+            }
+            M = mb;
+          }
+        }
+        chat[r][j] = L == 0.0f ? 0.0f : (kept ? A / L : 0.0f) + mv;
+        if (j == 0) write_lse(kv * a.n_qh + h, M, L);
+      }
+      __syncthreads();
+      const int n = a.n_qh - h0 < ROWS ? a.n_qh - h0 : ROWS;
+      for (int x = 0; x < n; ++x) {
+        const float* ch = chat[x] + 16 * rpart;
+        float o = 0.0f;
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+          o = __builtin_fmaf(ch[k], v0[k], o);
+          o = __builtin_fmaf(ch[4 + k], v1[k], o);
+          o = __builtin_fmaf(ch[8 + k], v2[k], o);
+          o = __builtin_fmaf(ch[12 + k], v3[k], o);
+        }
+        o += __shfl_xor(o, 1);
+        o += __shfl_xor(o, 2);
+        o += __shfl_xor(o, 4);
+        if (rpart == 0) store(kv * a.n_qh + h0 + x, ri, o);
+      }
+      __syncthreads();  // the next heads' coefficients may come
+    }
+  }
 }
 
 }  // namespace spectra_dev
@@ -927,15 +1009,17 @@ static Split launch_nq_pw(const AttnArgs& a, const PagedAttnArgs* p, hipStream_t
   const int fit = (int)(LDS_MOST / (lds + attn_static_lds(NQ)));
   if (a.app_k && (size_t)append_stage_bytes(a.app_f32 != 0) > lds) lds = append_stage_bytes(a.app_f32 != 0);
   const int per_cu = fit < 1 ? 1 : fit < REGS ? fit : REGS;
-  const Split split = p ? paged_scan_split(groups, (a.n_tokens + 63) / 64, per_cu)
-                        : scan_split(groups, (a.n_tokens + 63) / 64, per_cu, NQ * (a.Wk + a.Wv));
+  if (p) {
+    PagedAttnArgs q = *p;
+    q.scan_items = (int32_t)paged_scan_items(a.n_kv_heads, per_cu);
+    hipLaunchKernelGGL((paged_scan_kernel<NQ, PK, PV, EXACT>), dim3((unsigned)((q.scan_items + a.batch) * a.n_kv_heads)), dim3(256), lds, st, g, q);
+    return Split{0, q.scan_items};
+  }
+  const Split split = scan_split(groups, (a.n_tokens + 63) / 64, per_cu, NQ * (a.Wk + a.Wv));
   g.tiles_per_chunk = split.tiles_per_chunk;
   g.n_chunks = split.n_chunks;
   const dim3 grid = g.group_major ? dim3(g.n_chunks * a.n_kv_heads * a.batch, 1, 1) : dim3(g.n_chunks, a.n_kv_heads, a.batch);
-  if (p)
-    hipLaunchKernelGGL((paged_scan_kernel<NQ, PK, PV, EXACT>), grid, dim3(256), lds, st, g, *p);
-  else
-    hipLaunchKernelGGL((attn_kernel<NQ, PK, PV, EXACT>), grid, dim3(256), lds, st, g);
+  hipLaunchKernelGGL((attn_kernel<NQ, PK, PV, EXACT>), grid, dim3(256), lds, st, g);
   return split;
 }
 
@@ -987,7 +1071,10 @@ hipError_t launch_attention(const AttnArgs& a, hipStream_t st) {
 static_assert(PART * sizeof(float) == SCAN_PART_BYTES, "workspace of a scanned row");
 
 // The sequences of a paged call with at most p.scan_tokens new tokens.
-hipError_t launch_paged_scan(const PagedAttnArgs& p, float* partial, hipStream_t st) {
+hipError_t launch_paged_scan(const PagedAttnArgs& args, int32_t* plan, float* partial, hipStream_t st) {
+  PagedAttnArgs p = args;
+  p.scan_least = PAGED_SCAN_LEAST;
+  p.scan_plan = plan;
   AttnArgs a{};
   a.packed_k = p.pool_k;
   a.packed_v = p.pool_v;
@@ -1014,9 +1101,12 @@ hipError_t launch_paged_scan(const PagedAttnArgs& p, float* partial, hipStream_t
     case 3: split = launch_nq<3>(a, &p, st); break;
     default: split = launch_nq<4>(a, &p, st); break;
   }
-  a.tiles_per_chunk = split.tiles_per_chunk;
-  a.n_chunks = split.n_chunks;
-  hipLaunchKernelGGL(paged_combine_kernel, dim3((unsigned)(a.n_q_heads * p.c.batch * p.scan_tokens)), dim3(1024), 0, st, a, p);
+  p.scan_items = split.n_chunks;
+  const int64_t tokens = (int64_t)p.c.batch * p.scan_tokens;
+  if (tokens * a.n_q_heads <= 2 * N_CU)  // a CU holds two of these workgroups
+    hipLaunchKernelGGL(paged_combine_kernel<1>, dim3((unsigned)(tokens * a.n_q_heads)), dim3(1024), 0, st, a, p);
+  else
+    hipLaunchKernelGGL(paged_combine_kernel<8>, dim3((unsigned)(tokens * a.n_kv_heads)), dim3(1024), 0, st, a, p);
   return hipGetLastError();
 }
 

@@ -864,7 +864,7 @@ hipError_t launch_paged_attention(const PagedAttnArgs& args, void* workspace, hi
     }
     e = hipGetLastError();
   }
-  if (e == hipSuccess && p.scan_tokens > 0) e = launch_paged_scan(a, reinterpret_cast<float*>(ws + p.scan_at), st);
+  if (e == hipSuccess && p.scan_tokens > 0) e = launch_paged_scan(a, reinterpret_cast<int32_t*>(ws + p.plan_at), reinterpret_cast<float*>(ws + p.scan_at), st);
   return e;
 }
 

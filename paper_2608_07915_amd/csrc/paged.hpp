@@ -71,6 +71,8 @@ struct PagedAttnArgs {
   int32_t n_q_heads, n_qh;
   int32_t max_new;
   int32_t scan_tokens;  // sequences with at most so many new tokens are the scan kernel's
+  int32_t scan_items, scan_least;  // its workgroups per KV head, and the fewest tiles of one
+  int32_t* scan_plan;   // workspace: [batch][2], a sequence's first item and how many it has
   int32_t Wk, Wv;
   int64_t max_tokens;
   float scale_log2;  // softmax scale * log2(e)
@@ -98,7 +100,7 @@ hipError_t launch_pages_compact(const spectra_dev::PageMap& m, int32_t* moved, c
 hipError_t launch_page_copies(const spectra_dev::PoolList& pools, const spectra_dev::PageMoves& mv, int64_t most_moves,
                               hipStream_t st);
 hipError_t launch_paged_encode(const spectra_dev::PagedEncodeArgs& a, bool f32_input, hipStream_t st);
-// Sequences of at most a.scan_tokens new tokens (a.scan_tokens * n_qh <= scan_rows), partials in `partial`.
-hipError_t launch_paged_scan(const spectra_dev::PagedAttnArgs& a, float* partial, hipStream_t st);
+// Sequences of at most a.scan_tokens new tokens (a.scan_tokens * n_qh <= scan_rows): its plan [batch][2] and partials.
+hipError_t launch_paged_scan(const spectra_dev::PagedAttnArgs& a, int32_t* plan, float* partial, hipStream_t st);
 hipError_t launch_paged_attention(const spectra_dev::PagedAttnArgs& a, void* workspace, hipStream_t st);
 }  // namespace spectra

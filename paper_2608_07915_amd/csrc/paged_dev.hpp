@@ -51,6 +51,88 @@ __device__ __forceinline__ bool scanned(const PagedAttnArgs& a, const PagedSeq& 
   return s.n > 0 && s.n <= a.scan_tokens && attended(a, s);
 }
 
+// Where the scan's work lies: chunks of tiles_per_chunk tiles, the sequences' one after the
+// other (items), about as many as the call has workgroups for (p.scan_items). The length of a
+// chunk comes from what the sequences hold, not from the longest that the call allows.
+struct ScanPlace {
+  int b, chunk;    // of an item; b < 0: none
+  int n_chunks;    // of its sequence
+  int tiles_per_chunk;
+};
+struct ScanScratch {
+  int64_t part[4];
+  int64_t total;
+  int32_t b, at, n;
+};
+// Of an item; the same in every thread of a workgroup of 256.
+__device__ __forceinline__ ScanPlace scan_place(const PagedAttnArgs& p, int item, ScanScratch& s) {
+  constexpr int NT = 256;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  auto tiles_of = [&](int b) -> int64_t {
+    if (b >= p.c.batch) return 0;
+    const PagedSeq q = paged_seq(p.c, b);
+    return scanned(p, q) ? (q.len + TILE - 1) / TILE : 0;
+  };
+  // inclusive sum of v over the workgroup; the total in s.total
+  auto sum = [&](int64_t v) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t u = __shfl_up(v, o);
+      if (lane >= o) v += u;
+    }
+    __syncthreads();
+    if (lane == 63) s.part[wave] = v;
+    __syncthreads();
+    int64_t before = 0;
+    for (int w = 0; w < wave; ++w) before += s.part[w];
+    if (tid == NT - 1) s.total = before + v;
+    __syncthreads();
+    return before + v;
+  };
+  const int64_t mine = tiles_of(tid);  // of the first NT sequences
+  int64_t total = 0;
+  if (p.c.batch == 1) {
+    total = tiles_of(0);
+  } else {
+    int64_t v = mine;
+    for (int b = tid + NT; b < p.c.batch; b += NT) v += tiles_of(b);
+    sum(v);
+    total = s.total;
+  }
+  ScanPlace r;
+  // every sequence ends in half a chunk on average: those count too
+  const int64_t whole = p.scan_items - (p.c.batch < p.scan_items ? p.c.batch : p.scan_items) / 2;
+  int64_t tpc = (total + whole - 1) / whole;
+  tpc = (tpc + 3) & ~(int64_t)3;  // whole steps of four wavefronts
+  r.tiles_per_chunk = (int)(tpc < p.scan_least ? p.scan_least : tpc);
+  if (p.c.batch == 1) {
+    r.n_chunks = (int)((total + r.tiles_per_chunk - 1) / r.tiles_per_chunk);
+    r.chunk = item;
+    r.b = item < r.n_chunks ? 0 : -1;
+    return r;
+  }
+  if (tid == 0) s.b = -1;
+  int base = 0;
+  for (int b0 = 0; b0 < p.c.batch; b0 += NT) {
+    const int64_t t = b0 == 0 ? mine : tiles_of(b0 + tid);
+    const int n = (int)((t + r.tiles_per_chunk - 1) / r.tiles_per_chunk);
+    const int lo = base + (int)sum(n) - n;
+    if (item >= lo && item < lo + n) {
+      s.b = b0 + tid;
+      s.at = lo;
+      s.n = n;
+    }
+    __syncthreads();
+    if (s.b >= 0) break;
+    base += (int)s.total;
+    __syncthreads();
+  }
+  r.b = __builtin_amdgcn_readfirstlane(s.b);
+  r.n_chunks = __builtin_amdgcn_readfirstlane(s.n);
+  r.chunk = item - __builtin_amdgcn_readfirstlane(s.at);
+  return r;
+}
+
 __device__ __forceinline__ float query_at(const PagedAttnArgs& a, int64_t i) {
   return a.q_f32 ? reinterpret_cast<const float*>(a.q)[i] : bf2f(reinterpret_cast<const uint16_t*>(a.q)[i]);
 }

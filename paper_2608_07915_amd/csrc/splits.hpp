@@ -209,21 +209,18 @@ inline RopeSplit rope_split(int64_t groups, int n_qh, int words, int64_t n_tiles
 // ---------------------------------------------------------------------------
 // Paged attention
 // ---------------------------------------------------------------------------
-// Scan of sequences with few new tokens: chunks of whole steps of four wavefronts for at most
-// one round of workgroups over all sequences at the longest length.
-inline int64_t paged_scan_wanted(int64_t groups, int per_cu) {
-  const int64_t n = N_CU * per_cu / groups;
+// Scan of sequences with few new tokens, for a kernel of which a CU holds per_cu workgroups: the
+// chunks of a KV head that make one round of workgroups (their length is found on the device), and
+// the fewest tiles that are a chunk.
+constexpr int64_t PAGED_SCAN_LEAST = SCAN_WAVES;
+inline int64_t paged_scan_items(int64_t n_kv, int per_cu) {
+  const int64_t n = N_CU * per_cu / n_kv;
   return n < 1 ? 1 : n;
 }
-inline Split paged_scan_split(int64_t groups, int64_t n_tiles, int per_cu) {
-  int64_t tpc = ceil_div(n_tiles, paged_scan_wanted(groups, per_cu));
-  if (tpc < 2 * SCAN_WAVES) tpc = 2 * SCAN_WAVES;
-  return split_tiles(n_tiles, ceil_div(tpc, SCAN_WAVES) * SCAN_WAVES);
-}
-// The most chunks that any cache of up to n_tiles tiles is split into.
-inline int64_t paged_scan_chunks(int64_t groups, int64_t n_tiles) {
-  const int64_t most = ceil_div(n_tiles, 2 * SCAN_WAVES), want = paged_scan_wanted(groups, 3);
-  return most < want ? most : want;
+// The most chunks of all KV heads that sequences of up to n_tiles tiles come to.
+inline int64_t paged_scan_chunks(int64_t batch, int64_t n_kv, int64_t n_tiles) {
+  const int64_t most = batch * ceil_div(n_tiles, PAGED_SCAN_LEAST), some = paged_scan_items(n_kv, 3) + batch;
+  return n_kv * (most < some ? most : some);
 }
 
 // Workgroups of 256 rows, of which a CU holds one, take a step of 128 slots at a time. With
@@ -258,7 +255,7 @@ struct PagedPlan {
   int32_t scan_tokens;  // sequences of at most so many new tokens are scanned (0: none)
   int64_t units;        // of PAGED_ROWS rows, for the others (0: none)
   ChunkSplit split;
-  size_t scan_at, part_at, bytes;  // workspace: lse terms, then the scan's partials, then the parts
+  size_t plan_at, scan_at, part_at, bytes;  // workspace: lse terms, the scan's plan, its partials, the parts
 };
 inline size_t paged_round(size_t b) { return (b + 255) / 256 * 256; }
 inline int64_t paged_units(int32_t batch, int64_t n_new, int32_t n_qh, int32_t max_new) {
@@ -276,11 +273,11 @@ inline PagedPlan paged_plan(int32_t batch, int64_t n_new, int32_t n_q_heads, int
     p.units = paged_units(batch, n_new, n_qh, max_new);
     p.split = paged_chunk_split(p.units * n_kv, max_tokens);
   }
-  p.scan_at = paged_round((size_t)n_kv * 128 * sizeof(float));
+  p.plan_at = paged_round((size_t)n_kv * 128 * sizeof(float));
+  p.scan_at = p.plan_at + paged_round((size_t)batch * 2 * sizeof(int32_t));
   p.part_at = p.scan_at;
   if (p.scan_tokens > 0)
-    p.part_at += paged_round((size_t)batch * p.scan_tokens * n_q_heads * SCAN_PART_BYTES *
-                             (size_t)paged_scan_chunks((int64_t)batch * n_kv, ceil_div(max_tokens, 64)));
+    p.part_at += paged_round((size_t)(paged_scan_chunks(batch, n_kv, ceil_div(max_tokens, 64)) * p.scan_tokens * n_qh) * SCAN_PART_BYTES);
   p.bytes = p.part_at + (p.split.parts > 1 ? (size_t)(p.units * n_kv * p.split.parts) * PAGED_PART_BYTES : 0);
   return p;
 }
@@ -288,12 +285,9 @@ inline PagedPlan paged_plan(int32_t batch, int64_t n_new, int32_t n_q_heads, int
 // serves every smaller one.
 inline size_t paged_workspace_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv, int32_t max_new, int64_t max_tokens) {
   const int32_t n_qh = n_q_heads / n_kv, few = 16 / n_qh;
-  const int64_t groups = (int64_t)batch * n_kv, tiles = ceil_div(max_tokens, 64), steps = ceil_div(max_tokens, PAGED_STEP);
-  int64_t scan = groups * ceil_div(tiles, 2 * SCAN_WAVES);  // chunks of all sequences
-  const int64_t round = groups > 3 * N_CU ? groups : 3 * N_CU;
-  if (scan > round) scan = round;
-  size_t b = paged_round((size_t)n_kv * 128 * sizeof(float)) +
-             paged_round((size_t)(scan * n_qh * (max_new < few ? max_new : few)) * SCAN_PART_BYTES);
+  const int64_t steps = ceil_div(max_tokens, PAGED_STEP);
+  size_t b = paged_round((size_t)n_kv * 128 * sizeof(float)) + paged_round((size_t)batch * 2 * sizeof(int32_t)) +
+             paged_round((size_t)(paged_scan_chunks(batch, n_kv, ceil_div(max_tokens, 64)) * n_qh * (max_new < few ? max_new : few)) * SCAN_PART_BYTES);
   if (max_new > 12 / n_qh) {
     int64_t parts = paged_units(batch, n_new, n_qh, max_new) * n_kv * (steps < 64 ? steps : 64);
     if (parts > 2 * N_CU) parts = 2 * N_CU;

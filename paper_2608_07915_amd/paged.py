@@ -26,35 +26,34 @@ class PagedCache:
         self.refs = torch.zeros(self.n_pages, dtype=torch.int32, device=device)
         self.struct = spectra_pages(self.n_pages, self.page_tokens, self.rows, self.row_pages, 0, self.table.data_ptr(),
                                     self.lens.data_ptr(), self.refs.data_ptr())
+        self.ref = ctypes.byref(self.struct)
 
     def empty_pool(self, codec: Codec):
         """A pool for the codec's records: int32 [n_pages, words of a page], zeros."""
         import torch
-        words = int(_lib.get().spectra_paged_pool_words(ctypes.byref(self.struct), ctypes.byref(codec.struct)))
+        words = int(_lib.get().spectra_paged_pool_words(self.ref, ctypes.byref(codec.struct)))
         return torch.zeros((self.n_pages, words // self.n_pages), dtype=torch.int32, device=self.table.device)
 
 
-class _Stream:
+class _Call:
     """The call's stream, with the cache's device current while the call is made."""
+    __slots__ = ("given", "handle", "ctx")
 
     def __init__(self, device, stream):
         import torch
         _need(device.type == "cuda", "the page map must be on a device")
         _need(stream is None or stream.device == device, f"the stream belongs to another device than the page map's {device}")
-        self.ctx = torch.cuda.device(device)
         self.given = stream
-        self.stream = stream if stream is not None else torch.cuda.current_stream(device)
+        self.handle = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index)
+        self.ctx = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
 
     def __enter__(self):
-        self.ctx.__enter__()
+        if self.ctx is not None:
+            self.ctx.__enter__()
         return self
 
     def __exit__(self, *exc):
-        return self.ctx.__exit__(*exc)
-
-    @property
-    def handle(self):
-        return ctypes.c_void_p(self.stream.cuda_stream)
+        return self.ctx.__exit__(*exc) if self.ctx is not None else None
 
     def keep(self, *made):
         """Tensors made here for the call: not reused before a given stream has passed it."""
@@ -69,22 +68,25 @@ def _ints(t, name: str, device, n=None):
     import torch
     if t is None:
         return None
-    _need(t.device == device and t.dtype == torch.int32 and t.is_contiguous() and t.dim() == 1,
-          f"{name} must be a contiguous one-dimensional int32 tensor on {device}")
-    _need(n is None or t.numel() == n, f"{name} must have {n} elements, got {t.numel()}")
+    if not (t.device == device and t.dtype == torch.int32 and t.dim() == 1 and t.is_contiguous()):
+        raise ValueError(f"{name} must be a contiguous one-dimensional int32 tensor on {device}")
+    if n is not None and t.numel() != n:
+        raise ValueError(f"{name} must have {n} elements, got {t.numel()}")
     return t.data_ptr()
 
 
 def _pools(cache: PagedCache, pools):
     import torch
-    pools = [pools] if isinstance(pools, torch.Tensor) else list(pools)
-    made = (spectra_pool * max(len(pools), 1))()
+    pools = [pools] if isinstance(pools, torch.Tensor) else pools
+    dev, n_pages, flat = cache.table.device, cache.n_pages, []
     for i, p in enumerate(pools):
-        _need(p.device == cache.table.device and p.dtype == torch.int32 and p.is_contiguous(),
-              f"pool {i} must be a contiguous int32 tensor on {cache.table.device}")
-        _need(p.numel() % (64 * cache.n_pages) == 0, f"pool {i}: {p.numel()} words are not {cache.n_pages} pages of whole tiles")
-        made[i].base, made[i].page_words = p.data_ptr(), p.numel() // cache.n_pages
-    return made, len(pools)
+        n = p.numel()
+        if not (p.device == dev and p.dtype == torch.int32 and p.is_contiguous()):
+            raise ValueError(f"pool {i} must be a contiguous int32 tensor on {dev}")
+        if n % (64 * n_pages):
+            raise ValueError(f"pool {i}: {n} words are not {n_pages} pages of whole tiles")
+        flat.append((p.data_ptr(), n // n_pages))
+    return (spectra_pool * max(len(flat), 1))(*flat), len(flat)
 
 
 def _workspace(cache: PagedCache, workspace, need: int):
@@ -101,7 +103,7 @@ def _bytes(t) -> int:
 
 
 def spectra_pages_workspace_bytes(cache: PagedCache) -> int:
-    return int(_lib.get().spectra_pages_workspace_bytes(ctypes.byref(cache.struct)))
+    return int(_lib.get().spectra_pages_workspace_bytes(cache.ref))
 
 
 def spectra_pages_extend(cache: PagedCache, rows, counts, pools, ends=None, workspace=None, stream=None):
@@ -110,13 +112,13 @@ def spectra_pages_extend(cache: PagedCache, rows, counts, pools, ends=None, work
     import torch
     dev = cache.table.device
     n = rows.numel()
-    with _Stream(dev, stream) as s:
+    with _Call(dev, stream) as s:
         args = (_ints(rows, "rows", dev), _ints(counts, "counts", dev, n))
         made, n_pools = _pools(cache, pools)
         new_ends = torch.empty_like(rows) if ends is None else None
         ends = new_ends if ends is None else ends
         ws = _workspace(cache, workspace, spectra_pages_workspace_bytes(cache))
-        check(_lib.get().spectra_pages_extend(ctypes.byref(cache.struct), *args, n, made, n_pools,
+        check(_lib.get().spectra_pages_extend(cache.ref, *args, n, made, n_pools,
                                               _ints(ends, "ends", dev, n), ws.data_ptr(), _bytes(ws), s.handle))
         s.keep(new_ends, ws if workspace is None else None)
     return ends
@@ -128,10 +130,10 @@ def spectra_pages_fork(cache: PagedCache, parents, children, ends=None, stream=N
     import torch
     dev = cache.table.device
     n = parents.numel()
-    with _Stream(dev, stream) as s:
+    with _Call(dev, stream) as s:
         new_ends = torch.empty_like(parents) if ends is None else None
         ends = new_ends if ends is None else ends
-        check(_lib.get().spectra_pages_fork(ctypes.byref(cache.struct), _ints(parents, "parents", dev),
+        check(_lib.get().spectra_pages_fork(cache.ref, _ints(parents, "parents", dev),
                                             _ints(children, "children", dev, n), n, _ints(ends, "ends", dev, n), s.handle))
         s.keep(new_ends)
     return ends
@@ -141,8 +143,8 @@ def spectra_pages_truncate(cache: PagedCache, rows, keep=None, stream=None) -> N
     """Row rows[i] keeps its first keep[i] slots (keep None: the rows are emptied)."""
     dev = cache.table.device
     n = rows.numel()
-    with _Stream(dev, stream) as s:
-        check(_lib.get().spectra_pages_truncate(ctypes.byref(cache.struct), _ints(rows, "rows", dev),
+    with _Call(dev, stream) as s:
+        check(_lib.get().spectra_pages_truncate(cache.ref, _ints(rows, "rows", dev),
                                                 _ints(keep, "keep", dev, n), n, s.handle))
 
 
@@ -151,12 +153,12 @@ def spectra_pages_compact(cache: PagedCache, pools, moved=None, workspace=None, 
     afterwards, then the number of used pages."""
     import torch
     dev = cache.table.device
-    with _Stream(dev, stream) as s:
+    with _Call(dev, stream) as s:
         made, n_pools = _pools(cache, pools)
         new_moved = torch.empty(cache.n_pages + 1, dtype=torch.int32, device=dev) if moved is None else None
         moved = new_moved if moved is None else moved
         ws = _workspace(cache, workspace, spectra_pages_workspace_bytes(cache))
-        check(_lib.get().spectra_pages_compact(ctypes.byref(cache.struct), made, n_pools,
+        check(_lib.get().spectra_pages_compact(cache.ref, made, n_pools,
                                                _ints(moved, "moved", dev, cache.n_pages + 1), ws.data_ptr(), _bytes(ws),
                                                s.handle))
         s.keep(new_moved, ws if workspace is None else None)
@@ -173,9 +175,9 @@ def _sequences(cache: PagedCache, ck: Codec, cv: Codec, pool_k, pool_v, cu_new, 
         _need(codec.basis.device == dev, f"the codecs must be on {dev}")
         _need(pool.device == dev and pool.dtype == torch.int32 and pool.is_contiguous(),
               f"{name} must be a contiguous int32 tensor on {dev}")
-        need = int(_lib.get().spectra_paged_pool_words(ctypes.byref(cache.struct), ctypes.byref(codec.struct)))
+        need = int(_lib.get().spectra_paged_pool_words(cache.ref, ctypes.byref(codec.struct)))
         _need(pool.numel() == need, f"{name} holds {pool.numel()} words, the map and codec need {need}")
-    return batch, (ctypes.byref(cache.struct), ctypes.byref(ck.struct), ctypes.byref(cv.struct), pool_k.data_ptr(),
+    return batch, (cache.ref, ctypes.byref(ck.struct), ctypes.byref(cv.struct), pool_k.data_ptr(),
                    pool_v.data_ptr(), _ints(rows, "rows", dev, batch), _ints(ends, "ends", dev, batch),
                    _ints(cu_new, "cu_new", dev), batch)
 
@@ -197,7 +199,7 @@ def spectra_paged_encode(cache: PagedCache, ck: Codec, cv: Codec, pool_k, pool_v
     _rows(k, "k", dev, ck.n_streams)
     _rows(v, "v", dev, ck.n_streams, k.shape[0])
     _need(k.dtype == v.dtype, "k and v must have one dtype")
-    with _Stream(dev, stream) as s:
+    with _Call(dev, stream) as s:
         check(_lib.get().spectra_paged_encode(*head, k.shape[0], k.data_ptr(), k.stride(0), k.stride(1), v.data_ptr(),
                                               v.stride(0), v.stride(1), _dtype_code(k), s.handle))
 
@@ -223,7 +225,7 @@ def spectra_paged_attention(cache: PagedCache, ck: Codec, cv: Codec, pool_k, poo
     _need(n_q_heads % ck.n_streams == 0, f"n_q_heads={n_q_heads} is not a multiple of the codec's {ck.n_streams} KV heads")
     _need(lse is None or (lse.device == dev and lse.dtype == torch.float32 and lse.is_contiguous()
                           and tuple(lse.shape) == (n, n_q_heads)), f"lse must be a contiguous float32 tensor {(n, n_q_heads)}")
-    with _Stream(dev, stream) as s:
+    with _Call(dev, stream) as s:
         new_out = torch.empty((n, n_q_heads, 128), dtype=q.dtype, device=dev) if out is None else None
         out = new_out if out is None else out
         _need(out.device == dev and out.is_contiguous() and tuple(out.shape) == (n, n_q_heads, 128),

@@ -37,17 +37,23 @@ int main() {
     CHECK(p.units == 0 || p.split.slots % PAGED_STEP == 0);
     CHECK(p.scan_tokens * n_qh <= rows && (p.units > 0) == (max_new > p.scan_tokens));
     CHECK(p.scan_tokens > 0 || n_new >= (int64_t)batch * max_new || rows / n_qh == 0);
-    CHECK(p.scan_at <= p.part_at && p.part_at <= p.bytes);
+    CHECK(p.plan_at <= p.scan_at && p.scan_at <= p.part_at && p.part_at <= p.bytes);
     // units of every sequence: the worst cut of n_new tokens into `batch` sequences
     const int64_t all = n_new < (int64_t)batch * max_new ? n_new : (int64_t)batch * max_new;
     CHECK(p.units == 0 || p.units * PAGED_ROWS >= all * n_qh);
     const size_t room = paged_workspace_bytes(batch, n_new, q, kv, max_new, max_tokens);
     CHECK(room >= p.bytes);
-    const int64_t tiles = ceil_div(max_tokens, 64), groups = (int64_t)batch * kv;
+    // the scan's chunks, their length found from the sequences' tiles as on the device
     for (int per_cu = 1; per_cu <= 3; ++per_cu) {
-      const Split s = paged_scan_split(groups, tiles, per_cu);
-      CHECK(s.n_chunks <= paged_scan_chunks(groups, tiles) && (int64_t)s.n_chunks * s.tiles_per_chunk >= tiles);
-      CHECK(s.tiles_per_chunk % SCAN_WAVES == 0);
+      const int64_t items = paged_scan_items(kv, per_cu);
+      int64_t total = 0, chunks = 0, each[40];
+      const int nb = batch < 40 ? batch : 40;
+      for (int i = 0; i < nb; ++i) total += each[i] = ceil_div(pick(1, max_tokens), 64);
+      const int64_t whole = items - (nb < items ? nb : items) / 2;
+      int64_t tpc = ceil_div(ceil_div(total, whole), SCAN_WAVES) * SCAN_WAVES;
+      if (tpc < PAGED_SCAN_LEAST) tpc = PAGED_SCAN_LEAST;
+      for (int i = 0; i < nb; ++i) chunks += ceil_div(each[i], tpc);
+      CHECK(chunks <= items + nb && chunks * kv <= paged_scan_chunks(nb, kv, ceil_div(max_tokens, 64)));
     }
     // any smaller call
     const int b2 = (int)pick(1, batch), m2 = (int)pick(1, max_new);
