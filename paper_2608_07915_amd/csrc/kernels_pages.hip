@@ -5,6 +5,8 @@
 
 namespace spectra_dev {
 
+typedef int32_t i32x4 __attribute__((ext_vector_type(4)));
+
 constexpr int PLAN = 1024;  // threads of a planning workgroup
 static_assert(PAGES_LIST == PLAN, "an entry per thread");
 
@@ -47,8 +49,16 @@ __device__ __forceinline__ int64_t list_pages(const int32_t* __restrict__ refs, 
   for (int64_t p0 = lo; p0 < hi && found < most; p0 += PLAN * EACH) {
     const int64_t p = p0 + (int64_t)threadIdx.x * EACH;
     uint32_t mask = 0u;
+    if (p + EACH <= hi && (reinterpret_cast<uintptr_t>(refs + p) & 15) == 0) {
+      i32x4 r[EACH / 4];
 #pragma unroll
-    for (int i = 0; i < EACH; ++i) mask |= (p + i < hi && take(refs[p + i])) ? 1u << i : 0u;
+      for (int i = 0; i < EACH / 4; ++i) r[i] = reinterpret_cast<const i32x4*>(refs + p)[i];
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) mask |= take(r[i >> 2][i & 3]) ? 1u << i : 0u;
+    } else {
+#pragma unroll
+      for (int i = 0; i < EACH; ++i) mask |= (p + i < hi && take(refs[p + i])) ? 1u << i : 0u;
+    }
     const int mine = __popc(mask);
     const int64_t upto = block_scan(mine, part);
     if (threadIdx.x == PLAN - 1) total_s = upto;
@@ -226,9 +236,15 @@ __global__ __launch_bounds__(PLAN) void pages_compact_kernel(PageMap m, int32_t*
   __shared__ int64_t used_s;
   const int t = threadIdx.x;
   int64_t mine = 0;
-  for (int64_t p = t; p < m.n_pages; p += PLAN) {
-    mine += m.refs[p] > 0 ? 1 : 0;
-    moved[p] = (int32_t)p;
+  for (int64_t p0 = 0; p0 < m.n_pages; p0 += 8 * PLAN) {
+    int32_t r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = p0 + t + PLAN * i < m.n_pages ? m.refs[p0 + t + PLAN * i] : 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      mine += r[i] > 0 ? 1 : 0;
+      if (p0 + t + PLAN * i < m.n_pages) moved[p0 + t + PLAN * i] = (int32_t)(p0 + t + PLAN * i);
+    }
   }
   const int64_t upto = block_scan(mine, part);
   if (t == PLAN - 1) used_s = upto;
@@ -237,11 +253,23 @@ __global__ __launch_bounds__(PLAN) void pages_compact_kernel(PageMap m, int32_t*
   const int64_t holes = list_pages(m.refs, 0, used, used, mv.dst, part, [](int32_t r) { return r <= 0; });
   list_pages(m.refs, used, m.n_pages, holes, mv.src, part, [](int32_t r) { return r > 0; });
   __syncthreads();
-  for (int64_t k = t; k < holes; k += PLAN) {
-    const int32_t s = mv.src[k], d = mv.dst[k];
-    moved[s] = d;
-    m.refs[d] = m.refs[s];
-    m.refs[s] = 0;
+  for (int64_t k0 = t; k0 < holes; k0 += 8 * PLAN) {
+    int32_t s[8], d[8], r[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+      const int64_t k = k0 + PLAN * i;
+      s[i] = k < holes ? mv.src[k] : -1;
+      d[i] = k < holes ? mv.dst[k] : -1;
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) r[i] = s[i] >= 0 ? m.refs[s[i]] : 0;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (s[i] >= 0) {
+        moved[s[i]] = d[i];
+        m.refs[d[i]] = r[i];
+        m.refs[s[i]] = 0;
+      }
   }
   if (t == 0) {
     moved[m.n_pages] = (int32_t)used;
