@@ -326,9 +326,9 @@ spectra_status spectra_decode_step_static(const spectra_codec* ck, const spectra
  * ------------------------------------------------------------------------- */
 typedef struct {
   int64_t n_pages;     /* pages of every pool, < 2^31 - 1 */
-  int32_t page_tokens; /* slots of a page, a multiple of 64 */
+  int32_t page_tokens; /* slots of a page, a multiple of 64, <= 2^20 */
   int32_t rows;        /* sequences, <= 65535 */
-  int32_t row_pages;   /* entries of a table row; row_pages * page_tokens < 2^31 */
+  int32_t row_pages;   /* entries of a table row; row_pages * page_tokens <= 2^30 */
   int32_t reserved;
   int32_t* table;      /* device [rows][row_pages] */
   int32_t* lens;       /* device [rows] */
@@ -404,7 +404,9 @@ spectra_status spectra_paged_encode(const spectra_pages* m, const spectra_codec*
  * out_dt fp32: the error is that of fp32 sums (about 1e-6 of the result). bf16: operands are
  * rounded to fp16, which stays below the output's rounding; lse is then good to about 1e-3.
  * Coefficients are held in fp16 parts: those beyond 65504 are taken as 65504, and of those below
- * 2^-14 absolute errors of 2^-25 remain. softmax_scale <= 0 selects 1/sqrt(128). Workspace:
+ * 2^-14 absolute errors of 2^-25 remain; with bf16 outputs that holds for scale log2(e) q V_K too.
+ * NaN and infinities in a query row reach no other row. At most 2^30 query rows and 2^18 sequences
+ * times KV heads. softmax_scale <= 0 selects 1/sqrt(128). Workspace:
  * device, 256-byte aligned, spectra_paged_attention_workspace_bytes (never fewer for larger counts:
  * one taken for the largest call serves every smaller one of as many heads). Asynchronous. */
 size_t spectra_paged_attention_workspace_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv_heads,

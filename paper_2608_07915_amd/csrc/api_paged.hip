@@ -18,17 +18,19 @@ using spectra_dev::PoolList;
 namespace {
 
 constexpr int64_t kMaxBatch = 16384;
-constexpr int64_t kMost = (int64_t)1 << 31;  // slots, rows: counted in 32 bits
+constexpr int64_t kMost = (int64_t)1 << 30;       // slots of a row, query rows of a call: counted in 32 bits
+constexpr int32_t kMostPage = 1 << 20;            // slots of a page: a record's place in it too
+constexpr int64_t kMostGroups = (int64_t)1 << 18;  // sequences times KV heads: 16 workgroups each at most
 
 spectra_status check_map(const spectra_pages* m, const char* name, bool with_refs) {
   if (!m) return fail(SPECTRA_EINVAL, "%s: null page map", name);
   if (m->n_pages <= 0 || m->n_pages >= ((int64_t)1 << 31) - 1)
     return fail(SPECTRA_EINVAL, "%s: n_pages=%lld out of range", name, (long long)m->n_pages);
-  if (m->page_tokens <= 0 || m->page_tokens % 64 != 0)
-    return fail(SPECTRA_EINVAL, "%s: page_tokens=%d must be a positive multiple of 64", name, m->page_tokens);
+  if (m->page_tokens <= 0 || m->page_tokens % 64 != 0 || m->page_tokens > kMostPage)
+    return fail(SPECTRA_EINVAL, "%s: page_tokens=%d must be a positive multiple of 64 up to 2^20", name, m->page_tokens);
   if (m->rows <= 0 || m->rows > 65535) return fail(SPECTRA_EINVAL, "%s: rows=%d out of range [1, 65535]", name, m->rows);
-  if (m->row_pages <= 0 || (int64_t)m->row_pages * m->page_tokens >= ((int64_t)1 << 31))
-    return fail(SPECTRA_EINVAL, "%s: row_pages=%d must be positive and a row's slots below 2^31", name, m->row_pages);
+  if (m->row_pages <= 0 || (int64_t)m->row_pages * m->page_tokens > kMost)
+    return fail(SPECTRA_EINVAL, "%s: row_pages=%d must be positive and a row's slots at most 2^30", name, m->row_pages);
   if (!m->table || !m->lens || !aligned(m->table, 4) || !aligned(m->lens, 4))
     return fail(SPECTRA_EINVAL, "%s: table and lens must be non-null and 4-byte aligned", name);
   if (with_refs && (!m->refs || !aligned(m->refs, 4)))
@@ -213,7 +215,7 @@ spectra_status spectra_paged_encode(const spectra_pages* m, const spectra_codec*
 
 size_t spectra_paged_attention_workspace_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv_heads,
                                                int32_t max_new, int64_t max_tokens) {
-  if (batch <= 0 || batch > kMaxBatch || n_new <= 0 || n_new >= kMost || max_new <= 0 || max_tokens <= 0 || max_tokens >= kMost) return 0;
+  if (batch <= 0 || batch > kMaxBatch || n_new <= 0 || n_new > kMost || max_new <= 0 || max_tokens <= 0 || max_tokens > kMost) return 0;
   if (n_kv_heads <= 0 || n_kv_heads > 65535 || n_q_heads <= 0 || n_q_heads % n_kv_heads || n_q_heads / n_kv_heads > 16) return 0;
   return paged_workspace_bytes(batch, n_new, n_q_heads, n_kv_heads, max_new, max_tokens);
 }
@@ -231,9 +233,11 @@ spectra_status spectra_paged_attention(const spectra_pages* m, const spectra_cod
   if (n_q_heads <= 0 || n_q_heads % a.c.n_kv != 0)
     return fail(SPECTRA_EINVAL, "%s: n_q_heads=%d must be a positive multiple of the codecs' %d KV heads", name, n_q_heads, a.c.n_kv);
   if (n_q_heads / a.c.n_kv > 16) return fail(SPECTRA_EUNSUPPORTED, "%s: more than 16 query heads per KV head", name);
-  if (max_new < 0 || max_tokens < 0 || max_tokens >= kMost || (int64_t)max_new * n_q_heads >= kMost)
+  if (max_new < 0 || max_tokens < 0 || max_tokens > kMost || (int64_t)max_new * n_q_heads > kMost)
     return fail(SPECTRA_EINVAL, "%s: max_new=%d or max_tokens=%lld out of range", name, max_new, (long long)max_tokens);
-  if (n_new * n_q_heads >= kMost || (int64_t)batch * 16 * n_q_heads >= kMost) return fail(SPECTRA_EINVAL, "%s: n_new * n_q_heads and 16 * batch * n_q_heads must stay below 2^31", name);
+  if (n_new * n_q_heads > kMost || (int64_t)batch * a.c.n_kv >= kMostGroups)
+    return fail(SPECTRA_EINVAL, "%s: n_new=%lld times %d query heads passes 2^30, or batch=%d times %d KV heads 2^18", name,
+                (long long)n_new, n_q_heads, batch, a.c.n_kv);
   if (!(softmax_scale == softmax_scale) || std::isinf(softmax_scale)) return fail(SPECTRA_EINVAL, "%s: softmax_scale not finite", name);
   if (out_dt != SPECTRA_F32 && out_dt != SPECTRA_BF16) return fail(SPECTRA_EINVAL, "%s: output dtype %d not supported", name, (int)out_dt);
   if (batch == 0 || n_new == 0 || max_new == 0 || max_tokens == 0) return SPECTRA_OK;

@@ -183,7 +183,8 @@ __device__ __forceinline__ float prepare_query(const AttnArgs& a, int s, int nqh
     const float q =
         (h < nqh && kept) ? ((part[0][h][c] + part[1][h][c]) + (part[2][h][c] + part[3][h][c])) * a.scale_log2 : 0.0f;
     qs[h][c] = q;
-    amax = __builtin_fmaxf(amax, __builtin_fabsf(q));
+    const float m = __builtin_fabsf(q);
+    amax = __builtin_fmaxf(amax, m < __builtin_inff() ? m : 0.0f);  // one row's infinity is not the others'
   }
   amax = wave_max(amax);
   if ((tid & 63) == 0) red_s[tid >> 6] = amax;
@@ -783,9 +784,8 @@ __global__ __launch_bounds__(256, 2) void paged_scan_kernel(AttnArgs a, PagedAtt
 // states are then merged in LDS.
 // ---------------------------------------------------------------------------
 // combine_row: nch partials from ph on, `step` floats apart, value stream s; store(i, out_i) takes the row's channels,
-// stats(m, l) in one thread the overall maximum (log2 domain) and sum. With EMPTY, a row without
-// weights gets zeros.
-template <bool EMPTY, typename Store, typename Stats>
+// stats(m, l) in one thread the overall maximum (log2 domain) and sum.
+template <typename Store, typename Stats>
 __device__ __forceinline__ void combine_row(const AttnArgs& a, const float* __restrict__ ph, int64_t step, int nch, int s, Store&& store,
                                             Stats&& stats) {
   constexpr int CB = 12;  // 8 x 12 = 96 chunks per round: one round of loads for ~768 scan workgroups over 8 heads
@@ -851,9 +851,6 @@ __device__ __forceinline__ void combine_row(const AttnArgs& a, const float* __re
     }
     const bool kept = ((bw >> (8 * (tid >> 5))) & 0xFFu) != 0u;
     chat[tid] = (kept ? sacc / sl : 0.0f) + mv;
-    if constexpr (EMPTY) {
-      if (sl == 0.0f) chat[tid] = 0.0f;
-    }
     if (tid == 0) stats(Mx, sl);
   }
   __syncthreads();
@@ -876,7 +873,7 @@ __device__ __forceinline__ void combine_row(const AttnArgs& a, const float* __re
 __global__ __launch_bounds__(1024) void combine_kernel(AttnArgs a) {
   const int hq = blockIdx.x, b = blockIdx.y;
   const int64_t row = (int64_t)b * a.n_q_heads + hq;
-  combine_row<false>(a, a.partial + row * a.n_chunks * PART, PART, a.n_chunks, b * a.n_kv_heads + hq / a.n_qh,
+  combine_row(a, a.partial + row * a.n_chunks * PART, PART, a.n_chunks, b * a.n_kv_heads + hq / a.n_qh,
                      [&](int i, float o) { a.out[row * D + i] = o; }, [](float, float) {});
 }
 
@@ -893,7 +890,19 @@ __global__ __launch_bounds__(1024) void paged_combine_kernel(AttnArgs a, PagedAt
   const PagedSeq seq = paged_seq(p.c, b);
   if (!scanned(p, seq) || tok >= seq.n) return;
   const int kv = ROWS == 1 ? which / a.n_qh : which;
-  const int item0 = seq.len > 0 ? p.scan_plan[2 * b] : 0, n_items = seq.len > 0 ? p.scan_plan[2 * b + 1] : 0;
+  if (seq.len - seq.n + tok < 0) {  // it sees no slot
+    const int rows = ROWS == 1 ? 1 : a.n_qh, hq0 = ROWS == 1 ? which : kv * a.n_qh;
+    const int64_t row = (seq.first + tok) * a.n_q_heads + hq0;
+    for (int i = threadIdx.x; i < rows * D; i += 1024) {
+      if (p.out_f32)
+        reinterpret_cast<float*>(p.out)[row * D + i] = 0.0f;
+      else
+        reinterpret_cast<uint16_t*>(p.out)[row * D + i] = 0;
+    }
+    if (p.lse != nullptr && threadIdx.x < rows) p.lse[row + threadIdx.x] = -__builtin_inff();
+    return;
+  }
+  const int item0 = p.scan_plan[2 * b], n_items = p.scan_plan[2 * b + 1];
   const int rows = p.scan_tokens * a.n_qh;  // partials of an item and KV head
   const int64_t step = (int64_t)a.n_kv_heads * rows * PART;
   const float* first = a.partial + (((int64_t)item0 * a.n_kv_heads + kv) * rows + tok * a.n_qh) * PART;  // of the KV head's first row
@@ -909,10 +918,11 @@ __global__ __launch_bounds__(1024) void paged_combine_kernel(AttnArgs a, PagedAt
     const int64_t qo = (seq.first + tok) * p.q_token_stride + hq * p.q_head_stride;
     float u = 0.0f;
     for (int c = 0; c < D; ++c) u = __builtin_fmaf(query_at(p, qo + c), p.lse_u[kv * D + c], u);
-    p.lse[(seq.first + tok) * a.n_q_heads + hq] = l == 0.0f ? -__builtin_inff() : __builtin_fmaf(__builtin_amdgcn_logf(l) + m, LN2, u);
+    // (no sum: a query that is not finite)
+    p.lse[(seq.first + tok) * a.n_q_heads + hq] = l > 0.0f ? __builtin_fmaf(__builtin_amdgcn_logf(l) + m, LN2, u) : __builtin_nanf("");
   };
   if constexpr (ROWS == 1) {
-    combine_row<true>(a, first + (which - kv * a.n_qh) * PART, step, n_items, kv, [&](int i, float o) { store(which, i, o); },
+    combine_row(a, first + (which - kv * a.n_qh) * PART, step, n_items, kv, [&](int i, float o) { store(which, i, o); },
                       [&](float m, float l) { write_lse(which, m, l); });
   } else {
     __shared__ float chat[ROWS][D];
@@ -953,7 +963,7 @@ __global__ __launch_bounds__(1024) void paged_combine_kernel(AttnArgs a, PagedAt
             M = mb;
           }
         }
-        chat[r][j] = L == 0.0f ? 0.0f : (kept ? A / L : 0.0f) + mv;
+        chat[r][j] = (kept ? A / L : 0.0f) + mv;
         if (j == 0) write_lse(kv * a.n_qh + h, M, L);
       }
       __syncthreads();

@@ -698,7 +698,10 @@ __device__ __forceinline__ float rotate_queries(const PagedAttnArgs& a, const Pa
 #pragma unroll
       for (int j = 0; j < 4; ++j) {
         f32x2 x = f32x2{acc[sl][8 * s + 2 * j] * up, acc[sl][8 * s + 2 * j + 1] * up};
-        if constexpr (!PRECISE) x = f32x2{__builtin_amdgcn_fmed3f(x[0], -65504.0f, 65504.0f), __builtin_amdgcn_fmed3f(x[1], -65504.0f, 65504.0f)};
+        if constexpr (!PRECISE) {  // NaN stays
+#pragma unroll
+          for (int e = 0; e < 2; ++e) x[e] = x[e] > 65504.0f ? 65504.0f : x[e] < -65504.0f ? -65504.0f : x[e];
+        }
         const f16x2 hi = __builtin_convertvector(x, f16x2);
         rh[j] = __builtin_bit_cast(uint32_t, hi);
         rl[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{(x[0] - (float)hi[0]) * CA_LO, (x[1] - (float)hi[1]) * CA_LO}, f16x2));

@@ -104,7 +104,8 @@ __device__ __forceinline__ ScanPlace scan_place(const PagedAttnArgs& p, int item
   const int64_t whole = p.scan_items - (p.c.batch < p.scan_items ? p.c.batch : p.scan_items) / 2;
   int64_t tpc = (total + whole - 1) / whole;
   tpc = (tpc + 3) & ~(int64_t)3;  // whole steps of four wavefronts
-  r.tiles_per_chunk = (int)(tpc < p.scan_least ? p.scan_least : tpc);
+  constexpr int64_t most = (int64_t)1 << 24;  // tiles of the longest row
+  r.tiles_per_chunk = (int)(tpc < p.scan_least ? p.scan_least : tpc < most ? tpc : most);
   if (p.c.batch == 1) {
     r.n_chunks = (int)((total + r.tiles_per_chunk - 1) / r.tiles_per_chunk);
     r.chunk = item;

@@ -170,3 +170,14 @@ def test_binding_refuses_host_tensors():
         S.spectra_paged_attention(c, ck, cv, *pools, torch.zeros(1, 3, 128), cu, 1, 1)
     with pytest.raises(ValueError, match="lse"):
         S.spectra_paged_attention(c, ck, cv, *pools, x, cu, 1, 1, lse=torch.zeros(1, 3))
+
+
+def test_sizes_that_kernels_count_in_32_bits():
+    for call in (encode, attend):
+        assert call(m=_map(page_tokens=2 ** 20 + 64, row_pages=1)) == EINVAL
+        assert call(m=_map(row_pages=2 ** 24 + 1)) == EINVAL
+        assert call(m=_map(row_pages=2 ** 24), batch=0) == 0
+    assert attend(max_tokens=2 ** 30 + 1) == EINVAL
+    assert attend(n_new=2 ** 27 + 1) == EINVAL and attend(max_new=2 ** 27 + 1) == EINVAL
+    many = dict(m=_map(rows=65535), ck=_codec(32), cv=_codec(32), heads=32)
+    assert attend(batch=2 ** 13, **many) == EINVAL and b"2^18" in _lib.get().spectra_last_error()
