@@ -1081,10 +1081,7 @@ hipError_t launch_attention(const AttnArgs& a, hipStream_t st) {
 static_assert(PART * sizeof(float) == SCAN_PART_BYTES, "workspace of a scanned row");
 
 // The sequences of a paged call with at most p.scan_tokens new tokens.
-hipError_t launch_paged_scan(const PagedAttnArgs& args, int32_t* plan, float* partial, hipStream_t st) {
-  PagedAttnArgs p = args;
-  p.scan_least = PAGED_SCAN_LEAST;
-  p.scan_plan = plan;
+static AttnArgs paged_args(const PagedAttnArgs& p, float* partial) {
   AttnArgs a{};
   a.packed_k = p.pool_k;
   a.packed_v = p.pool_v;
@@ -1104,14 +1101,21 @@ hipError_t launch_paged_scan(const PagedAttnArgs& args, int32_t* plan, float* pa
   a.Wv = p.Wv;
   a.scale_log2 = p.scale_log2;
   a.partial = partial;
-  Split split{};
+  return a;
+}
+
+void launch_paged_scan(const PagedAttnArgs& p, float* partial, hipStream_t st) {
+  const AttnArgs a = paged_args(p, partial);
   switch ((p.scan_tokens * p.n_qh + 3) / 4) {
-    case 1: split = launch_nq<1>(a, &p, st); break;
-    case 2: split = launch_nq<2>(a, &p, st); break;
-    case 3: split = launch_nq<3>(a, &p, st); break;
-    default: split = launch_nq<4>(a, &p, st); break;
+    case 1: launch_nq<1>(a, &p, st); break;
+    case 2: launch_nq<2>(a, &p, st); break;
+    case 3: launch_nq<3>(a, &p, st); break;
+    default: launch_nq<4>(a, &p, st); break;
   }
-  p.scan_items = split.n_chunks;
+}
+
+hipError_t launch_paged_combine(const PagedAttnArgs& p, float* partial, hipStream_t st) {
+  const AttnArgs a = paged_args(p, partial);
   const int64_t tokens = (int64_t)p.c.batch * p.scan_tokens;
   if (tokens * a.n_q_heads <= 2 * N_CU)  // a CU holds two of these workgroups
     hipLaunchKernelGGL(paged_combine_kernel<1>, dim3((unsigned)(tokens * a.n_q_heads)), dim3(1024), 0, st, a, p);

@@ -815,6 +815,270 @@ __global__ __launch_bounds__(64) void paged_join_kernel(PagedAttnArgs a) {
 }
 
 // ---------------------------------------------------------------------------
+// Few rows (a decode step's single tokens, a few speculative ones), 16-bit outputs: a sequence's
+// rows on a KV head, at most 16, are the columns of 16 x 16 products, and a chunk of its slots a
+// workgroup's (scan_place). Each wavefront walks tiles of its own, a kept group at a time through
+// one 4 KB tile of LDS, the group's words loaded while the one before is multiplied; no barrier
+// until the wavefronts' sums are merged, and 16 wavefronts on a CU hide each other's chains.
+// ---------------------------------------------------------------------------
+constexpr int FEW_NW = 4, FEW_ROWS = 16, FEW_PITCH = D + 4;
+__global__ __launch_bounds__(64 * FEW_NW, 4) void paged_few_kernel(PagedAttnArgs a, float* __restrict__ partial) {
+  __shared__ ScanScratch place_s;
+  __shared__ float m_s[FEW_NW][FEW_ROWS], l_s[FEW_NW][FEW_ROWS];
+  __shared__ int32_t unit_s[2 * NG];
+  __shared__ __attribute__((aligned(16))) float sums_s[FEW_NW * FEW_ROWS * FEW_PITCH];  // the tiles while wavefronts walk
+  __shared__ __attribute__((aligned(16))) uint8_t q_s[NG][64 * 16];                      // q' as column operands, by lane
+  const int kv = (int)(blockIdx.x % (unsigned)a.c.n_kv), item = (int)(blockIdx.x / (unsigned)a.c.n_kv);
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quarter = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  const ScanPlace at = scan_place(a, item, place_s);
+  if (at.b < 0) return;
+  if (at.chunk == 0 && kv == 0 && tid == 0) {  // for the combine
+    a.scan_plan[2 * at.b] = item;
+    a.scan_plan[2 * at.b + 1] = at.n_chunks;
+  }
+  const PagedSeq seq = paged_seq(a.c, at.b);
+  const int n_rows = (int)seq.n * a.n_qh;
+  Kept Kk = read_kept(a.bits_k + kv * NG), Kv = read_kept(a.bits_v + kv * NG);
+  if (!Kk.ok || Kk.used > a.Wk) Kk.n = 0;  // width table inconsistent with the record
+  if (!Kv.ok || Kv.used > a.Wv) Kv.n = 0;
+  const int row = col < n_rows ? col : 0;  // columns past the rows repeat the first
+  const int tok = row / a.n_qh, head = row - tok * a.n_qh;
+  const int64_t past = seq.len - seq.n + 1;  // slots that token 0 sees
+  const int lim = past + tok < 0 ? 0 : (int)(past + tok), lim_first = past < 0 ? 0 : (int)past;
+
+  // q' of kept group `wave`: element e of quarter p is that of code 4 p + e / 2 + 16 (e % 2), as
+  // the tiles' places are; product x has e = 4 x .. 4 x + 3
+  if (wave < Kk.n) {
+    const int64_t qoff = (seq.first + tok) * a.q_token_stride + (kv * a.n_qh + head) * a.q_head_stride + 8 * quarter;
+    const float* V = a.basis_k + (int64_t)kv * D * D + (8 * quarter) * D + G * pick4(Kk.grp, wave) + 4 * (col >> 2) +
+                     ((col & 3) >> 1) + 16 * (col & 1);
+    f32x4 acc[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float v[2][8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[0][e] = V[(32 * k + e) * D];
+        v[1][e] = V[(32 * k + e) * D + 2];
+      }
+      bf16x8 qq[2];
+      if (a.q_f32) {
+        const f32x4* qp = reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.q) + qoff + 32 * k);
+        const f32x4 q0 = qp[0], q1 = qp[1];
+        const float qv[8] = {q0[0], q0[1], q0[2], q0[3], q1[0], q1[1], q1[2], q1[3]};
+        split8<2>(qv, qq);
+      } else {
+        qq[0] = as_bf16x8(*reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.q) + qoff + 32 * k));
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        bf16x8 vp[2];
+        split8<2>(v[x], vp);
+        acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vp[0], qq[0], acc[x], 0, 0, 0);
+        acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vp[1], qq[0], acc[x], 0, 0, 0);
+        if (a.q_f32) acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vp[0], qq[1], acc[x], 0, 0, 0);
+      }
+    }
+    u32x4 r;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      f32x2 x = f32x2{acc[j >> 1][2 * (j & 1)] * a.scale_log2, acc[j >> 1][2 * (j & 1) + 1] * a.scale_log2};
+#pragma unroll
+      for (int e = 0; e < 2; ++e) x[e] = x[e] > 65504.0f ? 65504.0f : x[e] < -65504.0f ? -65504.0f : x[e];
+      r[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(x, f16x2));
+    }
+    *reinterpret_cast<u32x4*>(q_s[wave] + 16 * lane) = r;
+  }
+
+  const int n_tiles = (int)((seq.len + TILE - 1) / TILE), tpp = a.c.page_tokens >> 6;
+  const int begin = at.chunk * at.tiles_per_chunk;
+  const int end = n_tiles - begin < at.tiles_per_chunk ? n_tiles : begin + at.tiles_per_chunk;
+  const int n_keys = Kk.n, n_units = Kk.n + Kv.n;
+  if (tid < 2 * NG) {  // a unit: a kept group of the keys, then of the values
+    const int s = tid < n_keys ? tid : tid - n_keys;
+    int b = 0, pay = 0;
+#pragma unroll
+    for (int x = 0; x < NG; ++x) {
+      b = x == s ? (tid < n_keys ? Kk.bits[x] : Kv.bits[x]) : b;
+      pay = x == s ? (tid < n_keys ? Kk.pay[x] : Kv.pay[x]) : pay;
+    }
+    unit_s[tid] = b | (s & 3) << 4 | pay << 6;
+  }
+  __syncthreads();  // q' and units
+  uint8_t* tile = reinterpret_cast<uint8_t*>(sums_s) + wave * CA_TILE;
+  uint32_t magic = 0x64006400u;  // exponent of 1024 in both halves, in a VGPR
+  asm volatile("" : "+v"(magic));
+  // the tile whose words are loaded: its page's place in the table, its own in the page, its records
+  int load_tt = begin + wave, idx = load_tt / tpp, in_page = load_tt - idx * tpp, page = -1;
+  const uint32_t *kp = a.pool_k, *vp = a.pool_v;
+  bool page_ok = false;
+  uint32_t words[8], meta = 0u;
+  auto look_up = [&]() __attribute__((always_inline)) {
+    page = load_tt < end ? __builtin_amdgcn_readfirstlane(a.c.table[(int64_t)seq.row * a.c.row_pages + idx]) : -1;
+  };
+  auto enter = [&]() __attribute__((always_inline)) {  // the tile looked up; the walk goes on
+    page_ok = page >= 0 && page < a.c.n_pages;
+    const int64_t rec = ((int64_t)(page_ok ? page : 0) * a.c.n_kv + kv) * tpp + in_page;
+    kp = a.pool_k + rec * (TILE * a.Wk) + lane;
+    vp = a.pool_v + rec * (TILE * a.Wv) + lane;
+    load_tt += FEW_NW;
+    in_page += FEW_NW;
+    while (in_page >= tpp) {
+      in_page -= tpp;
+      ++idx;
+    }
+    look_up();
+  };
+  // operands in the tile (the swizzle of piece_at repeats every 16 slots)
+  const uint8_t* key_at = tile + piece_at(col, quarter);
+  const uint8_t* val_at0 = tile + piece_at(4 * quarter + (col >> 2), (lane & 3) >> 1) + 8 * (lane & 1);
+  const uint8_t* val_at1 = tile + piece_at(4 * quarter + (col >> 2), 2 + ((lane & 3) >> 1)) + 8 * (lane & 1);
+  int bits = 0;  // of the unit whose words are loaded: kept group u of the keys, or u - Kk.n of the values
+  auto fetch = [&](int u) __attribute__((always_inline)) {
+    const int d = __builtin_amdgcn_readfirstlane(unit_s[u]);
+    const uint32_t* rec = u < n_keys ? kp : vp;
+    bits = d & 15;
+    meta = 0u;
+    if (!page_ok) return;
+    meta = rec[((d >> 4) & 3) * TILE];
+    rec += (d >> 6) * TILE;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < bits) words[i] = rec[i * TILE];
+  };
+  // unit u's coefficients into the tile (its last readers are done: LDS serves a wavefront in
+  // order), and the next unit's words
+  auto expand = [&](int u) __attribute__((always_inline)) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const uint32_t m = finite_meta(meta, bits);
+    with_bits(bits, [&](auto bc) __attribute__((always_inline)) { write_coefficients<decltype(bc)::value, false>(words, m, tile, lane, 0, magic); });
+    if (u + 1 == n_units) enter();
+    fetch(u + 1 == n_units ? 0 : u + 1);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+  look_up();
+  if (n_units > 0) {
+    enter();
+    fetch(0);
+  }
+  f32x4 acc[NG][2];
+#pragma unroll
+  for (int sl = 0; sl < NG; ++sl) acc[sl][0] = acc[sl][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  float ref = 0.0f, l = 0.0f;  // the reference less CA_LIFT
+#pragma unroll 1
+  for (int tt = begin + wave; tt < end; tt += FEW_NW) {
+    f32x4 S[4];  // slot 16 b + 4 quarter + i
+#pragma unroll
+    for (int b = 0; b < 4; ++b) S[b] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+    for (int u = 0; u < n_keys; ++u) {
+      expand(u);
+      const f16x8 qo = as_f16x8(*reinterpret_cast<const u32x4*>(q_s[u] + 16 * lane));
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+        S[b] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_f16x8(*reinterpret_cast<const u32x4*>(key_at + 16 * 64 * b)), qo, S[b], 0, 0, 0);
+    }
+    const int t0 = tt * TILE;
+    if (t0 + TILE > lim_first) {
+      const int left = lim - t0 - 4 * quarter;
+#pragma unroll
+      for (int b = 0; b < 4; ++b)
+#pragma unroll
+        for (int i = 0; i < 4; ++i) S[b][i] = 16 * b + i < left ? S[b][i] : -__builtin_inff();
+    }
+    float top = S[0][0];
+#pragma unroll
+    for (int i = 1; i < 16; ++i) top = __builtin_fmaxf(top, S[i >> 2][i & 3]);
+    top -= CA_LIFT + CA_SLACK;
+    const bool first = tt == begin + wave;
+    if (first || __any(top > ref)) {
+      top = __builtin_fmaxf(top, __shfl_xor(top, 16));
+      top = __builtin_fmaxf(top, other_half(top));
+      // a row that sees nothing in the first tile sees nothing later
+      const float d = first ? (top == -__builtin_inff() ? 0.0f : top + CA_SLACK) : top > ref ? top + CA_SLACK - ref : 0.0f;
+      const float f = __builtin_amdgcn_exp2f(-d);
+      ref += d;
+      if (!first) {
+        l *= f;
+#pragma unroll
+        for (int sl = 0; sl < NG; ++sl)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[sl][i >> 2][i & 3] *= f;
+      }
+    }
+    f16x8 w[2];  // weights of 32 slots: element e is slot 16 (e / 4) + 4 quarter + e % 4
+#pragma unroll
+    for (int hf = 0; hf < 2; ++hf) {
+      u32x4 x;
+#pragma unroll
+      for (int j = 0; j < 4; ++j) {
+        const f32x4 s = S[2 * hf + (j >> 1)];
+        const f32x2 e = f32x2{__builtin_amdgcn_exp2f(s[2 * (j & 1)] - ref), __builtin_amdgcn_exp2f(s[2 * (j & 1) + 1] - ref)};
+        const f16x2 r = __builtin_convertvector(e, f16x2);
+        x[j] = __builtin_bit_cast(uint32_t, r);
+        l = __builtin_amdgcn_fdot2(__builtin_bit_cast(h16x2, r), h16x2{(__fp16)1.0f, (__fp16)1.0f}, l, false);
+      }
+      w[hf] = as_f16x8(x);
+    }
+#pragma unroll
+    for (int sl = 0; sl < NG; ++sl) {
+      if (sl < n_units - n_keys) {
+        expand(n_keys + sl);
+#pragma unroll
+        for (int x = 0; x < 2; ++x)
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            const uint8_t* p = (x ? val_at1 : val_at0) + 32 * 64 * hf;
+            const u32x2 y0 = read_transposed(p), y1 = read_transposed(p + 16 * 64);
+            acc[sl][x] = __builtin_amdgcn_mfma_f32_16x16x32_f16(as_f16x8(u32x4{y0[0], y0[1], y1[0], y1[1]}), w[hf], acc[sl][x], 0, 0, 0);
+          }
+      }
+    }
+  }
+  // merge of the wavefronts, and the chunk's partial of every row
+  l += __shfl_xor(l, 16);
+  l += other_half(l);
+  __syncthreads();  // the tiles have been read
+  if (quarter == 0) {
+    m_s[wave][col] = l == 0.0f ? -__builtin_inff() : ref;
+    l_s[wave][col] = l;
+  }
+#pragma unroll
+  for (int sl = 0; sl < NG; ++sl)
+    if (sl < Kv.n)
+#pragma unroll
+      for (int x = 0; x < 2; ++x)
+        *reinterpret_cast<f32x4*>(sums_s + (wave * FEW_ROWS + col) * FEW_PITCH + G * sl + 16 * x + 4 * quarter) = acc[sl][x];
+  __syncthreads();
+  float* part = partial + ((int64_t)item * a.c.n_kv + kv) * (a.scan_tokens * a.n_qh) * PART;
+  for (int e = tid; e < n_rows * D; e += 64 * FEW_NW) {
+    const int r = e >> 7, j = e & 127, g = j >> 5, c = j & 31;
+    const int place = 8 * ((c & 15) >> 2) + 2 * (c & 3) + (c >> 4);
+    int sl = -1;
+#pragma unroll
+    for (int x = 0; x < NG; ++x) sl = (x < Kv.n && Kv.grp[x] == g) ? x : sl;
+    float m = -__builtin_inff(), sum = 0.0f, total = 0.0f;
+#pragma unroll
+    for (int w = 0; w < FEW_NW; ++w) m = __builtin_fmaxf(m, m_s[w][r]);
+#pragma unroll
+    for (int w = 0; w < FEW_NW; ++w) {
+      const float f = m_s[w][r] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m_s[w][r] - m);
+      if (sl >= 0) sum = __builtin_fmaf(f, sums_s[(w * FEW_ROWS + r) * FEW_PITCH + G * sl + place], sum);
+      total = __builtin_fmaf(f, l_s[w][r], total);
+    }
+    part[r * PART + 8 + j] = sum;
+    if (j < NG) part[r * PART + 2 + j] = 0.0f;
+    if (j == 0) {
+      part[r * PART] = m;
+      part[r * PART + 1] = total;
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
 // u = scale V_K m_K of each KV head: q . u is the part of the log-sum-exp that the softmax does
 // not need.
 // ---------------------------------------------------------------------------
@@ -841,7 +1105,7 @@ static_assert(CA_ROWS == PAGED_ROWS && CA_NW * (16 * NG + 2) * 64 * sizeof(float
 hipError_t launch_paged_attention(const PagedAttnArgs& args, void* workspace, hipStream_t st) {
   PagedAttnArgs a = args;
   const PagedPlan p = paged_plan(a.c.batch, a.c.n_new, a.n_q_heads, a.c.n_kv, a.max_new, a.max_tokens,
-                                 scan_rows(a.Wk, a.Wv));
+                                 a.out_f32 ? scan_rows(a.Wk, a.Wv) : FEW_ROWS);
   char* ws = static_cast<char*>(workspace);
   a.lse_u = reinterpret_cast<float*>(ws);
   a.scan_tokens = p.scan_tokens;
@@ -867,8 +1131,17 @@ hipError_t launch_paged_attention(const PagedAttnArgs& args, void* workspace, hi
     }
     e = hipGetLastError();
   }
-  if (e == hipSuccess && p.scan_tokens > 0) e = launch_paged_scan(a, reinterpret_cast<int32_t*>(ws + p.plan_at), reinterpret_cast<float*>(ws + p.scan_at), st);
-  return e;
+  if (e != hipSuccess || p.scan_tokens == 0) return e;
+  a.scan_least = PAGED_SCAN_LEAST;
+  a.scan_plan = reinterpret_cast<int32_t*>(ws + p.plan_at);
+  float* partial = reinterpret_cast<float*>(ws + p.scan_at);
+  if (a.out_f32) {
+    launch_paged_scan(a, partial, st);
+  } else {
+    a.scan_items = (int32_t)paged_scan_items(a.c.n_kv, PAGED_SCAN_PER_CU);
+    hipLaunchKernelGGL(paged_few_kernel, dim3((unsigned)((a.scan_items + a.c.batch) * a.c.n_kv)), dim3(64 * FEW_NW), 0, st, a, partial);
+  }
+  return launch_paged_combine(a, partial, st);
 }
 
 }  // namespace spectra

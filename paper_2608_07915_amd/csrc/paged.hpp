@@ -100,7 +100,8 @@ hipError_t launch_pages_compact(const spectra_dev::PageMap& m, int32_t* moved, c
 hipError_t launch_page_copies(const spectra_dev::PoolList& pools, const spectra_dev::PageMoves& mv, int64_t most_moves,
                               hipStream_t st);
 hipError_t launch_paged_encode(const spectra_dev::PagedEncodeArgs& a, bool f32_input, hipStream_t st);
-// Sequences of at most a.scan_tokens new tokens (a.scan_tokens * n_qh <= scan_rows): its plan [batch][2] and partials.
-hipError_t launch_paged_scan(const spectra_dev::PagedAttnArgs& a, int32_t* plan, float* partial, hipStream_t st);
+// Sequences of at most a.scan_tokens new tokens (a.scan_tokens * n_qh <= scan_rows): chunks into partial, and their join.
+void launch_paged_scan(const spectra_dev::PagedAttnArgs& a, float* partial, hipStream_t st);
+hipError_t launch_paged_combine(const spectra_dev::PagedAttnArgs& a, float* partial, hipStream_t st);
 hipError_t launch_paged_attention(const spectra_dev::PagedAttnArgs& a, void* workspace, hipStream_t st);
 }  // namespace spectra

@@ -213,13 +213,14 @@ inline RopeSplit rope_split(int64_t groups, int n_qh, int words, int64_t n_tiles
 // chunks of a KV head that make one round of workgroups (their length is found on the device), and
 // the fewest tiles that are a chunk.
 constexpr int64_t PAGED_SCAN_LEAST = SCAN_WAVES;
+constexpr int PAGED_SCAN_PER_CU = 4;  // at most
 inline int64_t paged_scan_items(int64_t n_kv, int per_cu) {
   const int64_t n = N_CU * per_cu / n_kv;
   return n < 1 ? 1 : n;
 }
 // The most chunks of all KV heads that sequences of up to n_tiles tiles come to.
 inline int64_t paged_scan_chunks(int64_t batch, int64_t n_kv, int64_t n_tiles) {
-  const int64_t most = batch * ceil_div(n_tiles, PAGED_SCAN_LEAST), some = paged_scan_items(n_kv, 3) + batch;
+  const int64_t most = batch * ceil_div(n_tiles, PAGED_SCAN_LEAST), some = paged_scan_items(n_kv, PAGED_SCAN_PER_CU) + batch;
   return n_kv * (most < some ? most : some);
 }
 
