@@ -770,7 +770,7 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
   attn_scan<NQ, PK, PV, EXACT, false>(a, PagedAttnArgs{});
 }
 
-// Sequences with few new rows: a decode step's single tokens, a few speculative ones.
+// Sequences with few new rows and fp32 outputs: a decode step's single tokens, a few speculative ones.
 template <int NQ, int PK, int PV, bool EXACT>
 __global__ __launch_bounds__(256, 2) void paged_scan_kernel(AttnArgs a, PagedAttnArgs p) {
   attn_scan<NQ, PK, PV, EXACT, true>(a, p);
@@ -784,11 +784,10 @@ __global__ __launch_bounds__(256, 2) void paged_scan_kernel(AttnArgs a, PagedAtt
 // states are then merged in LDS.
 // ---------------------------------------------------------------------------
 // combine_row: nch partials from ph on, `step` floats apart, value stream s; store(i, out_i) takes the row's channels,
-// stats(m, l) in one thread the overall maximum (log2 domain) and sum.
-template <typename Store, typename Stats>
+// stats(m, l) in one thread the overall maximum (log2 domain) and sum. A round loads 8 CB chunks.
+template <int CB, typename Store, typename Stats>
 __device__ __forceinline__ void combine_row(const AttnArgs& a, const float* __restrict__ ph, int64_t step, int nch, int s, Store&& store,
                                             Stats&& stats) {
-  constexpr int CB = 12;  // 8 x 12 = 96 chunks per round: one round of loads for ~768 scan workgroups over 8 heads
   __shared__ float accs[8][D];
   __shared__ float chat[D];
   __shared__ float gm[8], gl[8];
@@ -873,7 +872,8 @@ __device__ __forceinline__ void combine_row(const AttnArgs& a, const float* __re
 __global__ __launch_bounds__(1024) void combine_kernel(AttnArgs a) {
   const int hq = blockIdx.x, b = blockIdx.y;
   const int64_t row = (int64_t)b * a.n_q_heads + hq;
-  combine_row(a, a.partial + row * a.n_chunks * PART, PART, a.n_chunks, b * a.n_kv_heads + hq / a.n_qh,
+  // 96 chunks a round: one round of loads for ~768 scan workgroups over 8 heads
+  combine_row<12>(a, a.partial + row * a.n_chunks * PART, PART, a.n_chunks, b * a.n_kv_heads + hq / a.n_qh,
                      [&](int i, float o) { a.out[row * D + i] = o; }, [](float, float) {});
 }
 
@@ -922,7 +922,8 @@ __global__ __launch_bounds__(1024) void paged_combine_kernel(AttnArgs a, PagedAt
     p.lse[(seq.first + tok) * a.n_q_heads + hq] = l > 0.0f ? __builtin_fmaf(__builtin_amdgcn_logf(l) + m, LN2, u) : __builtin_nanf("");
   };
   if constexpr (ROWS == 1) {
-    combine_row(a, first + (which - kv * a.n_qh) * PART, step, n_items, kv, [&](int i, float o) { store(which, i, o); },
+    // 128 chunks a round: of the 1024 workgroups over 8 KV heads (131k slots: 9.3 us by two rounds of 96)
+    combine_row<16>(a, first + (which - kv * a.n_qh) * PART, step, n_items, kv, [&](int i, float o) { store(which, i, o); },
                       [&](float m, float l) { write_lse(which, m, l); });
   } else {
     __shared__ float chat[ROWS][D];

@@ -39,8 +39,9 @@ constexpr float CA_SLACK = 3.0f;       // log2: the running maximum moves when p
 constexpr float CA_LIFT = 12.0f;       // log2: weights are kept 2^12 above their share
 constexpr float CA_LO = 2048.0f;       // the second fp16 part of a number is scaled by 2^11
 
-// LDS byte of 16-byte piece `piece` of slot `t` in a slot tile.
-__device__ __forceinline__ int piece_at(int t, int piece) { return t * 64 + ((piece ^ ((t >> 2) & 3)) << 4); }
+// LDS byte of 16-byte piece `piece` of slot `t` in a slot tile. Slots 4 apart lie 2 pieces apart, so
+// that transposed reads of eight neighbouring slots use all banks.
+__device__ __forceinline__ int piece_at(int t, int piece) { return t * 64 + ((piece ^ ((t >> 1) & 2) ^ ((t >> 3) & 1)) << 4); }
 
 // A token's metadata word of a b-bit group, made finite: NaN or infinite scales count as 0, and
 // the scale is lowered where z + s (2^b - 1) would pass fp16's largest number.
@@ -820,6 +821,11 @@ __global__ __launch_bounds__(64) void paged_join_kernel(PagedAttnArgs a) {
 // workgroup's (scan_place). Each wavefront walks tiles of its own, a kept group at a time through
 // one 4 KB tile of LDS, the group's words loaded while the one before is multiplied; no barrier
 // until the wavefronts' sums are merged, and 16 wavefronts on a CU hide each other's chains.
+// 635 vector instructions a tile of seven heads (about 75 a group to make coefficients), where the
+// latent scan, whose products take bit fields and whose sums hold for fp32 outputs, has 1000: 48
+// sequences of 8k slots 53 us and 76. Bound by the chain of a group through LDS: all groups of a tile
+// loaded a tile ahead (three wavefronts a SIMD by registers) came to the same 54, with the next
+// group's coefficients made among the products to 62 (spills).
 // ---------------------------------------------------------------------------
 constexpr int FEW_NW = 4, FEW_ROWS = 16, FEW_PITCH = D + 4;
 __global__ __launch_bounds__(64 * FEW_NW, 4) void paged_few_kernel(PagedAttnArgs a, float* __restrict__ partial) {
