@@ -45,17 +45,17 @@ DECODE_STEP_SOURCES = ("kernels_attn.hip", "attn_common.hpp", "kplan.hpp", "enco
                        "kernels.hpp", "splits.hpp")
 # sha256 -> fetch / write bytes per call; per_kernel: [fetch, write]
 MEASURED_TRAFFIC = {
-    "1dabd5c89f623b1f30fca90c9d9e08e714d9e2ba24a4c1cc441ba19cea1e5927": {
-        "fetch_bytes": 74539970, "write_bytes": 1674243, "mfma_busy": 0.096,
-        "per_kernel": {"attn_kernel<1,8,8,true>": [70698946, 1657859], "combine_kernel": [3841024, 16384]}},
+    "65b6ee8395ee8f192022476f8c4ebfa1067e01af1bca803ff27da87e5e1a11ba": {
+        "fetch_bytes": 74539798, "write_bytes": 1674240, "mfma_busy": 0.093,
+        "per_kernel": {"attn_kernel<1,8,8,true>": [70696726, 1657856], "combine_kernel": [3843072, 16384]}},
 }
 # The same passes over the bulk encode of one codec (256 streams x 131072 tokens):
 # HBM bytes per call and the matrix cores' busy fraction (SQ_VALU_MFMA_BUSY_CYCLES
 # over GRBM_GUI_ACTIVE x 1024 SIMDs), keyed by sha256 over ENCODE_SOURCES.
 ENCODE_SOURCES = ("kernels_codec.hip", "encode_dev.hpp", "device_common.hpp", "kernels.hpp")
 MEASURED_ENCODE = {
-    "fb9a14b725b1e723ac5aafd8bb3ba212132534c397aa05c524a94e674f215aea": {
-        "fetch_bytes": 8665611008, "write_bytes": 1073741824, "mfma_busy": 0.365},
+    "2fd8876bc772814538acb7f072eb03001c7f5dbeef31e9df8c3e29dadc58c46d": {
+        "fetch_bytes": 8665792320, "write_bytes": 1073741824, "mfma_busy": 0.364},
 }
 
 
