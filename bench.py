@@ -47,7 +47,7 @@ DECODE_STEP_SOURCES = ("kernels_attn.hip", "attn_common.hpp", "kplan.hpp", "enco
 MEASURED_TRAFFIC = {
     "65b6ee8395ee8f192022476f8c4ebfa1067e01af1bca803ff27da87e5e1a11ba": {
         "fetch_bytes": 74539798, "write_bytes": 1674240, "mfma_busy": 0.093,
-        "per_kernel": {"attn_kernel<1,8,8,true>": [70696726, 1657856], "combine_kernel": [3843072, 16384]}},
+        "per_kernel": {"attn_kernel<1,8,8,true>": [70696726, 1657856], "combine_kernel": [int(1876.5 * 2048), 16384]}},
 }
 # The same passes over the bulk encode of one codec (256 streams x 131072 tokens):
 # HBM bytes per call and the matrix cores' busy fraction (SQ_VALU_MFMA_BUSY_CYCLES

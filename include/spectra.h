@@ -382,7 +382,8 @@ spectra_status spectra_pages_compact(const spectra_pages* m, const spectra_pool*
  * entries that do not fall, cut to [0, n_new]) and go to its last slots. k[t*k_token_stride +
  * kv*k_head_stride + c], v alike, kv < n_streams of the codecs, strides multiples of 16 bytes.
  * The records are those of spectra_encode for the same rows. Written are only those slots, so
- * pages must not be shared there (spectra_pages_extend). Not written: tokens before slot 0 (a
+ * pages must not be shared there (spectra_pages_extend) and no two sequences of a call may end in
+ * the same slots (what those hold is then unspecified). Not written: tokens before slot 0 (a
  * sequence with ends[b] = -1 gets none), and those whose page is out of range. Asynchronous. */
 spectra_status spectra_paged_encode(const spectra_pages* m, const spectra_codec* ck, const spectra_codec* cv,
                                     uint32_t* pool_k, uint32_t* pool_v, const int32_t* rows, const int32_t* ends,

@@ -1141,7 +1141,12 @@ hipError_t launch_paged_attention(const PagedAttnArgs& args, void* workspace, hi
   a.scan_least = PAGED_SCAN_LEAST;
   a.scan_plan = reinterpret_cast<int32_t*>(ws + p.plan_at);
   float* partial = reinterpret_cast<float*>(ws + p.scan_at);
-  if (a.out_f32) {
+  // Also for 16-bit outputs the latent scan where it has one quad of rows, sequences may be long and
+  // there is work for many tiles a wavefront: four heads on each of eight KV heads, 64 sequences of
+  // 30k slots 348 us and 423 by paged_few_kernel, of 8000 110 and 126; but one of 131k 50 and 47, 256
+  // of 100 63 and 54, of 1000 92 and 84.
+  const bool long_quad = p.scan_tokens * a.n_qh <= 4 && a.max_tokens > 2048 && a.c.batch * a.max_tokens * a.c.n_kv > (int64_t)1 << 22;
+  if (a.out_f32 || long_quad) {
     launch_paged_scan(a, partial, st);
   } else {
     a.scan_items = (int32_t)paged_scan_items(a.c.n_kv, PAGED_SCAN_PER_CU);

@@ -87,3 +87,13 @@ def test_pools_past_two_to_the_31_words():
     used = int((near.refs > 0).sum())
     assert int(moved[-1]) == used and (far.table[0, :11] < used).all() and int((far.refs > 0).sum()) == used
     assert torch.equal(c.run(), want)
+
+
+@pytest.mark.parametrize("n_qh,new", [(4, [1, 1, 1]), (1, [4, 2, 1]), (2, [2, 0, 2]), (5, [1, 1, 1])])
+@pytest.mark.parametrize("f32", [False, True], ids=["bf16", "f32"])
+def test_few_rows_whatever_the_longest_that_the_call_allows(n_qh, new, f32):
+    # short sequences under bounds of their own length and far above
+    c = Case([300, 65, 1], new, n_qh, ALL, ALL[::-1], 30, f32=f32, seed=25)
+    lse = torch.empty(c.q.shape[:2], device="cuda")
+    for bound in (300, 2049, 1_000_000):
+        c.check(c.run(max_tokens=bound, lse=lse), lse)
