@@ -207,3 +207,21 @@ def test_same_result_twice():
     outs = [S.spectra_paged_attention(s.map, s.ck, s.cv, *s.pools, q, cu, 100, 512) for _ in range(5)]
     for o in outs[1:]:
         assert torch.equal(o, outs[0])
+
+
+def test_padded_batch():
+    # a call of fixed size whose last sequences are padding: rows of -1, with and without tokens
+    a, b = Server(seed=5), Server(seed=5)
+    for s in (a, b):
+        s.step([0, 1], [130, 70], [0, 200])
+    ends, out, _ = a.step([0, 1], [1, 40], [300, 310])
+    padded, pout, _ = b.step([0, 1, -1, -1, 8], [1, 40, 0, 2, 30], [300, 310, 0, 5, 7])
+    assert padded == ends + [-1, -1, -1]
+    # padding of a chunk's rows can change how the slots are split: the order of fp32 sums
+    _close(pout[:41], out)
+    assert (pout[41:] == 0).all()
+    for x, y in zip((a.map.table, a.map.lens, a.map.refs, *a.pools), (b.map.table, b.map.lens, b.map.refs, *b.pools)):
+        assert torch.equal(x, y)
+    S.spectra_pages_truncate(b.map, _ints(-1, 1, 8, 1), _ints(0, 5, 0, 3))
+    assert b.map.lens.tolist() == [131, 3, 0, 0, 0, 0, 0, 0]
+    assert S.spectra_pages_fork(b.map, _ints(-1, 0, 8), _ints(2, -1, 3)).tolist() == [-1, -1, -1]
