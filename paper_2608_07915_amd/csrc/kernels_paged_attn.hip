@@ -372,8 +372,8 @@ struct GroupTiles {
   }
 };
 
-// The slots [from, to) of a pass over a workgroup's rows; lim: slots that the lane's row sees,
-// lim_first and lim_last: the wavefront's first row and its last.
+// The slots [from, to) of a pass over a workgroup's rows; lim: the slots that the lane's row sees, and
+// lim_first the wavefront's first row, none past `to`; lim_last: those of its last row.
 struct Pass {
   int row;  // of the table
   int from, to, lim_first, lim_last;
@@ -725,7 +725,10 @@ __device__ __forceinline__ void chunk_rows(const PagedAttnArgs& a, const PagedSe
   pass.row = seq.row;
   pass.from = (int)(part * a.part_slots);
   pass.to = rows.lim_unit < pass.from + a.part_slots ? rows.lim_unit : (int)(pass.from + a.part_slots);
-  pass.lim_first = rows.lim_first;
+  // No row sees past the part: the block that the 16-bit form scores ahead of a part's last one lies
+  // there, on tiles of zeros, whose scores of 0 would pass for its largest.
+  const int lim = rows.lim < pass.to ? rows.lim : pass.to;
+  pass.lim_first = rows.lim_first < pass.to ? rows.lim_first : pass.to;
   pass.lim_last = rows.lim_last;
 
   f16x8 qb[N][2], ql[PRECISE ? N : 1][2];
@@ -735,9 +738,9 @@ __device__ __forceinline__ void chunk_rows(const PagedAttnArgs& a, const PagedSe
   for (int sl = 0; sl < N; ++sl) acc[sl] = zero16();
   RowSum sum;
   if constexpr (PRECISE)
-    chunk_steps_precise<N, N>(a, kv, Kk, Kv, pass, rows.lim, unscale, tiles, wave, lane, qb, ql, acc, sum);
+    chunk_steps_precise<N, N>(a, kv, Kk, Kv, pass, lim, unscale, tiles, wave, lane, qb, ql, acc, sum);
   else
-    chunk_steps<N, N>(a, kv, Kk, Kv, pass, rows.lim, tiles, wave, lane, qb, acc, sum);
+    chunk_steps<N, N>(a, kv, Kk, Kv, pass, lim, tiles, wave, lane, qb, acc, sum);
   const float m = __builtin_fmaxf(sum.m, other_half(sum.m)), l = sum.l + other_half(sum.l);
   if (n_parts > 1) {
     float* p = a.partial + part_at(a, unit, kv, part, wave) + lane;
