@@ -4,8 +4,8 @@ import numpy as np
 import pytest
 
 import paper_2608_07915_amd as S
-from paged_cases import Built, check_split, records_of
-from paged_ref import D, G, default_scale
+from paged_cases import SPLIT, Built, check_split, records_of
+from paged_ref import D, G, default_scale, records
 
 pytestmark = pytest.mark.gpu
 
@@ -14,12 +14,34 @@ if not torch.cuda.is_available():
     pytest.skip("no GPU", allow_module_level=True)
 
 B8 = [[5, 1, 0, 0], [4, 2, 0, 0]]
+ALL = [[8, 7, 6, 5], [1, 2, 3, 4]]
 
 
 def _run(c, **kw):
     lse = torch.empty(c.q.shape[:2], device="cuda")
     out = S.spectra_paged_attention(c.cache, c.ck, c.cv, *c.pools, c.q, c.cu, max(c.new), max(c.lens), lse=lse, **kw)
     return out, lse
+
+
+def _random(lens, new, n_qh, bits_k, bits_v, words, seed, **kw):
+    rng = np.random.default_rng([seed, 29])
+    return Built(lens, new, n_qh, bits_k, bits_v, words, lambda b, h, t, bits, p, n: records(bits, p, n, rng),
+                 lambda c: 2.0 * rng.standard_normal((sum(new), c.H * n_qh, D)), seed=seed, **kw)
+
+
+@pytest.mark.parametrize("f32", [False, True], ids=["bf16", "f32"])
+@pytest.mark.parametrize("name", SPLIT)
+def test_split_chunks(name, f32):
+    lens, new, n_qh = SPLIT[name]
+    c = _random(lens, new, n_qh, B8, B8[::-1], 8, len(name), f32=f32)
+    check_split(c, *_run(c))
+
+
+@pytest.mark.parametrize("f32", [False, True], ids=["bf16", "f32"])
+def test_split_chunks_of_all_widths(f32):
+    for page in (64, 448):
+        c = _random([2900, 64], [50, 20], 3, ALL, ALL[::-1], 30, 7, page=page, f32=f32)
+        check_split(c, *_run(c))
 
 
 def _far_below(level, f32):
