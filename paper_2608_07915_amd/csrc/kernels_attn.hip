@@ -483,8 +483,10 @@ __device__ __forceinline__ void attn_scan(const AttnArgs& a, const PagedAttnArgs
   constexpr int PKR = PK > 0 ? PK : 1, PVR = PV > 0 ? PV : 1;
   uint32_t pk[PKR], pv[PVR];
   // every lane loads in-bounds words: the word index is clamped to the record (a
-  // uniform offset folded into the per-word base pointer), the token to the tile;
+  // uniform offset folded into the per-word base pointer; records of no words have
+  // word 0 of memory that the launch gives them), the token to the tile;
   // tokens past n_tokens are never weighted (their value metadata is zeroed)
+  const int last_k = Wk > 0 ? Wk - 1 : 0, last_v = Wv > 0 ? Wv - 1 : 0;
   const uint32_t* kps = a.packed_k + kbase;
   const uint32_t* vps = a.packed_v + vbase;
   // PAGED: the page of the next tile to load is read a tile ahead; a page outside the pool is
@@ -520,8 +522,8 @@ __device__ __forceinline__ void attn_scan(const AttnArgs& a, const PagedAttnArgs
     } else {
 #pragma unroll
       for (int w = 0; w < (PK > PV ? PK : PV); ++w) {
-        if (w < PK) pk[w] = (kps + 64 * (w < Wk ? w : Wk - 1))[ko];
-        if (w < PV) pv[w] = (vps + 64 * (w < Wv ? w : Wv - 1))[vo];
+        if (w < PK) pk[w] = (kps + 64 * (w < Wk ? w : last_k))[ko];
+        if (w < PV) pv[w] = (vps + 64 * (w < Wv ? w : last_v))[vo];
       }
     }
   };
@@ -1011,6 +1013,9 @@ static Split launch_nq_pw(const AttnArgs& a, const PagedAttnArgs* p, hipStream_t
   if ((size_t)qprep_scratch_bytes(NQ) > lds) lds = qprep_scratch_bytes(NQ);
   // more (sequence, kv head) groups than XCDs: chunks of a group kept on one XCD
   AttnArgs g = a;
+  // records of no words: their offsets are all 0, and what is read in their place is never used
+  if (a.Wk == 0) g.packed_k = reinterpret_cast<const uint32_t*>(a.basis_k);
+  if (a.Wv == 0) g.packed_v = reinterpret_cast<const uint32_t*>(a.basis_v);
   const int64_t groups = (int64_t)a.n_kv_heads * a.batch;
   g.group_major = groups > 8 ? 1 : 0;
   // workgroups a CU holds: three wavefronts per SIMD by the registers of the shapes with one

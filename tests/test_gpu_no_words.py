@@ -1,0 +1,98 @@
+"""Attention beside records of no words (a budget below one word a token): nothing is read for them,
+every slot's coefficients are zeros, and the other tensor's records count as ever."""
+import numpy as np
+import pytest
+
+import paper_2608_07915_amd as S
+from paged_cases import element_bound, score_error
+from paged_ref import D, attention64, codec, default_scale, records, to_pool
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+if not torch.cuda.is_available():
+    pytest.skip("no GPU", allow_module_level=True)
+
+BITS = {8: [[5, 1, 0, 0], [4, 2, 0, 0]], 30: [[8, 7, 6, 5], [1, 2, 3, 4]], 12: [[5, 3, 0, 0], [6, 2, 1, 0]]}
+H, T = 2, 300
+
+
+def _codec(words, seed):
+    """-> codec, records [H][T, W], coefficients [H][T, 128]."""
+    if words:
+        c, p = codec(BITS[words], words, seed)
+        got = [records(b, p, T, np.random.default_rng([seed, i])) for i, b in enumerate(BITS[words])]
+        return c, [g[0] for g in got], [g[1] for g in got]
+    like, _ = codec([[0] * 4] * H, 8, seed)
+    c = S.Codec(S.Params(ratio=100.0), H)
+    assert c.record_words == 0
+    for a, b in ((c.basis, like.basis), (c.mean, like.mean), (c.var, like.var), (c.bits, like.bits)):
+        a.copy_(b)
+    return c, [None] * H, [np.zeros((T, D))] * H
+
+
+def _check(out, q, ck, cv, coef_k, coef_v, bf16, few):
+    n_qh = q.shape[0] // H
+    got, q = out.double().cpu().numpy(), q.double().cpu().numpy()
+    for h in range(H):
+        hs = slice(h * n_qh, (h + 1) * n_qh)
+        st = [t.cpu().numpy().astype(np.float64) for t in (ck.basis[h], ck.mean[h], cv.basis[h], cv.mean[h])]
+        want, _, swing, most = attention64(q[None, hs], coef_k[h], coef_v[h], *st, 1, default_scale())
+        tol = element_bound(want, swing, score_error(most, bf16), T, bf16, few)
+        assert (np.abs(got[hs] - want[0]) <= tol[0]).all()
+
+
+WORDS = [(0, 0), (0, 8), (8, 0), (0, 12), (12, 0), (30, 0), (0, 30)]
+
+
+@pytest.mark.parametrize("wk,wv", WORDS)
+def test_paged(wk, wv):
+    (ck, rk, xk), (cv, rv, xv) = _codec(wk, 1), _codec(wv, 2)
+    cache = S.PagedCache(9, 64, 1, 6)
+    row = np.array([3, 1, 8, 0, 5])
+    cache.table[0, :5] = torch.from_numpy(row).int()
+    cache.lens[0] = T
+    pools = [cache.empty_pool(c) for c in (ck, cv)]
+    for pool, rec in zip(pools, (rk, rv)):
+        if pool.numel():
+            host = pool.cpu().numpy()
+            for h in range(H):
+                to_pool(host, rec[h], row, 64, h, H)
+            pool.copy_(torch.from_numpy(host))
+    cu = torch.tensor([0, 1], dtype=torch.int32, device="cuda")
+    # new tokens' keys and values: what has no words is not written
+    x = torch.randn((1, H, D), device="cuda")
+    before = [p.clone() for p in pools]
+    S.spectra_paged_encode(cache, ck, cv, *pools, x, x, cu, ends=torch.tensor([-1], dtype=torch.int32, device="cuda"))
+    assert all(torch.equal(a, b) for a, b in zip(pools, before))
+    for n_qh in (1, 4, 7, 12, 16):
+        for dtype in (torch.float32, torch.bfloat16):
+            q = (2 * torch.randn((1, H * n_qh, D), device="cuda")).to(dtype)
+            for bound in (T, 3_000_000):  # the longest that the call allows chooses the kernel of 16-bit outputs
+                out = S.spectra_paged_attention(cache, ck, cv, *pools, q, cu, 1, bound)
+                _check(out[0], q[0], ck, cv, xk, xv, dtype == torch.bfloat16, True)
+    # a chunk: its last token sees all
+    q = torch.randn((20, H * 4, D), device="cuda")
+    for dtype in (torch.float32, torch.bfloat16):
+        qq = q.to(dtype)
+        out = S.spectra_paged_attention(cache, ck, cv, *pools, qq, cu * 20, 20, T)
+        _check(out[-1], qq[-1], ck, cv, xk, xv, dtype == torch.bfloat16, False)
+
+
+@pytest.mark.parametrize("wk,wv", WORDS)
+def test_contiguous(wk, wv):
+    (ck, rk, xk), (cv, rv, xv) = _codec(wk, 3), _codec(wv, 4)
+    cap = 320
+    packed = []
+    for c, rec in ((ck, rk), (cv, rv)):
+        p = c.empty_packed(cap)
+        if c.record_words:
+            full = np.zeros((H, cap, c.record_words), np.uint32)
+            full[:, :T] = np.stack(rec)
+            tiled = full.reshape(H, cap // 64, 64, -1).transpose(0, 1, 3, 2).copy()
+            p.copy_(torch.from_numpy(tiled.view(np.int32).reshape(p.shape)))
+        packed.append(p)
+    for n_qh in (1, 4, 7, 12, 16):
+        q = 2 * torch.randn((1, H * n_qh, D), device="cuda")
+        out = S.spectra_decode_attention(ck, cv, *packed, cap, T, q, H)
+        _check(out[0], q[0], ck, cv, xk, xv, False, True)
