@@ -496,7 +496,7 @@ spectra_status spectra_decode_step(const spectra_codec* ck, const spectra_codec*
     return fail(SPECTRA_EINVAL, "decode_step: k_new / v_new must be non-null and 16-byte aligned");
   a.k_new = k_new;
   a.v_new = v_new;
-  a.app_k = packed_k;
+  a.app_k = packed_k ? packed_k : packed_v;  // null beside records of no words; non-null says that there is an append
   a.app_v = packed_v;
   a.t_new = t;
   a.app_f32 = kv_dt == SPECTRA_F32;

@@ -96,3 +96,20 @@ def test_contiguous(wk, wv):
         q = 2 * torch.randn((1, H * n_qh, D), device="cuda")
         out = S.spectra_decode_attention(ck, cv, *packed, cap, T, q, H)
         _check(out[0], q[0], ck, cv, xk, xv, False, True)
+
+
+def test_decode_step_appends_values_beside_keys_of_no_words():
+    import ctypes
+    from paper_2608_07915_amd import _lib
+    (ck, _, _), (cv, _, _) = _codec(0, 5), _codec(8, 6)
+    packed, want = cv.empty_packed(64), cv.empty_packed(64)
+    x = torch.randn((1, H, D), device="cuda")
+    q = torch.randn((1, H * 4, D), device="cuda")
+    S.spectra_encode(cv, x.transpose(0, 1).contiguous(), 0, want, 64)
+    out = torch.empty_like(q)
+    ws = torch.empty(S.spectra_attention_workspace_bytes(1, H * 4, H, 1), dtype=torch.uint8, device="cuda")
+    _lib.check(_lib.get().spectra_decode_step(ctypes.byref(ck.struct), ctypes.byref(cv.struct), None, packed.data_ptr(), 64, 0,
+                                              x.data_ptr(), x.data_ptr(), 0, q.data_ptr(), 0, 1, H * 4, H, 0.0, out.data_ptr(),
+                                              ws.data_ptr(), ws.numel(), torch.cuda.current_stream().cuda_stream))
+    assert torch.equal(packed, want)
+    assert torch.equal(out, S.spectra_decode_attention(ck, cv, ck.empty_packed(64), want, 64, 1, q, H))
