@@ -319,9 +319,9 @@ __device__ __forceinline__ void score_slot(const uint32_t* __restrict__ kt, int 
 // coefficient) for every query row (nqh of them). smem: the tile buffers, free
 // once every wave has left its tile loop.
 // ---------------------------------------------------------------------------
-template <int NQ, typename R>
-__device__ __forceinline__ void write_chunk_partial(const AttnArgs& a, int nqh, R&& partial_at, int tid, int wave,
-                                                    int lane, int kq, int col, bool ok, const Kept& Kv,
+template <int NQ>
+__device__ __forceinline__ void write_chunk_partial(int nqh, float* part, int64_t step, int tid, int wave, int lane,
+                                                    int kq, int col, bool ok, const Kept& Kv,
                                                     const float (&m_run)[4 * NQ], const float (&l_run)[4 * NQ],
                                                     const float (&zacc)[4 * NQ][NG], const f32x4 (&vacc)[NG][2],
                                                     uint32_t* smem) {
@@ -386,7 +386,7 @@ __device__ __forceinline__ void write_chunk_partial(const AttnArgs& a, int nqh, 
       l += f * lst[w][h];
       if (j < NG) z += f * zst[w][h][j];
     }
-    float* ph = a.partial + partial_at(h) * PART;  // row h's partial of this chunk
+    float* ph = part + h * step;  // row h's partial of this chunk
     ph[8 + j] = acc;
     if (j == 0) {
       ph[0] = M;
@@ -396,12 +396,21 @@ __device__ __forceinline__ void write_chunk_partial(const AttnArgs& a, int nqh, 
   }
 }
 
-// PAGED: the tiles lie in pages (p: the paged call), the codec's streams are the KV heads
-// whatever the sequence, the rows are a sequence's new tokens times the query heads on the KV
-// head (row h = token h / n_qh, head h % n_qh; at most 4 NQ), each with a limit of its own,
-// and chunks come tiles_per_chunk at a time without a last one apart.
-template <int NQ, int PK, int PV, bool EXACT, bool PAGED>
-__device__ __forceinline__ void attn_scan(const AttnArgs& a, const PagedAttnArgs& p) {
+// The paged call whose sequences a scan takes, or nothing.
+__device__ __forceinline__ const PagedAttnArgs& paged_call(const PagedAttnArgs& p) { return p; }
+__device__ __forceinline__ int paged_call() { return 0; }
+
+// PAGED (with a paged call p: sequences with few new rows, a decode step's single tokens, a few
+// speculative ones): the tiles lie in pages, the codec's streams are the KV heads whatever the
+// sequence, the rows are a sequence's new tokens times the query heads on the KV head (row h =
+// token h / n_qh, head h % n_qh; at most 4 NQ), each with a limit of its own, and chunks come
+// tiles_per_chunk at a time without a last one apart. A kernel template with or without the
+// argument: as a function inlined into two kernels the contiguous one took 32.2 us and 31.6 now
+// (16-word records, 32k slots of eight KV heads).
+template <int NQ, int PK, int PV, bool EXACT, typename... Paged>
+__global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a, Paged... paged) {
+  constexpr bool PAGED = sizeof...(Paged) != 0;
+  [[maybe_unused]] const auto& p = paged_call(paged...);
   constexpr int NH = 4 * NQ;
   constexpr bool STACK = NQ <= 2;  // 2*NH <= 16: hi and lo weight rows share one MFMA
   extern __shared__ __attribute__((aligned(16))) uint32_t smem[];
@@ -491,7 +500,8 @@ __device__ __forceinline__ void attn_scan(const AttnArgs& a, const PagedAttnArgs
   const uint32_t* vps = a.packed_v + vbase;
   // PAGED: the page of the next tile to load is read a tile ahead; a page outside the pool is
   // read as page 0 with all metadata taken as zero
-  const int tpp = PAGED ? p.c.page_tokens >> 6 : 1;
+  int tpp = 1;
+  if constexpr (PAGED) tpp = p.c.page_tokens >> 6;
   int next_page = 0;
   bool loaded_ok = true, tile_ok = true;  // of the tile in flight, of the staged one
   auto look_up = [&](int64_t t2) {
@@ -546,12 +556,13 @@ __device__ __forceinline__ void attn_scan(const AttnArgs& a, const PagedAttnArgs
   // its loads ----
   __shared__ float red_s[WAVES];
   __shared__ float e2_s;
+  const int64_t q_first = PAGED ? 0 : ((int64_t)b * a.n_q_heads + kv * nqh) * D;
   const auto row_at = [&](int h) -> int64_t {
     if constexpr (PAGED) {
       const int tok = h / a.n_qh;
       return (seq.first + tok) * p.q_token_stride + (kv * a.n_qh + h - tok * a.n_qh) * p.q_head_stride;
     } else {
-      return ((int64_t)b * a.n_q_heads + kv * nqh + h) * D;
+      return q_first + h * D;
     }
   };
   const float E2q = prepare_query<NQ>(a, s, nqh, tid, reinterpret_cast<uint8_t*>(smem), qa_s, qbar_s, red_s, row_at, [&] {
@@ -758,24 +769,13 @@ __device__ __forceinline__ void attn_scan(const AttnArgs& a, const PagedAttnArgs
     __builtin_amdgcn_wave_barrier();
   }
 
-  const auto partial_at = [&](int h) -> int64_t {
-    if constexpr (PAGED)
-      return ((int64_t)item * a.n_kv_heads + kv) * (p.scan_tokens * a.n_qh) + h;
-    else
-      return ((int64_t)b * a.n_q_heads + kv * nqh + h) * a.n_chunks + chunk;
-  };
-  write_chunk_partial<NQ>(a, nqh, partial_at, tid, wave, lane, kq, col, ok, Kv, m_run, l_run, zacc, vacc, smem);
-}
-
-template <int NQ, int PK, int PV, bool EXACT>
-__global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a) {
-  attn_scan<NQ, PK, PV, EXACT, false>(a, PagedAttnArgs{});
-}
-
-// Sequences with few new rows and fp32 outputs: a decode step's single tokens, a few speculative ones.
-template <int NQ, int PK, int PV, bool EXACT>
-__global__ __launch_bounds__(256, 2) void paged_scan_kernel(AttnArgs a, PagedAttnArgs p) {
-  attn_scan<NQ, PK, PV, EXACT, true>(a, p);
+  const int64_t step = PAGED ? PART : (int64_t)a.n_chunks * PART;  // from a row's partial to the next one's
+  float* part = a.partial;
+  if constexpr (PAGED)
+    part += ((int64_t)item * a.n_kv_heads + kv) * (p.scan_tokens * a.n_qh) * PART;
+  else
+    part += ((int64_t)b * a.n_q_heads + kv * nqh) * step + (int64_t)chunk * PART;
+  write_chunk_partial<NQ>(nqh, part, step, tid, wave, lane, kq, col, ok, Kv, m_run, l_run, zacc, vacc, smem);
 }
 
 // ---------------------------------------------------------------------------
@@ -1028,7 +1028,7 @@ static Split launch_nq_pw(const AttnArgs& a, const PagedAttnArgs* p, hipStream_t
   if (p) {
     PagedAttnArgs q = *p;
     q.scan_items = (int32_t)paged_scan_items(a.n_kv_heads, per_cu);
-    hipLaunchKernelGGL((paged_scan_kernel<NQ, PK, PV, EXACT>), dim3((unsigned)((q.scan_items + a.batch) * a.n_kv_heads)), dim3(256), lds, st, g, q);
+    hipLaunchKernelGGL((attn_kernel<NQ, PK, PV, EXACT, PagedAttnArgs>), dim3((unsigned)((q.scan_items + a.batch) * a.n_kv_heads)), dim3(256), lds, st, g, q);
     return Split{0, q.scan_items};
   }
   const Split split = scan_split(groups, (a.n_tokens + 63) / 64, per_cu, NQ * (a.Wk + a.Wv));
