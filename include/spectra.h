@@ -401,7 +401,8 @@ spectra_status spectra_paged_encode(const spectra_pages* m, const spectra_codec*
  * as they were; so are those of sequences with more than max_new new tokens or max_tokens slots
  * (the call's bounds, by which the work is split). Slots past a sequence's end are never read
  * into a result; a page out of range counts as a page of zero records; in records, NaN or
- * infinite metadata counts as 0 (such tokens' codes are unspecified anyway).
+ * infinite metadata counts as 0 (such tokens' codes are unspecified anyway); a width table that
+ * does not fit its records counts as one that keeps nothing.
  * out_dt fp32: the error is that of fp32 sums (about 1e-6 of the result). bf16: operands are
  * rounded to fp16, which stays below the output's rounding; lse is then good to about 1e-3.
  * Coefficients are held in fp16 parts: those beyond 65504 are taken as 65504, and of those below

@@ -568,9 +568,13 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a, Paged... paged
   const float E2q = prepare_query<NQ>(a, s, nqh, tid, reinterpret_cast<uint8_t*>(smem), qa_s, qbar_s, red_s, row_at, [&] {
     if (PK > 0 && tt < tile_end) load_tile(tt);
   });
-  const Kept Kk = read_kept(a.bits_k + (int64_t)s * NG);
-  const Kept Kv = read_kept(a.bits_v + (int64_t)s * NG);
-  const bool ok = Kk.ok && Kv.ok && Kk.used <= Wk && Kv.used <= Wv;
+  Kept Kk = read_kept(a.bits_k + (int64_t)s * NG);
+  Kept Kv = read_kept(a.bits_v + (int64_t)s * NG);
+  if constexpr (PAGED) {  // width table inconsistent with the record: nothing is kept
+    if (!Kk.ok || Kk.used > Wk) Kk = Kept{};
+    if (!Kv.ok || Kv.used > Wv) Kv = Kept{};
+  }
+  const bool ok = PAGED || (Kk.ok && Kv.ok && Kk.used <= Wk && Kv.used <= Wv);
   if (tid == 0) e2_s = E2q;
   __syncthreads();  // prepared query data in LDS; the scratch may now hold tiles
   const float E2 = e2_s;
