@@ -35,3 +35,57 @@ def test_width_tables_that_do_not_fit_keep_nothing(table, tensor, lens, new, n_q
         gone[tensor] = np.zeros((n, D))
         c.coef[b][1] = tuple(gone)
     check_split(c, *_run(c))
+
+
+def _large(tensor, lens, new, n_qh, f32):
+    """Every third token's groups of one tensor reach past fp16's largest number, by either sign."""
+    rng = np.random.default_rng([41, tensor])
+
+    def coefs(b, h, t, bits, p, n):
+        if t != tensor:
+            return records(bits, p, n, rng)
+        codes = np.stack([rng.integers(0, 2 ** int(w), (n, G)) for w in bits], 1)
+        top = np.maximum(1, 2.0 ** np.asarray(bits) - 1)
+        codes[..., 0], codes[..., 1] = 0, top
+        codes = codes.reshape(n, D)
+        far = (np.arange(n) % 3 == 0)[:, None]
+        sign = rng.choice([-1.0, 1.0], (n, 1))
+        z = np.where(far, sign * 3e4, rng.standard_normal((n, len(bits))))
+        step = np.where(far, sign * rng.uniform(1e4, 6e4, (n, len(bits))), 1.0) / top
+        return records_of(codes, z, step, bits, p)
+    return Built(lens, new, n_qh, B8, B8, 8, coefs,
+                 lambda c: (2.0 ** -14 if tensor == 0 else 1.0) * rng.standard_normal((sum(new), c.H * n_qh, D)), f32=f32,
+                 mean_k=0.0, mean_v=0.0)
+
+
+def _lowered(c, tensor):
+    """The scale of a token's group with a coefficient past 65504 lowered until there is none, to fp16."""
+    changed = 0
+    for b, per in enumerate(c.coef):
+        for h, pair in enumerate(per):
+            x = pair[tensor].reshape(-1, D // G, G)
+            # every group holds codes 0 (the zero point) and 2^b - 1
+            bits = np.asarray(B8[h])
+            for g in np.flatnonzero(bits):
+                top = 2 ** int(bits[g]) - 1
+                z = np.where(x[:, g].mean(1) > 0, x[:, g].min(1), x[:, g].max(1))
+                end = np.where(x[:, g].mean(1) > 0, x[:, g].max(1), x[:, g].min(1))
+                far = np.abs(end) > 65504
+                code = (x[:, g] - z[:, None]) / np.where(end != z, (end - z) / top, 1.0)[:, None]
+                step = ((np.sign(end) * 65472 - z) / top).astype(np.float16).astype(np.float64)
+                low = z[:, None] + step[:, None] * np.rint(code)
+                x[far, g] = low[far]
+                changed += int(far.sum())
+    return changed
+
+
+# (keys beside 16-bit outputs would need queries below what fp16 holds in full)
+@pytest.mark.parametrize("tensor,f32", [(0, True), (1, True), (1, False)], ids=["keys-f32", "values-f32", "values-bf16"])
+@pytest.mark.parametrize("lens,new,n_qh", FORMS)
+def test_coefficients_past_the_largest_fp16_number(tensor, lens, new, n_qh, f32):
+    c = _large(tensor, lens, new, n_qh, f32)
+    out, lse = _run(c)
+    few_rows_in_fp32 = f32 and max(new) * n_qh <= 16
+    if not few_rows_in_fp32:
+        assert _lowered(c, tensor) > 50
+    check_split(c, out, lse)
