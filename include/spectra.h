@@ -407,8 +407,8 @@ spectra_status spectra_paged_encode(const spectra_pages* m, const spectra_codec*
  * rounded to fp16, which stays below the output's rounding; lse is then good to about 1e-3.
  * Coefficients are held in fp16 parts: a token's group in which one passes 65504 has its scale
  * lowered until none does, and of those below 2^-14 absolute errors of 2^-25 remain; with bf16
- * outputs that holds for scale log2(e) q V_K too. (fp32 outputs of at most 16 new rows of a
- * sequence and KV head, 12 beside records too wide for more, take coefficients as they are.)
+ * outputs that holds for scale log2(e) q V_K too. (Where a sequence has at most 16 new rows on a KV
+ * head, new tokens times query heads, coefficients past 65504 may also count as they are.)
  * NaN and infinities in a query row reach no other row. At most 2^30 query rows and 2^18 sequences
  * times KV heads. softmax_scale <= 0 selects 1/sqrt(128). Workspace:
  * device, 256-byte aligned, spectra_paged_attention_workspace_bytes (never fewer for larger counts:

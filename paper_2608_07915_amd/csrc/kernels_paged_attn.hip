@@ -1144,11 +1144,16 @@ hipError_t launch_paged_attention(const PagedAttnArgs& args, void* workspace, hi
   a.scan_least = PAGED_SCAN_LEAST;
   a.scan_plan = reinterpret_cast<int32_t*>(ws + p.plan_at);
   float* partial = reinterpret_cast<float*>(ws + p.scan_at);
-  // Also for 16-bit outputs the latent scan where it has one quad of rows, sequences may be long and
-  // there is work for many tiles a wavefront: four heads on each of eight KV heads, 64 sequences of
-  // 30k slots 348 us and 423 by paged_few_kernel, of 8000 110 and 126; but one of 131k 50 and 47, 256
-  // of 100 63 and 54, of 1000 92 and 84.
-  const bool long_quad = p.scan_tokens * a.n_qh <= 4 && a.max_tokens > 2048 && a.c.batch * a.max_tokens * a.c.n_kv > (int64_t)1 << 22;
+  // Also for 16-bit outputs the latent scan where it has one quad of rows and records of 8 words (no
+  // clamped loads, three workgroups on a CU), sequences may be long and there may be work for many
+  // tiles a wavefront. Scan and paged_few_kernel, four heads on each of eight KV heads: 64 sequences of
+  // 2048 slots 56 and 66 us, of 8192 141 and 170, of 32768 481 and 621; 8 of 32768 82 and 84; but one of
+  // 131072 53 and 51, 256 of 512 88 and 79, of 1024 111 and 104. Other records: 5 words, 64 sequences of
+  // 8192 118 and 121, one of 262144 64 and 60; 4 and 12 words 125 and 129, 68 and 61; 12 words 183 and
+  // 192, 101 and 82; 30 words 832 and 272, 421 and 128. The host knows the bound of the lengths only: many
+  // short sequences under a long one pay the difference (256 of 128 slots 72 and 61).
+  const bool long_quad = p.scan_tokens * a.n_qh <= 4 && a.Wk == 8 && a.Wv == 8 && a.max_tokens > 2048 &&
+                         a.c.batch * a.max_tokens * a.c.n_kv >= (int64_t)1 << 21;
   if (a.out_f32 || long_quad) {
     launch_paged_scan(a, partial, st);
   } else {

@@ -16,9 +16,9 @@ B8 = [[5, 1, 0, 0], [4, 2, 0, 0]]
 FORMS = [([200, 90], [1, 1], 4), ([200, 90], [40, 7], 4)]   # few rows, chunks
 
 
-def _run(c):
+def _run(c, bound=None):
     lse = torch.empty(c.q.shape[:2], device="cuda")
-    return S.spectra_paged_attention(c.cache, c.ck, c.cv, *c.pools, c.q, c.cu, max(c.new), max(c.lens), lse=lse), lse
+    return S.spectra_paged_attention(c.cache, c.ck, c.cv, *c.pools, c.q, c.cu, max(c.new), bound or max(c.lens), lse=lse), lse
 
 
 @pytest.mark.parametrize("f32", [False, True], ids=["bf16", "f32"])
@@ -89,3 +89,14 @@ def test_coefficients_past_the_largest_fp16_number(tensor, lens, new, n_qh, f32)
     if not few_rows_in_fp32:
         assert _lowered(c, tensor) > 50
     check_split(c, out, lse)
+
+
+@pytest.mark.parametrize("new,n_qh", [([1, 1, 1], 4), ([4, 1, 2], 1), ([2, 0, 1], 2)])
+@pytest.mark.parametrize("bound", [2600, 2 ** 20])
+def test_few_rows_by_either_kernel(bound, new, n_qh):
+    # records of 8 words and one quad of rows: a call that may hold many long sequences takes the latent scan
+    rng = np.random.default_rng(43)
+    lens = [2600, 70, 5]
+    c = Built(lens, new, n_qh, B8, B8[::-1], 8, lambda b, h, t, bits, p, n: records(bits, p, n, rng),
+              lambda c: 2.0 * rng.standard_normal((sum(new), c.H * n_qh, D)))
+    check_split(c, *_run(c, bound))
