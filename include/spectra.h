@@ -403,8 +403,15 @@ spectra_status spectra_paged_encode(const spectra_pages* m, const spectra_codec*
  * into a result; a page out of range counts as a page of zero records; in records, NaN or
  * infinite metadata counts as 0 (such tokens' codes are unspecified anyway); a width table that
  * does not fit its records counts as one that keeps nothing.
- * out_dt fp32: the error is that of fp32 sums (about 1e-6 of the result). bf16: operands are
- * rounded to fp16, which stays below the output's rounding; lse is then good to about 1e-3.
+ * out_dt fp32: factors are pairs of fp16 parts, sums fp32. With x the largest sum_j |q'_j c_j| of a
+ * row and a slot (q' = scale q V_K, c a record's coefficients), a score, lse and, relative, a softmax
+ * weight are off by about 2^-18 x at most; where a sequence has at most 16 new rows on a KV head (new
+ * tokens times query heads) the weights are pairs of bf16 parts besides (2^-16).
+ * bf16: q', c and the weights are rounded to fp16, so a score, lse and, relative, a weight are off by
+ * at most about 2^-10 x, typically 2^-12 of the root of sum_j (q'_j c_j)^2. Scores of a spread of 3
+ * nats (standard deviation over the slots) leave outputs off by a third of their own rounding, of 10 by
+ * about as much as that, of 30 by half as much again, rows whose weight lies on two or three slots by
+ * up to 3%. For more, ask for fp32 outputs (queries may be bf16).
  * Coefficients are held in fp16 parts: a token's group in which one passes 65504 has its scale
  * lowered until none does, and of those below 2^-14 absolute errors of 2^-25 remain; with bf16
  * outputs that holds for scale log2(e) q V_K too. (Where a sequence has at most 16 new rows on a KV

@@ -4,7 +4,7 @@ import pytest
 
 import paper_2608_07915_amd as S
 from paged_cases import Built, check_split, records_of
-from paged_ref import D, G, codec, records
+from paged_ref import D, G, default_scale, records
 
 pytestmark = pytest.mark.gpu
 
@@ -100,3 +100,34 @@ def test_few_rows_by_either_kernel(bound, new, n_qh):
     c = Built(lens, new, n_qh, B8, B8[::-1], 8, lambda b, h, t, bits, p, n: records(bits, p, n, rng),
               lambda c: 2.0 * rng.standard_normal((sum(new), c.H * n_qh, D)))
     check_split(c, *_run(c, bound))
+
+
+@pytest.mark.parametrize("f32", [False, True], ids=["bf16", "f32"])
+@pytest.mark.parametrize("lens,new,n_qh,bound", [([2600, 300], [1, 1], 4, None), ([2600, 300], [1, 1], 4, 2 ** 20),
+                                                 ([300, 50], [30, 9], 4, None), ([2600], [40], 4, None)],
+                         ids=["few", "scan", "chunk", "parts"])
+@pytest.mark.parametrize("spread", [1.0, 10.0, 30.0])
+def test_scores_of_a_spread(spread, lens, new, n_qh, bound, f32):
+    # the standard deviation of a row's scores over its slots, in nats
+    rng = np.random.default_rng(47)
+
+    def query(c):
+        q = rng.standard_normal((sum(new), c.H * n_qh, D))
+        for h in range(c.H):
+            hs = slice(h * n_qh, (h + 1) * n_qh)
+            s = default_scale() * (q[:, hs] @ c.state(h)[0]) @ c.coef[0][h][0].T
+            q[:, hs] *= (spread / s.std(-1))[..., None]
+        return q
+    c = Built(lens, new, n_qh, B8, B8[::-1], 8, lambda b, h, t, bits, p, n: records(bits, p, n, rng), query, f32=f32)
+    check_split(c, *_run(c, bound))
+
+
+@pytest.mark.parametrize("f32", [False, True], ids=["bf16", "f32"])
+@pytest.mark.parametrize("lens,new,n_qh", FORMS)
+@pytest.mark.parametrize("of_keys,of_values", [(2.0 ** -6, 2.0 ** 8), (2.0 ** 8, 2.0 ** -6)])
+def test_magnitudes(of_keys, of_values, lens, new, n_qh, f32):
+    # coefficients and q' of both stay where fp16 holds all its bits but for a few
+    rng = np.random.default_rng(53)
+    c = Built(lens, new, n_qh, B8, B8[::-1], 8, lambda b, h, t, bits, p, n: records(bits, p, n, rng, (of_keys, of_values)[t]),
+              lambda c: 2.0 / of_keys * rng.standard_normal((sum(new), c.H * n_qh, D)), mean_k=of_keys, mean_v=of_values, f32=f32)
+    check_split(c, *_run(c))
