@@ -94,6 +94,19 @@ def _stream(stream=None):
     return ctypes.c_void_p(s.cuda_stream)
 
 
+def _made(stream, shape, dtype, device):
+    """An empty tensor for a call on ``stream`` (None: the current one). It belongs to that stream: no
+    work still pending on another one uses its memory, and none gets it before the call has passed.
+    Freed, it is also kept until what the current stream then does with it is done."""
+    import torch
+    if stream is None:
+        return torch.empty(shape, dtype=dtype, device=device)
+    with torch.cuda.stream(stream):
+        t = torch.empty(shape, dtype=dtype, device=device)
+    t.record_stream(torch.cuda.current_stream(device))
+    return t
+
+
 class Codec:
     """Per-stream codec state (basis, mean, variances, group widths) in device memory."""
 

@@ -1,6 +1,9 @@
 """Binding of the paged cache (argument marshalling only): many sequences' records in pools of
 pages under one page map, their appends and the attention over them. Function names match the C
 ABI in ``include/spectra.h``.
+
+``stream`` (default: the current one) is where a call runs. Outputs and workspaces that are made for
+a call belong to that stream; other streams that use an output wait for it first.
 """
 from __future__ import annotations
 
@@ -8,7 +11,7 @@ import ctypes
 
 from . import _lib
 from ._lib import check, spectra_pages, spectra_pool
-from .codec import Codec, _dtype_code, _need
+from .codec import Codec, _dtype_code, _made, _need
 
 
 class PagedCache:
@@ -37,13 +40,12 @@ class PagedCache:
 
 class _Call:
     """The call's stream, with the cache's device current while the call is made."""
-    __slots__ = ("given", "handle", "ctx")
+    __slots__ = ("handle", "ctx")
 
     def __init__(self, device, stream):
         import torch
         _need(device.type == "cuda", "the page map must be on a device")
         _need(stream is None or stream.device == device, f"the stream belongs to another device than the page map's {device}")
-        self.given = stream
         self.handle = stream.cuda_stream if stream is not None else torch._C._cuda_getCurrentRawStream(device.index)
         self.ctx = None if torch.cuda.current_device() == device.index else torch.cuda.device(device)
 
@@ -54,13 +56,6 @@ class _Call:
 
     def __exit__(self, *exc):
         return self.ctx.__exit__(*exc) if self.ctx is not None else None
-
-    def keep(self, *made):
-        """Tensors made here for the call: not reused before a given stream has passed it."""
-        if self.given is not None:
-            for t in made:
-                if t is not None:
-                    t.record_stream(self.given)
 
 
 def _ints(t, name: str, device, n=None):
@@ -89,10 +84,10 @@ def _pools(cache: PagedCache, pools):
     return (spectra_pool * max(len(flat), 1))(*flat), len(flat)
 
 
-def _workspace(cache: PagedCache, workspace, need: int):
+def _workspace(cache: PagedCache, workspace, need: int, stream):
     import torch
     if workspace is None:
-        return torch.empty(max(need, 1), dtype=torch.uint8, device=cache.table.device)
+        return _made(stream, max(need, 1), torch.uint8, cache.table.device)
     _need(workspace.device == cache.table.device and workspace.is_contiguous(),
           f"workspace must be contiguous and on {cache.table.device}")
     return workspace
@@ -115,12 +110,10 @@ def spectra_pages_extend(cache: PagedCache, rows, counts, pools, ends=None, work
     with _Call(dev, stream) as s:
         args = (_ints(rows, "rows", dev), _ints(counts, "counts", dev, n))
         made, n_pools = _pools(cache, pools)
-        new_ends = torch.empty_like(rows) if ends is None else None
-        ends = new_ends if ends is None else ends
-        ws = _workspace(cache, workspace, spectra_pages_workspace_bytes(cache))
+        ends = _made(stream, n, torch.int32, dev) if ends is None else ends
+        ws = _workspace(cache, workspace, spectra_pages_workspace_bytes(cache), stream)
         check(_lib.get().spectra_pages_extend(cache.ref, *args, n, made, n_pools,
                                               _ints(ends, "ends", dev, n), ws.data_ptr(), _bytes(ws), s.handle))
-        s.keep(new_ends, ws if workspace is None else None)
     return ends
 
 
@@ -131,11 +124,9 @@ def spectra_pages_fork(cache: PagedCache, parents, children, ends=None, stream=N
     dev = cache.table.device
     n = parents.numel()
     with _Call(dev, stream) as s:
-        new_ends = torch.empty_like(parents) if ends is None else None
-        ends = new_ends if ends is None else ends
+        ends = _made(stream, n, torch.int32, dev) if ends is None else ends
         check(_lib.get().spectra_pages_fork(cache.ref, _ints(parents, "parents", dev),
                                             _ints(children, "children", dev, n), n, _ints(ends, "ends", dev, n), s.handle))
-        s.keep(new_ends)
     return ends
 
 
@@ -155,13 +146,11 @@ def spectra_pages_compact(cache: PagedCache, pools, moved=None, workspace=None, 
     dev = cache.table.device
     with _Call(dev, stream) as s:
         made, n_pools = _pools(cache, pools)
-        new_moved = torch.empty(cache.n_pages + 1, dtype=torch.int32, device=dev) if moved is None else None
-        moved = new_moved if moved is None else moved
-        ws = _workspace(cache, workspace, spectra_pages_workspace_bytes(cache))
+        moved = _made(stream, cache.n_pages + 1, torch.int32, dev) if moved is None else moved
+        ws = _workspace(cache, workspace, spectra_pages_workspace_bytes(cache), stream)
         check(_lib.get().spectra_pages_compact(cache.ref, made, n_pools,
                                                _ints(moved, "moved", dev, cache.n_pages + 1), ws.data_ptr(), _bytes(ws),
                                                s.handle))
-        s.keep(new_moved, ws if workspace is None else None)
     return moved
 
 
@@ -226,15 +215,13 @@ def spectra_paged_attention(cache: PagedCache, ck: Codec, cv: Codec, pool_k, poo
     _need(lse is None or (lse.device == dev and lse.dtype == torch.float32 and lse.is_contiguous()
                           and tuple(lse.shape) == (n, n_q_heads)), f"lse must be a contiguous float32 tensor {(n, n_q_heads)}")
     with _Call(dev, stream) as s:
-        new_out = torch.empty((n, n_q_heads, 128), dtype=q.dtype, device=dev) if out is None else None
-        out = new_out if out is None else out
+        out = _made(stream, (n, n_q_heads, 128), q.dtype, dev) if out is None else out
         _need(out.device == dev and out.is_contiguous() and tuple(out.shape) == (n, n_q_heads, 128),
               f"out must be a contiguous tensor {(n, n_q_heads, 128)} on {dev}")
         ws = _workspace(cache, workspace, spectra_paged_attention_workspace_bytes(batch, n, n_q_heads, ck.n_streams,
-                                                                                  max_new, max_tokens))
+                                                                                  max_new, max_tokens), stream)
         check(_lib.get().spectra_paged_attention(*head, n, int(max_new), int(max_tokens), q.data_ptr(), _dtype_code(q),
                                                  q.stride(0), q.stride(1), n_q_heads, float(softmax_scale), out.data_ptr(),
                                                  _dtype_code(out), lse.data_ptr() if lse is not None else None,
                                                  ws.data_ptr(), _bytes(ws), s.handle))
-        s.keep(new_out, ws if workspace is None else None)
     return out
