@@ -2,7 +2,8 @@
 
 Torch tensors provide device memory and the current stream; every step of the
 codec runs in the HIP library. Function names match the C ABI in
-``include/spectra.h``.
+``include/spectra.h``. Outputs and workspaces that are made for a call belong to
+the stream that it is given; other streams that use an output wait for it first.
 """
 from __future__ import annotations
 
@@ -180,7 +181,7 @@ def spectra_fit_basis(codec: Codec, x, n_tokens: Optional[int] = None, workspace
     _device_rows(codec, x, "x", n)
     need = spectra_fit_workspace_bytes(codec, n)
     if workspace is None:
-        workspace = torch.empty(need, dtype=torch.uint8, device=x.device)
+        workspace = _made(stream, need, torch.uint8, x.device)
     check(_lib.get().spectra_fit_basis(ctypes.byref(codec.struct), x.data_ptr(), _dtype_code(x), n, x.stride(0),
                                        x.stride(1), workspace.data_ptr(), workspace.numel(), _stream(stream)))
 
@@ -206,8 +207,7 @@ def spectra_fit_weights(codec: Codec, W, G, hbar=None, streams_per_layer: int = 
     _need(tuple(G.shape) == (layers, d_model, d_model), f"G must be [{layers}, {d_model}, {d_model}], got {tuple(G.shape)}")
     _need(hbar is None or tuple(hbar.shape) == (layers, d_model), f"hbar must be [{layers}, {d_model}]")
     if workspace is None:
-        workspace = torch.empty(spectra_fit_weights_workspace_bytes(codec, d_model), dtype=torch.uint8,
-                                device=W.device)
+        workspace = _made(stream, spectra_fit_weights_workspace_bytes(codec, d_model), torch.uint8, W.device)
     check(_lib.get().spectra_fit_weights(ctypes.byref(codec.struct), W.data_ptr(), d_model, G.data_ptr(),
                                          hbar.data_ptr() if hbar is not None else None, int(streams_per_layer),
                                          workspace.data_ptr(), workspace.numel(), _stream(stream)))
@@ -229,7 +229,7 @@ def spectra_decode(codec: Codec, packed, t_capacity: int, t0: int, n_tokens: int
     _packed_words(codec, packed, t_capacity, "packed")
     shape = (codec.n_streams, int(n_tokens), codec.params.head_dim)
     if out is None:
-        out = torch.empty(shape, dtype=torch.float32, device=packed.device)
+        out = _made(stream, shape, torch.float32, packed.device)
     _need(out.is_cuda and out.dtype == torch.float32 and out.is_contiguous() and tuple(out.shape) == shape,
           f"out must be a contiguous float32 device tensor {shape}")
     check(_lib.get().spectra_decode(ctypes.byref(codec.struct), packed.data_ptr(), int(t_capacity), int(t0),
@@ -247,10 +247,10 @@ def spectra_decode_attention(ck: Codec, cv: Codec, packed_k, packed_v, t_capacit
     import torch
     batch, n_q_heads, d = _attention_shapes(ck, cv, packed_k, packed_v, t_capacity, q, n_kv_heads, out)
     if out is None:
-        out = torch.empty((batch, n_q_heads, d), dtype=torch.float32, device=q.device)
+        out = _made(stream, (batch, n_q_heads, d), torch.float32, q.device)
     if workspace is None:
         need = spectra_attention_workspace_bytes(batch, n_q_heads, n_kv_heads, n_tokens)
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        workspace = _made(stream, need, torch.uint8, q.device)
     check(_lib.get().spectra_decode_attention(ctypes.byref(ck.struct), ctypes.byref(cv.struct), packed_k.data_ptr(),
                                               packed_v.data_ptr(), int(t_capacity), int(n_tokens), q.data_ptr(),
                                               _dtype_code(q), batch, n_q_heads, int(n_kv_heads), float(softmax_scale),
@@ -279,12 +279,12 @@ def spectra_layer_decode_attention(ck: Codec, cv: Codec, packed_k, packed_v, t_c
     _packed_words(ck, packed_k, t_capacity, "packed_k")
     _packed_words(cv, packed_v, t_capacity, "packed_v")
     if out is None:
-        out = torch.empty((batch, n_q_heads, 128), dtype=torch.float32, device=q.device)
+        out = _made(stream, (batch, n_q_heads, 128), torch.float32, q.device)
     _need(out.is_cuda and out.dtype == torch.float32 and out.is_contiguous() and tuple(out.shape) == (batch, n_q_heads, 128),
           f"out must be a contiguous float32 device tensor {(batch, n_q_heads, 128)}")
     if workspace is None:
         need = spectra_layer_attention_workspace_bytes(ck, batch, n_q_heads, n_tokens)
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        workspace = _made(stream, need, torch.uint8, q.device)
     check(_lib.get().spectra_layer_decode_attention(ctypes.byref(ck.struct), ctypes.byref(cv.struct), packed_k.data_ptr(),
                                                     packed_v.data_ptr(), int(t_capacity), int(n_tokens), q.data_ptr(),
                                                     _dtype_code(q), batch, n_q_heads, int(n_kv_heads),
@@ -304,10 +304,10 @@ def spectra_decode_attention_rope(ck: Codec, cv: Codec, packed_k, packed_v, t_ca
           and tuple(inv_freq.shape) == (d // 2,), f"inv_freq must be a contiguous float32 device tensor [{d // 2}]")
     pos = int(n_tokens) - 1 if q_position is None else int(q_position)
     if out is None:
-        out = torch.empty((batch, n_q_heads, d), dtype=torch.float32, device=q.device)
+        out = _made(stream, (batch, n_q_heads, d), torch.float32, q.device)
     if workspace is None:
         need = spectra_attention_workspace_bytes(batch, n_q_heads, n_kv_heads, n_tokens)
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        workspace = _made(stream, need, torch.uint8, q.device)
     check(_lib.get().spectra_decode_attention_rope(ctypes.byref(ck.struct), ctypes.byref(cv.struct),
                                                    packed_k.data_ptr(), packed_v.data_ptr(), int(t_capacity),
                                                    int(n_tokens), q.data_ptr(), _dtype_code(q), batch, n_q_heads,
@@ -328,10 +328,10 @@ def spectra_decode_step(ck: Codec, cv: Codec, packed_k, packed_v, t_capacity: in
     _need(k_new.dtype == v_new.dtype and tuple(k_new.shape) == tuple(v_new.shape) == (batch, n_kv_heads, d),
           f"k_new and v_new must be [{batch}, {n_kv_heads}, {d}] of one dtype")
     if out is None:
-        out = torch.empty((batch, n_q_heads, d), dtype=torch.float32, device=q.device)
+        out = _made(stream, (batch, n_q_heads, d), torch.float32, q.device)
     if workspace is None:
         need = spectra_attention_workspace_bytes(batch, n_q_heads, n_kv_heads, t + 1)
-        workspace = torch.empty(need, dtype=torch.uint8, device=q.device)
+        workspace = _made(stream, need, torch.uint8, q.device)
     check(_lib.get().spectra_decode_step(ctypes.byref(ck.struct), ctypes.byref(cv.struct), packed_k.data_ptr(),
                                          packed_v.data_ptr(), int(t_capacity), int(t), k_new.data_ptr(),
                                          v_new.data_ptr(), _dtype_code(k_new), q.data_ptr(), _dtype_code(q), batch,
@@ -353,7 +353,7 @@ def spectra_decode_step_static(ck: Codec, cv: Codec, packed_k, packed_v, t_capac
     _need(k_new.dtype == v_new.dtype and tuple(k_new.shape) == tuple(v_new.shape) == (batch, n_kv_heads, d),
           f"k_new and v_new must be [{batch}, {n_kv_heads}, {d}] of one dtype")
     if out is None:
-        out = torch.empty((batch, n_q_heads, d), dtype=torch.float32, device=q.device)
+        out = _made(stream, (batch, n_q_heads, d), torch.float32, q.device)
     check(_lib.get().spectra_decode_step_static(ctypes.byref(ck.struct), ctypes.byref(cv.struct), packed_k.data_ptr(),
                                                 packed_v.data_ptr(), int(t_capacity), int(t), k_new.data_ptr(),
                                                 v_new.data_ptr(), _dtype_code(k_new), q.data_ptr(), _dtype_code(q),
@@ -377,8 +377,8 @@ def spectra_unpack_codes(codec: Codec, packed, t_capacity: int, n_tokens: int, s
     import torch
     _packed_words(codec, packed, t_capacity, "packed")
     dev = packed.device
-    codes = torch.empty((codec.n_streams, n_tokens, codec.params.head_dim), dtype=torch.uint8, device=dev)
-    meta = torch.empty((codec.n_streams, n_tokens, codec.params.n_groups), dtype=torch.int32, device=dev)
+    codes = _made(stream, (codec.n_streams, n_tokens, codec.params.head_dim), torch.uint8, dev)
+    meta = _made(stream, (codec.n_streams, n_tokens, codec.params.n_groups), torch.int32, dev)
     check(_lib.get().spectra_unpack_codes(ctypes.byref(codec.struct), packed.data_ptr(), int(t_capacity),
                                           int(n_tokens), codes.data_ptr(), meta.data_ptr(), _stream(stream)))
     return codes, meta

@@ -88,3 +88,23 @@ def test_map_calls():
     need = S.spectra_pages_workspace_bytes(cache)
     for call in (extend, fork, compact):
         _under_pending_work(call, [512, need])
+
+
+def test_contiguous_calls():
+    (ck, _), (cv, _) = codec(BITS, 8, 3), codec(BITS, 8, 4)
+    cap, T = 320, 300
+    x = torch.randn((H, T, D), device="cuda")
+    packed = [c.empty_packed(cap) for c in (ck, cv)]
+    for c, p in zip((ck, cv), packed):
+        S.spectra_encode(c, x, 0, p, cap)
+    q = torch.randn((1, H * QH, D), device="cuda")
+    need = S.spectra_attention_workspace_bytes(1, H * QH, H, T)
+    freq = torch.rand(D // 2, device="cuda")
+    new = [x[:, i][None].contiguous() for i in (0, 1)]
+    _under_pending_work(lambda s: S.spectra_decode_attention(ck, cv, *packed, cap, T, q, H, stream=s), [q.numel() * 4, need])
+    _under_pending_work(lambda s: S.spectra_decode_attention_rope(ck, cv, *packed, cap, T, q, H, freq, stream=s),
+                        [q.numel() * 4, need])
+    _under_pending_work(lambda s: S.spectra_decode_step(ck, cv, *packed, cap, T, *new, q, H, stream=s),
+                        [q.numel() * 4, need])
+    _under_pending_work(lambda s: S.spectra_decode(cv, packed[1], cap, 0, T, stream=s), [H * T * D * 4])
+    _under_pending_work(lambda s: S.spectra_unpack_codes(cv, packed[1], cap, T, stream=s)[1], [H * T * D, H * T * 4 * 4])
