@@ -30,3 +30,12 @@ def test_calls_are_split(tmp_path):
     _, parts, slots, _ = plan(*SPLIT["last_part_of_one"])
     assert 2305 - (parts - 1) * slots == 1
     assert plan([2600] * 130, [40] * 130, 4)[1] == 1
+
+
+@pytest.mark.skipif(shutil.which("g++") is None, reason="g++ not available")
+def test_units_and_chunks_of_any_sequences(tmp_path):
+    exe = str(tmp_path / "units")
+    subprocess.run(["g++", "-std=c++17", "-O2", "-Wall", f"-I{CSRC}", os.path.join(ROOT, "tests", "paged_units_check.cpp"), "-o", exe],
+                   check=True)
+    r = subprocess.run([exe], capture_output=True, text=True, timeout=120)
+    assert r.returncode == 0 and r.stdout.strip() == "OK", r.stdout + r.stderr
