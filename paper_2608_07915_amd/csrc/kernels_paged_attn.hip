@@ -1146,14 +1146,16 @@ hipError_t launch_paged_attention(const PagedAttnArgs& args, void* workspace, hi
   float* partial = reinterpret_cast<float*>(ws + p.scan_at);
   // Also for 16-bit outputs the latent scan where it has one quad of rows and records of 8 words (no
   // clamped loads, three workgroups on a CU), sequences may be long and there may be work for many
-  // tiles a wavefront. Scan and paged_few_kernel, four heads on each of eight KV heads: 64 sequences of
-  // 2048 slots 56 and 66 us, of 8192 141 and 170, of 32768 481 and 621; 8 of 32768 82 and 84; but one of
-  // 131072 53 and 51, 256 of 512 88 and 79, of 1024 111 and 104. Other records: 5 words, 64 sequences of
-  // 8192 118 and 121, one of 262144 64 and 60; 4 and 12 words 125 and 129, 68 and 61; 12 words 183 and
-  // 192, 101 and 82; 30 words 832 and 272, 421 and 128. The host knows the bound of the lengths only: many
-  // short sequences under a long one pay the difference (256 of 128 slots 72 and 61).
+  // tiles a wavefront. Scan and paged_few_kernel, four heads on each of eight KV heads, lengths between a
+  // quarter of the bound and the bound: 100 sequences of up to 8192 slots 173 and 196 us, 64 of 16384 200
+  // and 206, 256 of 8192 357 and 427, one of 2^20 225 and 250; below the border 64 of 8192 116 and 109,
+  // 48 of 8192 91 and 90, one of 2^18 78 and 78 (though with equal lengths, which paged_few_kernel cuts
+  // badly, 64 of 8192 are 141 and 170). Other records, equal lengths: 5 words, 256 sequences of 4096 211
+  // and 203; 4 and 12 words 229 and 216; 12 words 369 and 297; 30 words 1717 and 431. The host knows the
+  // bound of the lengths only: many short sequences under a long one pay the difference (256 of 128
+  // slots 72 and 61).
   const bool long_quad = p.scan_tokens * a.n_qh <= 4 && a.Wk == 8 && a.Wv == 8 && a.max_tokens > 2048 &&
-                         a.c.batch * a.max_tokens * a.c.n_kv >= (int64_t)1 << 21;
+                         a.c.batch * a.max_tokens * a.c.n_kv > (int64_t)1 << 22;
   if (a.out_f32 || long_quad) {
     launch_paged_scan(a, partial, st);
   } else {

@@ -92,7 +92,7 @@ def test_coefficients_past_the_largest_fp16_number(tensor, lens, new, n_qh, f32)
 
 
 @pytest.mark.parametrize("new,n_qh", [([1, 1, 1], 4), ([4, 1, 2], 1), ([2, 0, 1], 2)])
-@pytest.mark.parametrize("bound", [2600, 2 ** 20])
+@pytest.mark.parametrize("bound", [2600, 2 ** 22])
 def test_few_rows_by_either_kernel(bound, new, n_qh):
     # records of 8 words and one quad of rows: a call that may hold many long sequences takes the latent scan
     rng = np.random.default_rng(43)
@@ -103,7 +103,7 @@ def test_few_rows_by_either_kernel(bound, new, n_qh):
 
 
 @pytest.mark.parametrize("f32", [False, True], ids=["bf16", "f32"])
-@pytest.mark.parametrize("lens,new,n_qh,bound", [([2600, 300], [1, 1], 4, None), ([2600, 300], [1, 1], 4, 2 ** 20),
+@pytest.mark.parametrize("lens,new,n_qh,bound", [([2600, 300], [1, 1], 4, None), ([2600, 300], [1, 1], 4, 2 ** 22),
                                                  ([300, 50], [30, 9], 4, None), ([2600], [40], 4, None)],
                          ids=["few", "scan", "chunk", "parts"])
 @pytest.mark.parametrize("spread", [1.0, 10.0, 30.0])
