@@ -500,18 +500,23 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a, Paged... paged
   const uint32_t* vps = a.packed_v + vbase;
   // PAGED: the page of the next tile to load is read a tile ahead; a page outside the pool is
   // read as page 0 with all metadata taken as zero
-  int tpp = 1;
-  if constexpr (PAGED) tpp = p.c.page_tokens >> 6;
+  int tpp = 1, n_pages = 0;
+  const int32_t* row_table = nullptr;
+  if constexpr (PAGED) {
+    tpp = p.c.page_tokens >> 6;
+    n_pages = p.c.n_pages;
+    row_table = p.c.table + (int64_t)seq.row * p.c.row_pages;
+  }
   int next_page = 0;
   bool loaded_ok = true, tile_ok = true;  // of the tile in flight, of the staged one
   auto look_up = [&](int64_t t2) {
     if constexpr (PAGED)
-      next_page = t2 < tile_end ? p.c.table[(int64_t)seq.row * p.c.row_pages + (int)t2 / tpp] : 0;
+      next_page = t2 < tile_end ? row_table[(int)t2 / tpp] : 0;
   };
   auto load_tile = [&](int64_t tt) {
     uint32_t ko, vo;
     if constexpr (PAGED) {
-      loaded_ok = next_page >= 0 && next_page < p.c.n_pages;
+      loaded_ok = next_page >= 0 && next_page < n_pages;
       const int64_t at = ((int64_t)(loaded_ok ? next_page : 0) * a.n_kv_heads + kv) * tpp + (int)tt % tpp;
       kps = a.packed_k + at * (64 * Wk);
       vps = a.packed_v + at * (64 * Wv);
@@ -571,8 +576,8 @@ __global__ __launch_bounds__(256, 2) void attn_kernel(AttnArgs a, Paged... paged
   Kept Kk = read_kept(a.bits_k + (int64_t)s * NG);
   Kept Kv = read_kept(a.bits_v + (int64_t)s * NG);
   if constexpr (PAGED) {  // width table inconsistent with the record: nothing is kept
-    if (!Kk.ok || Kk.used > Wk) Kk = Kept{};
-    if (!Kv.ok || Kv.used > Wv) Kv = Kept{};
+    if (!Kk.ok || Kk.used > Wk) Kk.n = Kk.used = 0;
+    if (!Kv.ok || Kv.used > Wv) Kv.n = Kv.used = 0;
   }
   const bool ok = PAGED || (Kk.ok && Kv.ok && Kk.used <= Wk && Kv.used <= Wv);
   if (tid == 0) e2_s = E2q;
