@@ -45,9 +45,9 @@ DECODE_STEP_SOURCES = ("kernels_attn.hip", "attn_common.hpp", "kplan.hpp", "enco
                        "kernels.hpp", "splits.hpp")
 # sha256 -> fetch / write bytes per call; per_kernel: [fetch, write]
 MEASURED_TRAFFIC = {
-    "65b6ee8395ee8f192022476f8c4ebfa1067e01af1bca803ff27da87e5e1a11ba": {
-        "fetch_bytes": 74539798, "write_bytes": 1674240, "mfma_busy": 0.093,
-        "per_kernel": {"attn_kernel<1,8,8,true>": [70696726, 1657856], "combine_kernel": [int(1876.5 * 2048), 16384]}},
+    "1056cce1a9efdb41f5db318a092e35b90ca9b7c41f43962698013537b7178a6d": {
+        "fetch_bytes": 74545766, "write_bytes": 1674240, "mfma_busy": 0.095,
+        "per_kernel": {"attn_kernel<1,8,8,true>": [70702694, 1657856], "combine_kernel": [int(1876.5 * 2048), 16384]}},
 }
 # The same passes over the bulk encode of one codec (256 streams x 131072 tokens):
 # HBM bytes per call and the matrix cores' busy fraction (SQ_VALU_MFMA_BUSY_CYCLES

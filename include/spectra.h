@@ -416,8 +416,8 @@ spectra_status spectra_paged_encode(const spectra_pages* m, const spectra_codec*
  * lowered until none does, and of those below 2^-14 absolute errors of 2^-25 remain; with bf16
  * outputs that holds for scale log2(e) q V_K too. (Where a sequence has at most 16 new rows on a KV
  * head, new tokens times query heads, coefficients past 65504 may also count as they are.)
- * NaN and infinities in a query row reach no other row. At most 2^30 query rows and 2^18 sequences
- * times KV heads. softmax_scale <= 0 selects 1/sqrt(128). Workspace:
+ * NaN and infinities in a query row reach no other row. out and q must not overlap. At most 2^30
+ * query rows and 2^18 sequences times KV heads. softmax_scale <= 0 selects 1/sqrt(128). Workspace:
  * device, 256-byte aligned, spectra_paged_attention_workspace_bytes (never fewer for larger counts:
  * one taken for the largest call serves every smaller one of as many heads). Asynchronous. */
 size_t spectra_paged_attention_workspace_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv_heads,

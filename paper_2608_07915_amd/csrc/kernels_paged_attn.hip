@@ -21,8 +21,12 @@
 // (ds_read_b64_tr_b16: four slots of a coefficient per lane).
 //
 // With 16-bit outputs the operands are single fp16 numbers (p between 2^-26 and 8 of the
-// running maximum in the normal range). With fp32 outputs q', p and the coefficients are two
-// fp16 parts each and a product is three (relative error about 2^-21).
+// running maximum in the normal range). A coefficient's rounding is at most 2^(b-11) of the step of
+// its b-bit code where the codes' range holds 0, against half a step of the codec's own, and makes
+// most of the error: a score is off by up to 2^-10 sum_j |q'_j c_j|. Two parts of q' alone would leave
+// the larger half of that; of the keys too they would take three products for one in the scores.
+// With fp32 outputs q', p and the coefficients are two fp16 parts each and a product is three
+// (relative error about 2^-21).
 #include "attn_common.hpp"
 #include "code_operands.hpp"
 #include "encode_dev.hpp"
