@@ -108,3 +108,54 @@ def test_contiguous_calls():
                         [q.numel() * 4, need])
     _under_pending_work(lambda s: S.spectra_decode(cv, packed[1], cap, 0, T, stream=s), [H * T * D * 4])
     _under_pending_work(lambda s: S.spectra_unpack_codes(cv, packed[1], cap, T, stream=s)[1], [H * T * D, H * T * 4 * 4])
+
+
+def test_captured_with_the_stream_given():
+    # outputs and workspaces made during the capture, two graphs replayed in turn
+    cache, ck, cv, pools = _cache([300, 200, 100])
+    graphs = []
+    for new in (1, 60):
+        q = torch.randn((3 * new, H * QH, D), device="cuda")
+        cu = torch.arange(4, dtype=torch.int32, device="cuda") * new
+        call = lambda s: S.spectra_paged_attention(cache, ck, cv, *pools, q, cu, new, 300, stream=s)  # noqa: E731
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g):
+            out = call(torch.cuda.current_stream())
+        graphs.append((g, q, out, cu, new))
+    for _ in range(3):
+        for g, q, out, cu, new in graphs:
+            q.normal_()
+            g.replay()
+            got = out.clone()
+            assert torch.equal(got, S.spectra_paged_attention(cache, ck, cv, *pools, q, cu, new, 300))
+
+
+def test_two_captured_calls_share_a_workspace():
+    # single tokens, and chunks whose slots are split, with their log-sum-exp
+    (ck, _), (cv, _) = codec(BITS, 8, 1), codec(BITS, 8, 2)
+    cache = S.PagedCache(50, 64, 1, 50)
+    cache.table[0, :47] = torch.randperm(47).int()
+    cache.lens[0] = 3000
+    pools = [cache.empty_pool(c) for c in (ck, cv)]
+    x = torch.randn((3000, H, D), device="cuda")
+    S.spectra_paged_encode(cache, ck, cv, *pools, x, x, torch.tensor([0, 3000], dtype=torch.int32, device="cuda"))
+    need = S.spectra_paged_attention_workspace_bytes(1, 64, H * QH, H, 64, 3000)
+    ws = torch.empty(need, dtype=torch.uint8, device="cuda")
+    graphs = []
+    for new in (1, 64):
+        for dtype in (torch.float32, torch.bfloat16):
+            q = torch.randn((new, H * QH, D), device="cuda").to(dtype)
+            cu = torch.tensor([0, new], dtype=torch.int32, device="cuda")
+            out, lse = torch.empty_like(q), torch.empty((new, H * QH), device="cuda")
+            g = torch.cuda.CUDAGraph()
+            with torch.cuda.graph(g):
+                S.spectra_paged_attention(cache, ck, cv, *pools, q, cu, new, 3000, out=out, lse=lse, workspace=ws)
+            graphs.append((g, q, cu, out, lse, new))
+    for _ in range(3):
+        for g, q, cu, out, lse, new in graphs:
+            q.normal_()
+            ws.fill_(255)
+            g.replay()
+            want_lse = torch.empty_like(lse)
+            want = S.spectra_paged_attention(cache, ck, cv, *pools, q, cu, new, 3000, lse=want_lse)
+            assert torch.equal(out, want) and torch.equal(lse, want_lse)
