@@ -431,6 +431,103 @@ spectra_status spectra_paged_attention(const spectra_pages* m, const spectra_cod
                                        void* workspace, size_t ws_bytes, void* stream);
 
 /* ---------------------------------------------------------------------------
+ * Drafted trees over a paged cache (speculative decoding): several continuations of a sequence
+ * are appended at once (spectra_pages_extend, spectra_paged_encode), attended in one call, and the
+ * accepted path is kept.
+ *
+ * Attention of drafted tokens. Everything is as in spectra_paged_attention but for what a token
+ * sees: parents[t] (device, n_new entries) is the place of new token t's parent among the new tokens of
+ * its sequence (0 for the first of them), -1 where it continues the history. New token i of the n of a
+ * sequence with L slots sees the history, slots t < L - n, and of the new tokens its parent, the
+ * parent's parent and so on, and itself. A parent that is no earlier new token of the sequence counts
+ * as -1. A token whose own slot would lie before slot 0 sees none. At most 64 new tokens of a
+ * sequence (max_new). The bounds of spectra_paged_attention's errors hold; with fp32 outputs all
+ * weights are pairs of fp16 parts. Workspace: spectra_paged_tree_attention_workspace_bytes, never
+ * fewer for larger counts. Asynchronous. */
+size_t spectra_paged_tree_attention_workspace_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv_heads,
+                                                    int32_t max_new, int64_t max_tokens);
+spectra_status spectra_paged_tree_attention(const spectra_pages* m, const spectra_codec* ck, const spectra_codec* cv,
+                                            const uint32_t* pool_k, const uint32_t* pool_v, const int32_t* rows,
+                                            const int32_t* ends, const int32_t* cu_new, const int32_t* parents,
+                                            int32_t batch, int64_t n_new, int32_t max_new, int64_t max_tokens,
+                                            const void* q, spectra_dtype q_dt, int64_t q_token_stride,
+                                            int64_t q_head_stride, int32_t n_q_heads, float softmax_scale, void* out,
+                                            spectra_dtype out_dt, float* lse, void* workspace, size_t ws_bytes,
+                                            void* stream);
+
+/* The last drafted[i] slots of row rows[i] are reduced to counts[i] of them: in every pool the records
+ * of slot L - drafted[i] + path[i * path_stride + j] move to slot L - drafted[i] + j, j < counts[i], L =
+ * lens[rows[i]]; the slots behind leave the row, and its pages behind them are free once no row holds
+ * them (the row's new length, ends[i]). The pools are pools of records of n_kv_heads KV heads, any
+ * number of words (page_words a multiple of page_tokens * n_kv_heads); boxes (spectra_paged_bounds)
+ * are not: those of the kept slots' blocks are made again. ends[i] = -1 and nothing changed:
+ * a row out of range or listed before, drafted[i] not in [0, min(L, 64)], counts[i] not in [0,
+ * drafted[i]] or greater than path_stride, a path that does not ascend or leaves [0, drafted[i]), a
+ * drafted slot whose page is out of range or has other owners (spectra_pages_extend leaves none).
+ * path_stride <= 64. Asynchronous. */
+spectra_status spectra_pages_accept(const spectra_pages* m, const int32_t* rows, const int32_t* drafted,
+                                    const int32_t* path, int32_t path_stride, const int32_t* counts, int32_t n,
+                                    const spectra_pool* pools, int32_t n_pools, int32_t n_kv_heads, int32_t* ends,
+                                    void* stream);
+
+/* ---------------------------------------------------------------------------
+ * Attention over selected blocks of a paged cache, for long contexts. A block is a tile of 64 slots.
+ *
+ * Its box: the least and the largest value of every kept key coefficient over its slots, in fp16 (the
+ * numbers that attention with 16-bit outputs multiplies). A box pool has
+ * spectra_paged_bounds_words(m, n_kv) words, of page_words = n_kv * (page_tokens / 64) * 128 each page:
+ *   (fp16) box[(((page*n_kv + kv)*(page_tokens/64) + tile)*4 + slot)*64 + 32*side + j],
+ * slot the place of a group among the kept ones of its head, side 0 the least, 1 the largest, j the
+ * coefficient in the group. It may be among the pools of spectra_pages_extend and _compact.
+ *
+ * spectra_paged_bounds makes the boxes of every block that holds new tokens (sequences as in
+ * spectra_paged_encode, n_new = the tokens of cu_new) from all its slots up to the sequence's end; other
+ * boxes, and places of groups that are not kept, are not written. To call it after each append; after a
+ * truncation the box of a cut block is still one that holds its slots. Metadata that is not finite counts
+ * as in spectra_paged_attention. Asynchronous. */
+int64_t spectra_paged_bounds_words(const spectra_pages* m, int32_t n_kv_heads);
+spectra_status spectra_paged_bounds(const spectra_pages* m, const spectra_codec* ck, const uint32_t* pool_k,
+                                    uint32_t* bounds, const int32_t* rows, const int32_t* ends, const int32_t* cu_new,
+                                    int32_t batch, int64_t n_new, void* stream);
+
+/* The blocks that each new token attends over, for every KV head. With q' = q V_K, head h bounds its
+ * product with any slot of block b by B_h(b) = sum_j max(q'_j least_j, q'_j largest_j); the block's
+ * value is the largest, over the query heads of the KV head, of B_h(b) - max_b' B_h(b'), over the
+ * blocks that the token sees (new token i of the n of a sequence with L slots: those that begin at or
+ * before slot L - n + i). blocks[(t*n_kv + kv)*n_blocks ...]: the first `first` and the last `last` blocks
+ * that it sees and those of the largest value, n_blocks in all (all that it sees where they are no
+ * more), ascending, -1 behind them. Equal values: the lowest index first. Values are computed to about
+ * 2^-20 of sum_j |q'_j box_j|; NaN counts as the least. Rows of no sequence and of those with more than
+ * max_tokens slots are left as they were. first, last >= 0, first + last <= n_blocks <= 4096; at most
+ * 2^24 query rows and 2^18 sequences times KV heads, here and in the attentions of this part.
+ * A page out of range counts as boxes of zeros. Workspace: device, 256-byte aligned,
+ * spectra_paged_select_workspace_bytes, never fewer for larger counts. Asynchronous. */
+size_t spectra_paged_select_workspace_bytes(int64_t n_new, int32_t n_q_heads, int32_t n_kv_heads, int64_t max_tokens);
+spectra_status spectra_paged_select(const spectra_pages* m, const spectra_codec* ck, const uint32_t* bounds,
+                                    const int32_t* rows, const int32_t* ends, const int32_t* cu_new, int32_t batch,
+                                    int64_t n_new, int64_t max_tokens, const void* q, spectra_dtype q_dt,
+                                    int64_t q_token_stride, int64_t q_head_stride, int32_t n_q_heads, int32_t n_blocks,
+                                    int32_t first, int32_t last, int32_t* blocks, void* workspace, size_t ws_bytes,
+                                    void* stream);
+
+/* Causal attention as spectra_paged_attention, where the query heads of KV head kv see the slots of the
+ * listed blocks only: blocks[(t*n_kv + kv)*n_blocks ...] of new token t (device), as
+ * spectra_paged_select writes them. Entries that are negative, past the blocks that the token sees, or not
+ * greater than every entry before them in the list are passed over, so no block counts twice. A token
+ * that sees no slot gets zeros and -inf. Sequences of any length and number of new tokens take part.
+ * With fp32 outputs all weights are pairs of fp16 parts. n_blocks <= 4096, n_new * n_kv * n_blocks <=
+ * 2^32. Workspace: device, 256-byte aligned, spectra_paged_sparse_attention_workspace_bytes, never fewer
+ * for larger counts. Asynchronous. */
+size_t spectra_paged_sparse_attention_workspace_bytes(int64_t n_new, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_blocks);
+spectra_status spectra_paged_sparse_attention(const spectra_pages* m, const spectra_codec* ck, const spectra_codec* cv,
+                                              const uint32_t* pool_k, const uint32_t* pool_v, const int32_t* rows,
+                                              const int32_t* ends, const int32_t* cu_new, int32_t batch, int64_t n_new,
+                                              const int32_t* blocks, int32_t n_blocks, const void* q, spectra_dtype q_dt,
+                                              int64_t q_token_stride, int64_t q_head_stride, int32_t n_q_heads,
+                                              float softmax_scale, void* out, spectra_dtype out_dt, float* lse,
+                                              void* workspace, size_t ws_bytes, void* stream);
+
+/* ---------------------------------------------------------------------------
  * Host-side pieces of the fit, exported so they can be checked without a GPU.
  * ------------------------------------------------------------------------- */
 

@@ -17,6 +17,9 @@ from .codec import (  # noqa: F401
 )
 from .paged import (  # noqa: F401
     PagedCache,
+    spectra_paged_bounds, spectra_paged_select, spectra_paged_select_workspace_bytes, spectra_paged_sparse_attention,
+    spectra_paged_sparse_attention_workspace_bytes, spectra_paged_tree_attention,
+    spectra_paged_tree_attention_workspace_bytes, spectra_pages_accept,
     spectra_paged_attention, spectra_paged_attention_workspace_bytes, spectra_paged_encode, spectra_pages_compact,
     spectra_pages_extend, spectra_pages_fork, spectra_pages_truncate, spectra_pages_workspace_bytes,
 )

@@ -85,6 +85,18 @@ _SIGNATURES = {
     "spectra_paged_attention_workspace_bytes": (_SZ, [_I32, _I64, _I32, _I32, _I32, _I64]),
     "spectra_paged_attention": (_I32, [_PM, _PC, _PC, _P, _P, _P, _P, _P, _I32, _I64, _I32, _I64, _P, _I32, _I64, _I64,
                                        _I32, _F32, _P, _I32, _P, _P, _SZ, _P]),
+    "spectra_pages_accept": (_I32, [_PM, _P, _P, _P, _I32, _P, _I32, _PL, _I32, _I32, _P, _P]),
+    "spectra_paged_tree_attention_workspace_bytes": (_SZ, [_I32, _I64, _I32, _I32, _I32, _I64]),
+    "spectra_paged_tree_attention": (_I32, [_PM, _PC, _PC, _P, _P, _P, _P, _P, _P, _I32, _I64, _I32, _I64, _P, _I32, _I64,
+                                            _I64, _I32, _F32, _P, _I32, _P, _P, _SZ, _P]),
+    "spectra_paged_bounds_words": (_I64, [_PM, _I32]),
+    "spectra_paged_bounds": (_I32, [_PM, _PC, _P, _P, _P, _P, _P, _I32, _I64, _P]),
+    "spectra_paged_select_workspace_bytes": (_SZ, [_I64, _I32, _I32, _I64]),
+    "spectra_paged_select": (_I32, [_PM, _PC, _P, _P, _P, _P, _I32, _I64, _I64, _P, _I32, _I64, _I64, _I32, _I32, _I32, _I32,
+                                    _P, _P, _SZ, _P]),
+    "spectra_paged_sparse_attention_workspace_bytes": (_SZ, [_I64, _I32, _I32, _I32]),
+    "spectra_paged_sparse_attention": (_I32, [_PM, _PC, _PC, _P, _P, _P, _P, _P, _I32, _I64, _P, _I32, _P, _I32, _I64, _I64,
+                                              _I32, _F32, _P, _I32, _P, _P, _SZ, _P]),
     "spectra_allocate_bits": (_I32, [_P, _PP, _P]),
     "spectra_eigh_host": (_I32, [_P, _I32, _P, _P]),
     "spectra_fit_from_moments_host": (_I32, [_PP, _I64, _P, _P, _P, _P, _P, _P]),

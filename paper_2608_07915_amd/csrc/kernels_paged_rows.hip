@@ -1,0 +1,880 @@
+// Attention of a few query rows over tiles of a paged packed cache: the drafted trees of sequences
+// (rows = drafted tokens x query heads of a KV head, tiles = all of the sequence's) and single tokens over
+// listed blocks (rows = query heads of a KV head, tiles = the list's).
+//
+//   q'  = scale * log2(e) * q V_K
+//   S   = q' . c_hat_K(t)                     (the constant q' . m_K cancels in the softmax)
+//   p   = exp2(S - m), l = sum p, a = sum p c_hat_V(t)   in one pass, m the running maximum
+//   out = (a / l + m_V) V_V^T
+//
+// A unit is NB blocks of 16 rows, a workgroup a chunk of the unit's tiles, a wavefront tiles of its
+// own: it turns a kept group of 64 slots into fp16 coefficients in 4 KB of LDS, once for all rows of
+// the unit, and multiplies them on 16 x 16 x 32 products whose columns are the rows. No barrier until
+// the wavefronts' sums are merged. The chunks' partial sums meet in paged_rows_combine_kernel.
+// With 16-bit outputs q', c and p are single fp16 numbers; with fp32 outputs (PRECISE) pairs of fp16 parts,
+// every product three.
+//
+// What a row of a tree sees behind the history is a bit mask of at most 64 drafted slots: its own bit and
+// its ancestors'.
+#include "encode_dev.hpp"
+#include "paged_coef.hpp"
+#include "paged_dev.hpp"
+#include "splits.hpp"
+
+namespace spectra_dev {
+
+constexpr int RO_NW = 4, RO_NT = 64 * RO_NW;
+constexpr int RO_PITCH = D + 4;
+constexpr int DRAFT = 64;  // drafted tokens of a sequence at most
+
+// ---------------------------------------------------------------------------
+// Where a workgroup's work lies
+// ---------------------------------------------------------------------------
+struct RowsPlace {
+  int b;        // sequence; < 0: none
+  int unit;     // of the sequence's units
+  int chunk, n_chunks;
+  int tiles;    // of a chunk
+};
+struct RowsScratch {
+  int64_t part[2][RO_NW], total[2];
+  int32_t b, at, n;
+};
+
+// Trees: sequence b has ceil(n_b n_qh / rows) units, each cut into chunks of `tiles` tiles, the same
+// for all, so that about p.want chunks come out; items are the chunks, the sequences' one after the
+// other. The same in every thread.
+__device__ __forceinline__ RowsPlace tree_place(const PagedRowsArgs& p, int rows, int item, RowsScratch& s) {
+  const PagedCache& c = p.a.c;
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  auto look = [&](int b, int& units, int& tiles) {
+    units = tiles = 0;
+    if (b >= c.batch) return;
+    const PagedSeq q = paged_seq(c, b);
+    if (!attended(p.a, q)) return;
+    units = (int)((q.n * p.a.n_qh + rows - 1) / rows);
+    tiles = units > 0 ? (int)((q.len + TILE - 1) / TILE) : 0;
+  };
+  // inclusive sums over the workgroup, their totals in s.total
+  auto sum = [&](int64_t& u, int64_t& v) {
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int64_t x = __shfl_up(u, o), y = __shfl_up(v, o);
+      if (lane >= o) {
+        u += x;
+        v += y;
+      }
+    }
+    __syncthreads();
+    if (lane == 63) {
+      s.part[0][wave] = u;
+      s.part[1][wave] = v;
+    }
+    __syncthreads();
+    for (int w = 0; w < wave; ++w) {
+      u += s.part[0][w];
+      v += s.part[1][w];
+    }
+    if (tid == RO_NT - 1) {
+      s.total[0] = u;
+      s.total[1] = v;
+    }
+    __syncthreads();
+  };
+  int units0, tiles0;  // of the first sequences, a thread each
+  look(c.batch == 1 ? 0 : tid, units0, tiles0);
+  int64_t n_units = units0, work = (int64_t)units0 * tiles0;
+  if (c.batch > 1) {
+    for (int b = tid + RO_NT; b < c.batch; b += RO_NT) {
+      int u, t;
+      look(b, u, t);
+      n_units += u;
+      work += (int64_t)u * t;
+    }
+    sum(n_units, work);
+    n_units = s.total[0];
+    work = s.total[1];
+  }
+  RowsPlace r;
+  r.b = -1;
+  r.unit = r.chunk = r.n_chunks = 0;
+  // every unit ends in half a chunk on average: those count too
+  const int64_t whole = p.want - (n_units < p.want ? n_units : p.want) / 2;
+  int64_t each = (work + whole - 1) / whole;
+  each = (each + RO_NW - 1) / RO_NW * RO_NW;
+  constexpr int64_t most = (int64_t)1 << 24;  // tiles of the longest row
+  r.tiles = (int)(each < RO_NW ? RO_NW : each < most ? each : most);
+  auto chunks = [&](int tiles) { return (tiles + r.tiles - 1) / r.tiles; };
+  if (c.batch == 1) {
+    r.n_chunks = chunks(tiles0);
+    if (r.n_chunks == 0 || item >= units0 * r.n_chunks) return r;
+    r.b = 0;
+    r.unit = item / r.n_chunks;
+    r.chunk = item - r.unit * r.n_chunks;
+    return r;
+  }
+  if (tid == 0) s.b = -1;
+  int64_t base = 0;
+  for (int b0 = 0; b0 < c.batch; b0 += RO_NT) {
+    int u = units0, t = tiles0;
+    if (b0 > 0) look(b0 + tid, u, t);
+    const int n = chunks(t);
+    int64_t v = (int64_t)u * n, none = 0;
+    const int64_t mine = v;
+    sum(v, none);
+    const int64_t lo = base + v - mine;
+    if (item >= lo && item < lo + mine) {
+      s.b = b0 + tid;
+      s.at = (int)(item - lo);
+      s.n = n;
+    }
+    __syncthreads();
+    if (s.b >= 0) break;
+    base += s.total[0];
+    __syncthreads();
+  }
+  r.b = __builtin_amdgcn_readfirstlane(s.b);
+  if (r.b < 0) return r;
+  r.n_chunks = __builtin_amdgcn_readfirstlane(s.n);
+  r.unit = __builtin_amdgcn_readfirstlane(s.at) / r.n_chunks;
+  r.chunk = __builtin_amdgcn_readfirstlane(s.at) - r.unit * r.n_chunks;
+  return r;
+}
+
+// The place of a sequence's unit in the plan: units of two sequences never meet.
+__device__ __forceinline__ int64_t plan_at(const PagedRowsArgs& p, int rows, const PagedSeq& seq, int b, int unit) {
+  return seq.first * p.a.n_qh / rows + b + unit;
+}
+
+// The last sequence that holds new token t, -1: none. Every thread of NT.
+template <int NT>
+__device__ __forceinline__ int holder(const PagedCache& c, int64_t t, int32_t& b_s) {
+  if (threadIdx.x == 0) b_s = -1;
+  __syncthreads();
+  for (int b = threadIdx.x; b < c.batch; b += NT) {
+    const PagedSeq q = paged_seq(c, b);
+    if (t >= q.first && t < q.first + q.n) atomicMax(&b_s, b);
+  }
+  __syncthreads();
+  return __builtin_amdgcn_readfirstlane(b_s);
+}
+
+// Of lane i < n: the drafted tokens that token i sees, its ancestors and itself, as bits. Halving by
+// doubled steps: after k of them a lane holds its 2^k nearest.
+__device__ __forceinline__ uint64_t ancestors(const int32_t* __restrict__ parents, int64_t first, int n, int lane) {
+  int up = lane < n ? parents[first + lane] : -1;
+  if (up < 0 || up >= lane) up = -1;
+  uint64_t seen = (uint64_t)1 << lane;
+#pragma unroll
+  for (int k = 0; k < 6; ++k) {
+    const int src = up < 0 ? lane : up;
+    const uint64_t more = __shfl(seen, src);
+    const int next = __shfl(up, src);
+    if (up >= 0) {
+      seen |= more;
+      up = next;
+    }
+  }
+  return seen;
+}
+
+// The chunk's entries of a list [from, to) that name blocks the token sees (below `blocks`) and are
+// greater than all entries before them, packed into sel; returns how many.
+struct ListScratch {
+  int32_t top[RO_NW], count[RO_NW];
+};
+__device__ __forceinline__ int read_list(const int32_t* __restrict__ list, int from, int to, int blocks, int32_t* sel, ListScratch& s) {
+  const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
+  int before = -1, n = 0;
+  for (int e0 = 0; e0 < to; e0 += RO_NT) {
+    const int e = e0 + tid, x = e < to ? list[e] : -1;
+    int top = x;
+#pragma unroll
+    for (int o = 1; o < 64; o <<= 1) {
+      const int u = __shfl_up(top, o);
+      if (lane >= o && u > top) top = u;
+    }
+    int prev = __shfl_up(top, 1);
+    if (lane == 0) prev = -1;
+    __syncthreads();
+    if (lane == 63) s.top[wave] = top;
+    __syncthreads();
+    int all = before;
+    for (int w = 0; w < RO_NW; ++w) {
+      if (w < wave && s.top[w] > prev) prev = s.top[w];
+      if (s.top[w] > all) all = s.top[w];
+    }
+    if (before > prev) prev = before;
+    const bool take = e >= from && e < to && x > prev && x < blocks;
+    const uint64_t m = __ballot(take);
+    if (lane == 0) s.count[wave] = __popcll(m);
+    __syncthreads();
+    int at = n, total = n;
+    for (int w = 0; w < RO_NW; ++w) {
+      if (w < wave) at += s.count[w];
+      total += s.count[w];
+    }
+    if (take) sel[at + __popcll(m & (((uint64_t)1 << lane) - 1))] = x;
+    n = total;
+    before = all;
+  }
+  __syncthreads();
+  return n;
+}
+
+constexpr int LIST_CHUNK = 256;  // entries of a workgroup at most
+
+// ---------------------------------------------------------------------------
+// The sums of a unit over a chunk
+// ---------------------------------------------------------------------------
+template <int NB, bool PRECISE, bool TREE>
+__global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows_kernel(PagedRowsArgs p) {
+  constexpr int ROWS = 16 * NB, NP = PRECISE ? 2 : 1, QP = PRECISE ? 3 : 2;
+  __shared__ RowsScratch place_s;
+  __shared__ ListScratch list_s;
+  __shared__ int32_t sel_s[TREE ? 1 : LIST_CHUNK], b_s;
+  __shared__ uint64_t anc_s[TREE ? DRAFT : 1];
+  __shared__ float m_s[RO_NW][16], l_s[RO_NW][16], un_s[NG][ROWS];
+  __shared__ int32_t unit_s[2 * NG];
+  __shared__ __attribute__((aligned(16))) float sums_s[RO_NW * 16 * RO_PITCH];  // the tiles while wavefronts walk
+  __shared__ __attribute__((aligned(16))) uint8_t q_s[NG][NB][NP][64 * 16];      // q' as column operands, by lane
+  static_assert(sizeof(sums_s) >= RO_NW * NP * CA_TILE, "the tiles lie where the sums do");
+  const PagedAttnArgs& a = p.a;
+  const int kv = (int)(blockIdx.x % (unsigned)a.c.n_kv);
+  const int64_t item = blockIdx.x / (unsigned)a.c.n_kv;
+  const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quarter = lane >> 4;
+  const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  int b, row0, begin = 0, count;
+  PagedSeq seq;
+  int64_t tok0 = 0;  // lists: the token
+  if constexpr (TREE) {
+    const RowsPlace at = tree_place(p, ROWS, (int)item, place_s);
+    if (at.b < 0) return;
+    b = at.b;
+    seq = paged_seq(a.c, b);
+    row0 = at.unit * ROWS;
+    if (at.chunk == 0 && kv == 0 && tid == 0) {  // for the combine
+      const int64_t u = plan_at(p, ROWS, seq, b, at.unit);
+      p.plan[2 * u] = (int32_t)item;
+      p.plan[2 * u + 1] = at.n_chunks;
+    }
+    const int n_tiles = (int)((seq.len + TILE - 1) / TILE);
+    begin = at.chunk * at.tiles;
+    count = n_tiles - begin < at.tiles ? n_tiles - begin : at.tiles;
+  } else {
+    const int64_t t = item / p.n_chunks;
+    b = holder<RO_NT>(a.c, t, b_s);
+    if (b < 0) return;
+    seq = paged_seq(a.c, b);
+    tok0 = t - seq.first;
+    row0 = 0;
+    const int64_t see = seq.len - seq.n + tok0 + 1;
+    const int blocks = see > 0 ? (int)((see + TILE - 1) / TILE) : 0;
+    const int from = (int)(item % p.n_chunks) * p.chunk, to = from + p.chunk < p.n_blocks ? from + p.chunk : p.n_blocks;
+    count = read_list(p.blocks + (t * a.c.n_kv + kv) * p.n_blocks, from, to, blocks, sel_s, list_s);
+  }
+  const int n_rows = TREE ? (int)(seq.n * a.n_qh) - row0 : a.n_qh;  // of the unit, and those behind it
+  Kept Kk = read_kept(a.bits_k + kv * NG), Kv = read_kept(a.bits_v + kv * NG);
+  if (!Kk.ok || Kk.used > a.Wk) Kk.n = 0;  // width table inconsistent with the record
+  if (!Kv.ok || Kv.used > a.Wv) Kv.n = 0;
+  // the lane's row of block nb: token of the sequence, query head (rows past the last repeat the first)
+  auto row_of = [&](int nb, int& tok, int& head) __attribute__((always_inline)) {
+    const int r = row0 + (16 * nb + col < n_rows ? 16 * nb + col : 0);
+    tok = TREE ? r / a.n_qh : 0;
+    head = TREE ? r - tok * a.n_qh : r;
+    if (!TREE) tok = (int)tok0;
+  };
+  if constexpr (TREE) {
+    if (wave == 0) anc_s[lane] = ancestors(p.parents, seq.first, (int)seq.n, lane);
+  }
+
+  // q': element e of quarter p is that of code 4 p + e / 2 + 16 (e % 2), as the tiles' places are;
+  // product x has e = 4 x .. 4 x + 3. PRECISE: a row's group is scaled by 2^E into [2^8, 2^9).
+  for (int pair = wave; pair < Kk.n * NB; pair += RO_NW) {
+    const int sl = pair / NB, nb = pair - sl * NB;
+    int tok, head;
+    row_of(nb, tok, head);
+    const int64_t qoff = (seq.first + tok) * a.q_token_stride + (kv * a.n_qh + head) * a.q_head_stride + 8 * quarter;
+    const float* V = a.basis_k + (int64_t)kv * D * D + (8 * quarter) * D + G * pick4(Kk.grp, sl) + 4 * (col >> 2) +
+                     ((col & 3) >> 1) + 16 * (col & 1);
+    f32x4 acc[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+    for (int k = 0; k < 4; ++k) {
+      float v[2][8];
+#pragma unroll
+      for (int e = 0; e < 8; ++e) {
+        v[0][e] = V[(32 * k + e) * D];
+        v[1][e] = V[(32 * k + e) * D + 2];
+      }
+      bf16x8 qq[QP];
+      if (a.q_f32) {
+        const f32x4* qp = reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.q) + qoff + 32 * k);
+        const f32x4 q0 = qp[0], q1 = qp[1];
+        const float qv[8] = {q0[0], q0[1], q0[2], q0[3], q1[0], q1[1], q1[2], q1[3]};
+        split8<QP>(qv, qq);
+      } else {
+        qq[0] = as_bf16x8(*reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.q) + qoff + 32 * k));
+      }
+#pragma unroll
+      for (int x = 0; x < 2; ++x) {
+        bf16x8 vp[QP];
+        split8<QP>(v[x], vp);
+#pragma unroll
+        for (int i = 0; i < QP; ++i) acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vp[i], qq[0], acc[x], 0, 0, 0);
+        if (a.q_f32) {
+#pragma unroll
+          for (int i = 0; i < QP; ++i)
+#pragma unroll
+            for (int j = 1; i + j < QP; ++j) acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vp[i], qq[j], acc[x], 0, 0, 0);
+        }
+      }
+    }
+    float y[8], most = 0.0f, up = 1.0f;
+#pragma unroll
+    for (int e = 0; e < 8; ++e) {
+      y[e] = acc[e >> 2][e & 3] * a.scale_log2;
+      most = __builtin_fmaxf(most, __builtin_fabsf(y[e]));
+    }
+    if constexpr (PRECISE) {
+      most = __builtin_fmaxf(most, __shfl_xor(most, 16));
+      most = __builtin_fmaxf(most, other_half(most));
+      up = __builtin_ldexpf(1.0f, 9 - scale_exponent(most));
+      if (quarter == 0) un_s[sl][16 * nb + col] = 1.0f / up;
+    }
+    u32x4 rh, rl;
+#pragma unroll
+    for (int j = 0; j < 4; ++j) {
+      f32x2 x = f32x2{y[2 * j] * up, y[2 * j + 1] * up};
+      if constexpr (!PRECISE) {  // NaN stays
+#pragma unroll
+        for (int e = 0; e < 2; ++e) x[e] = x[e] > 65504.0f ? 65504.0f : x[e] < -65504.0f ? -65504.0f : x[e];
+      }
+      const f16x2 hi = __builtin_convertvector(x, f16x2);
+      rh[j] = __builtin_bit_cast(uint32_t, hi);
+      rl[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{(x[0] - (float)hi[0]) * CA_LO, (x[1] - (float)hi[1]) * CA_LO}, f16x2));
+    }
+    *reinterpret_cast<u32x4*>(q_s[sl][nb][0] + 16 * lane) = rh;
+    if constexpr (PRECISE) *reinterpret_cast<u32x4*>(q_s[sl][nb][1] + 16 * lane) = rl;
+  }
+  const int tpp = a.c.page_tokens >> 6, n_keys = Kk.n, n_units = Kk.n + Kv.n;
+  if (tid < 2 * NG) {  // a kept group of the keys, then of the values
+    const int s = tid < n_keys ? tid : tid - n_keys;
+    int bb = 0, pay = 0;
+#pragma unroll
+    for (int x = 0; x < NG; ++x) {
+      bb = x == s ? (tid < n_keys ? Kk.bits[x] : Kv.bits[x]) : bb;
+      pay = x == s ? (tid < n_keys ? Kk.pay[x] : Kv.pay[x]) : pay;
+    }
+    unit_s[tid] = bb | (s & 3) << 4 | pay << 6;
+  }
+  __syncthreads();  // q', groups, ancestors
+  uint8_t* tile = reinterpret_cast<uint8_t*>(sums_s) + wave * NP * CA_TILE;
+  uint32_t magic = 0x64006400u;  // exponent of 1024 in both halves, in a VGPR
+  asm volatile("" : "+v"(magic));
+  auto tile_of = [&](int x) __attribute__((always_inline)) { return TREE ? begin + x : __builtin_amdgcn_readfirstlane(sel_s[x]); };
+  // the tile whose words are loaded: its page, its own place in it, its records
+  int load_x = wave, in_page = 0, page = -1;
+  const uint32_t *kp = a.pool_k, *vp = a.pool_v;
+  bool page_ok = false;
+  uint32_t words[8], meta = 0u;
+  auto look_up = [&]() __attribute__((always_inline)) {
+    page = -1;
+    if (load_x < count) {
+      const int t = tile_of(load_x), idx = t / tpp;
+      in_page = t - idx * tpp;
+      page = __builtin_amdgcn_readfirstlane(a.c.table[(int64_t)seq.row * a.c.row_pages + idx]);
+    }
+  };
+  auto enter = [&]() __attribute__((always_inline)) {  // the tile looked up; the walk goes on
+    page_ok = page >= 0 && page < a.c.n_pages;
+    const int64_t rec = ((int64_t)(page_ok ? page : 0) * a.c.n_kv + kv) * tpp + in_page;
+    kp = a.pool_k + rec * (TILE * a.Wk) + lane;
+    vp = a.pool_v + rec * (TILE * a.Wv) + lane;
+    load_x += RO_NW;
+    look_up();
+  };
+  // operands in the tile (the swizzle of piece_at repeats every 16 slots)
+  const uint8_t* key_at = tile + piece_at(col, quarter);
+  const uint8_t* val_at0 = tile + piece_at(4 * quarter + (col >> 2), (lane & 3) >> 1) + 8 * (lane & 1);
+  const uint8_t* val_at1 = tile + piece_at(4 * quarter + (col >> 2), 2 + ((lane & 3) >> 1)) + 8 * (lane & 1);
+  int bits = 0;  // of the group whose words are loaded
+  auto fetch = [&](int u) __attribute__((always_inline)) {
+    const int d = __builtin_amdgcn_readfirstlane(unit_s[u]);
+    const uint32_t* rec = u < n_keys ? kp : vp;
+    bits = d & 15;
+    meta = 0u;
+    if (!page_ok) return;
+    meta = rec[((d >> 4) & 3) * TILE];
+    rec += (d >> 6) * TILE;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < bits) words[i] = rec[i * TILE];
+  };
+  // group u's coefficients into the tile (its last readers are done: LDS serves a wavefront in
+  // order), and the next group's words
+  auto expand = [&](int u) __attribute__((always_inline)) {
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    const uint32_t m = finite_meta(meta, bits);
+    with_bits(bits, [&](auto bc) __attribute__((always_inline)) {
+      write_coefficients<decltype(bc)::value, PRECISE>(words, m, tile, lane, CA_TILE, magic);
+    });
+    if (u + 1 == n_units) enter();
+    fetch(u + 1 == n_units ? 0 : u + 1);
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  };
+  look_up();
+  if (n_units > 0) {
+    enter();
+    fetch(0);
+  }
+  const int64_t past = seq.len - seq.n;  // slots of the history
+  const int64_t common = TREE ? past : past + tok0 + 1;  // slots that every row sees
+  f32x4 acc[NG][2][NB];
+  float ref[NB], l[NB];  // the reference less CA_LIFT (-inf: nothing seen yet)
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    ref[nb] = -__builtin_inff();
+    l[nb] = 0.0f;
+#pragma unroll
+    for (int sl = 0; sl < NG; ++sl) acc[sl][0][nb] = acc[sl][1][nb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+  }
+#pragma unroll 1
+  for (int x = wave; x < count; x += RO_NW) {
+    const int64_t t0 = (int64_t)tile_of(x) * TILE;
+    f32x4 S[NB][4];  // slot 16 s + 4 quarter + i
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+      for (int s = 0; s < 4; ++s) S[nb][s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+    for (int u = 0; u < n_keys; ++u) {
+      expand(u);
+      f16x8 qo[NB][NP];
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+        for (int y = 0; y < NP; ++y) qo[nb][y] = as_f16x8(*reinterpret_cast<const u32x4*>(q_s[u][nb][y] + 16 * lane));
+#pragma unroll
+      for (int s = 0; s < 4; ++s) {
+        const f16x8 kh = as_f16x8(*reinterpret_cast<const u32x4*>(key_at + 16 * 64 * s));
+        if constexpr (!PRECISE) {
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) S[nb][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qo[nb][0], S[nb][s], 0, 0, 0);
+        } else {
+          const f16x8 kl = as_f16x8(*reinterpret_cast<const u32x4*>(key_at + CA_TILE + 16 * 64 * s));
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            const f32x4 z = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+            const f32x4 hi = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qo[nb][0], z, 0, 0, 0);
+            f32x4 lo = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qo[nb][1], z, 0, 0, 0);
+            lo = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl, qo[nb][0], lo, 0, 0, 0);
+            const float un = un_s[u][16 * nb + col];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) S[nb][s][i] = __builtin_fmaf(__builtin_fmaf(lo[i], 1.0f / CA_LO, hi[i]), un, S[nb][s][i]);
+          }
+        }
+      }
+    }
+    if (t0 + TILE > common) {  // some row does not see the whole tile
+      const int64_t rel = t0 - common;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        uint64_t own = 0u;  // of the slots at and behind `common`
+        if constexpr (TREE) {
+          int tok, head;
+          row_of(nb, tok, head);
+          own = anc_s[tok];
+        }
+        uint64_t see = rel >= 64 ? 0u : rel >= 0 ? own >> rel : (own << -rel) | (((uint64_t)1 << -rel) - 1);
+        see >>= 4 * quarter;
+        const uint32_t half[2] = {(uint32_t)see, (uint32_t)(see >> 32)};
+#pragma unroll
+        for (int s = 0; s < 4; ++s)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) S[nb][s][i] = half[s >> 1] & (1u << (16 * (s & 1) + i)) ? S[nb][s][i] : -__builtin_inff();
+      }
+    }
+    float top[NB];
+    bool moves = false;
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      top[nb] = S[nb][0][0];
+#pragma unroll
+      for (int i = 1; i < 16; ++i) top[nb] = __builtin_fmaxf(top[nb], S[nb][i >> 2][i & 3]);
+      top[nb] -= CA_LIFT + CA_SLACK;
+      moves = moves || top[nb] > ref[nb];
+    }
+    if (__any(moves)) {
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        top[nb] = __builtin_fmaxf(top[nb], __shfl_xor(top[nb], 16));
+        top[nb] = __builtin_fmaxf(top[nb], other_half(top[nb]));
+        const float next = top[nb] > ref[nb] ? top[nb] + CA_SLACK : ref[nb];
+        const float f = ref[nb] == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(ref[nb] - next);  // 1: the sums are zeros (or NaN)
+        ref[nb] = next;
+        l[nb] *= f;
+#pragma unroll
+        for (int sl = 0; sl < NG; ++sl)
+#pragma unroll
+          for (int i = 0; i < 8; ++i) acc[sl][i >> 2][nb][i & 3] *= f;
+      }
+    }
+    f16x8 w[NB][2][NP];  // weights of 32 slots: element e is slot 16 (e / 4) + 4 quarter + e % 4
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      const float base = ref[nb] == -__builtin_inff() ? 0.0f : ref[nb];
+#pragma unroll
+      for (int hf = 0; hf < 2; ++hf) {
+        u32x4 xh, xl;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+          const f32x4 s = S[nb][2 * hf + (j >> 1)];
+          const f32x2 e = f32x2{__builtin_amdgcn_exp2f(s[2 * (j & 1)] - base), __builtin_amdgcn_exp2f(s[2 * (j & 1) + 1] - base)};
+          const f16x2 r = __builtin_convertvector(e, f16x2);
+          xh[j] = __builtin_bit_cast(uint32_t, r);
+          if constexpr (PRECISE) {
+            l[nb] += e[0] + e[1];
+            xl[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{(e[0] - (float)r[0]) * CA_LO, (e[1] - (float)r[1]) * CA_LO}, f16x2));
+          } else {
+            l[nb] = __builtin_amdgcn_fdot2(__builtin_bit_cast(h16x2, r), h16x2{(__fp16)1.0f, (__fp16)1.0f}, l[nb], false);
+          }
+        }
+        w[nb][hf][0] = as_f16x8(xh);
+        if constexpr (PRECISE) w[nb][hf][1] = as_f16x8(xl);
+      }
+    }
+#pragma unroll
+    for (int sl = 0; sl < NG; ++sl) {
+      if (sl < n_units - n_keys) {
+        expand(n_keys + sl);
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          f32x4 lo[NB];
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) lo[nb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+          for (int hf = 0; hf < 2; ++hf) {
+            const uint8_t* pt = (y ? val_at1 : val_at0) + 32 * 64 * hf;
+            const u32x2 y0 = read_transposed(pt), y1 = read_transposed(pt + 16 * 64);
+            const f16x8 vh = as_f16x8(u32x4{y0[0], y0[1], y1[0], y1[1]});
+            f16x8 vl = vh;
+            if constexpr (PRECISE) {
+              const u32x2 z0 = read_transposed(pt + CA_TILE), z1 = read_transposed(pt + CA_TILE + 16 * 64);
+              vl = as_f16x8(u32x4{z0[0], z0[1], z1[0], z1[1]});
+            }
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) {
+              acc[sl][y][nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, w[nb][hf][0], acc[sl][y][nb], 0, 0, 0);
+              if constexpr (PRECISE) {
+                lo[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vl, w[nb][hf][0], lo[nb], 0, 0, 0);
+                lo[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, w[nb][hf][NP - 1], lo[nb], 0, 0, 0);
+              }
+            }
+          }
+          if constexpr (PRECISE) {
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+              for (int i = 0; i < 4; ++i) acc[sl][y][nb][i] = __builtin_fmaf(lo[nb][i], 1.0f / CA_LO, acc[sl][y][nb][i]);
+          }
+        }
+      }
+    }
+  }
+  // merge of the wavefronts, and the chunk's partial of every row, 16 rows at a time
+  float* part = p.partial + (item * a.c.n_kv + kv) * (int64_t)((TREE ? ROWS : a.n_qh) * PART);
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    if (16 * nb >= n_rows) break;
+    float ll = l[nb] + __shfl_xor(l[nb], 16);
+    ll += other_half(ll);
+    __syncthreads();  // the tiles, or the sums before, have been read
+    if (quarter == 0) {
+      m_s[wave][col] = ll == 0.0f ? -__builtin_inff() : ref[nb] == -__builtin_inff() ? 0.0f : ref[nb];
+      l_s[wave][col] = ll;
+    }
+#pragma unroll
+    for (int sl = 0; sl < NG; ++sl)
+      if (sl < Kv.n)
+#pragma unroll
+        for (int y = 0; y < 2; ++y)
+          *reinterpret_cast<f32x4*>(sums_s + (wave * 16 + col) * RO_PITCH + G * sl + 16 * y + 4 * quarter) = acc[sl][y][nb];
+    __syncthreads();
+    const int here = n_rows - 16 * nb < 16 ? n_rows - 16 * nb : 16;
+    for (int e = tid; e < here * D; e += RO_NT) {
+      const int r = e >> 7, j = e & 127, g = j >> 5, c = j & 31;
+      const int place = 8 * ((c & 15) >> 2) + 2 * (c & 3) + (c >> 4);
+      int sl = -1;
+#pragma unroll
+      for (int y = 0; y < NG; ++y) sl = (y < Kv.n && Kv.grp[y] == g) ? y : sl;
+      float m = -__builtin_inff(), sum = 0.0f, total = 0.0f;
+#pragma unroll
+      for (int v = 0; v < RO_NW; ++v) m = __builtin_fmaxf(m, m_s[v][r]);
+#pragma unroll
+      for (int v = 0; v < RO_NW; ++v) {
+        const float f = m_s[v][r] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m_s[v][r] - m);
+        if (sl >= 0) sum = __builtin_fmaf(f, sums_s[(v * 16 + r) * RO_PITCH + G * sl + place], sum);
+        total = __builtin_fmaf(f, l_s[v][r], total);
+      }
+      float* o = part + (16 * nb + r) * PART;
+      o[8 + j] = sum;
+      if (j == 0) {
+        o[0] = m;
+        o[1] = total;
+      }
+    }
+  }
+}
+
+// ---------------------------------------------------------------------------
+// Join of the chunks, the rotation back, and the outputs: a workgroup for CR neighbouring rows (new token x
+// query heads of a KV head, of all sequences) of one KV head. A thread group of 128 sums a row's
+// coefficients, 8 / CR of them share a row's chunks; then a channel is 8 threads' dot product.
+// ---------------------------------------------------------------------------
+template <int CR, bool TREE>
+__global__ __launch_bounds__(1024) void paged_rows_combine_kernel(PagedRowsArgs p, int rows) {
+  constexpr int SHARE = 8 / CR;
+  __shared__ int32_t b_s[CR + 1];
+  __shared__ float m_s[8], l_s[8], sums_s[8][D];
+  __shared__ __attribute__((aligned(16))) float chat_s[CR][D];
+  __shared__ float lse_s[16];
+  const PagedAttnArgs& a = p.a;
+  const int kv = (int)(blockIdx.x % (unsigned)a.c.n_kv);
+  const int64_t row0 = (int64_t)(blockIdx.x / (unsigned)a.c.n_kv) * CR, n_all = a.c.n_new * a.n_qh;
+  const int tid = threadIdx.x, j = tid & 127, group = tid >> 7, r = group % CR, share = group / CR;
+  const int ri = tid >> 3, rpart = tid & 7;
+  const f32x4* Vr = reinterpret_cast<const f32x4*>(a.basis_v + (int64_t)kv * D * D + (int64_t)ri * D + 16 * rpart);
+  const f32x4 v0 = Vr[0], v1 = Vr[1], v2 = Vr[2], v3 = Vr[3];
+  const float mv = a.mean_v[(int64_t)kv * D + j];
+  // the sequences of the rows' tokens
+  const int64_t t_lo = row0 / a.n_qh, t_hi = (row0 + CR - 1) / a.n_qh;
+  if (tid <= CR) b_s[tid] = -1;
+  __syncthreads();
+  for (int b = tid; b < a.c.batch; b += 1024) {
+    const PagedSeq q = paged_seq(a.c, b);
+    for (int64_t t = t_lo < q.first ? q.first : t_lo; t <= t_hi && t < q.first + q.n; ++t) atomicMax(&b_s[t - t_lo], b);
+  }
+  __syncthreads();
+  const int64_t row = row0 + r, tok = row / a.n_qh;
+  const int head = (int)(row - tok * a.n_qh);
+  const int b = row < n_all ? b_s[tok - t_lo] : -1;
+  PagedSeq seq{};
+  bool live = b >= 0;
+  int n = 0;
+  const float* first = p.partial;
+  const int64_t step = (int64_t)a.c.n_kv * rows * PART;
+  if (live) {
+    seq = paged_seq(a.c, b);
+    if constexpr (TREE) {
+      live = attended(a, seq);
+      const int64_t in_seq = (tok - seq.first) * a.n_qh + head, unit = in_seq / rows;
+      const int64_t u = plan_at(p, rows, seq, b, (int)unit);
+      if (live && seq.len > 0) {
+        const int item0 = p.plan[2 * u], most = p.plan[2 * u + 1];
+        // (within the workspace whatever the lists of sequences hold)
+        n = item0 < 0 || item0 >= p.items ? 0 : most < p.items - item0 ? most : p.items - item0;
+        first += ((int64_t)(n > 0 ? item0 : 0) * a.c.n_kv + kv) * (rows * PART) + (in_seq - unit * rows) * PART;
+      }
+    } else {
+      n = p.n_chunks;
+      first += (tok * n * a.c.n_kv + kv) * (int64_t)(rows * PART) + head * PART;
+    }
+  }
+  float M = -__builtin_inff(), L = 0.0f, A = 0.0f;
+  constexpr int CB = 4;
+  for (int c0 = share; c0 < n; c0 += CB * SHARE) {
+    float m[CB], l[CB], x[CB];
+#pragma unroll
+    for (int k = 0; k < CB; ++k) {
+      const int c = c0 + k * SHARE;
+      const float* pc = first + (c < n ? c : c0) * step;
+      m[k] = c < n ? pc[0] : -__builtin_inff();
+      l[k] = pc[1];
+      x[k] = pc[8 + j];
+    }
+    float mb = M;
+#pragma unroll
+    for (int k = 0; k < CB; ++k) mb = __builtin_fmaxf(mb, m[k]);
+    if (mb != -__builtin_inff()) {
+      const float f = M == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(M - mb);
+      L *= f;
+      A *= f;
+#pragma unroll
+      for (int k = 0; k < CB; ++k) {
+        const float w = m[k] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m[k] - mb);
+        L = __builtin_fmaf(w, l[k], L);
+        A = __builtin_fmaf(w, x[k], A);
+      }
+      M = mb;
+    }
+  }
+  if constexpr (SHARE > 1) {
+    if (j == 0) {
+      m_s[group] = M;
+      l_s[group] = L;
+    }
+    sums_s[group][j] = A;
+    __syncthreads();
+    if (share == 0) {
+      float mb = M;
+#pragma unroll
+      for (int k = 1; k < SHARE; ++k) mb = __builtin_fmaxf(mb, m_s[r + k * CR]);
+      L = A = 0.0f;
+#pragma unroll
+      for (int k = 0; k < SHARE; ++k) {
+        const float mk = m_s[r + k * CR], f = mk == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(mk - mb);
+        L = __builtin_fmaf(f, l_s[r + k * CR], L);
+        A = __builtin_fmaf(f, sums_s[r + k * CR][j], A);
+      }
+      M = mb;
+    }
+  }
+  const bool seen = L > 0.0f || L != L;
+  if (share == 0) chat_s[r][j] = seen ? A / L + mv : 0.0f;
+  if (a.lse != nullptr) {
+    float u = 0.0f;
+    if (live && share == 0) {
+      const int64_t qo = tok * a.q_token_stride + (kv * a.n_qh + head) * a.q_head_stride;
+      u = query_at(a, qo + j) * a.lse_u[kv * D + j];
+    }
+#pragma unroll
+    for (int o = 32; o > 0; o >>= 1) u += __shfl_xor(u, o);
+    if ((tid & 63) == 0) lse_s[tid >> 6] = u;
+    __syncthreads();
+    if (live && share == 0 && j == 0)
+      a.lse[tok * a.n_q_heads + kv * a.n_qh + head] =
+          seen ? __builtin_fmaf(__builtin_amdgcn_logf(L) + M, LN2, lse_s[2 * group] + lse_s[2 * group + 1]) : -__builtin_inff();
+  }
+  __syncthreads();
+  auto channel = [&](int x) {
+    const f32x4* c = reinterpret_cast<const f32x4*>(&chat_s[x][16 * rpart]);
+    float s = 0.0f;
+    const f32x4 c0 = c[0], c1 = c[1], c2 = c[2], c3 = c[3];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      s = __builtin_fmaf(v0[i], c0[i], s);
+      s = __builtin_fmaf(v1[i], c1[i], s);
+      s = __builtin_fmaf(v2[i], c2[i], s);
+      s = __builtin_fmaf(v3[i], c3[i], s);
+    }
+    s += __shfl_xor(s, 1);
+    s += __shfl_xor(s, 2);
+    s += __shfl_xor(s, 4);
+    return s;
+  };
+  float mine = 0.0f;
+#pragma unroll
+  for (int x = 0; x < CR; ++x) {
+    const float s = channel(x);
+    mine = rpart == x ? s : mine;
+  }
+  if (rpart < CR) {
+    const int64_t w = row0 + rpart, t = w / a.n_qh;
+    if (w >= n_all) return;
+    const int wb = b_s[t - t_lo];
+    if (wb < 0 || (TREE && !attended(a, paged_seq(a.c, wb)))) return;
+    const int64_t o = (t * a.n_q_heads + kv * a.n_qh + (w - t * a.n_qh)) * D + ri;
+    if (a.out_f32)
+      reinterpret_cast<float*>(a.out)[o] = mine;
+    else
+      reinterpret_cast<__bf16*>(a.out)[o] = (__bf16)mine;
+  }
+}
+
+}  // namespace spectra_dev
+
+namespace spectra {
+using namespace spectra_dev;
+
+namespace {
+
+constexpr int64_t kPerCu = 4;  // workgroups wanted of a CU at most
+
+int64_t tree_units(int32_t batch, int64_t n_new, int32_t n_qh, int rows) { return n_new * n_qh / rows + batch; }
+int64_t wanted(int32_t n_kv) { return N_CU * kPerCu / n_kv > 0 ? N_CU * kPerCu / n_kv : 1; }
+
+template <bool TREE>
+hipError_t launch_combine(const PagedRowsArgs& p, int rows, hipStream_t st) {
+  const int64_t all = p.a.c.n_new * p.a.n_qh;
+  if (all * p.a.c.n_kv <= 2 * N_CU)  // a CU holds two of these workgroups
+    hipLaunchKernelGGL((paged_rows_combine_kernel<1, TREE>), dim3((unsigned)(all * p.a.c.n_kv)), dim3(1024), 0, st, p, rows);
+  else
+    hipLaunchKernelGGL((paged_rows_combine_kernel<8, TREE>), dim3((unsigned)(ceil_div(all, 8) * p.a.c.n_kv)), dim3(1024), 0, st, p, rows);
+  return hipGetLastError();
+}
+
+}  // namespace
+
+// The plan and the partials of any unit size.
+size_t paged_tree_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv) {
+  const int64_t n_qh = n_q_heads / n_kv;
+  const size_t lse = paged_round((size_t)n_kv * D * sizeof(float));
+  const size_t plan = paged_round((size_t)tree_units(batch, n_new, (int32_t)n_qh, 16) * 2 * sizeof(int32_t));
+  return lse + plan + (size_t)((wanted(n_kv) + batch) * 64 + n_new * n_qh) * n_kv * PART * sizeof(float);
+}
+
+hipError_t launch_paged_tree(const PagedRowsArgs& args, void* workspace, hipStream_t st) {
+  PagedRowsArgs p = args;
+  const int32_t n_kv = p.a.c.n_kv, batch = p.a.c.batch;
+  char* ws = static_cast<char*>(workspace);
+  p.a.lse_u = reinterpret_cast<float*>(ws);
+  ws += paged_round((size_t)n_kv * D * sizeof(float));
+  p.plan = reinterpret_cast<int32_t*>(ws);
+  ws += paged_round((size_t)tree_units(batch, p.a.c.n_new, p.a.n_qh, 16) * 2 * sizeof(int32_t));
+  p.partial = reinterpret_cast<float*>(ws);
+  if (p.a.lse != nullptr) launch_paged_lse(p.a, st);
+  const int64_t most = (int64_t)p.a.max_new * p.a.n_qh;
+  const int nb = most <= 16 ? 1 : most <= 32 || p.a.out_f32 ? 2 : 4;
+  p.want = (int32_t)(nb == 1 ? wanted(n_kv) : (wanted(n_kv) + 1) / 2);
+  p.items = (int32_t)(p.want + tree_units(batch, p.a.c.n_new, p.a.n_qh, 16 * nb));
+  const dim3 grid((unsigned)((int64_t)p.items * n_kv));
+  if (p.a.out_f32) {
+    if (nb == 1)
+      hipLaunchKernelGGL((paged_rows_kernel<1, true, true>), grid, dim3(RO_NT), 0, st, p);
+    else
+      hipLaunchKernelGGL((paged_rows_kernel<2, true, true>), grid, dim3(RO_NT), 0, st, p);
+  } else {
+    if (nb == 1)
+      hipLaunchKernelGGL((paged_rows_kernel<1, false, true>), grid, dim3(RO_NT), 0, st, p);
+    else if (nb == 2)
+      hipLaunchKernelGGL((paged_rows_kernel<2, false, true>), grid, dim3(RO_NT), 0, st, p);
+    else
+      hipLaunchKernelGGL((paged_rows_kernel<4, false, true>), grid, dim3(RO_NT), 0, st, p);
+  }
+  return launch_combine<true>(p, 16 * nb, st);
+}
+
+// Workgroups of a list: about as many in all as the card holds, of four entries at least.
+static int64_t list_chunk(int64_t n_new, int32_t n_kv, int32_t n_blocks) {
+  int64_t n = N_CU * kPerCu / (n_new * n_kv);
+  if (n < 1) n = 1;
+  int64_t each = ceil_div(ceil_div(n_blocks, n), RO_NW) * RO_NW;
+  return each < LIST_CHUNK ? each : LIST_CHUNK;
+}
+
+size_t paged_sparse_bytes(int64_t n_new, int32_t n_q_heads, int32_t n_kv, int32_t n_blocks) {
+  // chunks of all lists: what the card holds and one more of every list, or whole chunks of 256
+  const int64_t most = N_CU * kPerCu + n_new * n_kv * (1 + ceil_div(n_blocks, LIST_CHUNK));
+  return paged_round((size_t)n_kv * D * sizeof(float)) + (size_t)most * (n_q_heads / n_kv) * PART * sizeof(float);
+}
+
+hipError_t launch_paged_sparse(const PagedRowsArgs& args, void* workspace, hipStream_t st) {
+  PagedRowsArgs p = args;
+  const int32_t n_kv = p.a.c.n_kv;
+  char* ws = static_cast<char*>(workspace);
+  p.a.lse_u = reinterpret_cast<float*>(ws);
+  p.partial = reinterpret_cast<float*>(ws + paged_round((size_t)n_kv * D * sizeof(float)));
+  if (p.a.lse != nullptr) launch_paged_lse(p.a, st);
+  p.chunk = (int32_t)list_chunk(p.a.c.n_new, n_kv, p.n_blocks);
+  p.n_chunks = (int32_t)ceil_div(p.n_blocks, p.chunk);
+  const dim3 grid((unsigned)(p.a.c.n_new * n_kv * p.n_chunks));
+  if (p.a.out_f32)
+    hipLaunchKernelGGL((paged_rows_kernel<1, true, false>), grid, dim3(RO_NT), 0, st, p);
+  else
+    hipLaunchKernelGGL((paged_rows_kernel<1, false, false>), grid, dim3(RO_NT), 0, st, p);
+  return launch_combine<false>(p, p.a.n_qh, st);
+}
+
+}  // namespace spectra

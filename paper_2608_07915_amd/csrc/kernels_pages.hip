@@ -227,6 +227,89 @@ __global__ __launch_bounds__(256) void pages_truncate_kernel(PageMap m, const in
 }
 
 // ---------------------------------------------------------------------------
+// Keeping one path of drafted slots. Every workgroup judges its entry for itself, from the map as it was
+// before the call: the records are moved by one launch, the map is changed by the next.
+// ---------------------------------------------------------------------------
+struct Accept {
+  int64_t first;  // the first drafted slot
+  int drafted, keep;
+  int row;        // -1: refused
+  int from;       // of the lane: the path's entry, or -1
+};
+// Of entry i; the same in every thread of the workgroup but for `from`, which each lane of every wavefront has.
+template <int NT>
+__device__ __forceinline__ Accept accept_entry(const PageMap& m, const PathList& p, int i) {
+  const int t = threadIdx.x, lane = t & 63;
+  Accept a;
+  a.row = p.rows[i];
+  a.drafted = p.drafted[i];
+  a.keep = p.counts[i];
+  const int64_t len = row_len(m, a.row);
+  bool bad = len < 0 || a.drafted < 0 || a.drafted > len || a.drafted > 64 || a.keep < 0 || a.keep > a.drafted || a.keep > p.stride;
+  a.first = len - a.drafted;
+  a.from = !bad && lane < a.keep ? p.path[(int64_t)i * p.stride + lane] : -1;
+  const int prev = __shfl_up(a.from, 1);
+  if (!bad && lane < a.keep) bad = a.from < 0 || a.from >= a.drafted || (lane > 0 && a.from <= prev);
+  // the drafted slots' pages: theirs alone. At most 64 slots and 64 to a page: two pages
+  if (len >= 0 && a.drafted > 0 && a.drafted <= len && lane < 2) {
+    const int64_t k = (lane == 0 ? a.first : len - 1) / m.page_tokens;
+    const int page = m.table[(int64_t)a.row * m.row_pages + k];
+    bad = bad || page < 0 || page >= m.n_pages || m.refs[page] != 1;
+  }
+  for (int j = t; j < i; j += NT) bad = bad || p.rows[j] == a.row;  // a row listed again is refused
+  if (__syncthreads_or(bad)) a.row = -1;
+  return a;
+}
+
+// Workgroup = (entry; pool; a share of its word columns). A wavefront reads a column of all kept slots
+// before it writes any, and no other touches that column. Bound by latency: two dependent table
+// reads, one of records.
+__global__ __launch_bounds__(256) void pages_accept_move_kernel(PageMap m, PathList p, PoolList pools, int32_t n_kv) {
+  const Accept a = accept_entry<256>(m, p, blockIdx.x);
+  if (a.row < 0 || a.keep == 0) return;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tpp = m.page_tokens >> 6;
+  const int cols = (int)(pools.words[blockIdx.y] / m.page_tokens), W = cols / n_kv;  // of all KV heads
+  const bool live = lane < a.keep;
+  const int64_t src = a.first + (live ? a.from : 0), dst = a.first + (live ? lane : 0);
+  const int32_t* tab = m.table + (int64_t)a.row * m.row_pages;
+  const int64_t ps = src / m.page_tokens, pd = dst / m.page_tokens;
+  const int ss = (int)(src - ps * m.page_tokens), sd = (int)(dst - pd * m.page_tokens);
+  uint32_t* base = pools.base[blockIdx.y];
+  const uint32_t* from = base + tab[ps] * pools.words[blockIdx.y] + (int64_t)(ss >> 6) * (64 * W) + (ss & 63);
+  uint32_t* to = base + tab[pd] * pools.words[blockIdx.y] + (int64_t)(sd >> 6) * (64 * W) + (sd & 63);
+  const int64_t head = (int64_t)tpp * 64 * W;  // words of a KV head's records in a page
+  for (int c = blockIdx.z * 4 + wave; c < cols; c += 4 * gridDim.z) {
+    const int kv = c / W;
+    const int64_t at = kv * head + (int64_t)(c - kv * W) * 64;
+    uint32_t v = 0u;
+    if (live) v = from[at];
+    asm volatile("" : "+v"(v));
+    if (live && a.from != lane) to[at] = v;
+  }
+}
+
+__global__ __launch_bounds__(256) void pages_accept_map_kernel(PageMap m, PathList p, int32_t* __restrict__ ends) {
+  const int i = blockIdx.x, t = threadIdx.x;
+  const Accept a = accept_entry<256>(m, p, i);
+  if (a.row < 0) {
+    if (t == 0) ends[i] = -1;
+    return;
+  }
+  int32_t* tab = m.table + (int64_t)a.row * m.row_pages;
+  const int64_t left = a.first + a.keep;
+  const int64_t k = ceil_pages(left, m.page_tokens) + t;
+  if (k < ceil_pages(a.first + a.drafted, m.page_tokens)) {
+    const int32_t page = tab[k];
+    tab[k] = -1;
+    if (page >= 0 && page < m.n_pages) atomicSub(&m.refs[page], 1);
+  }
+  if (t == 0) {
+    m.lens[a.row] = (int32_t)left;
+    ends[i] = (int32_t)left;
+  }
+}
+
+// ---------------------------------------------------------------------------
 // Compaction: with U used pages, the k-th used page at or past U moves to the k-th free page
 // before U. Sources and destinations are disjoint, so the copies need no order. The plan is
 // one workgroup's two passes over the counts (16 k pages a round).
@@ -330,6 +413,23 @@ hipError_t launch_pages_fork(const PageMap& m, const int32_t* parents, const int
 
 hipError_t launch_pages_truncate(const PageMap& m, const int32_t* rows, const int32_t* keep, int32_t n, hipStream_t st) {
   hipLaunchKernelGGL(pages_truncate_kernel, dim3(n), dim3(256), 0, st, m, rows, keep, n);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_accept_move(const PageMap& m, const PathList& p, int32_t n, const PoolList& pools, int32_t n_kv,
+                                    hipStream_t st) {
+  int64_t cols = 0;
+  for (int i = 0; i < pools.n; ++i) cols = pools.words[i] / m.page_tokens > cols ? pools.words[i] / m.page_tokens : cols;
+  // four word columns a wavefront, fewer workgroups where there are many entries and pools
+  int64_t z = (cols + 15) / 16;
+  const int64_t most = 4096 / ((int64_t)n * pools.n) + 1;
+  if (z > most) z = most;
+  hipLaunchKernelGGL(pages_accept_move_kernel, dim3(n, pools.n, (unsigned)z), dim3(256), 0, st, m, p, pools, n_kv);
+  return hipGetLastError();
+}
+
+hipError_t launch_pages_accept_map(const PageMap& m, const PathList& p, int32_t n, int32_t* ends, hipStream_t st) {
+  hipLaunchKernelGGL(pages_accept_map_kernel, dim3(n), dim3(256), 0, st, m, p, ends);
   return hipGetLastError();
 }
 

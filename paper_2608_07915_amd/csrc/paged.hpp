@@ -24,6 +24,15 @@ struct PoolList {
   int32_t n;
 };
 
+// The accepted paths of drafted slots, entry by entry (spectra_pages_accept).
+struct PathList {
+  const int32_t* rows;
+  const int32_t* drafted;
+  const int32_t* path;  // [n][stride]
+  const int32_t* counts;
+  int32_t stride;
+};
+
 // Workspace of the page-map calls: the number of pages to copy, then their sources and their
 // destinations (n_pages of each).
 struct PageMoves {
@@ -85,9 +94,60 @@ struct PagedAttnArgs {
   float* partial;
 };
 
+struct PagedBoundsArgs {
+  PagedCache c;
+  const uint32_t* pool_k;
+  const uint8_t* bits_k;
+  uint32_t* bounds;
+  int32_t Wk;
+  int32_t tokens;  // of a wavefront
+};
+
+struct PagedSelectArgs {
+  PagedCache c;
+  const uint32_t* bounds;
+  const float* basis_k;
+  const uint8_t* bits_k;
+  const void* q;
+  int64_t q_token_stride, q_head_stride;
+  int32_t q_f32;
+  int32_t n_q_heads, n_qh, Wk;
+  int64_t max_tokens;
+  int32_t n_blocks, first, last;
+  int32_t* blocks;
+  float* scores;        // workspace: [n_new][n_q_heads][most_blocks]
+  int32_t most_blocks;  // that a sequence of max_tokens has
+};
+
+// Attention of a few rows a sequence (drafted trees) or a token (listed blocks) over tiles.
+struct PagedRowsArgs {
+  PagedAttnArgs a;
+  const int32_t* parents;  // trees: [n_new]
+  const int32_t* blocks;   // lists: [n_new][n_kv][n_blocks]
+  int32_t n_blocks;
+  int32_t chunk, n_chunks;  // lists: entries of a workgroup, workgroups of a list
+  int32_t items;            // trees: workgroups per KV head (a bound), and how many are wanted
+  int32_t want;
+  int32_t* plan;            // trees: workspace, [units][2], a unit's first item and how many it has
+  float* partial;           // workspace: [items][n_kv][rows of a unit][PART]
+};
+
 }  // namespace spectra_dev
 
 namespace spectra {
+hipError_t launch_pages_accept_move(const spectra_dev::PageMap& m, const spectra_dev::PathList& p, int32_t n,
+                                    const spectra_dev::PoolList& pools, int32_t n_kv, hipStream_t st);
+hipError_t launch_pages_accept_map(const spectra_dev::PageMap& m, const spectra_dev::PathList& p, int32_t n, int32_t* ends,
+                                   hipStream_t st);
+hipError_t launch_paged_bounds(const spectra_dev::PagedBoundsArgs& a, hipStream_t st);
+size_t paged_select_bytes(int64_t n_new, int32_t n_q_heads, int32_t n_kv, int64_t max_tokens);
+hipError_t launch_paged_select(const spectra_dev::PagedSelectArgs& a, void* workspace, hipStream_t st);
+// The constants of the log-sum-exp (a.lse_u) of every KV head.
+void launch_paged_lse(const spectra_dev::PagedAttnArgs& a, hipStream_t st);
+size_t paged_tree_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv);
+size_t paged_sparse_bytes(int64_t n_new, int32_t n_q_heads, int32_t n_kv, int32_t n_blocks);
+hipError_t launch_paged_tree(const spectra_dev::PagedRowsArgs& p, void* workspace, hipStream_t st);
+hipError_t launch_paged_sparse(const spectra_dev::PagedRowsArgs& p, void* workspace, hipStream_t st);
 hipError_t launch_pages_extend(const spectra_dev::PageMap& m, const int32_t* rows, const int32_t* counts, int32_t n,
                                int32_t* ends, const spectra_dev::PageMoves& mv, hipStream_t st);
 hipError_t launch_pages_fork(const spectra_dev::PageMap& m, const int32_t* parents, const int32_t* children, int32_t n,

@@ -37,6 +37,13 @@ class PagedCache:
         words = int(_lib.get().spectra_paged_pool_words(self.ref, ctypes.byref(codec.struct)))
         return torch.zeros((self.n_pages, words // self.n_pages), dtype=torch.int32, device=self.table.device)
 
+    def empty_bounds(self, codec: Codec):
+        """A box pool for the keys' codec (``spectra_paged_bounds``): int32 [n_pages, words of a page],
+        zeros. As float16 it is [n_pages, KV head, tile, place of a kept group, least / largest, 32]."""
+        import torch
+        words = int(_lib.get().spectra_paged_bounds_words(self.ref, codec.n_streams))
+        return torch.zeros((self.n_pages, words // self.n_pages), dtype=torch.int32, device=self.table.device)
+
 
 class _Call:
     """The call's stream, with the cache's device current while the call is made."""
@@ -154,18 +161,23 @@ def spectra_pages_compact(cache: PagedCache, pools, moved=None, workspace=None, 
     return moved
 
 
+def _records(cache: PagedCache, codec: Codec, pool, name: str) -> None:
+    import torch
+    dev = cache.table.device
+    _need(codec.basis.device == dev, f"the codecs must be on {dev}")
+    _need(pool.device == dev and pool.dtype == torch.int32 and pool.is_contiguous(),
+          f"{name} must be a contiguous int32 tensor on {dev}")
+    need = int(_lib.get().spectra_paged_pool_words(cache.ref, ctypes.byref(codec.struct)))
+    _need(pool.numel() == need, f"{name} holds {pool.numel()} words, the map and codec need {need}")
+
+
 def _sequences(cache: PagedCache, ck: Codec, cv: Codec, pool_k, pool_v, cu_new, rows, ends):
     """Checks of what append and attention share -> (batch, pointers of the C call's head)."""
-    import torch
     dev = cache.table.device
     _need(cu_new.numel() >= 1, "cu_new must have batch + 1 elements")
     batch = cu_new.numel() - 1
-    for codec, pool, name in ((ck, pool_k, "pool_k"), (cv, pool_v, "pool_v")):
-        _need(codec.basis.device == dev, f"the codecs must be on {dev}")
-        _need(pool.device == dev and pool.dtype == torch.int32 and pool.is_contiguous(),
-              f"{name} must be a contiguous int32 tensor on {dev}")
-        need = int(_lib.get().spectra_paged_pool_words(cache.ref, ctypes.byref(codec.struct)))
-        _need(pool.numel() == need, f"{name} holds {pool.numel()} words, the map and codec need {need}")
+    _records(cache, ck, pool_k, "pool_k")
+    _records(cache, cv, pool_v, "pool_v")
     return batch, (cache.ref, ctypes.byref(ck.struct), ctypes.byref(cv.struct), pool_k.data_ptr(),
                    pool_v.data_ptr(), _ints(rows, "rows", dev, batch), _ints(ends, "ends", dev, batch),
                    _ints(cu_new, "cu_new", dev), batch)
@@ -224,4 +236,150 @@ def spectra_paged_attention(cache: PagedCache, ck: Codec, cv: Codec, pool_k, poo
                                                  q.stride(0), q.stride(1), n_q_heads, float(softmax_scale), out.data_ptr(),
                                                  _dtype_code(out), lse.data_ptr() if lse is not None else None,
                                                  ws.data_ptr(), _bytes(ws), s.handle))
+    return out
+
+
+def spectra_pages_accept(cache: PagedCache, rows, drafted, path, counts, pools, n_kv_heads: int, ends=None, stream=None):
+    """One path of each drafted tree stays: of the last drafted[i] slots of row rows[i] those at path[i, j], j <
+    counts[i] (ascending, from 0), move to the front of them in every pool, and the row ends behind them -> ends
+    (int32): the new lengths, -1 where refused. ``pools``: the record pools of n_kv_heads KV heads each; boxes
+    of the kept slots' blocks are made again by spectra_paged_bounds."""
+    import torch
+    dev = cache.table.device
+    n = rows.numel()
+    _need(path.device == dev and path.dtype == torch.int32 and path.dim() == 2 and path.is_contiguous() and path.shape[0] == n,
+          f"path must be a contiguous int32 tensor [{n}, most] on {dev}")
+    with _Call(dev, stream) as s:
+        made, n_pools = _pools(cache, pools)
+        ends = _made(stream, n, torch.int32, dev) if ends is None else ends
+        check(_lib.get().spectra_pages_accept(cache.ref, _ints(rows, "rows", dev), _ints(drafted, "drafted", dev, n),
+                                              path.data_ptr(), path.shape[1], _ints(counts, "counts", dev, n), n, made, n_pools,
+                                              int(n_kv_heads), _ints(ends, "ends", dev, n), s.handle))
+    return ends
+
+
+def _attended(cache: PagedCache, ck: Codec, q, lse):
+    """Queries and log-sum-exp of an attention call -> (tokens, query heads)."""
+    import torch
+    dev = cache.table.device
+    n, n_q_heads = q.shape[0], q.shape[1]
+    _rows(q, "q", dev, n_q_heads)
+    _need(n_q_heads % ck.n_streams == 0, f"n_q_heads={n_q_heads} is not a multiple of the codec's {ck.n_streams} KV heads")
+    _need(lse is None or (lse.device == dev and lse.dtype == torch.float32 and lse.is_contiguous()
+                          and tuple(lse.shape) == (n, n_q_heads)), f"lse must be a contiguous float32 tensor {(n, n_q_heads)}")
+    return n, n_q_heads
+
+
+def _output(out, q, stream):
+    shape = tuple(q.shape)
+    if out is None:
+        return _made(stream, shape, q.dtype, q.device)
+    _need(out.device == q.device and out.is_contiguous() and tuple(out.shape) == shape,
+          f"out must be a contiguous tensor {shape} on {q.device}")
+    return out
+
+
+def spectra_paged_tree_attention_workspace_bytes(batch: int, n_new: int, n_q_heads: int, n_kv_heads: int, max_new: int,
+                                                 max_tokens: int) -> int:
+    return int(_lib.get().spectra_paged_tree_attention_workspace_bytes(int(batch), int(n_new), int(n_q_heads),
+                                                                       int(n_kv_heads), int(max_new), int(max_tokens)))
+
+
+def spectra_paged_tree_attention(cache: PagedCache, ck: Codec, cv: Codec, pool_k, pool_v, q, cu_new, parents, max_new: int,
+                                 max_tokens: int, rows=None, ends=None, softmax_scale: float = 0.0, out=None, lse=None,
+                                 workspace=None, stream=None):
+    """Attention of drafted tokens: as spectra_paged_attention, but of its sequence's new tokens a token sees
+    itself and its ancestors only. ``parents`` (int32 [n]): the place of each token's parent among the new tokens
+    of its sequence, -1 where it continues the history. At most 64 new tokens of a sequence."""
+    dev = cache.table.device
+    batch, head = _sequences(cache, ck, cv, pool_k, pool_v, cu_new, rows, ends)
+    n, n_q_heads = _attended(cache, ck, q, lse)
+    up = _ints(parents, "parents", dev, n)
+    with _Call(dev, stream) as s:
+        out = _output(out, q, stream)
+        ws = _workspace(cache, workspace, spectra_paged_tree_attention_workspace_bytes(batch, n, n_q_heads, ck.n_streams, max_new,
+                                                                                       max_tokens), stream)
+        check(_lib.get().spectra_paged_tree_attention(*head[:-1], up, batch, n, int(max_new), int(max_tokens), q.data_ptr(),
+                                                      _dtype_code(q), q.stride(0), q.stride(1), n_q_heads,
+                                                      float(softmax_scale), out.data_ptr(), _dtype_code(out),
+                                                      lse.data_ptr() if lse is not None else None, ws.data_ptr(), _bytes(ws),
+                                                      s.handle))
+    return out
+
+
+def _keys(cache: PagedCache, ck: Codec, bounds, cu_new, rows, ends):
+    """Checks of the calls on boxes -> (batch, pointers of the sequences)."""
+    import torch
+    dev = cache.table.device
+    _need(cu_new.numel() >= 1, "cu_new must have batch + 1 elements")
+    batch = cu_new.numel() - 1
+    _need(ck.basis.device == dev, f"the codecs must be on {dev}")
+    need = int(_lib.get().spectra_paged_bounds_words(cache.ref, ck.n_streams))
+    _need(bounds.device == dev and bounds.dtype == torch.int32 and bounds.is_contiguous() and bounds.numel() == need,
+          f"bounds must be a contiguous int32 tensor of {need} elements on {dev}")
+    return batch, (_ints(rows, "rows", dev, batch), _ints(ends, "ends", dev, batch), _ints(cu_new, "cu_new", dev))
+
+
+def spectra_paged_bounds(cache: PagedCache, ck: Codec, pool_k, bounds, cu_new, n_new: int, rows=None, ends=None,
+                         stream=None) -> None:
+    """Boxes (least and largest key coefficients of 64 slots) of the blocks that hold the sequences' new tokens, from
+    their records in pool_k. Sequences as in spectra_paged_encode; n_new: tokens of cu_new."""
+    batch, seqs = _keys(cache, ck, bounds, cu_new, rows, ends)
+    _records(cache, ck, pool_k, "pool_k")
+    with _Call(cache.table.device, stream) as s:
+        check(_lib.get().spectra_paged_bounds(cache.ref, ctypes.byref(ck.struct), pool_k.data_ptr(), bounds.data_ptr(), *seqs,
+                                              batch, int(n_new), s.handle))
+
+
+def spectra_paged_select_workspace_bytes(n_new: int, n_q_heads: int, n_kv_heads: int, max_tokens: int) -> int:
+    return int(_lib.get().spectra_paged_select_workspace_bytes(int(n_new), int(n_q_heads), int(n_kv_heads), int(max_tokens)))
+
+
+def spectra_paged_select(cache: PagedCache, ck: Codec, bounds, q, cu_new, n_blocks: int, max_tokens: int, first: int = 1,
+                         last: int = 1, rows=None, ends=None, out=None, workspace=None, stream=None):
+    """The blocks that each new token q [n, n_q_heads, 128] attends over -> int32 [n, n_kv_heads, n_blocks], ascending, -1
+    behind the last: its first ``first`` and last ``last`` and those whose boxes bound the largest scores.
+    Sequences as in spectra_paged_encode, none with more than max_tokens slots."""
+    import torch
+    dev = cache.table.device
+    batch, seqs = _keys(cache, ck, bounds, cu_new, rows, ends)
+    n, n_q_heads = _attended(cache, ck, q, None)
+    shape = (n, ck.n_streams, int(n_blocks))
+    with _Call(dev, stream) as s:
+        out = _made(stream, shape, torch.int32, dev) if out is None else out
+        _need(out.device == dev and out.dtype == torch.int32 and out.is_contiguous() and tuple(out.shape) == shape,
+              f"out must be a contiguous int32 tensor {shape} on {dev}")
+        ws = _workspace(cache, workspace, spectra_paged_select_workspace_bytes(n, n_q_heads, ck.n_streams, max_tokens), stream)
+        check(_lib.get().spectra_paged_select(cache.ref, ctypes.byref(ck.struct), bounds.data_ptr(), *seqs, batch, n,
+                                              int(max_tokens), q.data_ptr(), _dtype_code(q), q.stride(0), q.stride(1),
+                                              n_q_heads, int(n_blocks), int(first), int(last), out.data_ptr(), ws.data_ptr(),
+                                              _bytes(ws), s.handle))
+    return out
+
+
+def spectra_paged_sparse_attention_workspace_bytes(n_new: int, n_q_heads: int, n_kv_heads: int, n_blocks: int) -> int:
+    return int(_lib.get().spectra_paged_sparse_attention_workspace_bytes(int(n_new), int(n_q_heads), int(n_kv_heads),
+                                                                         int(n_blocks)))
+
+
+def spectra_paged_sparse_attention(cache: PagedCache, ck: Codec, cv: Codec, pool_k, pool_v, q, cu_new, blocks, rows=None,
+                                   ends=None, softmax_scale: float = 0.0, out=None, lse=None, workspace=None, stream=None):
+    """Causal attention of the new tokens q [n, n_q_heads, 128] over listed blocks of their sequences: ``blocks`` (int32
+    [n, n_kv_heads, most]) as spectra_paged_select returns them, 64 slots each. The rest as spectra_paged_attention."""
+    import torch
+    dev = cache.table.device
+    batch, head = _sequences(cache, ck, cv, pool_k, pool_v, cu_new, rows, ends)
+    n, n_q_heads = _attended(cache, ck, q, lse)
+    _need(blocks.device == dev and blocks.dtype == torch.int32 and blocks.dim() == 3 and blocks.is_contiguous()
+          and tuple(blocks.shape[:2]) == (n, ck.n_streams),
+          f"blocks must be a contiguous int32 tensor {(n, ck.n_streams, 'most')} on {dev}")
+    with _Call(dev, stream) as s:
+        out = _output(out, q, stream)
+        ws = _workspace(cache, workspace, spectra_paged_sparse_attention_workspace_bytes(n, n_q_heads, ck.n_streams,
+                                                                                         blocks.shape[2]), stream)
+        check(_lib.get().spectra_paged_sparse_attention(*head, n, blocks.data_ptr(), blocks.shape[2], q.data_ptr(), _dtype_code(q),
+                                                        q.stride(0), q.stride(1), n_q_heads, float(softmax_scale),
+                                                        out.data_ptr(), _dtype_code(out),
+                                                        lse.data_ptr() if lse is not None else None, ws.data_ptr(), _bytes(ws),
+                                                        s.handle))
     return out
