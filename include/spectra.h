@@ -499,7 +499,7 @@ spectra_status spectra_paged_bounds(const spectra_pages* m, const spectra_codec*
  * more), ascending, -1 behind them. Equal values: the lowest index first. Values are computed to about
  * 2^-20 of sum_j |q'_j box_j|; NaN counts as the least. Rows of no sequence and of those with more than
  * max_tokens slots are left as they were. first, last >= 0, first + last <= n_blocks <= 4096; at most
- * 2^24 query rows and 2^18 sequences times KV heads, here and in the attentions of this part.
+ * 2^21 query rows and 2^18 sequences times KV heads, here and in the attentions of this part.
  * A page out of range counts as boxes of zeros. Workspace: device, 256-byte aligned,
  * spectra_paged_select_workspace_bytes, never fewer for larger counts. Asynchronous. */
 size_t spectra_paged_select_workspace_bytes(int64_t n_new, int32_t n_q_heads, int32_t n_kv_heads, int64_t max_tokens);
@@ -515,8 +515,8 @@ spectra_status spectra_paged_select(const spectra_pages* m, const spectra_codec*
  * spectra_paged_select writes them. Entries that are negative, past the blocks that the token sees, or not
  * greater than every entry before them in the list are passed over, so no block counts twice. A token
  * that sees no slot gets zeros and -inf. Sequences of any length and number of new tokens take part.
- * With fp32 outputs all weights are pairs of fp16 parts. n_blocks <= 4096, n_new * n_kv * n_blocks <=
- * 2^32. Workspace: device, 256-byte aligned, spectra_paged_sparse_attention_workspace_bytes, never fewer
+ * With fp32 outputs all weights are pairs of fp16 parts. n_blocks <= 4096, n_new * n_kv * n_blocks
+ * (in whole 256s) <= 2^29. Workspace: device, 256-byte aligned, spectra_paged_sparse_attention_workspace_bytes, never fewer
  * for larger counts. Asynchronous. */
 size_t spectra_paged_sparse_attention_workspace_bytes(int64_t n_new, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_blocks);
 spectra_status spectra_paged_sparse_attention(const spectra_pages* m, const spectra_codec* ck, const spectra_codec* cv,

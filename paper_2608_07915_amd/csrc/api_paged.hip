@@ -24,7 +24,7 @@ namespace {
 constexpr int64_t kMaxBatch = 16384;
 constexpr int64_t kMost = (int64_t)1 << 30;       // slots of a row, query rows of a call: counted in 32 bits
 constexpr int32_t kMostPage = 1 << 20;            // slots of a page: a record's place in it too
-constexpr int64_t kMostRows = 1 << 24;            // query rows of a call on trees or listed blocks: its grid
+constexpr int64_t kMostRows = 1 << 21;            // query rows of a call on trees or blocks: threads of its grids in 32 bits
 constexpr int32_t kMostDraft = 64;                // drafted tokens of a sequence: bits of a mask
 constexpr int32_t kMostBlocks = 4096;             // listed blocks of a token
 constexpr int64_t kMostGroups = (int64_t)1 << 18;  // sequences times KV heads: 16 workgroups each at most
@@ -151,7 +151,7 @@ spectra_status check_attention(const char* name, const PagedCache& c, int32_t n_
   spectra_status st = check_heads(name, n_q_heads, c.n_kv);
   if (st != SPECTRA_OK) return st;
   if (c.n_new * n_q_heads > kMostRows || (int64_t)c.batch * c.n_kv >= kMostGroups)
-    return fail(SPECTRA_EINVAL, "%s: n_new=%lld times %d query heads passes 2^24, or batch=%d times %d KV heads 2^18", name,
+    return fail(SPECTRA_EINVAL, "%s: n_new=%lld times %d query heads passes 2^21, or batch=%d times %d KV heads 2^18", name,
                 (long long)c.n_new, n_q_heads, c.batch, c.n_kv);
   if (!(softmax_scale == softmax_scale) || std::isinf(softmax_scale)) return fail(SPECTRA_EINVAL, "%s: softmax_scale not finite", name);
   if (out_dt != SPECTRA_F32 && out_dt != SPECTRA_BF16) return fail(SPECTRA_EINVAL, "%s: output dtype %d not supported", name, (int)out_dt);
@@ -484,7 +484,7 @@ spectra_status spectra_paged_sparse_attention(const spectra_pages* m, const spec
   if (n_blocks <= 0 || n_blocks > kMostBlocks)
     return fail(SPECTRA_EINVAL, "%s: n_blocks=%d out of range [1, %d]", name, n_blocks, kMostBlocks);
   if (n_new * p.a.c.n_kv * ((n_blocks + 255) / 256) > kMostRows)
-    return fail(SPECTRA_EINVAL, "%s: n_new=%lld times %d KV heads times %d blocks passes 2^32", name, (long long)n_new, p.a.c.n_kv, n_blocks);
+    return fail(SPECTRA_EINVAL, "%s: n_new=%lld times %d KV heads times %d blocks passes 2^29", name, (long long)n_new, p.a.c.n_kv, n_blocks);
   if (batch == 0 || n_new == 0) return SPECTRA_OK;
   if (!blocks || !aligned(blocks, 4)) return fail(SPECTRA_EINVAL, "%s: blocks must be non-null and 4-byte aligned", name);
   if ((st = check_rows(name, "q", q, q_dt, q_token_stride, q_head_stride)) != SPECTRA_OK) return st;

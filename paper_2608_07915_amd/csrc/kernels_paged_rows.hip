@@ -311,14 +311,14 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
         const f32x4* qp = reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.q) + qoff + 32 * k);
         const f32x4 q0 = qp[0], q1 = qp[1];
         const float qv[8] = {q0[0], q0[1], q0[2], q0[3], q1[0], q1[1], q1[2], q1[3]};
-        split8<QP>(qv, qq);
+        split8_pairs<QP>(qv, qq);
       } else {
         qq[0] = as_bf16x8(*reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.q) + qoff + 32 * k));
       }
 #pragma unroll
       for (int x = 0; x < 2; ++x) {
         bf16x8 vp[QP];
-        split8<QP>(v[x], vp);
+        split8_pairs<QP>(v[x], vp);
 #pragma unroll
         for (int i = 0; i < QP; ++i) acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vp[i], qq[0], acc[x], 0, 0, 0);
         if (a.q_f32) {

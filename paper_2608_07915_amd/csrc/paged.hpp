@@ -115,8 +115,11 @@ struct PagedSelectArgs {
   int64_t max_tokens;
   int32_t n_blocks, first, last;
   int32_t* blocks;
-  float* scores;        // workspace: [n_new][n_q_heads][most_blocks]
+  float* scores;        // workspace: [n_new][n_q_heads][most_blocks], or the values [n_new][n_kv][most_blocks]
+  float* tops;          // workspace: [n_new][n_q_heads][n_chunks], the heads' best scores
   int32_t most_blocks;  // that a sequence of max_tokens has
+  int32_t n_chunks;     // of its blocks
+  int32_t pitch_log2;   // columns of a token's heads
 };
 
 // Attention of a few rows a sequence (drafted trees) or a token (listed blocks) over tiles.

@@ -93,4 +93,23 @@ __device__ __forceinline__ void split8(const float (&v)[8], bf16x8 (&p)[NP]) {
     p[q] = as_bf16x8(u32x4{pack2(a[q][0], a[q][1]), pack2(a[q][2], a[q][3]), pack2(a[q][4], a[q][5]), pack2(a[q][6], a[q][7])});
 }
 
+// The same by the conversion instruction, two numbers at a time (a third of the instructions; finite
+// numbers alike).
+template <int NP>
+__device__ __forceinline__ void split8_pairs(const float (&v)[8], bf16x8 (&p)[NP]) {
+  u32x4 w[NP];
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    f32x2 r = f32x2{v[2 * i], v[2 * i + 1]};
+#pragma unroll
+    for (int q = 0; q < NP; ++q) {
+      const uint32_t b = __builtin_bit_cast(uint32_t, __builtin_convertvector(r, bf16x2));
+      w[q][i] = b;
+      r = f32x2{r[0] - __uint_as_float(b << 16), r[1] - __uint_as_float(b & 0xFFFF0000u)};
+    }
+  }
+#pragma unroll
+  for (int q = 0; q < NP; ++q) p[q] = as_bf16x8(w[q]);
+}
+
 }  // namespace spectra_dev

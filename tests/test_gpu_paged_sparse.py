@@ -193,29 +193,42 @@ def test_selection_long():
         assert v[mine[1:-1]].min() >= v[left].max() - 4 * 2.0 ** -20 * size
 
 
-def test_selection_of_equal_values():
-    """Boxes of small whole numbers and an identity basis: values are exact, ties go to the lowest index."""
+@pytest.mark.parametrize("n", [40, 500, 1500, 3000, 10000, 17000])
+def test_selection_of_equal_values(n):
+    """Boxes of small whole numbers and an identity basis: values are exact, ties go to the lowest index, however many
+    there are."""
     ck, _ = codec([[4, 0, 0, 0]], 10, 1)
     ck.basis[0] = torch.eye(D)
-    m = S.PagedCache(40, 64, 1, 40)
-    m.table[0] = ints(np.arange(40)[::-1].copy())
-    m.lens[0] = 40 * 64
-    vals = np.array([3, 7, 7, 1, 7, 2, 5, 5] * 5)
-    box = torch.zeros((40, 1, 1, 4, 2, 32), dtype=torch.float16, device="cuda")
+    m = S.PagedCache(n, 64, 1, n)
+    m.table[0] = ints(np.arange(n)[::-1].copy())
+    m.lens[0] = n * 64
+    box = torch.zeros((n, 1, 1, 4, 2, 32), dtype=torch.float16, device="cuda")
+    pool = box.view(torch.int32).view(n, -1)
+    rng = np.random.default_rng(n)
+    ks = [1, 2, 5, 15, 16, 20, 25, 39] + [k for k in (n // 3, n // 2, n - 1) if k <= 4096]
+    # a few values again and again; one block far below, beside which the others are nearly alike; two values; all alike
+    for vals in (np.array([3, 7, 7, 1, 7, 2, 5, 5] * n)[:n], np.where(np.arange(n) == 11, -60000, rng.integers(0, 5, n)),
+                 rng.integers(0, 2, n), np.zeros(n, np.int64)):
+        box[m.table[0].long(), 0, 0, 0, 1, 0] = torch.tensor(vals, dtype=torch.float16, device="cuda")
+        for heads in (1, 4):
+            q = torch.zeros((1, heads, D), device="cuda")
+            q[:, :, 0] = 2.0
+            for k in ks:
+                got = S.spectra_paged_select(m, ck, pool, q, ints([0, 1]), k, n * 64, first=0, last=0).cpu().numpy()[0, 0]
+                assert np.array_equal(got, np.sort(np.argsort(-vals, kind="stable")[:k])), (heads, k)
+            got = S.spectra_paged_select(m, ck, pool, q, ints([0, 1]), 6, n * 64, first=1, last=2).cpu().numpy()[0, 0]
+            rest = 1 + np.argsort(-vals[1:n - 2], kind="stable")[:3]
+            assert got.tolist() == sorted([0, n - 2, n - 1, *rest.tolist()])
+    # many tokens: another way through the scores
+    vals = np.where(np.arange(n) == 11, -60000, rng.integers(0, 5, n))
     box[m.table[0].long(), 0, 0, 0, 1, 0] = torch.tensor(vals, dtype=torch.float16, device="cuda")
-    for heads in (1, 4):
-        q = torch.zeros((1, heads, D), device="cuda")
-        q[:, :, 0] = 2.0
-        for k in (1, 2, 5, 15, 16, 20, 25, 39):
-            got = S.spectra_paged_select(m, ck, box.view(torch.int32).view(40, -1), q, ints([0, 1]), k, 2560, first=0, last=0).cpu().numpy()[0, 0]
-            want = np.sort(np.argsort(-vals, kind="stable")[:k])
-            assert np.array_equal(got, want), (heads, k)
-        # with forced ones
-        got = S.spectra_paged_select(m, ck, box.view(torch.int32).view(40, -1), q, ints([0, 1]), 6, 2560, first=1, last=2).cpu().numpy()[0, 0]
-        assert got.tolist() == [0, 1, 2, 4, 38, 39]
-        # all alike
-        got = S.spectra_paged_select(m, ck, torch.zeros_like(box).view(torch.int32).view(40, -1), q, ints([0, 1]), 6, 2560, first=0, last=1).cpu().numpy()[0, 0]
-        assert got.tolist() == [0, 1, 2, 3, 4, 39]
+    for heads in (1, 3, 7, 16):
+        q = torch.zeros((300, heads, D), device="cuda")
+        q[:, :, 0] = 1.0 + torch.arange(300, device="cuda")[:, None] % 3
+        got = S.spectra_paged_select(m, ck, pool, q, ints([0, 300]), 20, n * 64, first=0, last=0).cpu().numpy()[:, 0]
+        for t in (0, 36, 100, 299):
+            have = -(-(n * 64 - 300 + t + 1) // 64)
+            assert np.array_equal(got[t], np.sort(np.argsort(-vals[:have], kind="stable")[:20])), (heads, t)
 
 
 def test_selection_of_what_is_not_finite():
