@@ -1,6 +1,6 @@
 // Attention of a few query rows over tiles of a paged packed cache: the drafted trees of sequences
-// (rows = drafted tokens x query heads of a KV head, tiles = all of the sequence's) and single tokens over
-// listed blocks (rows = query heads of a KV head, tiles = the list's).
+// (rows = drafted tokens x query heads of a KV head, tiles = all of the sequence's) and tokens over
+// listed blocks (rows = neighbouring tokens x query heads of a KV head, tiles = what their lists name together).
 //
 //   q'  = scale * log2(e) * q V_K
 //   S   = q' . c_hat_K(t)                     (the constant q' . m_K cancels in the softmax)
@@ -146,17 +146,30 @@ __device__ __forceinline__ int64_t plan_at(const PagedRowsArgs& p, int rows, con
   return seq.first * p.a.n_qh / rows + b + unit;
 }
 
-// The last sequence that holds new token t, -1: none. Every thread of NT.
-template <int NT>
-__device__ __forceinline__ int holder(const PagedCache& c, int64_t t, int32_t& b_s) {
-  if (threadIdx.x == 0) b_s = -1;
-  __syncthreads();
-  for (int b = threadIdx.x; b < c.batch; b += NT) {
-    const PagedSeq q = paged_seq(c, b);
-    if (t >= q.first && t < q.first + q.n) atomicMax(&b_s, b);
+// Lists: a unit is p.tokens neighbouring new tokens of one sequence (sequence b's units begin at first_b /
+// tokens + b, so those of two sequences never meet; with single tokens, at first_b). The last sequence that
+// unit u belongs to, -1: none, and its first token. Every thread.
+__device__ __forceinline__ int list_unit(const PagedRowsArgs& p, int64_t u, int32_t& b_s, int64_t& tok0) {
+  const PagedCache& c = p.a.c;
+  auto at = [&](int b, const PagedSeq& q) { return u - (p.tokens == 1 ? q.first : q.first / p.tokens + b); };
+  auto has = [&](int b, const PagedSeq& q) {
+    const int64_t x = at(b, q);
+    return x >= 0 && x < (q.n + p.tokens - 1) / p.tokens;
+  };
+  int b = 0;
+  if (c.batch > 1) {
+    if (threadIdx.x == 0) b_s = -1;
+    __syncthreads();
+    for (int i = threadIdx.x; i < c.batch; i += RO_NT)
+      if (has(i, paged_seq(c, i))) atomicMax(&b_s, i);
+    __syncthreads();
+    b = __builtin_amdgcn_readfirstlane(b_s);
+    if (b < 0) return -1;
   }
-  __syncthreads();
-  return __builtin_amdgcn_readfirstlane(b_s);
+  const PagedSeq q = paged_seq(c, b);
+  if (!has(b, q)) return -1;
+  tok0 = at(b, q) * p.tokens;
+  return b;
 }
 
 // Of lane i < n: the drafted tokens that token i sees, its ancestors and itself, as bits. Halving by
@@ -222,31 +235,110 @@ __device__ __forceinline__ int read_list(const int32_t* __restrict__ list, int f
   return n;
 }
 
-constexpr int LIST_CHUNK = 256;  // entries of a workgroup at most
+constexpr int LIST_CHUNK = 256;   // entries of a workgroup at most, where a unit is one token
+constexpr int LIST_ALL = 256;     // entries of a unit's tokens at most, where it is several
+
+// What the lists of n tokens name together, each block once, with the tokens that name it as bits. Lists as
+// in read_list, token i's below blocks(i). A wavefront packs a token's list; then each of its entries is looked up in the
+// others' (by halves, they ascend): the first token that names a block brings it in. Returns how many.
+struct UnionScratch {
+  int32_t count[16], own[16];
+};
+template <typename Blocks>
+__device__ __forceinline__ int read_lists(const int32_t* __restrict__ lists, int64_t stride, int n_blocks, int n, Blocks&& blocks,
+                                          int32_t* packed, int32_t* sel, uint16_t* bits, UnionScratch& s) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+  const uint64_t below = ((uint64_t)1 << lane) - 1;
+  for (int i = wave; i < n; i += RO_NW) {
+    const int32_t* list = lists + i * stride;
+    const int end = blocks(i);
+    int before = -1, at = 0;
+    for (int e0 = 0; e0 < n_blocks; e0 += 64) {
+      const int x = e0 + lane < n_blocks ? list[e0 + lane] : -1;
+      int top = x;
+#pragma unroll
+      for (int o = 1; o < 64; o <<= 1) {
+        const int u = __shfl_up(top, o);
+        if (lane >= o && u > top) top = u;
+      }
+      int prev = __shfl_up(top, 1);
+      prev = lane == 0 || before > prev ? before : prev;
+      const bool take = x > prev && x < end;
+      const uint64_t m = __ballot(take);
+      if (take) packed[i * n_blocks + at + __popcll(m & below)] = x;
+      at += __popcll(m);
+      const int last = __shfl(top, 63);
+      before = last > before ? last : before;
+    }
+    if (lane == 0) s.count[i] = at;
+  }
+  __syncthreads();
+  auto names = [&](int i, int x) {
+    int lo = 0, hi = s.count[i];
+    while (lo < hi) {
+      const int mid = (lo + hi) >> 1;
+      if (packed[i * n_blocks + mid] < x) lo = mid + 1; else hi = mid;
+    }
+    return lo < s.count[i] && packed[i * n_blocks + lo] == x;
+  };
+  // twice: first how many a token brings in, then where they go
+  int total = 0;
+  for (int pass = 0; pass < 2; ++pass) {
+    for (int i = wave; i < n; i += RO_NW) {
+      int at = 0;
+      if (pass > 0)
+        for (int j = 0; j < i; ++j) at += s.own[j];
+      for (int e0 = 0; e0 < s.count[i]; e0 += 64) {
+        const int e = e0 + lane;
+        bool own = e < s.count[i];
+        const int x = own ? packed[i * n_blocks + e] : 0;
+        for (int j = 0; j < i && own; ++j) own = !names(j, x);
+        const uint64_t m = __ballot(own);
+        if (pass > 0 && own) {
+          uint32_t who = 1u << i;
+          for (int j = i + 1; j < n; ++j) who |= names(j, x) ? 1u << j : 0u;
+          sel[at + __popcll(m & below)] = x;
+          bits[at + __popcll(m & below)] = (uint16_t)who;
+        }
+        at += __popcll(m);
+      }
+      if (pass == 0 && lane == 0) s.own[i] = at;
+    }
+    __syncthreads();
+  }
+  for (int i = 0; i < n; ++i) total += s.own[i];
+  return total;
+}
 
 // ---------------------------------------------------------------------------
-// The sums of a unit over a chunk
+// The sums of a unit over a chunk. A group's words are loaded while the one before is multiplied (a whole
+// tile ahead, in registers, came to 45 us for 39: 48 tokens of seven heads over 64 blocks).
 // ---------------------------------------------------------------------------
 template <int NB, bool PRECISE, bool TREE>
 __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows_kernel(PagedRowsArgs p) {
   constexpr int ROWS = 16 * NB, NP = PRECISE ? 2 : 1, QP = PRECISE ? 3 : 2;
   __shared__ RowsScratch place_s;
   __shared__ ListScratch list_s;
-  __shared__ int32_t sel_s[TREE ? 1 : LIST_CHUNK], b_s;
+  __shared__ UnionScratch union_s;
+  __shared__ int32_t sel_s[TREE ? 1 : LIST_ALL], b_s;
+  __shared__ uint16_t who_s[TREE ? 1 : LIST_ALL];
   __shared__ uint64_t anc_s[TREE ? DRAFT : 1];
-  __shared__ float m_s[RO_NW][16], l_s[RO_NW][16], un_s[NG][ROWS];
+  __shared__ float m_s[RO_NW][ROWS], l_s[RO_NW][ROWS], un_s[PRECISE ? NG : 1][ROWS];
   __shared__ int32_t unit_s[2 * NG];
   __shared__ __attribute__((aligned(16))) float sums_s[RO_NW * 16 * RO_PITCH];  // the tiles while wavefronts walk
   __shared__ __attribute__((aligned(16))) uint8_t q_s[NG][NB][NP][64 * 16];      // q' as column operands, by lane
   static_assert(sizeof(sums_s) >= RO_NW * NP * CA_TILE, "the tiles lie where the sums do");
+  static_assert(sizeof(sums_s) >= LIST_ALL * sizeof(int32_t), "and the packed lists before them");
   const PagedAttnArgs& a = p.a;
   const int kv = (int)(blockIdx.x % (unsigned)a.c.n_kv);
   const int64_t item = blockIdx.x / (unsigned)a.c.n_kv;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quarter = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
-  int b, row0, begin = 0, count;
+  int b, row0 = 0, begin = 0, count, chunk = 0;
   PagedSeq seq;
-  int64_t tok0 = 0;  // lists: the token
+  int64_t tok0 = 0;  // lists: the unit's first token
+  int n_tok = 1;
+  uint32_t all = 1u;  // lists: the unit's tokens as bits
   if constexpr (TREE) {
     const RowsPlace at = tree_place(p, ROWS, (int)item, place_s);
     if (at.b < 0) return;
@@ -262,99 +354,131 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
     begin = at.chunk * at.tiles;
     count = n_tiles - begin < at.tiles ? n_tiles - begin : at.tiles;
   } else {
-    const int64_t t = item / p.n_chunks;
-    b = holder<RO_NT>(a.c, t, b_s);
+    const int64_t u = item / p.n_chunks;
+    chunk = (int)(item - u * p.n_chunks);
+    b = list_unit(p, u, b_s, tok0);
     if (b < 0) return;
     seq = paged_seq(a.c, b);
-    tok0 = t - seq.first;
-    row0 = 0;
-    const int64_t see = seq.len - seq.n + tok0 + 1;
-    const int blocks = see > 0 ? (int)((see + TILE - 1) / TILE) : 0;
-    const int from = (int)(item % p.n_chunks) * p.chunk, to = from + p.chunk < p.n_blocks ? from + p.chunk : p.n_blocks;
-    count = read_list(p.blocks + (t * a.c.n_kv + kv) * p.n_blocks, from, to, blocks, sel_s, list_s);
+    n_tok = (int)(seq.n - tok0 < p.tokens ? seq.n - tok0 : p.tokens);
+    auto blocks = [&](int i) {  // that token i of the unit sees
+      const int64_t see = seq.len - seq.n + tok0 + i + 1;
+      return see > 0 ? (int)((see + TILE - 1) / TILE) : 0;
+    };
+    const int32_t* list = p.blocks + ((seq.first + tok0) * a.c.n_kv + kv) * p.n_blocks;
+    if (p.tokens == 1) {
+      const int from = chunk * p.chunk, to = from + p.chunk < p.n_blocks ? from + p.chunk : p.n_blocks;
+      count = read_list(list, from, to, blocks(0), sel_s, list_s);
+    } else {
+      all = (1u << n_tok) - 1;
+      const int n = read_lists(list, (int64_t)a.c.n_kv * p.n_blocks, p.n_blocks, n_tok, blocks, reinterpret_cast<int32_t*>(sums_s),
+                               sel_s, who_s, union_s);
+      int each = (n + p.n_chunks - 1) / p.n_chunks;
+      each = (each + RO_NW - 1) / RO_NW * RO_NW;
+      begin = chunk * each < n ? chunk * each : n;
+      count = n - begin < each ? n - begin : each;
+    }
   }
-  const int n_rows = TREE ? (int)(seq.n * a.n_qh) - row0 : a.n_qh;  // of the unit, and those behind it
+  const int n_rows = TREE ? (int)(seq.n * a.n_qh) - row0 : n_tok * a.n_qh;  // of the unit, and those behind it
   Kept Kk = read_kept(a.bits_k + kv * NG), Kv = read_kept(a.bits_v + kv * NG);
   if (!Kk.ok || Kk.used > a.Wk) Kk.n = 0;  // width table inconsistent with the record
   if (!Kv.ok || Kv.used > a.Wv) Kv.n = 0;
   // the lane's row of block nb: token of the sequence, query head (rows past the last repeat the first)
   auto row_of = [&](int nb, int& tok, int& head) __attribute__((always_inline)) {
     const int r = row0 + (16 * nb + col < n_rows ? 16 * nb + col : 0);
-    tok = TREE ? r / a.n_qh : 0;
-    head = TREE ? r - tok * a.n_qh : r;
-    if (!TREE) tok = (int)tok0;
+    tok = r / a.n_qh;
+    head = r - tok * a.n_qh;
+    if (!TREE) tok += (int)tok0;
   };
   if constexpr (TREE) {
     if (wave == 0) anc_s[lane] = ancestors(p.parents, seq.first, (int)seq.n, lane);
   }
 
-  // q': element e of quarter p is that of code 4 p + e / 2 + 16 (e % 2), as the tiles' places are;
-  // product x has e = 4 x .. 4 x + 3. PRECISE: a row's group is scaled by 2^E into [2^8, 2^9).
-  for (int pair = wave; pair < Kk.n * NB; pair += RO_NW) {
-    const int sl = pair / NB, nb = pair - sl * NB;
-    int tok, head;
-    row_of(nb, tok, head);
-    const int64_t qoff = (seq.first + tok) * a.q_token_stride + (kv * a.n_qh + head) * a.q_head_stride + 8 * quarter;
-    const float* V = a.basis_k + (int64_t)kv * D * D + (8 * quarter) * D + G * pick4(Kk.grp, sl) + 4 * (col >> 2) +
-                     ((col & 3) >> 1) + 16 * (col & 1);
-    f32x4 acc[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
+  // q': element e of quarter p is that of code 4 p + e / 2 + 16 (e % 2), as the tiles' places are; product y has
+  // e = (i / 2) * 4 + i % 2 + 2 y, i < 4, so that a lane's codes of both products are neighbours. A wavefront takes
+  // a group, or half of the row blocks of one where there are two at most, and cuts its basis into
+  // parts once. PRECISE: a row's group is scaled by 2^E into [2^8, 2^9).
+  {
+    const bool halves = NB > 1 && Kk.n <= 2;
+    const int sl = halves ? wave & 1 : wave, nb0 = halves && wave > 1 ? NB / 2 : 0, nb1 = halves && wave < 2 ? NB / 2 : NB;
+    if (sl < Kk.n) {
+      f32x4 acc[NB][2];
+      int64_t qoff[NB];
 #pragma unroll
-    for (int k = 0; k < 4; ++k) {
-      float v[2][8];
-#pragma unroll
-      for (int e = 0; e < 8; ++e) {
-        v[0][e] = V[(32 * k + e) * D];
-        v[1][e] = V[(32 * k + e) * D + 2];
+      for (int nb = 0; nb < NB; ++nb) {
+        acc[nb][0] = acc[nb][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        int tok, head;
+        row_of(nb, tok, head);
+        qoff[nb] = (seq.first + tok) * a.q_token_stride + (kv * a.n_qh + head) * a.q_head_stride + 8 * quarter;
       }
-      bf16x8 qq[QP];
-      if (a.q_f32) {
-        const f32x4* qp = reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.q) + qoff + 32 * k);
-        const f32x4 q0 = qp[0], q1 = qp[1];
-        const float qv[8] = {q0[0], q0[1], q0[2], q0[3], q1[0], q1[1], q1[2], q1[3]};
-        split8_pairs<QP>(qv, qq);
-      } else {
-        qq[0] = as_bf16x8(*reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.q) + qoff + 32 * k));
-      }
+      const float* V = a.basis_k + (int64_t)kv * D * D + (8 * quarter) * D + G * pick4(Kk.grp, sl) + 4 * (col >> 2) + (col & 2) + 16 * (col & 1);
 #pragma unroll
-      for (int x = 0; x < 2; ++x) {
-        bf16x8 vp[QP];
-        split8_pairs<QP>(v[x], vp);
+      for (int k = 0; k < 4; ++k) {
+        float v[2][8];
 #pragma unroll
-        for (int i = 0; i < QP; ++i) acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vp[i], qq[0], acc[x], 0, 0, 0);
-        if (a.q_f32) {
+        for (int e = 0; e < 8; ++e) {
+          const f32x2 x = *reinterpret_cast<const f32x2*>(V + (32 * k + e) * D);
+          v[0][e] = x[0];
+          v[1][e] = x[1];
+        }
+        bf16x8 vp[2][QP];
+        split8_pairs<QP>(v[0], vp[0]);
+        split8_pairs<QP>(v[1], vp[1]);
 #pragma unroll
-          for (int i = 0; i < QP; ++i)
+        for (int nb = 0; nb < NB; ++nb) {
+          if (nb < nb0 || nb >= nb1) continue;
+          bf16x8 qq[QP];
+          if (a.q_f32) {
+            const f32x4* qp = reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.q) + qoff[nb] + 32 * k);
+            const f32x4 q0 = qp[0], q1 = qp[1];
+            const float qv[8] = {q0[0], q0[1], q0[2], q0[3], q1[0], q1[1], q1[2], q1[3]};
+            split8_pairs<QP>(qv, qq);
+          } else {
+            qq[0] = as_bf16x8(*reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.q) + qoff[nb] + 32 * k));
+          }
 #pragma unroll
-            for (int j = 1; i + j < QP; ++j) acc[x] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vp[i], qq[j], acc[x], 0, 0, 0);
+          for (int y = 0; y < 2; ++y) {
+#pragma unroll
+            for (int i = 0; i < QP; ++i) acc[nb][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vp[y][i], qq[0], acc[nb][y], 0, 0, 0);
+            if (a.q_f32) {
+#pragma unroll
+              for (int i = 0; i < QP; ++i)
+#pragma unroll
+                for (int j = 1; i + j < QP; ++j) acc[nb][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vp[y][i], qq[j], acc[nb][y], 0, 0, 0);
+            }
+          }
         }
       }
-    }
-    float y[8], most = 0.0f, up = 1.0f;
 #pragma unroll
-    for (int e = 0; e < 8; ++e) {
-      y[e] = acc[e >> 2][e & 3] * a.scale_log2;
-      most = __builtin_fmaxf(most, __builtin_fabsf(y[e]));
-    }
-    if constexpr (PRECISE) {
-      most = __builtin_fmaxf(most, __shfl_xor(most, 16));
-      most = __builtin_fmaxf(most, other_half(most));
-      up = __builtin_ldexpf(1.0f, 9 - scale_exponent(most));
-      if (quarter == 0) un_s[sl][16 * nb + col] = 1.0f / up;
-    }
-    u32x4 rh, rl;
+      for (int nb = 0; nb < NB; ++nb) {
+        if (nb < nb0 || nb >= nb1) continue;
+        float y[8], most = 0.0f, up = 1.0f;
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-      f32x2 x = f32x2{y[2 * j] * up, y[2 * j + 1] * up};
-      if constexpr (!PRECISE) {  // NaN stays
+        for (int e = 0; e < 8; ++e) {
+          y[e] = acc[nb][(e >> 1) & 1][2 * (e >> 2) + (e & 1)] * a.scale_log2;
+          most = __builtin_fmaxf(most, __builtin_fabsf(y[e]));
+        }
+        if constexpr (PRECISE) {
+          most = __builtin_fmaxf(most, __shfl_xor(most, 16));
+          most = __builtin_fmaxf(most, other_half(most));
+          up = __builtin_ldexpf(1.0f, 9 - scale_exponent(most));
+          if (quarter == 0) un_s[sl][16 * nb + col] = 1.0f / up;
+        }
+        u32x4 rh, rl;
 #pragma unroll
-        for (int e = 0; e < 2; ++e) x[e] = x[e] > 65504.0f ? 65504.0f : x[e] < -65504.0f ? -65504.0f : x[e];
+        for (int j = 0; j < 4; ++j) {
+          f32x2 x = f32x2{y[2 * j] * up, y[2 * j + 1] * up};
+          if constexpr (!PRECISE) {  // NaN stays
+#pragma unroll
+            for (int e = 0; e < 2; ++e) x[e] = x[e] > 65504.0f ? 65504.0f : x[e] < -65504.0f ? -65504.0f : x[e];
+          }
+          const f16x2 hi = __builtin_convertvector(x, f16x2);
+          rh[j] = __builtin_bit_cast(uint32_t, hi);
+          rl[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{(x[0] - (float)hi[0]) * CA_LO, (x[1] - (float)hi[1]) * CA_LO}, f16x2));
+        }
+        *reinterpret_cast<u32x4*>(q_s[sl][nb][0] + 16 * lane) = rh;
+        if constexpr (PRECISE) *reinterpret_cast<u32x4*>(q_s[sl][nb][1] + 16 * lane) = rl;
       }
-      const f16x2 hi = __builtin_convertvector(x, f16x2);
-      rh[j] = __builtin_bit_cast(uint32_t, hi);
-      rl[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{(x[0] - (float)hi[0]) * CA_LO, (x[1] - (float)hi[1]) * CA_LO}, f16x2));
     }
-    *reinterpret_cast<u32x4*>(q_s[sl][nb][0] + 16 * lane) = rh;
-    if constexpr (PRECISE) *reinterpret_cast<u32x4*>(q_s[sl][nb][1] + 16 * lane) = rl;
   }
   const int tpp = a.c.page_tokens >> 6, n_keys = Kk.n, n_units = Kk.n + Kv.n;
   if (tid < 2 * NG) {  // a kept group of the keys, then of the values
@@ -371,7 +495,7 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
   uint8_t* tile = reinterpret_cast<uint8_t*>(sums_s) + wave * NP * CA_TILE;
   uint32_t magic = 0x64006400u;  // exponent of 1024 in both halves, in a VGPR
   asm volatile("" : "+v"(magic));
-  auto tile_of = [&](int x) __attribute__((always_inline)) { return TREE ? begin + x : __builtin_amdgcn_readfirstlane(sel_s[x]); };
+  auto tile_of = [&](int x) __attribute__((always_inline)) { return TREE ? begin + x : __builtin_amdgcn_readfirstlane(sel_s[begin + x]); };
   // the tile whose words are loaded: its page, its own place in it, its records
   int load_x = wave, in_page = 0, page = -1;
   const uint32_t *kp = a.pool_k, *vp = a.pool_v;
@@ -430,7 +554,7 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
     fetch(0);
   }
   const int64_t past = seq.len - seq.n;  // slots of the history
-  const int64_t common = TREE ? past : past + tok0 + 1;  // slots that every row sees
+  const int64_t common = TREE ? past : past + tok0 + 1;  // slots that every row sees, as far as its list goes
   f32x4 acc[NG][2][NB];
   float ref[NB], l[NB];  // the reference less CA_LIFT (-inf: nothing seen yet)
 #pragma unroll
@@ -477,17 +601,20 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
         }
       }
     }
-    if (t0 + TILE > common) {  // some row does not see the whole tile
+    const uint32_t who = TREE || p.tokens == 1 ? all : (uint32_t)__builtin_amdgcn_readfirstlane(who_s[begin + x]);
+    if (t0 + TILE > common || who != all) {  // some row does not see the whole tile
       const int64_t rel = t0 - common;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         uint64_t own = 0u;  // of the slots at and behind `common`
-        if constexpr (TREE) {
-          int tok, head;
-          row_of(nb, tok, head);
+        int tok, head;
+        row_of(nb, tok, head);
+        if constexpr (TREE)
           own = anc_s[tok];
-        }
-        uint64_t see = rel >= 64 ? 0u : rel >= 0 ? own >> rel : (own << -rel) | (((uint64_t)1 << -rel) - 1);
+        else
+          own = ((uint64_t)1 << (tok - (int)tok0)) - 1;  // a token sees one slot more than the one before it
+        uint64_t see = rel >= 64 ? 0u : rel >= 0 ? own >> rel : rel > -64 ? (own << -rel) | (((uint64_t)1 << -rel) - 1) : ~(uint64_t)0;
+        if (!TREE && !(who >> (tok - (int)tok0) & 1u)) see = 0u;
         see >>= 4 * quarter;
         const uint32_t half[2] = {(uint32_t)see, (uint32_t)(see >> 32)};
 #pragma unroll
@@ -584,115 +711,159 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
     }
   }
   // merge of the wavefronts, and the chunk's partial of every row, 16 rows at a time
-  float* part = p.partial + (item * a.c.n_kv + kv) * (int64_t)((TREE ? ROWS : a.n_qh) * PART);
+  // (lists: [chunk][token][KV head][query head], trees: [item][KV head][row])
+  float* part = p.partial + (item * a.c.n_kv + kv) * (int64_t)(ROWS * PART);
+  const int64_t token_step = (int64_t)a.c.n_kv * a.n_qh * PART;
+  if (!TREE) part = p.partial + ((chunk * a.c.n_new + seq.first + tok0) * a.c.n_kv + kv) * (int64_t)(a.n_qh * PART);
+  float m[NB];
+#pragma unroll
+  for (int nb = 0; nb < NB; ++nb) {
+    float ll = l[nb] + __shfl_xor(l[nb], 16);
+    ll += other_half(ll);
+    m[nb] = ll == 0.0f ? -__builtin_inff() : ref[nb] == -__builtin_inff() ? 0.0f : ref[nb];
+    if (quarter == 0) {
+      m_s[wave][16 * nb + col] = m[nb];
+      l_s[wave][16 * nb + col] = ll;
+    }
+  }
+  __syncthreads();  // the maxima; the tiles have been read
+  auto factor = [&](float mine, float top) __attribute__((always_inline)) { return mine == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(mine - top); };
+  auto top_of = [&](int r) __attribute__((always_inline)) {
+    float t = m_s[0][r];
+#pragma unroll
+    for (int v = 1; v < RO_NW; ++v) t = __builtin_fmaxf(t, m_s[v][r]);
+    return t;
+  };
 #pragma unroll
   for (int nb = 0; nb < NB; ++nb) {
     if (16 * nb >= n_rows) break;
-    float ll = l[nb] + __shfl_xor(l[nb], 16);
-    ll += other_half(ll);
-    __syncthreads();  // the tiles, or the sums before, have been read
-    if (quarter == 0) {
-      m_s[wave][col] = ll == 0.0f ? -__builtin_inff() : ref[nb] == -__builtin_inff() ? 0.0f : ref[nb];
-      l_s[wave][col] = ll;
-    }
+    const float f = factor(m[nb], top_of(16 * nb + col));
 #pragma unroll
     for (int sl = 0; sl < NG; ++sl)
       if (sl < Kv.n)
 #pragma unroll
         for (int y = 0; y < 2; ++y)
-          *reinterpret_cast<f32x4*>(sums_s + (wave * 16 + col) * RO_PITCH + G * sl + 16 * y + 4 * quarter) = acc[sl][y][nb];
+          *reinterpret_cast<f32x4*>(sums_s + (wave * 16 + col) * RO_PITCH + G * sl + 16 * y + 4 * quarter) =
+              f32x4{acc[sl][y][nb][0] * f, acc[sl][y][nb][1] * f, acc[sl][y][nb][2] * f, acc[sl][y][nb][3] * f};
     __syncthreads();
     const int here = n_rows - 16 * nb < 16 ? n_rows - 16 * nb : 16;
-    for (int e = tid; e < here * D; e += RO_NT) {
-      const int r = e >> 7, j = e & 127, g = j >> 5, c = j & 31;
-      const int place = 8 * ((c & 15) >> 2) + 2 * (c & 3) + (c >> 4);
-      int sl = -1;
+    auto out = [&](int r) __attribute__((always_inline)) {
+      const int row = 16 * nb + r, tok = TREE ? 0 : row / a.n_qh;
+      return part + tok * token_step + (row - tok * a.n_qh) * PART;
+    };
+    // sums as they lie: [kept group][place]
+    for (int e = tid; e < here * (D / 4); e += RO_NT) {
+      const int r = e / (D / 4), x = 4 * (e % (D / 4));
+      if (x >= G * Kv.n) continue;
+      f32x4 sum = *reinterpret_cast<const f32x4*>(sums_s + r * RO_PITCH + x);
 #pragma unroll
-      for (int y = 0; y < NG; ++y) sl = (y < Kv.n && Kv.grp[y] == g) ? y : sl;
-      float m = -__builtin_inff(), sum = 0.0f, total = 0.0f;
+      for (int v = 1; v < RO_NW; ++v) {
+        const f32x4 y = *reinterpret_cast<const f32x4*>(sums_s + (v * 16 + r) * RO_PITCH + x);
 #pragma unroll
-      for (int v = 0; v < RO_NW; ++v) m = __builtin_fmaxf(m, m_s[v][r]);
-#pragma unroll
-      for (int v = 0; v < RO_NW; ++v) {
-        const float f = m_s[v][r] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m_s[v][r] - m);
-        if (sl >= 0) sum = __builtin_fmaf(f, sums_s[(v * 16 + r) * RO_PITCH + G * sl + place], sum);
-        total = __builtin_fmaf(f, l_s[v][r], total);
+        for (int i = 0; i < 4; ++i) sum[i] += y[i];
       }
-      float* o = part + (16 * nb + r) * PART;
-      o[8 + j] = sum;
-      if (j == 0) {
-        o[0] = m;
-        o[1] = total;
-      }
+      *reinterpret_cast<f32x4*>(out(r) + 8 + x) = sum;
     }
+    if (tid < here) {
+      const int r = 16 * nb + tid;
+      const float top = top_of(r);
+      float total = 0.0f;
+#pragma unroll
+      for (int v = 0; v < RO_NW; ++v) total = __builtin_fmaf(factor(m_s[v][r], top), l_s[v][r], total);
+      *reinterpret_cast<f32x2*>(out(tid)) = f32x2{top, total};
+    }
+    if (nb + 1 < NB) __syncthreads();  // the sums have been read
   }
 }
 
 // ---------------------------------------------------------------------------
-// Join of the chunks, the rotation back, and the outputs: a workgroup for CR neighbouring rows (new token x
-// query heads of a KV head, of all sequences) of one KV head. A thread group of 128 sums a row's
-// coefficients, 8 / CR of them share a row's chunks; then a channel is 8 threads' dot product.
+// Join of the chunks, the rotation back, and the outputs, for neighbouring rows (new token x query heads of a
+// KV head, of all sequences) of one KV head.
 // ---------------------------------------------------------------------------
-template <int CR, bool TREE>
-__global__ __launch_bounds__(1024) void paged_rows_combine_kernel(PagedRowsArgs p, int rows) {
-  constexpr int SHARE = 8 / CR;
-  __shared__ int32_t b_s[CR + 1];
-  __shared__ float m_s[8], l_s[8], sums_s[8][D];
-  __shared__ __attribute__((aligned(16))) float chat_s[CR][D];
-  __shared__ float lse_s[16];
+struct RowParts {
+  const float* first;  // the first chunk's
+  int64_t step;        // to the next one's
+  int n;               // chunks; 0: the row sees nothing
+  bool live;
+};
+// Of row `row` (token x query heads) whose token's sequence is b (-1: none).
+template <bool TREE>
+__device__ __forceinline__ RowParts row_parts(const PagedRowsArgs& p, int rows, int64_t row, int b, int kv) {
+  const PagedAttnArgs& a = p.a;
+  RowParts r{p.partial, 0, 0, b >= 0};
+  if (!r.live) return r;
+  const int64_t tok = row / a.n_qh;
+  const int head = (int)(row - tok * a.n_qh);
+  if constexpr (TREE) {
+    const PagedSeq seq = paged_seq(a.c, b);
+    r.live = attended(a, seq);
+    r.step = (int64_t)a.c.n_kv * rows * PART;
+    if (!r.live || seq.len <= 0) return r;
+    const int64_t in_seq = (tok - seq.first) * a.n_qh + head, unit = in_seq / rows;
+    const int64_t u = plan_at(p, rows, seq, b, (int)unit);
+    const int item0 = p.plan[2 * u], most = p.plan[2 * u + 1];
+    // (within the workspace whatever the lists of sequences hold)
+    r.n = item0 < 0 || item0 >= p.items ? 0 : most < p.items - item0 ? most : p.items - item0;
+    r.first += ((int64_t)(r.n > 0 ? item0 : 0) * a.c.n_kv + kv) * (rows * PART) + (in_seq - unit * rows) * PART;
+  } else {
+    r.n = p.n_chunks;
+    r.step = a.c.n_new * a.n_q_heads * PART;
+    r.first += ((tok * a.c.n_kv + kv) * a.n_qh + head) * PART;
+  }
+  return r;
+}
+// The sequences of the tokens t_lo .. t_lo + n - 1 into b_s. Every thread of NT.
+template <int NT>
+__device__ __forceinline__ void sequences_of(const PagedCache& c, int64_t t_lo, int n, int32_t* b_s) {
+  for (int i = threadIdx.x; i < n; i += NT) b_s[i] = -1;
+  __syncthreads();
+  for (int b = threadIdx.x; b < c.batch; b += NT) {
+    const PagedSeq q = paged_seq(c, b);
+    const int64_t lo = t_lo < q.first ? q.first : t_lo, hi = t_lo + n < q.first + q.n ? t_lo + n : q.first + q.n;
+    for (int64_t t = lo; t < hi; ++t) atomicMax(&b_s[t - t_lo], b);
+  }
+  __syncthreads();
+}
+
+// Few rows: a workgroup each. Eight thread groups of 128 share the row's chunks; then a channel is 8 threads' dot
+// product.
+template <bool TREE>
+__global__ __launch_bounds__(1024) void paged_row_combine_kernel(PagedRowsArgs p, int rows) {
+  constexpr int SHARE = 8;
+  __shared__ int32_t b_s[1];
+  __shared__ float m_s[SHARE], l_s[SHARE], sums_s[SHARE][D], lse_s[2];
+  __shared__ __attribute__((aligned(16))) float chat_s[D];
   const PagedAttnArgs& a = p.a;
   const int kv = (int)(blockIdx.x % (unsigned)a.c.n_kv);
-  const int64_t row0 = (int64_t)(blockIdx.x / (unsigned)a.c.n_kv) * CR, n_all = a.c.n_new * a.n_qh;
-  const int tid = threadIdx.x, j = tid & 127, group = tid >> 7, r = group % CR, share = group / CR;
+  const int64_t row = blockIdx.x / (unsigned)a.c.n_kv, tok = row / a.n_qh;
+  const int head = (int)(row - tok * a.n_qh);
+  const int tid = threadIdx.x, j = tid & 127, share = tid >> 7;
   const int ri = tid >> 3, rpart = tid & 7;
   const f32x4* Vr = reinterpret_cast<const f32x4*>(a.basis_v + (int64_t)kv * D * D + (int64_t)ri * D + 16 * rpart);
   const f32x4 v0 = Vr[0], v1 = Vr[1], v2 = Vr[2], v3 = Vr[3];
   const float mv = a.mean_v[(int64_t)kv * D + j];
-  // the sequences of the rows' tokens
-  const int64_t t_lo = row0 / a.n_qh, t_hi = (row0 + CR - 1) / a.n_qh;
-  if (tid <= CR) b_s[tid] = -1;
-  __syncthreads();
-  for (int b = tid; b < a.c.batch; b += 1024) {
-    const PagedSeq q = paged_seq(a.c, b);
-    for (int64_t t = t_lo < q.first ? q.first : t_lo; t <= t_hi && t < q.first + q.n; ++t) atomicMax(&b_s[t - t_lo], b);
-  }
-  __syncthreads();
-  const int64_t row = row0 + r, tok = row / a.n_qh;
-  const int head = (int)(row - tok * a.n_qh);
-  const int b = row < n_all ? b_s[tok - t_lo] : -1;
-  PagedSeq seq{};
-  bool live = b >= 0;
-  int n = 0;
-  const float* first = p.partial;
-  const int64_t step = (int64_t)a.c.n_kv * rows * PART;
-  if (live) {
-    seq = paged_seq(a.c, b);
-    if constexpr (TREE) {
-      live = attended(a, seq);
-      const int64_t in_seq = (tok - seq.first) * a.n_qh + head, unit = in_seq / rows;
-      const int64_t u = plan_at(p, rows, seq, b, (int)unit);
-      if (live && seq.len > 0) {
-        const int item0 = p.plan[2 * u], most = p.plan[2 * u + 1];
-        // (within the workspace whatever the lists of sequences hold)
-        n = item0 < 0 || item0 >= p.items ? 0 : most < p.items - item0 ? most : p.items - item0;
-        first += ((int64_t)(n > 0 ? item0 : 0) * a.c.n_kv + kv) * (rows * PART) + (in_seq - unit * rows) * PART;
-      }
-    } else {
-      n = p.n_chunks;
-      first += (tok * n * a.c.n_kv + kv) * (int64_t)(rows * PART) + head * PART;
-    }
-  }
+  Kept Kv = read_kept(a.bits_v + kv * NG);
+  if (!Kv.ok || Kv.used > a.Wv) Kv.n = 0;
+  int sl = -1;
+#pragma unroll
+  for (int x = 0; x < NG; ++x) sl = x < Kv.n && Kv.grp[x] == j >> 5 ? x : sl;
+  const int at = sl < 0 ? 0 : 8 + G * sl + 8 * ((j & 15) >> 2) + 2 * (j & 3) + ((j >> 4) & 1);  // (none: m, not used)
+  float u = 0.0f;
+  if (a.lse != nullptr && share == 0) u = query_at(a, tok * a.q_token_stride + (kv * a.n_qh + head) * a.q_head_stride + j) * a.lse_u[kv * D + j];
+  sequences_of<1024>(a.c, tok, 1, b_s);
+  const RowParts r = row_parts<TREE>(p, rows, row, b_s[0], kv);
+  if (!r.live) return;
   float M = -__builtin_inff(), L = 0.0f, A = 0.0f;
-  constexpr int CB = 4;
-  for (int c0 = share; c0 < n; c0 += CB * SHARE) {
+  constexpr int CB = 8;
+  for (int c0 = share; c0 < r.n; c0 += CB * SHARE) {
     float m[CB], l[CB], x[CB];
 #pragma unroll
     for (int k = 0; k < CB; ++k) {
       const int c = c0 + k * SHARE;
-      const float* pc = first + (c < n ? c : c0) * step;
-      m[k] = c < n ? pc[0] : -__builtin_inff();
+      const float* pc = r.first + (c < r.n ? c : c0) * r.step;
+      m[k] = c < r.n ? pc[0] : -__builtin_inff();
       l[k] = pc[1];
-      x[k] = pc[8 + j];
+      x[k] = pc[at];
     }
     float mb = M;
 #pragma unroll
@@ -710,76 +881,192 @@ __global__ __launch_bounds__(1024) void paged_rows_combine_kernel(PagedRowsArgs 
       M = mb;
     }
   }
-  if constexpr (SHARE > 1) {
-    if (j == 0) {
-      m_s[group] = M;
-      l_s[group] = L;
-    }
-    sums_s[group][j] = A;
-    __syncthreads();
-    if (share == 0) {
-      float mb = M;
-#pragma unroll
-      for (int k = 1; k < SHARE; ++k) mb = __builtin_fmaxf(mb, m_s[r + k * CR]);
-      L = A = 0.0f;
-#pragma unroll
-      for (int k = 0; k < SHARE; ++k) {
-        const float mk = m_s[r + k * CR], f = mk == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(mk - mb);
-        L = __builtin_fmaf(f, l_s[r + k * CR], L);
-        A = __builtin_fmaf(f, sums_s[r + k * CR][j], A);
-      }
-      M = mb;
-    }
+  if (j == 0) {
+    m_s[share] = M;
+    l_s[share] = L;
   }
-  const bool seen = L > 0.0f || L != L;
-  if (share == 0) chat_s[r][j] = seen ? A / L + mv : 0.0f;
-  if (a.lse != nullptr) {
-    float u = 0.0f;
-    if (live && share == 0) {
-      const int64_t qo = tok * a.q_token_stride + (kv * a.n_qh + head) * a.q_head_stride;
-      u = query_at(a, qo + j) * a.lse_u[kv * D + j];
-    }
+  sums_s[share][j] = A;
+  if (a.lse != nullptr && share == 0) {
 #pragma unroll
     for (int o = 32; o > 0; o >>= 1) u += __shfl_xor(u, o);
     if ((tid & 63) == 0) lse_s[tid >> 6] = u;
-    __syncthreads();
-    if (live && share == 0 && j == 0)
-      a.lse[tok * a.n_q_heads + kv * a.n_qh + head] =
-          seen ? __builtin_fmaf(__builtin_amdgcn_logf(L) + M, LN2, lse_s[2 * group] + lse_s[2 * group + 1]) : -__builtin_inff();
   }
   __syncthreads();
-  auto channel = [&](int x) {
-    const f32x4* c = reinterpret_cast<const f32x4*>(&chat_s[x][16 * rpart]);
-    float s = 0.0f;
-    const f32x4 c0 = c[0], c1 = c[1], c2 = c[2], c3 = c[3];
+  if (share == 0) {
+    M = m_s[0];
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-      s = __builtin_fmaf(v0[i], c0[i], s);
-      s = __builtin_fmaf(v1[i], c1[i], s);
-      s = __builtin_fmaf(v2[i], c2[i], s);
-      s = __builtin_fmaf(v3[i], c3[i], s);
+    for (int k = 1; k < SHARE; ++k) M = __builtin_fmaxf(M, m_s[k]);
+    L = A = 0.0f;
+#pragma unroll
+    for (int k = 0; k < SHARE; ++k) {
+      const float f = m_s[k] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m_s[k] - M);
+      L = __builtin_fmaf(f, l_s[k], L);
+      A = __builtin_fmaf(f, sums_s[k][j], A);
     }
-    s += __shfl_xor(s, 1);
-    s += __shfl_xor(s, 2);
-    s += __shfl_xor(s, 4);
-    return s;
-  };
-  float mine = 0.0f;
-#pragma unroll
-  for (int x = 0; x < CR; ++x) {
-    const float s = channel(x);
-    mine = rpart == x ? s : mine;
+    const bool seen = L > 0.0f || L != L;
+    const float c = (sl >= 0 ? A / L : L != L ? L : 0.0f) + mv;
+    chat_s[j] = seen ? c : 0.0f;
+    if (a.lse != nullptr && j == 0)
+      a.lse[tok * a.n_q_heads + kv * a.n_qh + head] = seen ? __builtin_fmaf(__builtin_amdgcn_logf(L) + M, LN2, lse_s[0] + lse_s[1]) : -__builtin_inff();
   }
-  if (rpart < CR) {
-    const int64_t w = row0 + rpart, t = w / a.n_qh;
-    if (w >= n_all) return;
-    const int wb = b_s[t - t_lo];
-    if (wb < 0 || (TREE && !attended(a, paged_seq(a.c, wb)))) return;
-    const int64_t o = (t * a.n_q_heads + kv * a.n_qh + (w - t * a.n_qh)) * D + ri;
+  __syncthreads();
+  const f32x4* c = reinterpret_cast<const f32x4*>(chat_s + 16 * rpart);
+  const f32x4 c0 = c[0], c1 = c[1], c2 = c[2], c3 = c[3];
+  float s = 0.0f;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    s = __builtin_fmaf(v0[i], c0[i], s);
+    s = __builtin_fmaf(v1[i], c1[i], s);
+    s = __builtin_fmaf(v2[i], c2[i], s);
+    s = __builtin_fmaf(v3[i], c3[i], s);
+  }
+  s += __shfl_xor(s, 1);
+  s += __shfl_xor(s, 2);
+  s += __shfl_xor(s, 4);
+  if (rpart == 0) {
+    const int64_t o = (tok * a.n_q_heads + kv * a.n_qh + head) * D + ri;
     if (a.out_f32)
-      reinterpret_cast<float*>(a.out)[o] = mine;
+      reinterpret_cast<float*>(a.out)[o] = s;
     else
-      reinterpret_cast<__bf16*>(a.out)[o] = (__bf16)mine;
+      reinterpret_cast<__bf16*>(a.out)[o] = (__bf16)s;
+  }
+}
+
+// Many rows: 16 to a workgroup, 16 threads a row; then the rotation as 16 x 16 x 32 products of channels and rows, a
+// wavefront 32 channels, both sides in NP bf16 parts.
+constexpr int CO_ROWS = 16, CO_PITCH = D + 4;
+template <bool TREE, int NP>
+__global__ __launch_bounds__(256) void paged_rows_combine_kernel(PagedRowsArgs p, int rows) {
+  __shared__ int32_t b_s[CO_ROWS + 1];
+  __shared__ __attribute__((aligned(16))) float chat_s[CO_ROWS][CO_PITCH];
+  const PagedAttnArgs& a = p.a;
+  const int kv = (int)(blockIdx.x % (unsigned)a.c.n_kv);
+  const int64_t row0 = (int64_t)(blockIdx.x / (unsigned)a.c.n_kv) * CO_ROWS, n_all = a.c.n_new * a.n_qh;
+  const int tid = threadIdx.x, r = tid >> 4, part = tid & 15, lane = tid & 63, col = lane & 15, quarter = lane >> 4, wave = tid >> 6;
+  // the basis: channel 32 wave + 16 t + col, coefficients 32 k + 8 quarter ..
+  f32x4 v[2][4][2];
+#pragma unroll
+  for (int t = 0; t < 2; ++t)
+#pragma unroll
+    for (int k = 0; k < 4; ++k)
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        v[t][k][i] = *reinterpret_cast<const f32x4*>(a.basis_v + ((int64_t)kv * D + 32 * wave + 16 * t + col) * D + 32 * k + 8 * quarter + 4 * i);
+  Kept Kv = read_kept(a.bits_v + kv * NG);
+  if (!Kv.ok || Kv.used > a.Wv) Kv.n = 0;
+  const int64_t t_lo = row0 / a.n_qh, t_hi = (row0 + CO_ROWS - 1) / a.n_qh;
+  sequences_of<256>(a.c, t_lo, (int)(t_hi - t_lo) + 1, b_s);
+  const int64_t row = row0 + r, tok = row / a.n_qh;
+  const int head = (int)(row - tok * a.n_qh);
+  const RowParts parts = row_parts<TREE>(p, rows, row, row < n_all ? b_s[tok - t_lo] : -1, kv);
+  float M = -__builtin_inff(), L = 0.0f;
+  f32x4 A[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
+  constexpr int CB = 4;
+  for (int c0 = 0; c0 < parts.n; c0 += CB) {
+    f32x2 ml[CB];
+    f32x4 x[CB][2];
+#pragma unroll
+    for (int k = 0; k < CB; ++k) {
+      const float* pc = parts.first + (c0 + k < parts.n ? c0 + k : c0) * parts.step;
+      ml[k] = *reinterpret_cast<const f32x2*>(pc);
+      if (c0 + k >= parts.n) ml[k][0] = -__builtin_inff();
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+        if (4 * part + 64 * i < G * Kv.n) x[k][i] = *reinterpret_cast<const f32x4*>(pc + 8 + 4 * part + 64 * i);
+    }
+    float mb = M;
+#pragma unroll
+    for (int k = 0; k < CB; ++k) mb = __builtin_fmaxf(mb, ml[k][0]);
+    if (mb == -__builtin_inff()) continue;
+    const float f = M == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(M - mb);
+    L *= f;
+#pragma unroll
+    for (int i = 0; i < 2; ++i)
+#pragma unroll
+      for (int e = 0; e < 4; ++e) A[i][e] *= f;
+#pragma unroll
+    for (int k = 0; k < CB; ++k) {
+      const float w = ml[k][0] == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(ml[k][0] - mb);
+      L = __builtin_fmaf(w, ml[k][1], L);
+#pragma unroll
+      for (int i = 0; i < 2; ++i)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) A[i][e] = __builtin_fmaf(w, x[k][i][e], A[i][e]);
+    }
+    M = mb;
+  }
+  const bool seen = L > 0.0f || L != L;
+  // coefficients: the means, then what the kept groups have on top (a row of a wavefront alone: its own order)
+#pragma unroll
+  for (int i = 0; i < 2; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      const int j = part + 16 * (4 * i + e);
+      chat_s[r][j] = !seen ? 0.0f : L != L ? L : a.mean_v[(int64_t)kv * D + j];
+    }
+  __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+  __builtin_amdgcn_wave_barrier();
+  if (seen) {
+    const float inv = 1.0f / L;
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+      const int x = 4 * part + 64 * i, sl = x >> 5, place = x & 31;
+      if (sl < Kv.n) {
+        float* c = &chat_s[r][G * pick4(Kv.grp, sl) + 4 * (place >> 3) + ((place & 7) >> 1)];
+        c[0] = __builtin_fmaf(A[i][0], inv, c[0]);
+        c[16] = __builtin_fmaf(A[i][1], inv, c[16]);
+        c[1] = __builtin_fmaf(A[i][2], inv, c[1]);
+        c[17] = __builtin_fmaf(A[i][3], inv, c[17]);
+      }
+    }
+  }
+  if (a.lse != nullptr) {
+    float u = 0.0f;
+    if (parts.live) {
+      const int64_t qo = tok * a.q_token_stride + (kv * a.n_qh + head) * a.q_head_stride;
+#pragma unroll
+      for (int e = 0; e < 8; ++e) u = __builtin_fmaf(query_at(a, qo + part + 16 * e), a.lse_u[kv * D + part + 16 * e], u);
+    }
+#pragma unroll
+    for (int o = 8; o > 0; o >>= 1) u += __shfl_xor(u, o);
+    if (parts.live && part == 0)
+      a.lse[tok * a.n_q_heads + kv * a.n_qh + head] = seen ? __builtin_fmaf(__builtin_amdgcn_logf(L) + M, LN2, u) : -__builtin_inff();
+  }
+  __syncthreads();
+  f32x4 out[2] = {f32x4{0.0f, 0.0f, 0.0f, 0.0f}, f32x4{0.0f, 0.0f, 0.0f, 0.0f}};
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const f32x4 c0 = *reinterpret_cast<const f32x4*>(&chat_s[col][32 * k + 8 * quarter]), c1 = *reinterpret_cast<const f32x4*>(&chat_s[col][32 * k + 8 * quarter + 4]);
+    const float cf[8] = {c0[0], c0[1], c0[2], c0[3], c1[0], c1[1], c1[2], c1[3]};
+    bf16x8 cp[NP];
+    split8_pairs<NP>(cf, cp);
+#pragma unroll
+    for (int t = 0; t < 2; ++t) {
+      const f32x4 x = v[t][k][0], y = v[t][k][1];
+      const float vf[8] = {x[0], x[1], x[2], x[3], y[0], y[1], y[2], y[3]};
+      bf16x8 vp[NP];
+      split8_pairs<NP>(vf, vp);
+#pragma unroll
+      for (int i = 0; i < NP; ++i)
+#pragma unroll
+        for (int j = 0; i + j < NP; ++j) out[t] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vp[i], cp[j], out[t], 0, 0, 0);
+    }
+  }
+  // lane: row `col`, channels 32 wave + 16 t + 4 quarter ..
+  const int64_t w = row0 + col, t = w / a.n_qh;
+  if (w >= n_all) return;
+  const int wb = b_s[t - t_lo];
+  if (wb < 0 || (TREE && !attended(a, paged_seq(a.c, wb)))) return;
+  const int64_t o = (t * a.n_q_heads + kv * a.n_qh + (w - t * a.n_qh)) * D + 32 * wave + 4 * quarter;
+#pragma unroll
+  for (int i = 0; i < 2; ++i) {
+    if (a.out_f32) {
+      *reinterpret_cast<f32x4*>(reinterpret_cast<float*>(a.out) + o + 16 * i) = out[i];
+    } else {
+      const uint32_t lo = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{out[i][0], out[i][1]}, bf16x2));
+      const uint32_t hi = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{out[i][2], out[i][3]}, bf16x2));
+      *reinterpret_cast<u32x2*>(reinterpret_cast<uint16_t*>(a.out) + o + 16 * i) = u32x2{lo, hi};
+    }
   }
 }
 
@@ -795,13 +1082,21 @@ constexpr int64_t kPerCu = 4;  // workgroups wanted of a CU at most
 int64_t tree_units(int32_t batch, int64_t n_new, int32_t n_qh, int rows) { return n_new * n_qh / rows + batch; }
 int64_t wanted(int32_t n_kv) { return N_CU * kPerCu / n_kv > 0 ? N_CU * kPerCu / n_kv : 1; }
 
+template <int NB, bool PRECISE, bool TREE>
+void launch_rows(const PagedRowsArgs& p, dim3 grid, hipStream_t st) {
+  hipLaunchKernelGGL((paged_rows_kernel<NB, PRECISE, TREE>), grid, dim3(RO_NT), 0, st, p);
+}
+
 template <bool TREE>
 hipError_t launch_combine(const PagedRowsArgs& p, int rows, hipStream_t st) {
-  const int64_t all = p.a.c.n_new * p.a.n_qh;
-  if (all * p.a.c.n_kv <= 2 * N_CU)  // a CU holds two of these workgroups
-    hipLaunchKernelGGL((paged_rows_combine_kernel<1, TREE>), dim3((unsigned)(all * p.a.c.n_kv)), dim3(1024), 0, st, p, rows);
+  const int64_t all = p.a.c.n_new * p.a.n_qh, n_kv = p.a.c.n_kv;
+  const dim3 grid((unsigned)(ceil_div(all, CO_ROWS) * n_kv));
+  if (all * n_kv <= 2 * N_CU)  // a CU holds two of these workgroups
+    hipLaunchKernelGGL((paged_row_combine_kernel<TREE>), dim3((unsigned)(all * n_kv)), dim3(1024), 0, st, p, rows);
+  else if (p.a.out_f32)
+    hipLaunchKernelGGL((paged_rows_combine_kernel<TREE, 3>), grid, dim3(256), 0, st, p, rows);
   else
-    hipLaunchKernelGGL((paged_rows_combine_kernel<8, TREE>), dim3((unsigned)(ceil_div(all, 8) * p.a.c.n_kv)), dim3(1024), 0, st, p, rows);
+    hipLaunchKernelGGL((paged_rows_combine_kernel<TREE, 2>), grid, dim3(256), 0, st, p, rows);
   return hipGetLastError();
 }
 
@@ -832,32 +1127,31 @@ hipError_t launch_paged_tree(const PagedRowsArgs& args, void* workspace, hipStre
   const dim3 grid((unsigned)((int64_t)p.items * n_kv));
   if (p.a.out_f32) {
     if (nb == 1)
-      hipLaunchKernelGGL((paged_rows_kernel<1, true, true>), grid, dim3(RO_NT), 0, st, p);
+      launch_rows<1, true, true>(p, grid, st);
     else
-      hipLaunchKernelGGL((paged_rows_kernel<2, true, true>), grid, dim3(RO_NT), 0, st, p);
+      launch_rows<2, true, true>(p, grid, st);
   } else {
     if (nb == 1)
-      hipLaunchKernelGGL((paged_rows_kernel<1, false, true>), grid, dim3(RO_NT), 0, st, p);
+      launch_rows<1, false, true>(p, grid, st);
     else if (nb == 2)
-      hipLaunchKernelGGL((paged_rows_kernel<2, false, true>), grid, dim3(RO_NT), 0, st, p);
+      launch_rows<2, false, true>(p, grid, st);
     else
-      hipLaunchKernelGGL((paged_rows_kernel<4, false, true>), grid, dim3(RO_NT), 0, st, p);
+      launch_rows<4, false, true>(p, grid, st);
   }
   return launch_combine<true>(p, 16 * nb, st);
 }
 
-// Workgroups of a list: about as many in all as the card holds, of four entries at least.
-static int64_t list_chunk(int64_t n_new, int32_t n_kv, int32_t n_blocks) {
-  int64_t n = N_CU * kPerCu / (n_new * n_kv);
-  if (n < 1) n = 1;
-  int64_t each = ceil_div(ceil_div(n_blocks, n), RO_NW) * RO_NW;
-  return each < LIST_CHUNK ? each : LIST_CHUNK;
+// New tokens of a unit: as many as its rows hold, where sequences have several on average and their lists fit.
+static int32_t list_tokens(int32_t batch, int64_t n_new, int32_t n_qh, int32_t n_blocks) {
+  int32_t t = 16 / n_qh;
+  if (t > LIST_ALL / n_blocks) t = LIST_ALL / n_blocks;
+  return n_new >= 2 * (int64_t)batch && n_blocks <= LIST_CHUNK && t > 1 ? t : 1;
 }
 
 size_t paged_sparse_bytes(int64_t n_new, int32_t n_q_heads, int32_t n_kv, int32_t n_blocks) {
-  // chunks of all lists: what the card holds and one more of every list, or whole chunks of 256
-  const int64_t most = N_CU * kPerCu + n_new * n_kv * (1 + ceil_div(n_blocks, LIST_CHUNK));
-  return paged_round((size_t)n_kv * D * sizeof(float)) + (size_t)most * (n_q_heads / n_kv) * PART * sizeof(float);
+  // chunks of all rows: what the card's workgroups hold, and each row's own (more where chunks are full)
+  const int64_t rows = N_CU * kPerCu * 16 + n_new * n_q_heads * (1 + ceil_div(n_blocks, LIST_CHUNK));
+  return paged_round((size_t)n_kv * D * sizeof(float)) + (size_t)rows * PART * sizeof(float);
 }
 
 hipError_t launch_paged_sparse(const PagedRowsArgs& args, void* workspace, hipStream_t st) {
@@ -867,13 +1161,21 @@ hipError_t launch_paged_sparse(const PagedRowsArgs& args, void* workspace, hipSt
   p.a.lse_u = reinterpret_cast<float*>(ws);
   p.partial = reinterpret_cast<float*>(ws + paged_round((size_t)n_kv * D * sizeof(float)));
   if (p.a.lse != nullptr) launch_paged_lse(p.a, st);
-  p.chunk = (int32_t)list_chunk(p.a.c.n_new, n_kv, p.n_blocks);
+  p.tokens = list_tokens(p.a.c.batch, p.a.c.n_new, p.a.n_qh, p.n_blocks);
+  // about as many workgroups as the card holds, of four entries at least
+  const int64_t units = p.tokens == 1 ? p.a.c.n_new : p.a.c.n_new / p.tokens + p.a.c.batch;
+  const int64_t real = ceil_div(p.a.c.n_new, p.tokens) * n_kv;
+  int64_t n = N_CU * kPerCu / real;
+  if (n < 1) n = 1;
+  int64_t each = ceil_div(ceil_div(p.n_blocks, n), RO_NW) * RO_NW;
+  if (p.tokens == 1 && each > LIST_CHUNK) each = LIST_CHUNK;
+  p.chunk = (int32_t)each;
   p.n_chunks = (int32_t)ceil_div(p.n_blocks, p.chunk);
-  const dim3 grid((unsigned)(p.a.c.n_new * n_kv * p.n_chunks));
+  const dim3 grid((unsigned)(units * p.n_chunks * n_kv));
   if (p.a.out_f32)
-    hipLaunchKernelGGL((paged_rows_kernel<1, true, false>), grid, dim3(RO_NT), 0, st, p);
+    launch_rows<1, true, false>(p, grid, st);
   else
-    hipLaunchKernelGGL((paged_rows_kernel<1, false, false>), grid, dim3(RO_NT), 0, st, p);
+    launch_rows<1, false, false>(p, grid, st);
   return launch_combine<false>(p, p.a.n_qh, st);
 }
 

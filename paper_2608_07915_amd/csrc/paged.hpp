@@ -128,7 +128,8 @@ struct PagedRowsArgs {
   const int32_t* parents;  // trees: [n_new]
   const int32_t* blocks;   // lists: [n_new][n_kv][n_blocks]
   int32_t n_blocks;
-  int32_t chunk, n_chunks;  // lists: entries of a workgroup, workgroups of a list
+  int32_t tokens;           // lists: new tokens of a unit
+  int32_t chunk, n_chunks;  // lists: entries of a workgroup (of one token), workgroups of a unit
   int32_t items;            // trees: workgroups per KV head (a bound), and how many are wanted
   int32_t want;
   int32_t* plan;            // trees: workspace, [units][2], a unit's first item and how many it has
