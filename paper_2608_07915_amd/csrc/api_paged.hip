@@ -356,9 +356,9 @@ spectra_status spectra_pages_accept(const spectra_pages* m, const int32_t* rows,
 
 size_t spectra_paged_tree_attention_workspace_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv_heads,
                                                     int32_t max_new, int64_t max_tokens) {
-  if (batch <= 0 || batch > kMaxBatch || n_new <= 0 || max_new <= 0 || max_tokens <= 0 || !heads_ok(n_q_heads, n_kv_heads)) return 0;
+  if (batch <= 0 || batch > kMaxBatch || n_new <= 0 || max_new <= 0 || max_tokens <= 0 || max_tokens > kMost || !heads_ok(n_q_heads, n_kv_heads)) return 0;
   if (n_new > kMostRows / n_q_heads) return 0;
-  return paged_tree_bytes(batch, n_new, n_q_heads, n_kv_heads);
+  return paged_tree_bytes(batch, n_new, n_q_heads, n_kv_heads, max_new, max_tokens);
 }
 
 spectra_status spectra_paged_tree_attention(const spectra_pages* m, const spectra_codec* ck, const spectra_codec* cv,
@@ -386,7 +386,7 @@ spectra_status spectra_paged_tree_attention(const spectra_pages* m, const spectr
   fill_attention(p.a, ck, cv, pool_k, pool_v, q, q_dt, q_token_stride, q_head_stride, n_q_heads, softmax_scale, out, out_dt, lse);
   p.a.max_new = max_new;
   p.a.max_tokens = max_tokens;
-  p.parents = parents;
+  p.a.parents = parents;
   const hipError_t e = launch_paged_tree(p, workspace, (hipStream_t)stream);
   return e == hipSuccess ? SPECTRA_OK : hip_fail(e, "paged_tree_attention launch");
 }

@@ -93,11 +93,15 @@ struct Rows {
   bool live;
   int lim;        // slots that it sees
   int lim_first, lim_last, lim_unit;  // that the block's first row sees, its last, the unit's last
+  int past;       // trees: slots of the history, which every row sees (lim_first; the others: all slots), and of
+  uint64_t own;   // the slots behind it those that the row sees
 };
+template <bool TREE>
 __device__ __forceinline__ Rows rows_of(const PagedAttnArgs& a, const PagedSeq& seq, int64_t tile, int block, int col) {
   const int n_rows = (int)(seq.n * a.n_qh), past = (int)(seq.len - seq.n) + 1;  // slots that token 0 sees
   const int row0 = (int)tile * CA_ROWS + 32 * block, row = row0 + col;
   auto limit = [&](int r) {
+    if constexpr (TREE) return (int)seq.len;
     const int l = past + (r < n_rows ? r : n_rows - 1) / a.n_qh;
     return l < 0 ? 0 : l;
   };
@@ -106,10 +110,16 @@ __device__ __forceinline__ Rows rows_of(const PagedAttnArgs& a, const PagedSeq& 
   const int rc = x.live ? row : n_rows - 1;
   x.tok = rc / a.n_qh;
   x.head = rc - x.tok * a.n_qh;
-  x.lim = past + x.tok < 0 ? 0 : past + x.tok;
+  x.lim = TREE ? (int)seq.len : past + x.tok < 0 ? 0 : past + x.tok;
+  x.past = past - 1;
+  x.own = 0u;
   x.lim_first = __builtin_amdgcn_readfirstlane(limit(row0));
   x.lim_last = __builtin_amdgcn_readfirstlane(limit(row0 + 31));
   x.lim_unit = __builtin_amdgcn_readfirstlane(limit((int)tile * CA_ROWS + CA_ROWS - 1));
+  if constexpr (TREE) {
+    x.own = __shfl(ancestors(a.parents, seq.first, (int)seq.n, threadIdx.x & 63), x.tok);
+    x.lim_first = x.past < 0 ? 0 : x.past;
+  }
   return x;
 }
 
@@ -297,7 +307,15 @@ struct GroupTiles {
 struct Pass {
   int row;  // of the table
   int from, to, lim_first, lim_last;
+  int past;      // trees: as in Rows
+  uint64_t own;
 };
+// Trees: which of the 32 slots from t0 on the lane's row sees, no slot past the pass's last.
+__device__ __forceinline__ uint32_t seen_block(const Pass& pass, int t0) {
+  const uint32_t see = (uint32_t)seen_slots(t0, pass.past, pass.own);
+  const int n = pass.to - t0;
+  return n >= 32 ? see : n <= 0 ? 0u : see & ((1u << n) - 1);
+}
 
 // A lane's row in a row block: the result of a pass.
 struct RowSum {
@@ -337,7 +355,7 @@ __device__ __forceinline__ f16x8 key_operand(const uint8_t* tile, int k, int s, 
 // coefficients takes a fifth of the time (4096 rows of four heads a KV head over 32k slots, two
 // groups: 1.47 ms, 1.17 without it).
 // ---------------------------------------------------------------------------
-template <int NK, int NV>
+template <int NK, int NV, bool TREE>
 __device__ __forceinline__ void chunk_steps(const PagedAttnArgs& a, int kv, const Kept& Kk, const Kept& Kv, const Pass& pass, int lim,
                                             uint8_t* tiles, int wave, int lane, const f16x8 (&qb)[NK][2], f32x16 (&acc)[NV],
                                             RowSum& sum) {
@@ -363,7 +381,12 @@ __device__ __forceinline__ void chunk_steps(const PagedAttnArgs& a, int kv, cons
   // The scores of the block at slot t0 are there: what a row does not see weighs nothing; the
   // reference moves.
   auto settle = [&](f32x16& S, int t0, bool begin) {
-    if (t0 + 32 > pass.lim_first) {
+    if (TREE && t0 + 32 > pass.lim_first) {
+      uint32_t see = seen_block(pass, t0) >> (4 * h);
+      asm volatile("" : "+v"(see));  // a branch, as below
+#pragma unroll
+      for (int i = 0; i < 16; ++i) S[i] = see >> (8 * (i >> 2) + (i & 3)) & 1u ? S[i] : -__builtin_inff();
+    } else if (!TREE && t0 + 32 > pass.lim_first) {
       int left = lim - t0 - 4 * h;
       asm volatile("" : "+v"(left));  // a branch: as selects this took two instructions a score in every block
 #pragma unroll
@@ -372,12 +395,13 @@ __device__ __forceinline__ void chunk_steps(const PagedAttnArgs& a, int kv, cons
     float top = max16(S) - (CA_LIFT + CA_SLACK);
     if (begin) {  // the row's largest score so far (none: left at 0)
       top = __builtin_fmaxf(top, other_half(top));
-      ref = top == -__builtin_inff() ? 0.0f : top + CA_SLACK;
+      // (a row of a tree may see later slots yet: far below all scores)
+      ref = top == -__builtin_inff() ? (TREE ? -1e30f : 0.0f) : top + CA_SLACK;
     } else if (__any(top > ref)) {
       top = __builtin_fmaxf(top, other_half(top));
       const float d = top > ref ? top + CA_SLACK - ref : 0.0f, f = __builtin_amdgcn_exp2f(-d);
       l *= f;
-      ref += d;
+      ref = TREE ? (top > ref ? top + CA_SLACK : ref) : ref + d;
 #pragma unroll
       for (int sl = 0; sl < NV; ++sl)
 #pragma unroll
@@ -634,10 +658,10 @@ __device__ __forceinline__ float rotate_queries(const PagedAttnArgs& a, const Pa
 }
 
 // What a wavefront does, for N groups of each kind (missing ones are zeros).
-template <bool PRECISE, int N>
+template <bool PRECISE, bool TREE, int N>
 __device__ __forceinline__ void chunk_rows(const PagedAttnArgs& a, const PagedSeq& seq, int kv, const Kept& Kk, const Kept& Kv,
                                            int64_t unit, int64_t tile, int part, int wave, int lane, uint8_t* tiles) {
-  const Rows rows = rows_of(a, seq, tile, wave, lane & 31);
+  const Rows rows = rows_of<TREE>(a, seq, tile, wave, lane & 31);
   // the part's slots: those of a unit end at its last row's
   const int n_parts = parts_of(a, rows.lim_unit);
   if (part > 0 && part >= n_parts) return;
@@ -650,6 +674,8 @@ __device__ __forceinline__ void chunk_rows(const PagedAttnArgs& a, const PagedSe
   const int lim = rows.lim < pass.to ? rows.lim : pass.to;
   pass.lim_first = rows.lim_first < pass.to ? rows.lim_first : pass.to;
   pass.lim_last = rows.lim_last;
+  pass.past = rows.past;
+  pass.own = rows.own;
 
   f16x8 qb[N][2], ql[PRECISE ? N : 1][2];
   const float unscale = rotate_queries<PRECISE, N>(a, seq, rows, kv, Kk, lane, qb, ql);
@@ -660,7 +686,7 @@ __device__ __forceinline__ void chunk_rows(const PagedAttnArgs& a, const PagedSe
   if constexpr (PRECISE)
     chunk_steps_precise<N, N>(a, kv, Kk, Kv, pass, lim, unscale, tiles, wave, lane, qb, ql, acc, sum);
   else
-    chunk_steps<N, N>(a, kv, Kk, Kv, pass, lim, tiles, wave, lane, qb, acc, sum);
+    chunk_steps<N, N, TREE>(a, kv, Kk, Kv, pass, lim, tiles, wave, lane, qb, acc, sum);
   const float m = __builtin_fmaxf(sum.m, other_half(sum.m)), l = sum.l + other_half(sum.l);
   if (n_parts > 1) {
     float* p = a.partial + part_at(a, unit, kv, part, wave) + lane;
@@ -680,7 +706,7 @@ __device__ __forceinline__ void chunk_rows(const PagedAttnArgs& a, const PagedSe
 // device and differ from head to head: their cases share nothing but the scalars, so that each
 // has its own registers (with preparation and output outside the switch, the products of two
 // groups ran at the widest case's; as kernels of their own, the heads of one waited for the others').
-template <bool PRECISE>
+template <bool PRECISE, bool TREE>
 __global__ __launch_bounds__(64 * CA_NW, 2) void paged_chunk_kernel(PagedAttnArgs a) {
   extern __shared__ __attribute__((aligned(16))) uint8_t tiles[];
   __shared__ FindScratch find_s;
@@ -696,9 +722,9 @@ __global__ __launch_bounds__(64 * CA_NW, 2) void paged_chunk_kernel(PagedAttnArg
   if (!Kk.ok || Kk.used > a.Wk) Kk.n = 0;  // width table inconsistent with the record
   if (!Kv.ok || Kv.used > a.Wv) Kv.n = 0;
   switch (Kk.n > Kv.n ? Kk.n : Kv.n) {
-    case 4: chunk_rows<PRECISE, 4>(a, seq, kv, Kk, Kv, unit, tile, blockIdx.y, wave, lane, tiles); break;
-    case 3: chunk_rows<PRECISE, 3>(a, seq, kv, Kk, Kv, unit, tile, blockIdx.y, wave, lane, tiles); break;
-    default: chunk_rows<PRECISE, 2>(a, seq, kv, Kk, Kv, unit, tile, blockIdx.y, wave, lane, tiles);
+    case 4: chunk_rows<PRECISE, TREE, 4>(a, seq, kv, Kk, Kv, unit, tile, blockIdx.y, wave, lane, tiles); break;
+    case 3: chunk_rows<PRECISE, TREE, 3>(a, seq, kv, Kk, Kv, unit, tile, blockIdx.y, wave, lane, tiles); break;
+    default: chunk_rows<PRECISE, TREE, 2>(a, seq, kv, Kk, Kv, unit, tile, blockIdx.y, wave, lane, tiles);
   }
 }
 
@@ -714,7 +740,7 @@ __global__ __launch_bounds__(64) void paged_join_kernel(PagedAttnArgs a) {
   int64_t tile;
   if (!find_unit<1>(a, unit, find_s, b, tile)) return;
   const PagedSeq seq = paged_seq(a.c, b);
-  const Rows rows = rows_of(a, seq, tile, block, lane & 31);
+  const Rows rows = rows_of<false>(a, seq, tile, block, lane & 31);
   const int n_parts = parts_of(a, rows.lim_unit);
   if (n_parts <= 1) return;  // done by the part itself
   Kept Kv = read_kept(a.bits_v + kv * NG);
@@ -736,6 +762,62 @@ __global__ __launch_bounds__(64) void paged_join_kernel(PagedAttnArgs a) {
         for (int j = 0; j < 16; ++j) acc[sl][j] = __builtin_fmaf(f, p[(16 * sl + j) * 64 + lane], acc[sl][j]);
   }
   finish_rows<PRECISE ? 3 : 2, NG>(a, seq, rows, kv, Kv, acc, m, l, lane);
+}
+
+// The same for trees: four wavefronts share the parts.
+__global__ __launch_bounds__(256) void paged_tree_join_kernel(PagedAttnArgs a) {
+  constexpr int NW = 4, SIZE = (16 * NG + 2) * 64;
+  __shared__ FindScratch find_s;
+  __shared__ float sums_s[(NW - 1) * SIZE];
+  const int kv = (int)(blockIdx.x % (unsigned)a.c.n_kv), block = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  const int64_t unit = blockIdx.x / (unsigned)a.c.n_kv;
+  int b;
+  int64_t tile;
+  if (!find_unit<NW>(a, unit, find_s, b, tile)) return;
+  const PagedSeq seq = paged_seq(a.c, b);
+  const Rows rows = rows_of<true>(a, seq, tile, block, lane & 31);
+  const int n_parts = parts_of(a, rows.lim_unit);
+  if (n_parts <= 1) return;  // done by the part itself
+  Kept Kv = read_kept(a.bits_v + kv * NG);
+  if (!Kv.ok || Kv.used > a.Wv) Kv.n = 0;
+  float m = -__builtin_inff(), l = 0.0f;
+  f32x16 acc[NG];
+#pragma unroll
+  for (int sl = 0; sl < NG; ++sl) acc[sl] = zero16();
+  auto add = [&](const float* p) __attribute__((always_inline)) {
+    const float mi = p[16 * NG * 64], li = p[(16 * NG + 1) * 64], top = __builtin_fmaxf(m, mi);
+    f32x16 x[NG];
+#pragma unroll
+    for (int sl = 0; sl < NG; ++sl)
+      if (sl < Kv.n)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) x[sl][j] = p[(16 * sl + j) * 64];
+    const float f = m == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(m - top), fi = mi == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(mi - top);
+    l = __builtin_fmaf(fi, li, f * l);
+#pragma unroll
+    for (int sl = 0; sl < NG; ++sl)
+      if (sl < Kv.n)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) acc[sl][j] = __builtin_fmaf(fi, x[sl][j], f * acc[sl][j]);
+    m = top;
+  };
+#pragma unroll 1
+  for (int i = wave; i < n_parts; i += NW) add(a.partial + part_at(a, unit, kv, i, block) + lane);
+  if (wave > 0) {
+    float* p = sums_s + (wave - 1) * SIZE + lane;
+#pragma unroll
+    for (int sl = 0; sl < NG; ++sl)
+      if (sl < Kv.n)
+#pragma unroll
+        for (int j = 0; j < 16; ++j) p[(16 * sl + j) * 64] = acc[sl][j];
+    p[16 * NG * 64] = m;
+    p[(16 * NG + 1) * 64] = l;
+  }
+  __syncthreads();
+  if (wave > 0) return;
+#pragma unroll 1
+  for (int w = 1; w < NW; ++w) add(sums_s + (w - 1) * SIZE + lane);
+  finish_rows<2, NG>(a, seq, rows, kv, Kv, acc, m, l, lane);
 }
 
 // ---------------------------------------------------------------------------
@@ -1031,6 +1113,19 @@ static_assert(PAGED_STEP % (2 * TILE) == 0, "whole steps in a part");
 
 static_assert(CA_ROWS == PAGED_ROWS && CA_NW * (16 * NG + 2) * 64 * sizeof(float) == PAGED_PART_BYTES, "workspace of a part");
 
+// A kept group takes two words at least; two buffers of two slot tiles, or of one in two parts.
+static int chunk_lds(const PagedAttnArgs& a) {
+  auto groups = [](int W) { return W < 6 ? 2 : W / 2 < NG ? W / 2 : NG; };
+  return 2 * 2 * 2 * (groups(a.Wk) > groups(a.Wv) ? groups(a.Wk) : groups(a.Wv)) * CA_TILE;
+}
+
+hipError_t launch_paged_tree_chunks(const PagedAttnArgs& a, int64_t units, hipStream_t st) {
+  const unsigned groups = (unsigned)(units * a.c.n_kv);
+  hipLaunchKernelGGL((paged_chunk_kernel<false, true>), dim3(groups, (unsigned)a.parts), dim3(64 * CA_NW), chunk_lds(a), st, a);
+  if (a.parts > 1) hipLaunchKernelGGL(paged_tree_join_kernel, dim3(groups, CA_NW), dim3(256), 0, st, a);
+  return hipGetLastError();
+}
+
 void launch_paged_lse(const PagedAttnArgs& a, hipStream_t st) {
   hipLaunchKernelGGL(paged_lse_kernel, dim3(a.c.n_kv), dim3(256), 0, st, a);
 }
@@ -1048,14 +1143,12 @@ hipError_t launch_paged_attention(const PagedAttnArgs& args, void* workspace, hi
   if (a.lse != nullptr) launch_paged_lse(a, st);
   hipError_t e = hipSuccess;
   if (p.units > 0) {
-    // a kept group takes two words at least; two buffers of two slot tiles, or of one in two parts
-    auto groups = [](int W) { return W < 6 ? 2 : W / 2 < NG ? W / 2 : NG; };
-    const int lds = 2 * 2 * 2 * (groups(a.Wk) > groups(a.Wv) ? groups(a.Wk) : groups(a.Wv)) * CA_TILE;
+    const int lds = chunk_lds(a);
     const dim3 grid((unsigned)(p.units * a.c.n_kv), (unsigned)p.split.parts), join((unsigned)(p.units * a.c.n_kv), CA_NW);
     if (a.out_f32)
-      hipLaunchKernelGGL((paged_chunk_kernel<true>), grid, dim3(64 * CA_NW), lds, st, a);
+      hipLaunchKernelGGL((paged_chunk_kernel<true, false>), grid, dim3(64 * CA_NW), lds, st, a);
     else
-      hipLaunchKernelGGL((paged_chunk_kernel<false>), grid, dim3(64 * CA_NW), lds, st, a);
+      hipLaunchKernelGGL((paged_chunk_kernel<false, false>), grid, dim3(64 * CA_NW), lds, st, a);
     if (p.split.parts > 1) {
       if (a.out_f32)
         hipLaunchKernelGGL((paged_join_kernel<true>), join, dim3(64), 0, st, a);

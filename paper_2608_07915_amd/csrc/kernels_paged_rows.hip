@@ -25,7 +25,6 @@ namespace spectra_dev {
 
 constexpr int RO_NW = 4, RO_NT = 64 * RO_NW;
 constexpr int RO_PITCH = D + 4;
-constexpr int DRAFT = 64;  // drafted tokens of a sequence at most
 
 // ---------------------------------------------------------------------------
 // Where a workgroup's work lies
@@ -41,7 +40,7 @@ struct RowsScratch {
   int32_t b, at, n;
 };
 
-// Trees: sequence b has ceil(n_b n_qh / rows) units, each cut into chunks of `tiles` tiles, the same
+// Trees of few rows (the others are paged_chunk_kernel's): sequence b has ceil(n_b n_qh / rows) units, each cut into chunks of `tiles` tiles, the same
 // for all, so that about p.want chunks come out; items are the chunks, the sequences' one after the
 // other. The same in every thread.
 __device__ __forceinline__ RowsPlace tree_place(const PagedRowsArgs& p, int rows, int item, RowsScratch& s) {
@@ -51,7 +50,7 @@ __device__ __forceinline__ RowsPlace tree_place(const PagedRowsArgs& p, int rows
     units = tiles = 0;
     if (b >= c.batch) return;
     const PagedSeq q = paged_seq(c, b);
-    if (!attended(p.a, q)) return;
+    if (!scanned(p.a, q)) return;
     units = (int)((q.n * p.a.n_qh + rows - 1) / rows);
     tiles = units > 0 ? (int)((q.len + TILE - 1) / TILE) : 0;
   };
@@ -170,25 +169,6 @@ __device__ __forceinline__ int list_unit(const PagedRowsArgs& p, int64_t u, int3
   if (!has(b, q)) return -1;
   tok0 = at(b, q) * p.tokens;
   return b;
-}
-
-// Of lane i < n: the drafted tokens that token i sees, its ancestors and itself, as bits. Halving by
-// doubled steps: after k of them a lane holds its 2^k nearest.
-__device__ __forceinline__ uint64_t ancestors(const int32_t* __restrict__ parents, int64_t first, int n, int lane) {
-  int up = lane < n ? parents[first + lane] : -1;
-  if (up < 0 || up >= lane) up = -1;
-  uint64_t seen = (uint64_t)1 << lane;
-#pragma unroll
-  for (int k = 0; k < 6; ++k) {
-    const int src = up < 0 ? lane : up;
-    const uint64_t more = __shfl(seen, src);
-    const int next = __shfl(up, src);
-    if (up >= 0) {
-      seen |= more;
-      up = next;
-    }
-  }
-  return seen;
 }
 
 // The chunk's entries of a list [from, to) that name blocks the token sees (below `blocks`) and are
@@ -310,6 +290,22 @@ __device__ __forceinline__ int read_lists(const int32_t* __restrict__ lists, int
   return total;
 }
 
+// u = scale V_K m_K of a KV head, by a workgroup: q . u is the part of the log-sum-exp that the softmax does not need.
+__device__ __forceinline__ void lse_constants(const PagedAttnArgs& a, int kv) {
+  const int ch = threadIdx.x >> 1, half = threadIdx.x & 1;
+  const f32x4* v = reinterpret_cast<const f32x4*>(a.basis_k + ((int64_t)kv * D + ch) * D + 64 * half);
+  const float* m = a.mean_k + kv * D + 64 * half;
+  float s = 0.0f;
+#pragma unroll
+  for (int j = 0; j < 16; ++j) {
+    const f32x4 x = v[j];
+#pragma unroll
+    for (int i = 0; i < 4; ++i) s = __builtin_fmaf(x[i], m[4 * j + i], s);
+  }
+  s += __shfl_xor(s, 1);
+  if (half == 0) a.lse_u[kv * D + ch] = s * (a.scale_log2 * LN2);
+}
+
 // ---------------------------------------------------------------------------
 // The sums of a unit over a chunk. A group's words are loaded while the one before is multiplied (a whole
 // tile ahead, in registers, came to 45 us for 39: 48 tokens of seven heads over 64 blocks).
@@ -334,6 +330,7 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
   const int64_t item = blockIdx.x / (unsigned)a.c.n_kv;
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quarter = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
+  if (a.lse != nullptr && item == 0) lse_constants(a, kv);
   int b, row0 = 0, begin = 0, count, chunk = 0;
   PagedSeq seq;
   int64_t tok0 = 0;  // lists: the unit's first token
@@ -390,7 +387,7 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
     if (!TREE) tok += (int)tok0;
   };
   if constexpr (TREE) {
-    if (wave == 0) anc_s[lane] = ancestors(p.parents, seq.first, (int)seq.n, lane);
+    if (wave == 0) anc_s[lane] = ancestors(a.parents, seq.first, (int)seq.n, lane);
   }
 
   // q': element e of quarter p is that of code 4 p + e / 2 + 16 (e % 2), as the tiles' places are; product y has
@@ -548,231 +545,243 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   };
-  look_up();
-  if (n_units > 0) {
-    enter();
-    fetch(0);
-  }
-  const int64_t past = seq.len - seq.n;  // slots of the history
-  const int64_t common = TREE ? past : past + tok0 + 1;  // slots that every row sees, as far as its list goes
-  f32x4 acc[NG][2][NB];
-  float ref[NB], l[NB];  // the reference less CA_LIFT (-inf: nothing seen yet)
+  // for NV value groups at most: the sums of four are 128 registers at four row blocks, which spill (95 us for ...)
+  auto walk = [&](auto groups) __attribute__((always_inline)) {
+    constexpr int NV = decltype(groups)::value;
+    look_up();
+    if (n_units > 0) {
+      enter();
+      fetch(0);
+    }
+    const int64_t past = seq.len - seq.n;  // slots of the history
+    const int64_t common = TREE ? past : past + tok0 + 1;  // slots that every row sees, as far as its list goes
+    f32x4 acc[NV][2][NB];
+    float ref[NB], l[NB];  // the reference less CA_LIFT (-inf: nothing seen yet)
 #pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    ref[nb] = -__builtin_inff();
-    l[nb] = 0.0f;
+    for (int nb = 0; nb < NB; ++nb) {
+      ref[nb] = -__builtin_inff();
+      l[nb] = 0.0f;
 #pragma unroll
-    for (int sl = 0; sl < NG; ++sl) acc[sl][0][nb] = acc[sl][1][nb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-  }
+      for (int sl = 0; sl < NV; ++sl) acc[sl][0][nb] = acc[sl][1][nb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+    }
 #pragma unroll 1
-  for (int x = wave; x < count; x += RO_NW) {
-    const int64_t t0 = (int64_t)tile_of(x) * TILE;
-    f32x4 S[NB][4];  // slot 16 s + 4 quarter + i
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb)
-#pragma unroll
-      for (int s = 0; s < 4; ++s) S[nb][s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll 1
-    for (int u = 0; u < n_keys; ++u) {
-      expand(u);
-      f16x8 qo[NB][NP];
+    for (int x = wave; x < count; x += RO_NW) {
+      const int64_t t0 = (int64_t)tile_of(x) * TILE;
+      f32x4 S[NB][4];  // slot 16 s + 4 quarter + i
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-        for (int y = 0; y < NP; ++y) qo[nb][y] = as_f16x8(*reinterpret_cast<const u32x4*>(q_s[u][nb][y] + 16 * lane));
+        for (int s = 0; s < 4; ++s) S[nb][s] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll 1
+      for (int u = 0; u < n_keys; ++u) {
+        expand(u);
+        f16x8 qo[NB][NP];
 #pragma unroll
-      for (int s = 0; s < 4; ++s) {
-        const f16x8 kh = as_f16x8(*reinterpret_cast<const u32x4*>(key_at + 16 * 64 * s));
-        if constexpr (!PRECISE) {
+        for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) S[nb][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qo[nb][0], S[nb][s], 0, 0, 0);
-        } else {
-          const f16x8 kl = as_f16x8(*reinterpret_cast<const u32x4*>(key_at + CA_TILE + 16 * 64 * s));
+          for (int y = 0; y < NP; ++y) qo[nb][y] = as_f16x8(*reinterpret_cast<const u32x4*>(q_s[u][nb][y] + 16 * lane));
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb) {
-            const f32x4 z = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-            const f32x4 hi = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qo[nb][0], z, 0, 0, 0);
-            f32x4 lo = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qo[nb][1], z, 0, 0, 0);
-            lo = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl, qo[nb][0], lo, 0, 0, 0);
-            const float un = un_s[u][16 * nb + col];
+        for (int s = 0; s < 4; ++s) {
+          const f16x8 kh = as_f16x8(*reinterpret_cast<const u32x4*>(key_at + 16 * 64 * s));
+          if constexpr (!PRECISE) {
 #pragma unroll
-            for (int i = 0; i < 4; ++i) S[nb][s][i] = __builtin_fmaf(__builtin_fmaf(lo[i], 1.0f / CA_LO, hi[i]), un, S[nb][s][i]);
-          }
-        }
-      }
-    }
-    const uint32_t who = TREE || p.tokens == 1 ? all : (uint32_t)__builtin_amdgcn_readfirstlane(who_s[begin + x]);
-    if (t0 + TILE > common || who != all) {  // some row does not see the whole tile
-      const int64_t rel = t0 - common;
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        uint64_t own = 0u;  // of the slots at and behind `common`
-        int tok, head;
-        row_of(nb, tok, head);
-        if constexpr (TREE)
-          own = anc_s[tok];
-        else
-          own = ((uint64_t)1 << (tok - (int)tok0)) - 1;  // a token sees one slot more than the one before it
-        uint64_t see = rel >= 64 ? 0u : rel >= 0 ? own >> rel : rel > -64 ? (own << -rel) | (((uint64_t)1 << -rel) - 1) : ~(uint64_t)0;
-        if (!TREE && !(who >> (tok - (int)tok0) & 1u)) see = 0u;
-        see >>= 4 * quarter;
-        const uint32_t half[2] = {(uint32_t)see, (uint32_t)(see >> 32)};
-#pragma unroll
-        for (int s = 0; s < 4; ++s)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) S[nb][s][i] = half[s >> 1] & (1u << (16 * (s & 1) + i)) ? S[nb][s][i] : -__builtin_inff();
-      }
-    }
-    float top[NB];
-    bool moves = false;
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      top[nb] = S[nb][0][0];
-#pragma unroll
-      for (int i = 1; i < 16; ++i) top[nb] = __builtin_fmaxf(top[nb], S[nb][i >> 2][i & 3]);
-      top[nb] -= CA_LIFT + CA_SLACK;
-      moves = moves || top[nb] > ref[nb];
-    }
-    if (__any(moves)) {
-#pragma unroll
-      for (int nb = 0; nb < NB; ++nb) {
-        top[nb] = __builtin_fmaxf(top[nb], __shfl_xor(top[nb], 16));
-        top[nb] = __builtin_fmaxf(top[nb], other_half(top[nb]));
-        const float next = top[nb] > ref[nb] ? top[nb] + CA_SLACK : ref[nb];
-        const float f = ref[nb] == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(ref[nb] - next);  // 1: the sums are zeros (or NaN)
-        ref[nb] = next;
-        l[nb] *= f;
-#pragma unroll
-        for (int sl = 0; sl < NG; ++sl)
-#pragma unroll
-          for (int i = 0; i < 8; ++i) acc[sl][i >> 2][nb][i & 3] *= f;
-      }
-    }
-    f16x8 w[NB][2][NP];  // weights of 32 slots: element e is slot 16 (e / 4) + 4 quarter + e % 4
-#pragma unroll
-    for (int nb = 0; nb < NB; ++nb) {
-      const float base = ref[nb] == -__builtin_inff() ? 0.0f : ref[nb];
-#pragma unroll
-      for (int hf = 0; hf < 2; ++hf) {
-        u32x4 xh, xl;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-          const f32x4 s = S[nb][2 * hf + (j >> 1)];
-          const f32x2 e = f32x2{__builtin_amdgcn_exp2f(s[2 * (j & 1)] - base), __builtin_amdgcn_exp2f(s[2 * (j & 1) + 1] - base)};
-          const f16x2 r = __builtin_convertvector(e, f16x2);
-          xh[j] = __builtin_bit_cast(uint32_t, r);
-          if constexpr (PRECISE) {
-            l[nb] += e[0] + e[1];
-            xl[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{(e[0] - (float)r[0]) * CA_LO, (e[1] - (float)r[1]) * CA_LO}, f16x2));
+            for (int nb = 0; nb < NB; ++nb) S[nb][s] = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qo[nb][0], S[nb][s], 0, 0, 0);
           } else {
-            l[nb] = __builtin_amdgcn_fdot2(__builtin_bit_cast(h16x2, r), h16x2{(__fp16)1.0f, (__fp16)1.0f}, l[nb], false);
-          }
-        }
-        w[nb][hf][0] = as_f16x8(xh);
-        if constexpr (PRECISE) w[nb][hf][1] = as_f16x8(xl);
-      }
-    }
-#pragma unroll
-    for (int sl = 0; sl < NG; ++sl) {
-      if (sl < n_units - n_keys) {
-        expand(n_keys + sl);
-#pragma unroll
-        for (int y = 0; y < 2; ++y) {
-          f32x4 lo[NB];
-#pragma unroll
-          for (int nb = 0; nb < NB; ++nb) lo[nb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-#pragma unroll
-          for (int hf = 0; hf < 2; ++hf) {
-            const uint8_t* pt = (y ? val_at1 : val_at0) + 32 * 64 * hf;
-            const u32x2 y0 = read_transposed(pt), y1 = read_transposed(pt + 16 * 64);
-            const f16x8 vh = as_f16x8(u32x4{y0[0], y0[1], y1[0], y1[1]});
-            f16x8 vl = vh;
-            if constexpr (PRECISE) {
-              const u32x2 z0 = read_transposed(pt + CA_TILE), z1 = read_transposed(pt + CA_TILE + 16 * 64);
-              vl = as_f16x8(u32x4{z0[0], z0[1], z1[0], z1[1]});
-            }
+            const f16x8 kl = as_f16x8(*reinterpret_cast<const u32x4*>(key_at + CA_TILE + 16 * 64 * s));
 #pragma unroll
             for (int nb = 0; nb < NB; ++nb) {
-              acc[sl][y][nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, w[nb][hf][0], acc[sl][y][nb], 0, 0, 0);
-              if constexpr (PRECISE) {
-                lo[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vl, w[nb][hf][0], lo[nb], 0, 0, 0);
-                lo[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, w[nb][hf][NP - 1], lo[nb], 0, 0, 0);
-              }
+              const f32x4 z = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+              const f32x4 hi = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qo[nb][0], z, 0, 0, 0);
+              f32x4 lo = __builtin_amdgcn_mfma_f32_16x16x32_f16(kh, qo[nb][1], z, 0, 0, 0);
+              lo = __builtin_amdgcn_mfma_f32_16x16x32_f16(kl, qo[nb][0], lo, 0, 0, 0);
+              const float un = un_s[u][16 * nb + col];
+#pragma unroll
+              for (int i = 0; i < 4; ++i) S[nb][s][i] = __builtin_fmaf(__builtin_fmaf(lo[i], 1.0f / CA_LO, hi[i]), un, S[nb][s][i]);
             }
           }
-          if constexpr (PRECISE) {
+        }
+      }
+      const uint32_t who = TREE || p.tokens == 1 ? all : (uint32_t)__builtin_amdgcn_readfirstlane(who_s[begin + x]);
+      if (t0 + TILE > common || who != all) {  // some row does not see the whole tile
 #pragma unroll
-            for (int nb = 0; nb < NB; ++nb)
+        for (int nb = 0; nb < NB; ++nb) {
+          uint64_t own = 0u;  // of the slots at and behind `common`
+          int tok, head;
+          row_of(nb, tok, head);
+          if constexpr (TREE)
+            own = anc_s[tok];
+          else
+            own = ((uint64_t)1 << (tok - (int)tok0)) - 1;  // a token sees one slot more than the one before it
+          uint64_t see = seen_slots(t0, common, own);
+          if (!TREE && !(who >> (tok - (int)tok0) & 1u)) see = 0u;
+          see >>= 4 * quarter;
+          const uint32_t half[2] = {(uint32_t)see, (uint32_t)(see >> 32)};
 #pragma unroll
-              for (int i = 0; i < 4; ++i) acc[sl][y][nb][i] = __builtin_fmaf(lo[nb][i], 1.0f / CA_LO, acc[sl][y][nb][i]);
+          for (int s = 0; s < 4; ++s)
+#pragma unroll
+            for (int i = 0; i < 4; ++i) S[nb][s][i] = half[s >> 1] & (1u << (16 * (s & 1) + i)) ? S[nb][s][i] : -__builtin_inff();
+        }
+      }
+      float top[NB];
+      bool moves = false;
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        top[nb] = S[nb][0][0];
+#pragma unroll
+        for (int i = 1; i < 16; ++i) top[nb] = __builtin_fmaxf(top[nb], S[nb][i >> 2][i & 3]);
+        top[nb] -= CA_LIFT + CA_SLACK;
+        moves = moves || top[nb] > ref[nb];
+      }
+      if (__any(moves)) {
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          top[nb] = __builtin_fmaxf(top[nb], __shfl_xor(top[nb], 16));
+          top[nb] = __builtin_fmaxf(top[nb], other_half(top[nb]));
+          const float next = top[nb] > ref[nb] ? top[nb] + CA_SLACK : ref[nb];
+          const float f = ref[nb] == -__builtin_inff() ? 1.0f : __builtin_amdgcn_exp2f(ref[nb] - next);  // 1: the sums are zeros (or NaN)
+          ref[nb] = next;
+          l[nb] *= f;
+#pragma unroll
+          for (int sl = 0; sl < NV; ++sl)
+#pragma unroll
+            for (int i = 0; i < 8; ++i) acc[sl][i >> 2][nb][i & 3] *= f;
+        }
+      }
+      f16x8 w[NB][2][NP];  // weights of 32 slots: element e is slot 16 (e / 4) + 4 quarter + e % 4
+#pragma unroll
+      for (int nb = 0; nb < NB; ++nb) {
+        const float base = ref[nb] == -__builtin_inff() ? 0.0f : ref[nb];
+#pragma unroll
+        for (int hf = 0; hf < 2; ++hf) {
+          u32x4 xh, xl;
+#pragma unroll
+          for (int j = 0; j < 4; ++j) {
+            const f32x4 s = S[nb][2 * hf + (j >> 1)];
+            const f32x2 e = f32x2{__builtin_amdgcn_exp2f(s[2 * (j & 1)] - base), __builtin_amdgcn_exp2f(s[2 * (j & 1) + 1] - base)};
+            const f16x2 r = __builtin_convertvector(e, f16x2);
+            xh[j] = __builtin_bit_cast(uint32_t, r);
+            if constexpr (PRECISE) {
+              l[nb] += e[0] + e[1];
+              xl[j] = __builtin_bit_cast(uint32_t, __builtin_convertvector(f32x2{(e[0] - (float)r[0]) * CA_LO, (e[1] - (float)r[1]) * CA_LO}, f16x2));
+            } else {
+              l[nb] = __builtin_amdgcn_fdot2(__builtin_bit_cast(h16x2, r), h16x2{(__fp16)1.0f, (__fp16)1.0f}, l[nb], false);
+            }
+          }
+          w[nb][hf][0] = as_f16x8(xh);
+          if constexpr (PRECISE) w[nb][hf][1] = as_f16x8(xl);
+        }
+      }
+#pragma unroll
+      for (int sl = 0; sl < NV; ++sl) {
+        if (sl < n_units - n_keys) {
+          expand(n_keys + sl);
+#pragma unroll
+          for (int y = 0; y < 2; ++y) {
+            f32x4 lo[NB];
+#pragma unroll
+            for (int nb = 0; nb < NB; ++nb) lo[nb] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+#pragma unroll
+            for (int hf = 0; hf < 2; ++hf) {
+              const uint8_t* pt = (y ? val_at1 : val_at0) + 32 * 64 * hf;
+              const u32x2 y0 = read_transposed(pt), y1 = read_transposed(pt + 16 * 64);
+              const f16x8 vh = as_f16x8(u32x4{y0[0], y0[1], y1[0], y1[1]});
+              f16x8 vl = vh;
+              if constexpr (PRECISE) {
+                const u32x2 z0 = read_transposed(pt + CA_TILE), z1 = read_transposed(pt + CA_TILE + 16 * 64);
+                vl = as_f16x8(u32x4{z0[0], z0[1], z1[0], z1[1]});
+              }
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb) {
+                acc[sl][y][nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, w[nb][hf][0], acc[sl][y][nb], 0, 0, 0);
+                if constexpr (PRECISE) {
+                  lo[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vl, w[nb][hf][0], lo[nb], 0, 0, 0);
+                  lo[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, w[nb][hf][NP - 1], lo[nb], 0, 0, 0);
+                }
+              }
+            }
+            if constexpr (PRECISE) {
+#pragma unroll
+              for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+                for (int i = 0; i < 4; ++i) acc[sl][y][nb][i] = __builtin_fmaf(lo[nb][i], 1.0f / CA_LO, acc[sl][y][nb][i]);
+            }
           }
         }
       }
     }
-  }
-  // merge of the wavefronts, and the chunk's partial of every row, 16 rows at a time
-  // (lists: [chunk][token][KV head][query head], trees: [item][KV head][row])
-  float* part = p.partial + (item * a.c.n_kv + kv) * (int64_t)(ROWS * PART);
-  const int64_t token_step = (int64_t)a.c.n_kv * a.n_qh * PART;
-  if (!TREE) part = p.partial + ((chunk * a.c.n_new + seq.first + tok0) * a.c.n_kv + kv) * (int64_t)(a.n_qh * PART);
-  float m[NB];
+    // merge of the wavefronts, and the chunk's partial of every row, 16 rows at a time
+    // (lists: [chunk][token][KV head][query head], trees: [item][KV head][row])
+    float* part = p.partial + (item * a.c.n_kv + kv) * (int64_t)(ROWS * PART);
+    const int64_t token_step = (int64_t)a.c.n_kv * a.n_qh * PART;
+    if (!TREE) part = p.partial + ((chunk * a.c.n_new + seq.first + tok0) * a.c.n_kv + kv) * (int64_t)(a.n_qh * PART);
+    float m[NB];
 #pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    float ll = l[nb] + __shfl_xor(l[nb], 16);
-    ll += other_half(ll);
-    m[nb] = ll == 0.0f ? -__builtin_inff() : ref[nb] == -__builtin_inff() ? 0.0f : ref[nb];
-    if (quarter == 0) {
-      m_s[wave][16 * nb + col] = m[nb];
-      l_s[wave][16 * nb + col] = ll;
-    }
-  }
-  __syncthreads();  // the maxima; the tiles have been read
-  auto factor = [&](float mine, float top) __attribute__((always_inline)) { return mine == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(mine - top); };
-  auto top_of = [&](int r) __attribute__((always_inline)) {
-    float t = m_s[0][r];
-#pragma unroll
-    for (int v = 1; v < RO_NW; ++v) t = __builtin_fmaxf(t, m_s[v][r]);
-    return t;
-  };
-#pragma unroll
-  for (int nb = 0; nb < NB; ++nb) {
-    if (16 * nb >= n_rows) break;
-    const float f = factor(m[nb], top_of(16 * nb + col));
-#pragma unroll
-    for (int sl = 0; sl < NG; ++sl)
-      if (sl < Kv.n)
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-          *reinterpret_cast<f32x4*>(sums_s + (wave * 16 + col) * RO_PITCH + G * sl + 16 * y + 4 * quarter) =
-              f32x4{acc[sl][y][nb][0] * f, acc[sl][y][nb][1] * f, acc[sl][y][nb][2] * f, acc[sl][y][nb][3] * f};
-    __syncthreads();
-    const int here = n_rows - 16 * nb < 16 ? n_rows - 16 * nb : 16;
-    auto out = [&](int r) __attribute__((always_inline)) {
-      const int row = 16 * nb + r, tok = TREE ? 0 : row / a.n_qh;
-      return part + tok * token_step + (row - tok * a.n_qh) * PART;
-    };
-    // sums as they lie: [kept group][place]
-    for (int e = tid; e < here * (D / 4); e += RO_NT) {
-      const int r = e / (D / 4), x = 4 * (e % (D / 4));
-      if (x >= G * Kv.n) continue;
-      f32x4 sum = *reinterpret_cast<const f32x4*>(sums_s + r * RO_PITCH + x);
-#pragma unroll
-      for (int v = 1; v < RO_NW; ++v) {
-        const f32x4 y = *reinterpret_cast<const f32x4*>(sums_s + (v * 16 + r) * RO_PITCH + x);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) sum[i] += y[i];
+    for (int nb = 0; nb < NB; ++nb) {
+      float ll = l[nb] + __shfl_xor(l[nb], 16);
+      ll += other_half(ll);
+      m[nb] = ll == 0.0f ? -__builtin_inff() : ref[nb] == -__builtin_inff() ? 0.0f : ref[nb];
+      if (quarter == 0) {
+        m_s[wave][16 * nb + col] = m[nb];
+        l_s[wave][16 * nb + col] = ll;
       }
-      *reinterpret_cast<f32x4*>(out(r) + 8 + x) = sum;
     }
-    if (tid < here) {
-      const int r = 16 * nb + tid;
-      const float top = top_of(r);
-      float total = 0.0f;
+    __syncthreads();  // the maxima; the tiles have been read
+    auto factor = [&](float mine, float top) __attribute__((always_inline)) { return mine == -__builtin_inff() ? 0.0f : __builtin_amdgcn_exp2f(mine - top); };
+    auto top_of = [&](int r) __attribute__((always_inline)) {
+      float t = m_s[0][r];
 #pragma unroll
-      for (int v = 0; v < RO_NW; ++v) total = __builtin_fmaf(factor(m_s[v][r], top), l_s[v][r], total);
-      *reinterpret_cast<f32x2*>(out(tid)) = f32x2{top, total};
+      for (int v = 1; v < RO_NW; ++v) t = __builtin_fmaxf(t, m_s[v][r]);
+      return t;
+    };
+#pragma unroll
+    for (int nb = 0; nb < NB; ++nb) {
+      if (16 * nb >= n_rows) break;
+      const float f = factor(m[nb], top_of(16 * nb + col));
+#pragma unroll
+      for (int sl = 0; sl < NV; ++sl)
+        if (sl < Kv.n)
+#pragma unroll
+          for (int y = 0; y < 2; ++y)
+            *reinterpret_cast<f32x4*>(sums_s + (wave * 16 + col) * RO_PITCH + G * sl + 16 * y + 4 * quarter) =
+                f32x4{acc[sl][y][nb][0] * f, acc[sl][y][nb][1] * f, acc[sl][y][nb][2] * f, acc[sl][y][nb][3] * f};
+      __syncthreads();
+      const int here = n_rows - 16 * nb < 16 ? n_rows - 16 * nb : 16;
+      auto out = [&](int r) __attribute__((always_inline)) {
+        const int row = 16 * nb + r, tok = TREE ? 0 : row / a.n_qh;
+        return part + tok * token_step + (row - tok * a.n_qh) * PART;
+      };
+      // sums as they lie: [kept group][place]
+      for (int e = tid; e < here * (D / 4); e += RO_NT) {
+        const int r = e / (D / 4), x = 4 * (e % (D / 4));
+        if (x >= G * Kv.n) continue;
+        f32x4 sum = *reinterpret_cast<const f32x4*>(sums_s + r * RO_PITCH + x);
+#pragma unroll
+        for (int v = 1; v < RO_NW; ++v) {
+          const f32x4 y = *reinterpret_cast<const f32x4*>(sums_s + (v * 16 + r) * RO_PITCH + x);
+#pragma unroll
+          for (int i = 0; i < 4; ++i) sum[i] += y[i];
+        }
+        *reinterpret_cast<f32x4*>(out(r) + 8 + x) = sum;
+      }
+      if (tid < here) {
+        const int r = 16 * nb + tid;
+        const float top = top_of(r);
+        float total = 0.0f;
+#pragma unroll
+        for (int v = 0; v < RO_NW; ++v) total = __builtin_fmaf(factor(m_s[v][r], top), l_s[v][r], total);
+        *reinterpret_cast<f32x2*>(out(tid)) = f32x2{top, total};
+      }
+      if (nb + 1 < NB) __syncthreads();  // the sums have been read
     }
-    if (nb + 1 < NB) __syncthreads();  // the sums have been read
+  };
+  if constexpr (NB < 4) {
+    walk(std::integral_constant<int, NG>{});
+  } else {
+    switch (Kv.n) {
+      case 4: walk(std::integral_constant<int, 4>{}); break;
+      case 3: walk(std::integral_constant<int, 3>{}); break;
+      default: walk(std::integral_constant<int, 2>{});
+    }
   }
 }
 
@@ -796,7 +805,7 @@ __device__ __forceinline__ RowParts row_parts(const PagedRowsArgs& p, int rows, 
   const int head = (int)(row - tok * a.n_qh);
   if constexpr (TREE) {
     const PagedSeq seq = paged_seq(a.c, b);
-    r.live = attended(a, seq);
+    r.live = scanned(a, seq);
     r.step = (int64_t)a.c.n_kv * rows * PART;
     if (!r.live || seq.len <= 0) return r;
     const int64_t in_seq = (tok - seq.first) * a.n_qh + head, unit = in_seq / rows;
@@ -1056,7 +1065,7 @@ __global__ __launch_bounds__(256) void paged_rows_combine_kernel(PagedRowsArgs p
   const int64_t w = row0 + col, t = w / a.n_qh;
   if (w >= n_all) return;
   const int wb = b_s[t - t_lo];
-  if (wb < 0 || (TREE && !attended(a, paged_seq(a.c, wb)))) return;
+  if (wb < 0 || (TREE && !scanned(a, paged_seq(a.c, wb)))) return;
   const int64_t o = (t * a.n_q_heads + kv * a.n_qh + (w - t * a.n_qh)) * D + 32 * wave + 4 * quarter;
 #pragma unroll
   for (int i = 0; i < 2; ++i) {
@@ -1102,28 +1111,49 @@ hipError_t launch_combine(const PagedRowsArgs& p, int rows, hipStream_t st) {
 
 }  // namespace
 
-// The plan and the partials of any unit size.
-size_t paged_tree_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv) {
-  const int64_t n_qh = n_q_heads / n_kv;
+// With 16-bit outputs sequences of more rows on a KV head are paged_chunk_kernel's, in units of 256 rows that share the
+// making of the coefficients (64 tokens of seven heads over 131k slots 191 us and 242; up to 128 rows, which leave half of
+// its wavefronts empty, 16 trees of up to 32 tokens of four heads 176 and 108).
+constexpr int64_t kFewRows = 128;
+
+// The plan and the partials of any unit size, and the parts of the others' units.
+size_t paged_tree_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv, int32_t max_new, int64_t max_tokens) {
+  (void)max_tokens;
+  const int32_t n_qh = n_q_heads / n_kv;
   const size_t lse = paged_round((size_t)n_kv * D * sizeof(float));
-  const size_t plan = paged_round((size_t)tree_units(batch, n_new, (int32_t)n_qh, 16) * 2 * sizeof(int32_t));
-  return lse + plan + (size_t)((wanted(n_kv) + batch) * 64 + n_new * n_qh) * n_kv * PART * sizeof(float);
+  const size_t plan = paged_round((size_t)tree_units(batch, n_new, n_qh, 16) * 2 * sizeof(int32_t));
+  const size_t b = lse + plan + paged_round((size_t)((wanted(n_kv) + batch) * 64 + n_new * n_qh) * n_kv * PART * sizeof(float));
+  // (split calls have at most two parts for a CU)
+  return b + (max_new * n_qh > kFewRows ? 2 * N_CU * PAGED_PART_BYTES : 0);
 }
 
 hipError_t launch_paged_tree(const PagedRowsArgs& args, void* workspace, hipStream_t st) {
   PagedRowsArgs p = args;
-  const int32_t n_kv = p.a.c.n_kv, batch = p.a.c.batch;
+  const int32_t n_kv = p.a.c.n_kv, batch = p.a.c.batch, n_qh = p.a.n_qh;
+  const int64_t n_new = p.a.c.n_new, few = kFewRows / n_qh;
   char* ws = static_cast<char*>(workspace);
   p.a.lse_u = reinterpret_cast<float*>(ws);
   ws += paged_round((size_t)n_kv * D * sizeof(float));
   p.plan = reinterpret_cast<int32_t*>(ws);
-  ws += paged_round((size_t)tree_units(batch, p.a.c.n_new, p.a.n_qh, 16) * 2 * sizeof(int32_t));
+  ws += paged_round((size_t)tree_units(batch, n_new, n_qh, 16) * 2 * sizeof(int32_t));
   p.partial = reinterpret_cast<float*>(ws);
-  if (p.a.lse != nullptr) launch_paged_lse(p.a, st);
-  const int64_t most = (int64_t)p.a.max_new * p.a.n_qh;
+  ws += paged_round((size_t)((wanted(n_kv) + batch) * 64 + n_new * n_qh) * n_kv * PART * sizeof(float));
+  // none of few rows where every sequence has max_new; with fp32 outputs all are
+  p.a.scan_tokens = (int32_t)(p.a.out_f32 || p.a.max_new <= few ? p.a.max_new : n_new < (int64_t)batch * p.a.max_new ? few : 0);
+  if (p.a.max_new > p.a.scan_tokens) {
+    const int64_t units = paged_units(batch, n_new, n_qh, p.a.max_new);
+    const ChunkSplit split = paged_chunk_split(units * n_kv, p.a.max_tokens);
+    p.a.part_slots = split.slots;
+    p.a.parts = split.parts;
+    p.a.partial = reinterpret_cast<float*>(ws);
+    if (p.a.lse != nullptr) launch_paged_lse(p.a, st);
+    const hipError_t e = launch_paged_tree_chunks(p.a, units, st);
+    if (e != hipSuccess || p.a.scan_tokens == 0) return e;
+  }
+  const int64_t most = (int64_t)(p.a.max_new < p.a.scan_tokens ? p.a.max_new : p.a.scan_tokens) * n_qh;
   const int nb = most <= 16 ? 1 : most <= 32 || p.a.out_f32 ? 2 : 4;
   p.want = (int32_t)(nb == 1 ? wanted(n_kv) : (wanted(n_kv) + 1) / 2);
-  p.items = (int32_t)(p.want + tree_units(batch, p.a.c.n_new, p.a.n_qh, 16 * nb));
+  p.items = (int32_t)(p.want + tree_units(batch, n_new, n_qh, 16 * nb));
   const dim3 grid((unsigned)((int64_t)p.items * n_kv));
   if (p.a.out_f32) {
     if (nb == 1)
@@ -1160,7 +1190,6 @@ hipError_t launch_paged_sparse(const PagedRowsArgs& args, void* workspace, hipSt
   char* ws = static_cast<char*>(workspace);
   p.a.lse_u = reinterpret_cast<float*>(ws);
   p.partial = reinterpret_cast<float*>(ws + paged_round((size_t)n_kv * D * sizeof(float)));
-  if (p.a.lse != nullptr) launch_paged_lse(p.a, st);
   p.tokens = list_tokens(p.a.c.batch, p.a.c.n_new, p.a.n_qh, p.n_blocks);
   // about as many workgroups as the card holds, of four entries at least
   const int64_t units = p.tokens == 1 ? p.a.c.n_new : p.a.c.n_new / p.tokens + p.a.c.batch;

@@ -92,6 +92,7 @@ struct PagedAttnArgs {
   int64_t part_slots;
   int32_t parts;
   float* partial;
+  const int32_t* parents;  // drafted trees: of each new token, among its sequence's; otherwise not used
 };
 
 struct PagedBoundsArgs {
@@ -125,7 +126,6 @@ struct PagedSelectArgs {
 // Attention of a few rows a sequence (drafted trees) or a token (listed blocks) over tiles.
 struct PagedRowsArgs {
   PagedAttnArgs a;
-  const int32_t* parents;  // trees: [n_new]
   const int32_t* blocks;   // lists: [n_new][n_kv][n_blocks]
   int32_t n_blocks;
   int32_t tokens;           // lists: new tokens of a unit
@@ -148,7 +148,9 @@ size_t paged_select_bytes(int64_t n_new, int32_t n_q_heads, int32_t n_kv, int64_
 hipError_t launch_paged_select(const spectra_dev::PagedSelectArgs& a, void* workspace, hipStream_t st);
 // The constants of the log-sum-exp (a.lse_u) of every KV head.
 void launch_paged_lse(const spectra_dev::PagedAttnArgs& a, hipStream_t st);
-size_t paged_tree_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv);
+size_t paged_tree_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv, int32_t max_new, int64_t max_tokens);
+// Drafted trees of the sequences of more than a.scan_tokens new tokens, 16-bit outputs: `units` of PAGED_ROWS rows.
+hipError_t launch_paged_tree_chunks(const spectra_dev::PagedAttnArgs& a, int64_t units, hipStream_t st);
 size_t paged_sparse_bytes(int64_t n_new, int32_t n_q_heads, int32_t n_kv, int32_t n_blocks);
 hipError_t launch_paged_tree(const spectra_dev::PagedRowsArgs& p, void* workspace, hipStream_t st);
 hipError_t launch_paged_sparse(const spectra_dev::PagedRowsArgs& p, void* workspace, hipStream_t st);

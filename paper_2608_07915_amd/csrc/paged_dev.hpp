@@ -51,6 +51,32 @@ __device__ __forceinline__ bool scanned(const PagedAttnArgs& a, const PagedSeq& 
   return s.n > 0 && s.n <= a.scan_tokens && attended(a, s);
 }
 
+constexpr int DRAFT = 64;  // drafted tokens of a sequence at most
+// Of lane i < n: the drafted tokens that token i sees, its ancestors and itself, as bits. By doubled steps:
+// after k of them a lane holds its 2^k nearest. A parent that is no earlier token counts as none.
+__device__ __forceinline__ uint64_t ancestors(const int32_t* __restrict__ parents, int64_t first, int n, int lane) {
+  int up = lane < n ? parents[first + lane] : -1;
+  if (up < 0 || up >= lane) up = -1;
+  uint64_t seen = (uint64_t)1 << lane;
+#pragma unroll
+  for (int k = 0; k < 6; ++k) {
+    const int src = up < 0 ? lane : up;
+    const uint64_t more = __shfl(seen, src);
+    const int next = __shfl(up, src);
+    if (up >= 0) {
+      seen |= more;
+      up = next;
+    }
+  }
+  return seen;
+}
+// Which of the 64 slots from t0 on are seen by a row that sees all slots before `past`, and behind those the
+// ones of `own`.
+__device__ __forceinline__ uint64_t seen_slots(int64_t t0, int64_t past, uint64_t own) {
+  const int64_t rel = t0 - past;
+  return rel >= 64 ? 0u : rel >= 0 ? own >> rel : rel > -64 ? (own << -rel) | (((uint64_t)1 << -rel) - 1) : ~(uint64_t)0;
+}
+
 // Where the scan's work lies: chunks of tiles_per_chunk tiles, the sequences' one after the
 // other (items), about as many as the call has workgroups for (p.scan_items). The length of a
 // chunk comes from what the sequences hold, not from the longest that the call allows.

@@ -180,6 +180,18 @@ def test_queries_that_are_not_finite_reach_no_other_row(f32):
     assert torch.isfinite(lse[~bad]).all()
 
 
+@pytest.mark.parametrize("f32", [False, True], ids=["bf16", "f32"])
+@pytest.mark.parametrize("n_qh", [1, 4])
+def test_rows_that_see_their_own_slot_alone(n_qh, f32):
+    """No history, no parents: a token's weight lies on its own slot, however low its score."""
+    lens, new = [64, 40, 33], [64, 40, 33]
+    for q_scale in (2.0, 12.0):
+        c = cache(lens, new, n_qh=n_qh, f32=f32, seed=14, q_scale=q_scale)
+        p = tree("star", new)
+        lse = torch.empty(c.q.shape[:2], device="cuda")
+        check(c, tree_sees(lens, new, p), attend(c, p, lse=lse), lse)
+
+
 def test_pages_out_of_range_and_many_sequences():
     lens, new = [300, 64, 130], [20, 8, 64]
     c = cache(lens, new, seed=10)
