@@ -16,16 +16,17 @@ namespace spectra_dev {
 constexpr int BOX = 2 * G;             // fp16 of a group in a box: the least, then the largest
 constexpr int BOX_WORDS = NG * BOX / 2;  // words of a block's box
 
-// The sequence that new token `t` belongs to (the last one that begins at or before it), -1: none.
-// cu is searched by halves: log2(batch) dependent loads, a lane's own.
-__device__ __forceinline__ int sequence_of(const PagedCache& c, int64_t t) {
-  int lo = 0, hi = c.batch;  // first b with cu[b] > t lies in (lo, hi]
-  if (c.batch == 0 || c.cu[0] > t) return -1;
+// The sequence that new token `t` belongs to (the last one that begins at or before it), -1: none; starts(b) is
+// cu[b]. Searched by halves, a lane for itself.
+template <typename Starts>
+__device__ __forceinline__ int sequence_of(int batch, int64_t t, Starts&& starts) {
+  int lo = 0, hi = batch;  // first b with cu[b] > t lies in (lo, hi]
+  if (batch == 0 || starts(0) > t) return -1;
   while (hi - lo > 1) {
     const int mid = (lo + hi) >> 1;
-    if (c.cu[mid] <= t) lo = mid; else hi = mid;
+    if (starts(mid) <= t) lo = mid; else hi = mid;
   }
-  return t < c.cu[lo + 1] ? lo : -1;
+  return t < starts(lo + 1) ? lo : -1;
 }
 
 // ---------------------------------------------------------------------------
@@ -34,10 +35,20 @@ __device__ __forceinline__ int sequence_of(const PagedCache& c, int64_t t) {
 // holds one slot's coefficients, fp16 pairs as the attention kernels make them, and the 64 slots
 // are reduced by halving: at each of four exchanges a lane keeps half of its coefficients, the last
 // two within quads (per group 34 exchanges instead of 192). Words of HBM once, 128 bytes written
-// a group.
+// a group. The starts of up to BOX_STARTS sequences are searched in LDS.
 // ---------------------------------------------------------------------------
-__device__ __forceinline__ f16x2 pk_min(f16x2 a, f16x2 b) { return __builtin_elementwise_min(a, b); }
-__device__ __forceinline__ f16x2 pk_max(f16x2 a, f16x2 b) { return __builtin_elementwise_max(a, b); }
+// (as instructions: the compiler first makes every operand quiet, which doubles them; nothing here is NaN)
+__device__ __forceinline__ f16x2 pk_min(f16x2 a, f16x2 b) {
+  f16x2 d;
+  asm("v_pk_min_f16 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b));
+  return d;
+}
+__device__ __forceinline__ f16x2 pk_max(f16x2 a, f16x2 b) {
+  f16x2 d;
+  asm("v_pk_max_f16 %0, %1, %2" : "=v"(d) : "v"(a), "v"(b));
+  return d;
+}
+constexpr int BOX_STARTS = 512;
 template <int CTRL>
 __device__ __forceinline__ f16x2 dpp_pair(f16x2 v) {
   return __builtin_bit_cast(f16x2, __builtin_amdgcn_mov_dpp(__builtin_bit_cast(int, v), CTRL, 0xF, 0xF, true));
@@ -71,14 +82,20 @@ __device__ __forceinline__ f16x2 reduce_slots(const f16x2 (&r)[16], int lane, Op
 }
 
 __global__ __launch_bounds__(256) void paged_bounds_kernel(PagedBoundsArgs a) {
+  __shared__ int32_t starts_s[BOX_STARTS];
   const int lane = threadIdx.x & 63;
   const int64_t w = (int64_t)blockIdx.x * 4 + __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const int kv = (int)(w % a.c.n_kv);
   const int64_t t = w / a.c.n_kv * a.tokens + lane;
+  const bool in_lds = a.c.batch < BOX_STARTS;
+  if (in_lds) {
+    for (int i = threadIdx.x; i <= a.c.batch; i += 256) starts_s[i] = a.c.cu[i];
+    __syncthreads();
+  }
   int row = 0, slot = 0, len = 0;
   bool starts = false;
   if (lane < a.tokens && t < a.c.n_new) {
-    const int b = sequence_of(a.c, t);
+    const int b = in_lds ? sequence_of(a.c.batch, t, [&](int i) { return starts_s[i]; }) : sequence_of(a.c.batch, t, [&](int i) { return a.c.cu[i]; });
     if (b >= 0) {
       const PagedSeq s = paged_seq(a.c, b);
       const int64_t at = s.len - s.n + (t - s.first);
@@ -88,7 +105,7 @@ __global__ __launch_bounds__(256) void paged_bounds_kernel(PagedBoundsArgs a) {
       len = (int)s.len;
     }
   }
-  Kept K = read_kept(a.bits_k + kv * NG);
+  const Kept K = read_kept(a.bits_k + kv * NG);
   if (!K.ok || K.used > a.Wk) return;  // width table inconsistent with the record: write nothing
   const int tpp = a.c.page_tokens >> 6;
   uint32_t magic = 0x64006400u;  // exponent of 1024 in both halves, in a VGPR
@@ -104,16 +121,18 @@ __global__ __launch_bounds__(256) void paged_bounds_kernel(PagedBoundsArgs a) {
     const int64_t blk = ((int64_t)page * a.c.n_kv + kv) * tpp + (tile - at * tpp);
     const uint32_t* rec = a.pool_k + blk * (TILE * a.Wk) + lane;
     uint16_t* box = reinterpret_cast<uint16_t*>(a.bounds + blk * BOX_WORDS);
-    const bool live = tile * TILE + lane < end;
-#pragma unroll
-    for (int sl = 0; sl < NG; ++sl) {
-      if (sl >= K.n) break;
-      const int b = K.bits[sl];
+    const bool whole = tile * TILE + TILE <= end, live = tile * TILE + lane < end;
+    int pay = K.n;
+#pragma unroll 1
+    for (int sl = 0; sl < K.n; ++sl) {
+      const int b = pick4(K.bits, sl);
       uint32_t words[8];
-      const uint32_t meta = finite_meta(rec[sl * TILE], b);
+      const uint32_t word = rec[sl * TILE];
 #pragma unroll
       for (int i = 0; i < 8; ++i)
-        if (i < b) words[i] = rec[(K.pay[sl] + i) * TILE];
+        if (i < b) words[i] = rec[(pay + i) * TILE];
+      pay += b;
+      const uint32_t meta = finite_meta(word, b);
       f16x2 least[16], most[16];
       with_bits(b, [&](auto bc) __attribute__((always_inline)) {
         constexpr int B = decltype(bc)::value;
@@ -129,9 +148,13 @@ __global__ __launch_bounds__(256) void paged_bounds_kernel(PagedBoundsArgs a) {
         }
       });
 #pragma unroll
-      for (int i = 0; i < 16; ++i) {
-        most[i] = live ? least[i] : __builtin_bit_cast(f16x2, 0xFC00FC00u);
-        least[i] = live ? least[i] : __builtin_bit_cast(f16x2, 0x7C007C00u);
+      for (int i = 0; i < 16; ++i) most[i] = least[i];
+      if (!whole) {
+#pragma unroll
+        for (int i = 0; i < 16; ++i) {
+          most[i] = live ? most[i] : __builtin_bit_cast(f16x2, 0xFC00FC00u);
+          least[i] = live ? least[i] : __builtin_bit_cast(f16x2, 0x7C007C00u);
+        }
       }
       const f16x2 lo = reduce_slots(least, lane, pk_min), hi = reduce_slots(most, lane, pk_max);
       // lanes of a quad hold the same: each writes one of least x, least x + 16, largest x, largest x + 16

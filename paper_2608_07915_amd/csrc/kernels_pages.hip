@@ -261,30 +261,50 @@ __device__ __forceinline__ Accept accept_entry(const PageMap& m, const PathList&
   return a;
 }
 
-// Workgroup = (entry; pool; a share of its word columns). A wavefront reads a column of all kept slots
-// before it writes any, and no other touches that column. Bound by latency: two dependent table
-// reads, one of records.
+// Workgroup = (entry; every gridDim.y-th pool). A wavefront reads eight columns of words of all kept slots before it
+// writes any, and no other touches those columns. Bound by latency: the entry's checks, the table and one round of
+// records (a workgroup for each share of each pool checked the entry 4608 times: 20 us for 48 entries and 32 pools).
 __global__ __launch_bounds__(256) void pages_accept_move_kernel(PageMap m, PathList p, PoolList pools, int32_t n_kv) {
+  constexpr int AT_ONCE = 8;
   const Accept a = accept_entry<256>(m, p, blockIdx.x);
   if (a.row < 0 || a.keep == 0) return;
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tpp = m.page_tokens >> 6;
-  const int cols = (int)(pools.words[blockIdx.y] / m.page_tokens), W = cols / n_kv;  // of all KV heads
-  const bool live = lane < a.keep;
+  const bool live = lane < a.keep && a.from != lane;
   const int64_t src = a.first + (live ? a.from : 0), dst = a.first + (live ? lane : 0);
   const int32_t* tab = m.table + (int64_t)a.row * m.row_pages;
   const int64_t ps = src / m.page_tokens, pd = dst / m.page_tokens;
   const int ss = (int)(src - ps * m.page_tokens), sd = (int)(dst - pd * m.page_tokens);
-  uint32_t* base = pools.base[blockIdx.y];
-  const uint32_t* from = base + tab[ps] * pools.words[blockIdx.y] + (int64_t)(ss >> 6) * (64 * W) + (ss & 63);
-  uint32_t* to = base + tab[pd] * pools.words[blockIdx.y] + (int64_t)(sd >> 6) * (64 * W) + (sd & 63);
-  const int64_t head = (int64_t)tpp * 64 * W;  // words of a KV head's records in a page
-  for (int c = blockIdx.z * 4 + wave; c < cols; c += 4 * gridDim.z) {
-    const int kv = c / W;
-    const int64_t at = kv * head + (int64_t)(c - kv * W) * 64;
-    uint32_t v = 0u;
-    if (live) v = from[at];
-    asm volatile("" : "+v"(v));
-    if (live && a.from != lane) to[at] = v;
+  const int64_t page_s = tab[ps], page_d = tab[pd];
+  for (int y = blockIdx.y; y < pools.n; y += gridDim.y) {
+    const int64_t words = pools.words[y];
+    const int cols = (int)(words / m.page_tokens), W = cols / n_kv;  // columns of all KV heads
+    uint32_t* base = pools.base[y];
+    const uint32_t* from = base + page_s * words + (int64_t)(ss >> 6) * (64 * W) + (ss & 63);
+    uint32_t* to = base + page_d * words + (int64_t)(sd >> 6) * (64 * W) + (sd & 63);
+    for (int c0 = wave * AT_ONCE; c0 < cols; c0 += 4 * AT_ONCE) {
+      uint32_t v[AT_ONCE];
+      // column c: word c % W of KV head c / W, whose records begin tpp 64 W words after the last one's
+      int kv = c0 / W, w = c0 - kv * W;
+      const int kv0 = kv, w0 = w;
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        v[i] = 0u;
+        if (live && c0 + i < cols) v[i] = from[((int64_t)kv * tpp * W + w) * 64];
+        const bool next = ++w == W;
+        w = next ? 0 : w;
+        kv += next ? 1 : 0;
+      }
+      asm volatile("" : "+v"(v[0]), "+v"(v[1]), "+v"(v[2]), "+v"(v[3]), "+v"(v[4]), "+v"(v[5]), "+v"(v[6]), "+v"(v[7]));  // all are there
+      kv = kv0;
+      w = w0;
+#pragma unroll
+      for (int i = 0; i < AT_ONCE; ++i) {
+        if (live && c0 + i < cols) to[((int64_t)kv * tpp * W + w) * 64] = v[i];
+        const bool next = ++w == W;
+        w = next ? 0 : w;
+        kv += next ? 1 : 0;
+      }
+    }
   }
 }
 
@@ -418,13 +438,9 @@ hipError_t launch_pages_truncate(const PageMap& m, const int32_t* rows, const in
 
 hipError_t launch_pages_accept_move(const PageMap& m, const PathList& p, int32_t n, const PoolList& pools, int32_t n_kv,
                                     hipStream_t st) {
-  int64_t cols = 0;
-  for (int i = 0; i < pools.n; ++i) cols = pools.words[i] / m.page_tokens > cols ? pools.words[i] / m.page_tokens : cols;
-  // four word columns a wavefront, fewer workgroups where there are many entries and pools
-  int64_t z = (cols + 15) / 16;
-  const int64_t most = 4096 / ((int64_t)n * pools.n) + 1;
-  if (z > most) z = most;
-  hipLaunchKernelGGL(pages_accept_move_kernel, dim3(n, pools.n, (unsigned)z), dim3(256), 0, st, m, p, pools, n_kv);
+  int y = 2048 / n;  // one round of workgroups
+  y = y < 1 ? 1 : y < pools.n ? y : pools.n;
+  hipLaunchKernelGGL(pages_accept_move_kernel, dim3(n, y), dim3(256), 0, st, m, p, pools, n_kv);
   return hipGetLastError();
 }
 

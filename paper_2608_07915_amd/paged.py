@@ -8,6 +8,7 @@ a call belong to that stream; other streams that use an output wait for it first
 from __future__ import annotations
 
 import ctypes
+from array import array
 
 from . import _lib
 from ._lib import check, spectra_pages, spectra_pool
@@ -80,15 +81,19 @@ def _ints(t, name: str, device, n=None):
 def _pools(cache: PagedCache, pools):
     import torch
     pools = [pools] if isinstance(pools, torch.Tensor) else pools
-    dev, n_pages, flat = cache.table.device, cache.n_pages, []
-    for i, p in enumerate(pools):
+    dev, n_pages, flat = cache.table.device, cache.n_pages, array("q")
+    for p in pools:
         n = p.numel()
-        if not (p.device == dev and p.dtype == torch.int32 and p.is_contiguous()):
-            raise ValueError(f"pool {i} must be a contiguous int32 tensor on {dev}")
+        if p.device != dev or p.dtype != torch.int32 or not p.is_contiguous():
+            raise ValueError(f"pool {len(flat) // 2} must be a contiguous int32 tensor on {dev}")
         if n % (64 * n_pages):
-            raise ValueError(f"pool {i}: {n} words are not {n_pages} pages of whole tiles")
-        flat.append((p.data_ptr(), n // n_pages))
-    return (spectra_pool * max(len(flat), 1))(*flat), len(flat)
+            raise ValueError(f"pool {len(flat) // 2}: {n} words are not {n_pages} pages of whole tiles")
+        flat.append(p.data_ptr())
+        flat.append(n // n_pages)
+    made = (spectra_pool * max(len(flat) // 2, 1))()
+    if flat:
+        ctypes.memmove(made, flat.buffer_info()[0], ctypes.sizeof(made))
+    return made, len(flat) // 2
 
 
 def _workspace(cache: PagedCache, workspace, need: int, stream):
