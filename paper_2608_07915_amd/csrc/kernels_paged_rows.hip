@@ -26,6 +26,39 @@ namespace spectra_dev {
 constexpr int RO_NW = 4, RO_NT = 64 * RO_NW;
 constexpr int RO_PITCH = D + 4;
 
+// LDS byte of 16-byte piece `piece` of slot `t` in a slot tile: eight neighbouring slots' equal pieces, and
+// the two pieces of four slots that a transposed read takes, lie on distinct banks.
+__device__ __forceinline__ int slot_piece(int t, int piece) { return t * 64 + ((piece ^ (t & 2) ^ ((t >> 2) & 1)) << 4); }
+
+// One slot's group as fp16 coefficients z + s code into its LDS row, rounded once. PRECISE: and what the rounding
+// left, 2^11 (z + s code) - 2^11 hi, in the tile `lo` bytes further (its fp32 product and sum are rounded to 2^-24).
+template <int B, bool PRECISE>
+__device__ __forceinline__ void write_slot(const uint32_t (&w)[8], uint32_t meta, uint8_t* tile, int t, int lo, uint32_t magic) {
+  uint32_t Z[8];
+  join_halves<B>(w, Z);
+  const _Float16 s = __builtin_bit_cast(_Float16, (uint16_t)meta), z = __builtin_bit_cast(_Float16, (uint16_t)(meta >> 16));
+  const float s2 = (float)s * CA_LO, z2 = (float)z * CA_LO;
+#pragma unroll
+  for (int k = 0; k < 4; ++k) {
+    const f16x8 c = codes_f16<B, false>(Z, k, magic);
+    u32x4 rh, rl;
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const f16x2 hi = __builtin_elementwise_fma(f16x2{s, s}, f16x2{c[2 * i], c[2 * i + 1]}, f16x2{z, z});
+      rh[i] = __builtin_bit_cast(uint32_t, hi);
+      if constexpr (PRECISE) {
+        f16x2 rest;
+#pragma unroll
+        for (int e = 0; e < 2; ++e)
+          rest[e] = (_Float16)__builtin_fmaf((float)hi[e], -CA_LO, __builtin_fmaf(s2, (float)c[2 * i + e], z2));
+        rl[i] = __builtin_bit_cast(uint32_t, rest);
+      }
+    }
+    *reinterpret_cast<u32x4*>(tile + slot_piece(t, k)) = rh;
+    if constexpr (PRECISE) *reinterpret_cast<u32x4*>(tile + lo + slot_piece(t, k)) = rl;
+  }
+}
+
 // ---------------------------------------------------------------------------
 // Where a workgroup's work lies
 // ---------------------------------------------------------------------------
@@ -514,10 +547,10 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
     load_x += RO_NW;
     look_up();
   };
-  // operands in the tile (the swizzle of piece_at repeats every 16 slots)
-  const uint8_t* key_at = tile + piece_at(col, quarter);
-  const uint8_t* val_at0 = tile + piece_at(4 * quarter + (col >> 2), (lane & 3) >> 1) + 8 * (lane & 1);
-  const uint8_t* val_at1 = tile + piece_at(4 * quarter + (col >> 2), 2 + ((lane & 3) >> 1)) + 8 * (lane & 1);
+  // operands in the tile (the swizzle of slot_piece repeats every 8 slots)
+  const uint8_t* key_at = tile + slot_piece(col, quarter);
+  const uint8_t* val_at0 = tile + slot_piece(4 * quarter + (col >> 2), (lane & 3) >> 1) + 8 * (lane & 1);
+  const uint8_t* val_at1 = tile + slot_piece(4 * quarter + (col >> 2), 2 + ((lane & 3) >> 1)) + 8 * (lane & 1);
   int bits = 0;  // of the group whose words are loaded
   auto fetch = [&](int u) __attribute__((always_inline)) {
     const int d = __builtin_amdgcn_readfirstlane(unit_s[u]);
@@ -538,14 +571,15 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
     __builtin_amdgcn_wave_barrier();
     const uint32_t m = finite_meta(meta, bits);
     with_bits(bits, [&](auto bc) __attribute__((always_inline)) {
-      write_coefficients<decltype(bc)::value, PRECISE>(words, m, tile, lane, CA_TILE, magic);
+      write_slot<decltype(bc)::value, PRECISE>(words, m, tile, lane, CA_TILE, magic);
     });
     if (u + 1 == n_units) enter();
     fetch(u + 1 == n_units ? 0 : u + 1);
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   };
-  // for NV value groups at most: the sums of four are 128 registers at four row blocks, which spill (95 us for ...)
+  // for NV value groups at most: the sums of four are 128 registers at four row blocks and spill, those of the
+  // two or three that are kept mostly do not (16 trees of up to 32 tokens over 8k slots: 95 -> 81 us)
   auto walk = [&](auto groups) __attribute__((always_inline)) {
     constexpr int NV = decltype(groups)::value;
     look_up();
@@ -671,10 +705,11 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
           if constexpr (PRECISE) w[nb][hf][1] = as_f16x8(xl);
         }
       }
-#pragma unroll
-      for (int sl = 0; sl < NV; ++sl) {
-        if (sl < n_units - n_keys) {
-          expand(n_keys + sl);
+      // (one place that makes coefficients for all value groups: unrolled, twice the code for the same time)
+#pragma unroll 1
+      for (int g = 0; g < n_units - n_keys; ++g) {
+        expand(n_keys + g);
+        auto add = [&](f32x4 (&sum)[2][NB]) __attribute__((always_inline)) {
 #pragma unroll
           for (int y = 0; y < 2; ++y) {
             f32x4 lo[NB];
@@ -692,7 +727,7 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
               }
 #pragma unroll
               for (int nb = 0; nb < NB; ++nb) {
-                acc[sl][y][nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, w[nb][hf][0], acc[sl][y][nb], 0, 0, 0);
+                sum[y][nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, w[nb][hf][0], sum[y][nb], 0, 0, 0);
                 if constexpr (PRECISE) {
                   lo[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vl, w[nb][hf][0], lo[nb], 0, 0, 0);
                   lo[nb] = __builtin_amdgcn_mfma_f32_16x16x32_f16(vh, w[nb][hf][NP - 1], lo[nb], 0, 0, 0);
@@ -703,10 +738,13 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
 #pragma unroll
               for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-                for (int i = 0; i < 4; ++i) acc[sl][y][nb][i] = __builtin_fmaf(lo[nb][i], 1.0f / CA_LO, acc[sl][y][nb][i]);
+                for (int i = 0; i < 4; ++i) sum[y][nb][i] = __builtin_fmaf(lo[nb][i], 1.0f / CA_LO, sum[y][nb][i]);
             }
           }
-        }
+        };
+#pragma unroll
+        for (int sl = 0; sl < NV; ++sl)
+          if (sl == g) add(acc[sl]);
       }
     }
     // merge of the wavefronts, and the chunk's partial of every row, 16 rows at a time
