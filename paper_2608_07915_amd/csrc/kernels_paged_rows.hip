@@ -59,6 +59,14 @@ __device__ __forceinline__ void write_slot(const uint32_t (&w)[8], uint32_t meta
   }
 }
 
+// finite_meta with one test for all that is rare: z + s top is finite and within fp16 only where s and z are.
+__device__ __forceinline__ uint32_t finite_slot(uint32_t m, int bits, float top) {
+  const f16x2 sz = __builtin_bit_cast(f16x2, m);
+  const float x = __builtin_fmaf((float)sz[0], top, (float)sz[1]);
+  if (!(__builtin_fabsf(x) <= 65504.0f)) m = finite_meta(m, bits);
+  return m;
+}
+
 // ---------------------------------------------------------------------------
 // Where a workgroup's work lies
 // ---------------------------------------------------------------------------
@@ -353,7 +361,6 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
   __shared__ uint16_t who_s[TREE ? 1 : LIST_ALL];
   __shared__ uint64_t anc_s[TREE ? DRAFT : 1];
   __shared__ float m_s[RO_NW][ROWS], l_s[RO_NW][ROWS], un_s[PRECISE ? NG : 1][ROWS];
-  __shared__ int32_t unit_s[2 * NG];
   __shared__ __attribute__((aligned(16))) float sums_s[RO_NW * 16 * RO_PITCH];  // the tiles while wavefronts walk
   __shared__ __attribute__((aligned(16))) uint8_t q_s[NG][NB][NP][64 * 16];      // q' as column operands, by lane
   static_assert(sizeof(sums_s) >= RO_NW * NP * CA_TILE, "the tiles lie where the sums do");
@@ -423,6 +430,61 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
     if (wave == 0) anc_s[lane] = ancestors(a.parents, seq.first, (int)seq.n, lane);
   }
 
+  const int tpp = a.c.page_tokens >> 6, n_keys = Kk.n, n_units = Kk.n + Kv.n;
+  int unit_v = 0;  // lane u: kept group u of the keys, then of the values: bits, its place, its payload's first word
+  {
+    const int s = lane < n_keys ? lane : lane - n_keys;
+    int bb = 0, pay = 0;
+#pragma unroll
+    for (int x = 0; x < NG; ++x) {
+      bb = x == s ? (lane < n_keys ? Kk.bits[x] : Kv.bits[x]) : bb;
+      pay = x == s ? (lane < n_keys ? Kk.pay[x] : Kv.pay[x]) : pay;
+    }
+    unit_v = bb | (s & 3) << 4 | pay << 6;
+  }
+  auto tile_of = [&](int x) __attribute__((always_inline)) { return TREE ? begin + x : __builtin_amdgcn_readfirstlane(sel_s[begin + x]); };
+  // the tile whose words are loaded: `now` and its records; the one after it: `next`, its page, its place in that
+  int load_x = wave, in_page = 0, page = -1, now = 0, next = 0;
+  const uint32_t *kp = a.pool_k, *vp = a.pool_v;
+  bool page_ok = false;
+  uint32_t words[8], meta = 0u;
+  auto look_up = [&]() __attribute__((always_inline)) {
+    page = -1;
+    if (load_x < count) {
+      next = tile_of(load_x);
+      const int idx = next / tpp;
+      in_page = next - idx * tpp;
+      page = a.c.table[(int64_t)seq.row * a.c.row_pages + idx];  // (not waited for until it is entered)
+    }
+  };
+  auto enter = [&]() __attribute__((always_inline)) {  // the tile looked up; the walk goes on
+    const int at = __builtin_amdgcn_readfirstlane(page);
+    page_ok = at >= 0 && at < a.c.n_pages;
+    now = next;
+    const int64_t rec = ((int64_t)(page_ok ? at : 0) * a.c.n_kv + kv) * tpp + in_page;
+    kp = a.pool_k + rec * (TILE * a.Wk) + lane;
+    vp = a.pool_v + rec * (TILE * a.Wv) + lane;
+    load_x += RO_NW;
+    look_up();
+  };
+  int bits = 0;  // of the group whose words are loaded
+  auto fetch = [&](int u) __attribute__((always_inline)) {
+    const int d = __builtin_amdgcn_readlane(unit_v, u);
+    const uint32_t* rec = u < n_keys ? kp : vp;
+    bits = d & 15;
+    meta = 0u;
+    if (!page_ok) return;
+    meta = rec[((d >> 4) & 3) * TILE];
+    rec += (d >> 6) * TILE;
+#pragma unroll
+    for (int i = 0; i < 8; ++i)
+      if (i < bits) words[i] = rec[i * TILE];
+  };
+  look_up();
+  if (n_units > 0) {
+    enter();
+    fetch(0);
+  }
   // q': element e of quarter p is that of code 4 p + e / 2 + 16 (e % 2), as the tiles' places are; product y has
   // e = (i / 2) * 4 + i % 2 + 2 y, i < 4, so that a lane's codes of both products are neighbours. A wavefront takes
   // a group, or half of the row blocks of one where there are two at most, and cuts its basis into
@@ -431,8 +493,13 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
     const bool halves = NB > 1 && Kk.n <= 2;
     const int sl = halves ? wave & 1 : wave, nb0 = halves && wave > 1 ? NB / 2 : 0, nb1 = halves && wave < 2 ? NB / 2 : NB;
     if (sl < Kk.n) {
+      // KS of the four steps' loads at once (one by one they wait for memory four times), as registers allow
+      constexpr int KS = NB == 2 || PRECISE ? 4 : 2;
       f32x4 acc[NB][2];
+      u32x4 qr[NB][KS][2];
+      f32x2 V[KS][8];
       int64_t qoff[NB];
+      const float* v0 = a.basis_k + (int64_t)kv * D * D + (8 * quarter) * D + G * pick4(Kk.grp, sl) + 4 * (col >> 2) + (col & 2) + 16 * (col & 1);
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         acc[nb][0] = acc[nb][1] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
@@ -440,40 +507,59 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
         row_of(nb, tok, head);
         qoff[nb] = (seq.first + tok) * a.q_token_stride + (kv * a.n_qh + head) * a.q_head_stride + 8 * quarter;
       }
-      const float* V = a.basis_k + (int64_t)kv * D * D + (8 * quarter) * D + G * pick4(Kk.grp, sl) + 4 * (col >> 2) + (col & 2) + 16 * (col & 1);
 #pragma unroll
-      for (int k = 0; k < 4; ++k) {
-        float v[2][8];
+      for (int k0 = 0; k0 < 4; k0 += KS) {
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-          const f32x2 x = *reinterpret_cast<const f32x2*>(V + (32 * k + e) * D);
-          v[0][e] = x[0];
-          v[1][e] = x[1];
-        }
-        bf16x8 vp[2][QP];
-        split8_pairs<QP>(v[0], vp[0]);
-        split8_pairs<QP>(v[1], vp[1]);
+        for (int k = 0; k < KS; ++k)
+#pragma unroll
+          for (int e = 0; e < 8; ++e) V[k][e] = *reinterpret_cast<const f32x2*>(v0 + (32 * (k0 + k) + e) * D);
 #pragma unroll
         for (int nb = 0; nb < NB; ++nb) {
           if (nb < nb0 || nb >= nb1) continue;
-          bf16x8 qq[QP];
-          if (a.q_f32) {
-            const f32x4* qp = reinterpret_cast<const f32x4*>(reinterpret_cast<const float*>(a.q) + qoff[nb] + 32 * k);
-            const f32x4 q0 = qp[0], q1 = qp[1];
-            const float qv[8] = {q0[0], q0[1], q0[2], q0[3], q1[0], q1[1], q1[2], q1[3]};
-            split8_pairs<QP>(qv, qq);
-          } else {
-            qq[0] = as_bf16x8(*reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.q) + qoff[nb] + 32 * k));
-          }
 #pragma unroll
-          for (int y = 0; y < 2; ++y) {
-#pragma unroll
-            for (int i = 0; i < QP; ++i) acc[nb][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vp[y][i], qq[0], acc[nb][y], 0, 0, 0);
+          for (int k = 0; k < KS; ++k) {
             if (a.q_f32) {
+              const u32x4* x = reinterpret_cast<const u32x4*>(reinterpret_cast<const float*>(a.q) + qoff[nb] + 32 * (k0 + k));
+              qr[nb][k][0] = x[0];
+              qr[nb][k][1] = x[1];
+            } else {
+              qr[nb][k][0] = *reinterpret_cast<const u32x4*>(reinterpret_cast<const uint16_t*>(a.q) + qoff[nb] + 32 * (k0 + k));
+            }
+          }
+        }
 #pragma unroll
-              for (int i = 0; i < QP; ++i)
+        for (int k = 0; k < KS; ++k) {
+          float v[2][8];
 #pragma unroll
-                for (int j = 1; i + j < QP; ++j) acc[nb][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vp[y][i], qq[j], acc[nb][y], 0, 0, 0);
+          for (int e = 0; e < 8; ++e) {
+            v[0][e] = V[k][e][0];
+            v[1][e] = V[k][e][1];
+          }
+          bf16x8 vp[2][QP];
+          split8_pairs<QP>(v[0], vp[0]);
+          split8_pairs<QP>(v[1], vp[1]);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) {
+            if (nb < nb0 || nb >= nb1) continue;
+            bf16x8 qq[QP];
+            if (a.q_f32) {
+              float qv[8];
+#pragma unroll
+              for (int e = 0; e < 8; ++e) qv[e] = __uint_as_float(qr[nb][k][e >> 2][e & 3]);
+              split8_pairs<QP>(qv, qq);
+            } else {
+              qq[0] = as_bf16x8(qr[nb][k][0]);
+            }
+#pragma unroll
+            for (int y = 0; y < 2; ++y) {
+#pragma unroll
+              for (int i = 0; i < QP; ++i) acc[nb][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vp[y][i], qq[0], acc[nb][y], 0, 0, 0);
+              if (a.q_f32) {
+#pragma unroll
+                for (int i = 0; i < QP; ++i)
+#pragma unroll
+                  for (int j = 1; i + j < QP; ++j) acc[nb][y] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(vp[y][i], qq[j], acc[nb][y], 0, 0, 0);
+              }
             }
           }
         }
@@ -510,66 +596,20 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
       }
     }
   }
-  const int tpp = a.c.page_tokens >> 6, n_keys = Kk.n, n_units = Kk.n + Kv.n;
-  if (tid < 2 * NG) {  // a kept group of the keys, then of the values
-    const int s = tid < n_keys ? tid : tid - n_keys;
-    int bb = 0, pay = 0;
-#pragma unroll
-    for (int x = 0; x < NG; ++x) {
-      bb = x == s ? (tid < n_keys ? Kk.bits[x] : Kv.bits[x]) : bb;
-      pay = x == s ? (tid < n_keys ? Kk.pay[x] : Kv.pay[x]) : pay;
-    }
-    unit_s[tid] = bb | (s & 3) << 4 | pay << 6;
-  }
-  __syncthreads();  // q', groups, ancestors
+  __syncthreads();  // q', ancestors
   uint8_t* tile = reinterpret_cast<uint8_t*>(sums_s) + wave * NP * CA_TILE;
   uint32_t magic = 0x64006400u;  // exponent of 1024 in both halves, in a VGPR
   asm volatile("" : "+v"(magic));
-  auto tile_of = [&](int x) __attribute__((always_inline)) { return TREE ? begin + x : __builtin_amdgcn_readfirstlane(sel_s[begin + x]); };
-  // the tile whose words are loaded: its page, its own place in it, its records
-  int load_x = wave, in_page = 0, page = -1;
-  const uint32_t *kp = a.pool_k, *vp = a.pool_v;
-  bool page_ok = false;
-  uint32_t words[8], meta = 0u;
-  auto look_up = [&]() __attribute__((always_inline)) {
-    page = -1;
-    if (load_x < count) {
-      const int t = tile_of(load_x), idx = t / tpp;
-      in_page = t - idx * tpp;
-      page = __builtin_amdgcn_readfirstlane(a.c.table[(int64_t)seq.row * a.c.row_pages + idx]);
-    }
-  };
-  auto enter = [&]() __attribute__((always_inline)) {  // the tile looked up; the walk goes on
-    page_ok = page >= 0 && page < a.c.n_pages;
-    const int64_t rec = ((int64_t)(page_ok ? page : 0) * a.c.n_kv + kv) * tpp + in_page;
-    kp = a.pool_k + rec * (TILE * a.Wk) + lane;
-    vp = a.pool_v + rec * (TILE * a.Wv) + lane;
-    load_x += RO_NW;
-    look_up();
-  };
   // operands in the tile (the swizzle of slot_piece repeats every 8 slots)
   const uint8_t* key_at = tile + slot_piece(col, quarter);
   const uint8_t* val_at0 = tile + slot_piece(4 * quarter + (col >> 2), (lane & 3) >> 1) + 8 * (lane & 1);
   const uint8_t* val_at1 = tile + slot_piece(4 * quarter + (col >> 2), 2 + ((lane & 3) >> 1)) + 8 * (lane & 1);
-  int bits = 0;  // of the group whose words are loaded
-  auto fetch = [&](int u) __attribute__((always_inline)) {
-    const int d = __builtin_amdgcn_readfirstlane(unit_s[u]);
-    const uint32_t* rec = u < n_keys ? kp : vp;
-    bits = d & 15;
-    meta = 0u;
-    if (!page_ok) return;
-    meta = rec[((d >> 4) & 3) * TILE];
-    rec += (d >> 6) * TILE;
-#pragma unroll
-    for (int i = 0; i < 8; ++i)
-      if (i < bits) words[i] = rec[i * TILE];
-  };
   // group u's coefficients into the tile (its last readers are done: LDS serves a wavefront in
   // order), and the next group's words
   auto expand = [&](int u) __attribute__((always_inline)) {
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
-    const uint32_t m = finite_meta(meta, bits);
+    const uint32_t m = finite_slot(meta, bits, (float)((1 << bits) - 1));
     with_bits(bits, [&](auto bc) __attribute__((always_inline)) {
       write_slot<decltype(bc)::value, PRECISE>(words, m, tile, lane, CA_TILE, magic);
     });
@@ -582,11 +622,6 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
   // two or three that are kept mostly do not (16 trees of up to 32 tokens over 8k slots: 95 -> 81 us)
   auto walk = [&](auto groups) __attribute__((always_inline)) {
     constexpr int NV = decltype(groups)::value;
-    look_up();
-    if (n_units > 0) {
-      enter();
-      fetch(0);
-    }
     const int64_t past = seq.len - seq.n;  // slots of the history
     const int64_t common = TREE ? past : past + tok0 + 1;  // slots that every row sees, as far as its list goes
     f32x4 acc[NV][2][NB];
@@ -600,7 +635,7 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
     }
 #pragma unroll 1
     for (int x = wave; x < count; x += RO_NW) {
-      const int64_t t0 = (int64_t)tile_of(x) * TILE;
+      const int64_t t0 = (int64_t)(n_units > 0 ? now : tile_of(x)) * TILE;
       f32x4 S[NB][4];  // slot 16 s + 4 quarter + i
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb)
