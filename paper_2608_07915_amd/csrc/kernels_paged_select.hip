@@ -370,6 +370,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_block_scores_kernel(PagedSel
       head = head < a.n_qh ? head : 0;
       const float* tops = a.tops + row_of(tok, head) * a.n_chunks;
       float top = -__builtin_inff();
+#pragma unroll 16
       for (int i = 0; i < a.n_chunks; ++i) top = __builtin_fmaxf(top, tops[i]);
       top_s[0][c] = top;
     }
@@ -587,6 +588,23 @@ __device__ __forceinline__ void find_step(const int32_t* count, int left, int32_
   __syncthreads();
 }
 
+// The heads' best over their chunks (values have none: theirs is taken off already).
+template <int NT>
+__device__ __forceinline__ void best_of_heads(const PagedSelectArgs& a, int64_t t, int kv, int n_rows, float* top) {
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+  if (n_rows == 1) {
+    if (threadIdx.x == 0) top[0] = 0.0f;
+    return;
+  }
+  for (int h = wave; h < n_rows; h += NT / 64) {
+    const float* tops = a.tops + (t * a.n_q_heads + kv * a.n_qh + h) * a.n_chunks;
+    float x = -__builtin_inff();
+    for (int i = lane; i < a.n_chunks; i += 64) x = __builtin_fmaxf(x, tops[i]);
+    x = wave_max(x);
+    if (lane == 0) top[h] = x;
+  }
+}
+
 template <int NT, int IT>
 __global__ __launch_bounds__(NT, NT == 128 ? 4 : 1) void paged_pick_kernel(PagedSelectArgs a, int n_rows) {
   constexpr int STEPS = PickScratch<NT>::STEPS, FEW = PickScratch<NT>::FEW;
@@ -594,6 +612,20 @@ __global__ __launch_bounds__(NT, NT == 128 ? 4 : 1) void paged_pick_kernel(Paged
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int kv = (int)(blockIdx.x % (unsigned)a.c.n_kv);
   const int64_t t = blockIdx.x / (unsigned)a.c.n_kv;
+  const float* rows = a.scores + (t * a.c.n_kv + kv) * (int64_t)n_rows * a.most_blocks;
+  constexpr int HB = NT == 128 ? 1 : 16 / IT;  // rows at a time: 16 loads under way (values: one row)
+  f32x4 x[HB][IT];
+  auto load = [&](int h0) __attribute__((always_inline)) {  // (what lies behind the last block is not used)
+#pragma unroll
+    for (int h = 0; h < HB; ++h)
+#pragma unroll
+      for (int i = 0; i < IT; ++i) {
+        const int blk = 4 * (NT * i + tid);
+        x[h][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
+        if (blk < a.most_blocks && h0 + h < n_rows) x[h][i] = *reinterpret_cast<const f32x4*>(rows + (int64_t)(h0 + h) * a.most_blocks + blk);
+      }
+  };
+  load(0);  // while the token's sequence is looked for
   if (tid == 0) s.b = -1;
   __syncthreads();
   for (int b = tid; b < a.c.batch; b += NT) {
@@ -602,15 +634,7 @@ __global__ __launch_bounds__(NT, NT == 128 ? 4 : 1) void paged_pick_kernel(Paged
   }
   for (int i = tid; i < STEPS; i += NT) s.count[i] = 0;
   if (tid == 0) s.n = 0;
-  // the heads' best (values have none: theirs is taken off already)
-  if (tid < 16) {
-    float top = n_rows == 1 ? 0.0f : -__builtin_inff();
-    if (n_rows > 1 && tid < n_rows) {
-      const float* tops = a.tops + (t * a.n_q_heads + kv * a.n_qh + tid) * a.n_chunks;
-      for (int i = 0; i < a.n_chunks; ++i) top = __builtin_fmaxf(top, tops[i]);
-    }
-    s.top[tid] = top;
-  }
+  best_of_heads<NT>(a, t, kv, n_rows, s.top);
   __syncthreads();
   const int b = __builtin_amdgcn_readfirstlane(s.b);
   if (b < 0) return;
@@ -623,23 +647,13 @@ __global__ __launch_bounds__(NT, NT == 128 ? 4 : 1) void paged_pick_kernel(Paged
     for (int i = tid; i < want; i += NT) out[i] = i < have ? i : -1;
     return;
   }
-  const float* rows = a.scores + (t * a.c.n_kv + kv) * (int64_t)n_rows * a.most_blocks;
   float v[IT][4], least = 0.0f;
 #pragma unroll
   for (int i = 0; i < IT; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) v[i][e] = -__builtin_inff();
-  constexpr int HB = NT == 128 ? 1 : 16 / IT;  // rows at a time: 16 loads under way (values: one row)
   for (int h0 = 0; h0 < n_rows; h0 += HB) {
-    f32x4 x[HB][IT];
-#pragma unroll
-    for (int h = 0; h < HB; ++h)
-#pragma unroll
-      for (int i = 0; i < IT; ++i) {
-        const int blk = 4 * (NT * i + tid);
-        x[h][i] = f32x4{0.0f, 0.0f, 0.0f, 0.0f};
-        if (blk < have && h0 + h < n_rows) x[h][i] = *reinterpret_cast<const f32x4*>(rows + (int64_t)(h0 + h) * a.most_blocks + blk);
-      }
+    if (h0 > 0) load(h0);
 #pragma unroll
     for (int h = 0; h < HB; ++h) {
       if (h0 + h >= n_rows) break;
@@ -795,14 +809,7 @@ __global__ __launch_bounds__(PICK) void paged_pick_long_kernel(PagedSelectArgs a
     const PagedSeq q = paged_seq(a.c, b);
     if (t >= q.first && t < q.first + q.n) atomicMax(&b_s, b);
   }
-  if (tid < 16) {
-    float top = n_rows == 1 ? 0.0f : -__builtin_inff();
-    if (n_rows > 1 && tid < n_rows) {
-      const float* tops = a.tops + (t * a.n_q_heads + kv * a.n_qh + tid) * a.n_chunks;
-      for (int i = 0; i < a.n_chunks; ++i) top = __builtin_fmaxf(top, tops[i]);
-    }
-    top_s[tid] = top;
-  }
+  best_of_heads<PICK>(a, t, kv, n_rows, top_s);
   __syncthreads();
   if (b_s < 0) return;
   const PagedSeq seq = paged_seq(a.c, b_s);
