@@ -588,3 +588,58 @@ def test_boxes_follow_their_pages():
                 assert (np.abs(got - want[i])[:, live] <= (2 * 2.0 ** -11 * np.abs(want[i]) + 2.0 ** -24)[:, live]).all()
     sel = S.spectra_paged_select(mc, c.ck, box, q, ints([0, 1, 2]), 3, 300, rows=ints([2, 3]))
     assert sel.shape == (2, 2, 3) and sel.min() >= -1
+
+
+@pytest.mark.parametrize("n", [160, 1100])
+def test_selection_of_many_tokens_that_are_not_finite(n):
+    """Heads that have no number are passed over, and no token reaches another's, whichever way the best heads are found."""
+    c = cache([2600], [n], 4, f32=True, seed=9)
+    box = whole(c)
+    want = select(c, box, 8)
+    check_selection(c, want, box, B8, 64, 8)
+    q, copy = c.q.clone(), c.q.clone()
+    q[1, 0, 3], copy[1, 0] = float("nan"), c.q[1, 1]  # as if the head were another's twin
+    q[n // 2, :4] = float("nan")
+    q[n - 1, 5, 0] = float("inf")
+    got, twin = select(c, box, 8, q=q), select(c, box, 8, q=copy)
+    same = torch.ones(n, dtype=torch.bool, device="cuda")
+    same[[1, n // 2, n - 1]] = False
+    assert torch.equal(got[same], want[same]) and torch.equal(got[1], twin[1])
+    have = -(-(2600 - n + n // 2 + 1) // 64)
+    assert got[n // 2, 0].tolist() == [0, 1, 2, 3, 4, 5, 6, have - 1] and torch.equal(got[n // 2, 1], want[n // 2, 1])
+    assert torch.equal(got[n - 1, 0], want[n - 1, 0])
+
+
+@pytest.mark.parametrize("f32", [False, True], ids=["bf16", "f32"])
+@pytest.mark.parametrize("new", [1, 3, 40])
+def test_lists_over_metadata_that_is_not_finite(new, f32):
+    c = cache([300], [new], f32=f32, seed=10)
+    page = int(c.cache.table[0, 1])
+    k, v = (c.pools[i][page].view(2, 8, 64) for i in (0, 1))
+    k[0, 0, 5] = 0x7C00
+    k[1, 1, 9] = 0x7E00 << 16
+    v[0, 1, 7] = 0xFC00
+    v[0, 0, 11] = 0x7BFF
+    v[0, 2:6, 11] = 0x11111111
+    c.coef[0][0][0][69, :32] = c.coef[0][1][0][73, 32:64] = c.coef[0][0][1][71, 32:64] = 0.0
+    c.coef[0][0][1][75, :32] = float(np.float16(65472.0 / 15))
+    blocks = np.broadcast_to(np.array([0, 1, 3]), (new, 2, 3)).copy()
+    lse = torch.empty(c.q.shape[:2], device="cuda")
+    check(c, list_sees([300], [new], blocks), attend(c, blocks, lse=lse), lse)
+
+
+@pytest.mark.parametrize("f32", [False, True], ids=["bf16", "f32"])
+def test_more_sequences_than_threads(f32):
+    """Boxes, selection and lists of 300 short sequences over three KV heads, some with nothing new."""
+    rng = np.random.default_rng(18)
+    lens = rng.integers(6, 200, 300)
+    new = rng.integers(1, 6, 300) * (rng.random(300) > 0.1)
+    bits = [[5, 1, 0, 0], [4, 2, 0, 0], [1, 1, 1, 3]]
+    c = cache(lens.tolist(), new.tolist(), 4, bits, bits[::-1], 10, f32=f32, seed=18)
+    box = whole(c)
+    check_boxes(c, box, bits, 64, [0] * 300, start=0)
+    got = select(c, box, 3)
+    check_selection(c, got, box, bits, 64, 3)
+    blocks = got.cpu().numpy()
+    lse = torch.empty(c.q.shape[:2], device="cuda")
+    check(c, list_sees(lens, new, blocks), attend(c, blocks, lse=lse), lse)

@@ -385,3 +385,47 @@ def test_accept_of_many_pools_and_captured():
         torch.cuda.synchronize()
         assert all(torch.equal(x, y) for x, y in zip(pools, want))
         assert all(torch.equal(x, y) for x, y in zip((c.table, c.lens, c.refs), maps))
+
+
+@pytest.mark.parametrize("f32", [False, True], ids=["bf16", "f32"])
+@pytest.mark.parametrize("new", [4, 8, 20, 40])
+def test_metadata_that_is_not_finite(new, f32):
+    """It counts as 0 and reaches no other slot; a scale too large for fp16 is lowered."""
+    c = cache([150], [new], f32=f32, seed=16)
+    page = int(c.cache.table[0, 0])
+    k, v = (c.pools[i][page].view(2, 8, 64) for i in (0, 1))
+    k[0, 0, 5] = 0x7C00           # an infinite scale
+    k[1, 1, 9] = 0x7E00 << 16     # NaN as zero point
+    v[0, 1, 7] = 0xFC00           # minus infinity
+    v[0, 0, 11] = 0x7BFF          # 65504 as scale: codes 1, lowered to 65472 / 15
+    v[0, 2:6, 11] = 0x11111111
+    c.coef[0][0][0][5, :32] = c.coef[0][1][0][9, 32:64] = c.coef[0][0][1][7, 32:64] = 0.0
+    c.coef[0][0][1][11, :32] = float(np.float16(65472.0 / 15))
+    p = tree("random", [new])
+    lse = torch.empty(c.q.shape[:2], device="cuda")
+    check(c, tree_sees([150], [new], p), attend(c, p, lse=lse), lse)
+
+
+def test_few_and_many_rows_together_captured():
+    """Sequences on both sides of 128 rows a KV head in one call, in graphs replayed between eager calls."""
+    lens, new = [5000, 300, 700, 90, 2000], [64, 20, 40, 1, 33]
+    c = cache(lens, new, seed=17)
+    p = tree("random", new)
+    lse, out = torch.empty(c.q.shape[:2], device="cuda"), torch.empty_like(c.q)
+    want = attend(c, p, lse=lse)
+    check(c, tree_sees(lens, new, p), want, lse)
+    first, up = lse.clone(), ints(p)
+    ws = torch.empty(S.spectra_paged_tree_attention_workspace_bytes(5, sum(new), 8, 2, 64, 5000) + 4096, dtype=torch.uint8, device="cuda")
+    call = lambda: S.spectra_paged_tree_attention(c.cache, c.ck, c.cv, *c.pools, c.q, c.cu, up, 64, 5000, out=out, lse=lse, workspace=ws)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    for _ in range(4):
+        out.fill_(3.0)
+        lse.fill_(3.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out, want) and torch.equal(lse, first)
+        assert torch.equal(attend(c, p), want)
