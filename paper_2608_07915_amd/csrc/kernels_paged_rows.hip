@@ -16,6 +16,8 @@
 //
 // What a row of a tree sees behind the history is a bit mask of at most 64 drafted slots: its own bit and
 // its ancestors'.
+#include <algorithm>
+
 #include "encode_dev.hpp"
 #include "paged_coef.hpp"
 #include "paged_dev.hpp"
@@ -1173,7 +1175,8 @@ template <bool TREE>
 hipError_t launch_combine(const PagedRowsArgs& p, int rows, hipStream_t st) {
   const int64_t all = p.a.c.n_new * p.a.n_qh, n_kv = p.a.c.n_kv;
   const dim3 grid((unsigned)(ceil_div(all, CO_ROWS) * n_kv));
-  if (all * n_kv <= 2 * N_CU)  // a CU holds two of these workgroups
+  // a row a CU (8 tokens of 32 heads over 4k slots 21 us in all, and 24 by sixteen rows; 16 tokens 31 and 29)
+  if (all * n_kv <= N_CU)
     hipLaunchKernelGGL((paged_row_combine_kernel<TREE>), dim3((unsigned)(all * n_kv)), dim3(1024), 0, st, p, rows);
   else if (p.a.out_f32)
     hipLaunchKernelGGL((paged_rows_combine_kernel<TREE, 3>), grid, dim3(256), 0, st, p, rows);
@@ -1244,11 +1247,13 @@ hipError_t launch_paged_tree(const PagedRowsArgs& args, void* workspace, hipStre
   return launch_combine<true>(p, 16 * nb, st);
 }
 
-// New tokens of a unit: as many as its rows hold, where sequences have several on average and their lists fit.
-static int32_t list_tokens(int32_t batch, int64_t n_new, int32_t n_qh, int32_t n_blocks) {
+// New tokens of a unit: as many as its rows hold, where sequences have several on average, their lists fit and single
+// tokens have a workgroup for each CU (lists of 32 blocks over 60k slots, 8 KV heads: 8 tokens 25 us together and 20 single,
+// 24 tokens 30 both, 64 tokens 39 and 47, 200 tokens 57 and 110).
+static int32_t list_tokens(int32_t batch, int64_t n_new, int32_t n_qh, int32_t n_kv, int32_t n_blocks) {
   int32_t t = 16 / n_qh;
   if (t > LIST_ALL / n_blocks) t = LIST_ALL / n_blocks;
-  return n_new >= 2 * (int64_t)batch && n_blocks <= LIST_CHUNK && t > 1 ? t : 1;
+  return n_new >= 2 * (int64_t)batch && n_new * n_kv >= N_CU && n_blocks <= LIST_CHUNK && t > 1 ? t : 1;
 }
 
 size_t paged_sparse_bytes(int64_t n_new, int32_t n_q_heads, int32_t n_kv, int32_t n_blocks) {
@@ -1263,10 +1268,10 @@ hipError_t launch_paged_sparse(const PagedRowsArgs& args, void* workspace, hipSt
   char* ws = static_cast<char*>(workspace);
   p.a.lse_u = reinterpret_cast<float*>(ws);
   p.partial = reinterpret_cast<float*>(ws + paged_round((size_t)n_kv * D * sizeof(float)));
-  p.tokens = list_tokens(p.a.c.batch, p.a.c.n_new, p.a.n_qh, p.n_blocks);
+  p.tokens = list_tokens(p.a.c.batch, p.a.c.n_new, p.a.n_qh, n_kv, p.n_blocks);
   // about as many workgroups as the card holds, of four entries at least
   const int64_t units = p.tokens == 1 ? p.a.c.n_new : p.a.c.n_new / p.tokens + p.a.c.batch;
-  const int64_t real = ceil_div(p.a.c.n_new, p.tokens) * n_kv;
+  const int64_t real = std::max(ceil_div(p.a.c.n_new, p.tokens), std::min<int64_t>(p.a.c.batch, p.a.c.n_new)) * n_kv;
   int64_t n = N_CU * kPerCu / real;
   if (n < 1) n = 1;
   int64_t each = ceil_div(ceil_div(p.n_blocks, n), RO_NW) * RO_NW;

@@ -883,7 +883,10 @@ hipError_t launch_paged_bounds(const PagedBoundsArgs& args, hipStream_t st) {
 
 namespace {
 
-constexpr int64_t kFewPairs = 256;  // tokens times KV heads up to which every head's scores are kept
+// Tokens times KV heads up to which every head's scores are kept (one sweep over the boxes, more bytes for the pick): 8 KV
+// heads of four over 100k slots, 64 tokens 33 us and 44 by values, 128 tokens 49 and 53, 192 tokens 61 both, 512 tokens 120
+// and 82; 48 sequences' single tokens over 16k slots 22 and 44.
+constexpr int64_t kFewPairs = 1024;
 constexpr int64_t kMostChunks = 128;
 
 int64_t score_pitch(int64_t max_tokens) { return (max_tokens + 16 * PAIR * TILE - 1) / (16 * PAIR * TILE) * (16 * PAIR); }
@@ -909,7 +912,8 @@ hipError_t launch_paged_select(const PagedSelectArgs& args, void* workspace, hip
   const int nb = many ? 4 : 1, tg = 16 * nb >> a.pitch_log2;
   const int64_t units = a.c.n_new / tg + a.c.batch, all = a.most_blocks / (16 * PAIR);
   // Units for at least half of the CUs: both sweeps in one workgroup of eight wavefronts, one to a CU. Otherwise
-  // two workgroups of four on a CU.
+  // two workgroups of four on a CU (8 KV heads over 100k slots: 192 tokens 61 us and 69 by both sweeps in one, 256 tokens
+  // 69 and 69, 512 tokens 96 and 82).
   const bool both = many && 2 * units * n_kv > N_CU;
   const int waves = both ? 8 : 4;
   int64_t n = both ? 1 : (2 * N_CU - 1 + units * n_kv) / (units * n_kv);
@@ -928,6 +932,7 @@ hipError_t launch_paged_select(const PagedSelectArgs& args, void* workspace, hip
   }
   const dim3 rows((unsigned)pairs);
   const int n_rows = many ? 1 : a.n_qh;
+  // (of 512 tokens and 1600 blocks in all 82 us, and 96 with 256 threads a pair)
   if (many && a.most_blocks <= 2048)
     hipLaunchKernelGGL((paged_pick_kernel<128, 4>), rows, dim3(128), 0, st, a, n_rows);
   else if (a.most_blocks <= 1024)

@@ -590,7 +590,7 @@ def test_boxes_follow_their_pages():
     assert sel.shape == (2, 2, 3) and sel.min() >= -1
 
 
-@pytest.mark.parametrize("n", [160, 1100])
+@pytest.mark.parametrize("n", [160, 600, 1100])
 def test_selection_of_many_tokens_that_are_not_finite(n):
     """Heads that have no number are passed over, and no token reaches another's, whichever way the best heads are found."""
     c = cache([2600], [n], 4, f32=True, seed=9)
@@ -611,7 +611,7 @@ def test_selection_of_many_tokens_that_are_not_finite(n):
 
 
 @pytest.mark.parametrize("f32", [False, True], ids=["bf16", "f32"])
-@pytest.mark.parametrize("new", [1, 3, 40])
+@pytest.mark.parametrize("new", [1, 3, 40, 150])
 def test_lists_over_metadata_that_is_not_finite(new, f32):
     c = cache([300], [new], f32=f32, seed=10)
     page = int(c.cache.table[0, 1])
@@ -643,3 +643,83 @@ def test_more_sequences_than_threads(f32):
     blocks = got.cpu().numpy()
     lse = torch.empty(c.q.shape[:2], device="cuda")
     check(c, list_sees(lens, new, blocks), attend(c, blocks, lse=lse), lse)
+
+
+@pytest.mark.parametrize("tokens", [1030, 2100])
+@pytest.mark.parametrize("n", [200, 1500, 3000, 10000, 17000])
+def test_equal_values_of_many_tokens(n, tokens):
+    """As above, where a KV head's values are kept instead of its heads' scores."""
+    ck, _ = codec([[4, 0, 0, 0]], 10, 1)
+    ck.basis[0] = torch.eye(D)
+    m = S.PagedCache(n, 64, 1, n)
+    m.table[0] = ints(np.arange(n)[::-1].copy())
+    m.lens[0] = n * 64
+    box = torch.zeros((n, 1, 1, 4, 2, 32), dtype=torch.float16, device="cuda")
+    vals = np.where(np.arange(n) == 11, -60000, np.random.default_rng(n).integers(0, 5, n))
+    box[m.table[0].long(), 0, 0, 0, 1, 0] = torch.tensor(vals, dtype=torch.float16, device="cuda")
+    for heads in (1, 3, 7, 16):
+        q = torch.zeros((tokens, heads, D), device="cuda")
+        q[:, :, 0] = 1.0 + torch.arange(tokens, device="cuda")[:, None] % 3
+        got = S.spectra_paged_select(m, ck, box.view(torch.int32).view(n, -1), q, ints([0, tokens]), 20, n * 64, first=0, last=0)
+        got = got.cpu().numpy()[:, 0]
+        for t in (0, 36, 100, 299, tokens - 1):
+            have = -(-(n * 64 - tokens + t + 1) // 64)
+            assert np.array_equal(got[t], np.sort(np.argsort(-vals[:have], kind="stable")[:20])), (heads, t)
+
+
+@pytest.mark.parametrize("n_qh", [1, 3, 7, 16])
+@pytest.mark.parametrize("new", [[300, 0, 260], [1000, 7, 193]])
+def test_selection_heads_of_many_tokens(new, n_qh):
+    lens = [2600, 130, 700]
+    c = cache(lens, new, n_qh, seed=n_qh + len(new))
+    box = whole(c)
+    check_selection(c, select(c, box, 9, first=2, last=1), box, B8, 64, 9, first=2)
+
+
+@pytest.mark.parametrize("f32", [False, True], ids=["bf16", "f32"])
+@pytest.mark.parametrize("n_qh", [1, 3, 4, 7, 8])
+def test_lists_of_neighbouring_tokens(n_qh, f32):
+    """Tokens enough that neighbours' lists are read together: sequences of odd lengths, lists that fall, repeat, are
+    empty or name blocks that a token does not see."""
+    lens, new = [900, 2500, 64, 0, 333], [61, 83, 3, 0, 50]
+    c = cache(lens, new, n_qh, f32=f32, seed=n_qh + 30)
+    rng = np.random.default_rng(n_qh)
+    blocks = lists(c, 12, seed=n_qh)
+    blocks[5] = rng.integers(-3, 20, (2, 12))
+    blocks[6, 0] = blocks[6, 0][::-1].copy()
+    blocks[100:104, 1] = rng.integers(0, 60, (4, 12))
+    blocks[70:75] = -1
+    blocks[8, 1], blocks[9, 1] = 3, 2 ** 31 - 1
+    lse = torch.empty(c.q.shape[:2], device="cuda")
+    out = attend(c, blocks, lse=lse)
+    check(c, list_sees(lens, new, blocks), out, lse)
+    # a page out of range counts as nothing there, for its own sequence alone
+    table = c.cache.table.clone()
+    c.cache.table[1, 0] = -5
+    got = attend(c, blocks)
+    assert torch.isfinite(got.float()).all() and torch.equal(got[:61], out[:61]) and torch.equal(got[144:], out[144:])
+    c.cache.table.copy_(table)
+
+
+def test_lists_of_neighbouring_tokens_captured_and_not_finite():
+    c = cache([3000], [140], f32=True, seed=31)
+    blocks = ints(lists(c, 9, seed=31))
+    want = S.spectra_paged_sparse_attention(c.cache, c.ck, c.cv, *c.pools, c.q, c.cu, blocks)
+    q, out = c.q.clone(), torch.empty_like(c.q)
+    q[17, 3, 5], q[90, 0, 0] = float("nan"), float("inf")
+    ws = torch.empty(S.spectra_paged_sparse_attention_workspace_bytes(140, 8, 2, 9), dtype=torch.uint8, device="cuda")
+    call = lambda: S.spectra_paged_sparse_attention(c.cache, c.ck, c.cv, *c.pools, q, c.cu, blocks, out=out, workspace=ws)  # noqa: E731
+    call()
+    torch.cuda.synchronize()
+    g = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(g):
+        call()
+    same = torch.ones(q.shape[:2], dtype=torch.bool, device="cuda")
+    same[17, 3] = same[90, 0] = False
+    for _ in range(3):
+        out.fill_(9.0)
+        g.replay()
+        torch.cuda.synchronize()
+        assert torch.equal(out[same], want[same])
+        assert torch.isnan(out[17, 3]).all() or (blocks[17, 0] < 0).all()
+        assert torch.equal(S.spectra_paged_sparse_attention(c.cache, c.ck, c.cv, *c.pools, c.q, c.cu, blocks), want)
