@@ -10,7 +10,14 @@
 // A unit is NB blocks of 16 rows, a workgroup a chunk of the unit's tiles, a wavefront tiles of its
 // own: it turns a kept group of 64 slots into fp16 coefficients in 4 KB of LDS, once for all rows of
 // the unit, and multiplies them on 16 x 16 x 32 products whose columns are the rows. No barrier until
-// the wavefronts' sums are merged. The chunks' partial sums meet in paged_rows_combine_kernel.
+// the wavefronts' sums are merged. The chunks' partial sums meet in the combine kernels.
+//
+// Measured (8-word records): 48 tokens of 28 heads over 64 blocks 37 us (12300 tiles of 4 KB, 1.4 TB/s), with the join
+// 39; 16 trees of up to 32 tokens of 32 heads over 8k slots 76 + 14 us; in fp32, 200 tokens over 32 blocks 87 + 12. Bound
+// by instructions and their latencies: a tile costs a wavefront about 10000 clocks of the 2000 that its instructions
+// need alone, with three on a SIMD (VALU 40 to 60% busy, matrix units 7 to 9, more than half of the wavefronts' time
+// waiting). Making the coefficients is half of a tile. With all records in the first cache 35 us for 37; with a
+// second tile in LDS, filled while the first is multiplied, 38.
 // With 16-bit outputs q', c and p are single fp16 numbers; with fp32 outputs (PRECISE) pairs of fp16 parts,
 // every product three.
 //
@@ -910,7 +917,7 @@ __device__ __forceinline__ void sequences_of(const PagedCache& c, int64_t t_lo, 
 }
 
 // Few rows: a workgroup each. Eight thread groups of 128 share the row's chunks; then a channel is 8 threads' dot
-// product.
+// product. Bound by latency (the sequence, the plan, the partials, one after the other): 5.8 us for 256 rows.
 template <bool TREE>
 __global__ __launch_bounds__(1024) void paged_row_combine_kernel(PagedRowsArgs p, int rows) {
   constexpr int SHARE = 8;
@@ -1017,7 +1024,8 @@ __global__ __launch_bounds__(1024) void paged_row_combine_kernel(PagedRowsArgs p
 }
 
 // Many rows: 16 to a workgroup, 16 threads a row; then the rotation as 16 x 16 x 32 products of channels and rows, a
-// wavefront 32 channels, both sides in NP bf16 parts.
+// wavefront 32 channels, both sides in NP bf16 parts. Bound by the same chain, then by the partials' bytes: 7.2 us for 1344
+// rows of four chunks, 14 for 8200 rows of up to four chunks, 12 for 6400 fp32 rows of two.
 constexpr int CO_ROWS = 16, CO_PITCH = D + 4;
 template <bool TREE, int NP>
 __global__ __launch_bounds__(256) void paged_rows_combine_kernel(PagedRowsArgs p, int rows) {
@@ -1161,7 +1169,9 @@ using namespace spectra_dev;
 
 namespace {
 
-constexpr int64_t kPerCu = 4;  // workgroups wanted of a CU at most
+// Workgroups wanted of a CU at most (NB = 1: four are resident. More row blocks: half, as two are: 16 trees of up to 32 tokens
+// 76 us, with three 88; twice or half of all made 48 tokens over 64 blocks slower too).
+constexpr int64_t kPerCu = 4;
 
 int64_t tree_units(int32_t batch, int64_t n_new, int32_t n_qh, int rows) { return n_new * n_qh / rows + batch; }
 int64_t wanted(int32_t n_kv) { return N_CU * kPerCu / n_kv > 0 ? N_CU * kPerCu / n_kv : 1; }
@@ -1227,6 +1237,7 @@ hipError_t launch_paged_tree(const PagedRowsArgs& args, void* workspace, hipStre
     if (e != hipSuccess || p.a.scan_tokens == 0) return e;
   }
   const int64_t most = (int64_t)(p.a.max_new < p.a.scan_tokens ? p.a.max_new : p.a.scan_tokens) * n_qh;
+  // (16 trees of up to 32 tokens of four heads: four blocks of rows a unit 81 us, two 91)
   const int nb = most <= 16 ? 1 : most <= 32 || p.a.out_f32 ? 2 : 4;
   p.want = (int32_t)(nb == 1 ? wanted(n_kv) : (wanted(n_kv) + 1) / 2);
   p.items = (int32_t)(p.want + tree_units(batch, n_new, n_qh, 16 * nb));
@@ -1247,13 +1258,13 @@ hipError_t launch_paged_tree(const PagedRowsArgs& args, void* workspace, hipStre
   return launch_combine<true>(p, 16 * nb, st);
 }
 
-// New tokens of a unit: as many as its rows hold, where sequences have several on average, their lists fit and single
+// New tokens of a unit: as many as its rows hold, where sequences have 1.25 on average, their lists fit and single
 // tokens have a workgroup for each CU (lists of 32 blocks over 60k slots, 8 KV heads: 8 tokens 25 us together and 20 single,
-// 24 tokens 30 both, 64 tokens 39 and 47, 200 tokens 57 and 110).
+// 24 tokens 30 both, 64 tokens 39 and 47, 200 tokens 57 and 110; 64 blocks, 48 sequences of one or two tokens 79 and 105).
 static int32_t list_tokens(int32_t batch, int64_t n_new, int32_t n_qh, int32_t n_kv, int32_t n_blocks) {
   int32_t t = 16 / n_qh;
   if (t > LIST_ALL / n_blocks) t = LIST_ALL / n_blocks;
-  return n_new >= 2 * (int64_t)batch && n_new * n_kv >= N_CU && n_blocks <= LIST_CHUNK && t > 1 ? t : 1;
+  return 4 * n_new >= 5 * (int64_t)batch && n_new * n_kv >= N_CU && n_blocks <= LIST_CHUNK && t > 1 ? t : 1;
 }
 
 size_t paged_sparse_bytes(int64_t n_new, int32_t n_q_heads, int32_t n_kv, int32_t n_blocks) {
