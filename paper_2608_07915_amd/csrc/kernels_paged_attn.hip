@@ -131,17 +131,18 @@ __device__ __forceinline__ int64_t part_at(const PagedAttnArgs& a, int64_t unit,
 }
 
 // out = (a / l + m_V) V_V^T of a wavefront's 32 rows, the coefficients as column operand, and
-// both sides in NP bf16 parts; stores the rows and their log-sum-exp. m, l: of the lane's row.
-template <int NP, int N>
+// both sides in NP bf16 parts; stores the rows and their log-sum-exp. m, l: of the lane's row. NC of the four blocks of
+// 32 channels, from cb0 on.
+template <int NP, int N, int NC = 4>
 __device__ __forceinline__ void finish_rows(const PagedAttnArgs& a, const PagedSeq& seq, const Rows& r, int kv, const Kept& Kv,
-                                            const f32x16 (&acc)[N], float m, float l, int lane) {
+                                            const f32x16 (&acc)[N], float m, float l, int lane, int cb0 = 0) {
   const int h = lane >> 5, col = lane & 31;
   const bool seen = l > 0.0f || !(l == l);
   const float inv = 1.0f / l;
   const float* Vv = a.basis_v + (int64_t)kv * D * D;
-  f32x16 out[4];
+  f32x16 out[NC];
 #pragma unroll
-  for (int cb = 0; cb < 4; ++cb) out[cb] = zero16();
+  for (int cb = 0; cb < NC; ++cb) out[cb] = zero16();
   const int i0 = 4 * (col >> 3) + (col & 3), h0 = (col >> 2) & 1;
   const int chan = 16 * h0 + i0;  // MFMA row col of a 32-channel block: then a lane half has 16 neighbouring channels
 #pragma unroll
@@ -166,10 +167,10 @@ __device__ __forceinline__ void finish_rows(const PagedAttnArgs& a, const PagedS
       bf16x8 cp[NP];
       split8<NP>(cf, cp);
 #pragma unroll
-      for (int cb = 0; cb < 4; ++cb) {
+      for (int cb = 0; cb < NC; ++cb) {
         float v[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) v[e] = Vv[(32 * cb + chan) * D + at[e]];
+        for (int e = 0; e < 8; ++e) v[e] = Vv[(32 * (cb0 + cb) + chan) * D + at[e]];
         bf16x8 vp[NP];
         split8<NP>(v, vp);
 #pragma unroll
@@ -181,9 +182,9 @@ __device__ __forceinline__ void finish_rows(const PagedAttnArgs& a, const PagedS
     }
   }
   if (!r.live) return;
-  const int64_t o = ((seq.first + r.tok) * a.n_q_heads + kv * a.n_qh + r.head) * D + 16 * h;
+  const int64_t o = ((seq.first + r.tok) * a.n_q_heads + kv * a.n_qh + r.head) * D + 32 * cb0 + 16 * h;
 #pragma unroll
-  for (int cb = 0; cb < 4; ++cb) {
+  for (int cb = 0; cb < NC; ++cb) {
     if (a.out_f32) {
       float* op = reinterpret_cast<float*>(a.out) + o + 32 * cb;
 #pragma unroll
@@ -200,7 +201,7 @@ __device__ __forceinline__ void finish_rows(const PagedAttnArgs& a, const PagedS
       *reinterpret_cast<u32x4*>(op + 4) = u32x4{w[4], w[5], w[6], w[7]};
     }
   }
-  if (a.lse != nullptr && h == 0) {
+  if (a.lse != nullptr && h == 0 && cb0 == 0) {
     const int64_t qo = (seq.first + r.tok) * a.q_token_stride + (kv * a.n_qh + r.head) * a.q_head_stride;
     float s = 0.0f;
     for (int c = 0; c < D; ++c) s = __builtin_fmaf(query_at(a, qo + c), a.lse_u[kv * D + c], s);
@@ -764,12 +765,13 @@ __global__ __launch_bounds__(64) void paged_join_kernel(PagedAttnArgs a) {
   finish_rows<PRECISE ? 3 : 2, NG>(a, seq, rows, kv, Kv, acc, m, l, lane);
 }
 
-// The same for trees: four wavefronts share a unit's parts, which are many where a sequence is alone (64 tokens of seven
-// heads over 131k slots: 512 parts, 22 us of 185, bound by their bytes).
+// The same for trees: four wavefronts share a unit's parts, which are many where a sequence is alone, then each takes a
+// block of 32 channels (64 tokens of seven heads over 131k slots, 256 parts: 20 us, 22 with one that does all channels;
+// eight wavefronts the same: a chain of latencies).
 __global__ __launch_bounds__(256) void paged_tree_join_kernel(PagedAttnArgs a) {
   constexpr int NW = 4, SIZE = (16 * NG + 2) * 64;
   __shared__ FindScratch find_s;
-  __shared__ float sums_s[(NW - 1) * SIZE];
+  __shared__ float sums_s[NW * SIZE];
   const int kv = (int)(blockIdx.x % (unsigned)a.c.n_kv), block = blockIdx.y, lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t unit = blockIdx.x / (unsigned)a.c.n_kv;
   int b;
@@ -804,21 +806,22 @@ __global__ __launch_bounds__(256) void paged_tree_join_kernel(PagedAttnArgs a) {
   };
 #pragma unroll 1
   for (int i = wave; i < n_parts; i += NW) add(a.partial + part_at(a, unit, kv, i, block) + lane);
-  if (wave > 0) {
-    float* p = sums_s + (wave - 1) * SIZE + lane;
+  float* mine = sums_s + wave * SIZE + lane;
 #pragma unroll
-    for (int sl = 0; sl < NG; ++sl)
-      if (sl < Kv.n)
+  for (int sl = 0; sl < NG; ++sl)
+    if (sl < Kv.n)
 #pragma unroll
-        for (int j = 0; j < 16; ++j) p[(16 * sl + j) * 64] = acc[sl][j];
-    p[16 * NG * 64] = m;
-    p[(16 * NG + 1) * 64] = l;
-  }
+      for (int j = 0; j < 16; ++j) mine[(16 * sl + j) * 64] = acc[sl][j];
+  mine[16 * NG * 64] = m;
+  mine[(16 * NG + 1) * 64] = l;
   __syncthreads();
-  if (wave > 0) return;
+  m = -__builtin_inff();
+  l = 0.0f;
+#pragma unroll
+  for (int sl = 0; sl < NG; ++sl) acc[sl] = zero16();
 #pragma unroll 1
-  for (int w = 1; w < NW; ++w) add(sums_s + (w - 1) * SIZE + lane);
-  finish_rows<2, NG>(a, seq, rows, kv, Kv, acc, m, l, lane);
+  for (int w = 0; w < NW; ++w) add(sums_s + w * SIZE + lane);
+  finish_rows<2, NG, 1>(a, seq, rows, kv, Kv, acc, m, l, lane, wave);
 }
 
 // ---------------------------------------------------------------------------
