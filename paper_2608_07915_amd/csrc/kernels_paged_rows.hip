@@ -269,14 +269,15 @@ constexpr int LIST_CHUNK = 256;   // entries of a workgroup at most, where a uni
 constexpr int LIST_ALL = 256;     // entries of a unit's tokens at most, where it is several
 
 // What the lists of n tokens name together, each block once, with the tokens that name it as bits. Lists as
-// in read_list, token i's below blocks(i). A wavefront packs a token's list; then each of its entries is looked up in the
-// others' (by halves, they ascend): the first token that names a block brings it in. Returns how many.
+// in read_list, token i's below blocks(i). A wavefront packs a token's list; then each of its entries is looked up in all
+// (by halves, they ascend): the first token that names a block brings it in. packed, who: LIST_ALL entries. Returns how many.
 struct UnionScratch {
   int32_t count[16], own[16];
 };
 template <typename Blocks>
 __device__ __forceinline__ int read_lists(const int32_t* __restrict__ lists, int64_t stride, int n_blocks, int n, Blocks&& blocks,
-                                          int32_t* packed, int32_t* sel, uint16_t* bits, UnionScratch& s) {
+                                          int32_t* packed, uint16_t* who, int32_t* sel, uint16_t* bits, UnionScratch& s) {
+  constexpr int SEARCH = 4;  // lists searched side by side
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
   const uint64_t below = ((uint64_t)1 << lane) - 1;
   for (int i = wave; i < n; i += RO_NW) {
@@ -303,39 +304,56 @@ __device__ __forceinline__ int read_lists(const int32_t* __restrict__ lists, int
     if (lane == 0) s.count[i] = at;
   }
   __syncthreads();
-  auto names = [&](int i, int x) {
-    int lo = 0, hi = s.count[i];
-    while (lo < hi) {
-      const int mid = (lo + hi) >> 1;
-      if (packed[i * n_blocks + mid] < x) lo = mid + 1; else hi = mid;
-    }
-    return lo < s.count[i] && packed[i * n_blocks + lo] == x;
-  };
-  // twice: first how many a token brings in, then where they go
-  int total = 0;
-  for (int pass = 0; pass < 2; ++pass) {
-    for (int i = wave; i < n; i += RO_NW) {
-      int at = 0;
-      if (pass > 0)
-        for (int j = 0; j < i; ++j) at += s.own[j];
-      for (int e0 = 0; e0 < s.count[i]; e0 += 64) {
-        const int e = e0 + lane;
-        bool own = e < s.count[i];
-        const int x = own ? packed[i * n_blocks + e] : 0;
-        for (int j = 0; j < i && own; ++j) own = !names(j, x);
-        const uint64_t m = __ballot(own);
-        if (pass > 0 && own) {
-          uint32_t who = 1u << i;
-          for (int j = i + 1; j < n; ++j) who |= names(j, x) ? 1u << j : 0u;
-          sel[at + __popcll(m & below)] = x;
-          bits[at + __popcll(m & below)] = (uint16_t)who;
+  int most = 1;  // the search's first step
+  while (2 * most <= n_blocks) most *= 2;
+  for (int i = wave; i < n; i += RO_NW) {
+    int at = 0;
+    for (int e0 = 0; e0 < s.count[i]; e0 += 64) {
+      const int e = e0 + lane;
+      const bool live = e < s.count[i];
+      const int x = live ? packed[i * n_blocks + e] : 0;
+      uint32_t by = 0u;
+      for (int j0 = 0; j0 < n; j0 += SEARCH) {
+        int pos[SEARCH], end[SEARCH];
+#pragma unroll
+        for (int k = 0; k < SEARCH; ++k) {
+          pos[k] = 0;
+          end[k] = j0 + k < n ? s.count[j0 + k] : 0;
         }
-        at += __popcll(m);
+        for (int step = most; step > 0; step >>= 1) {
+#pragma unroll
+          for (int k = 0; k < SEARCH; ++k) {
+            const int to = pos[k] + step;
+            if (to <= end[k] && packed[(j0 + k) * n_blocks + to - 1] < x) pos[k] = to;
+          }
+        }
+#pragma unroll
+        for (int k = 0; k < SEARCH; ++k)
+          if (pos[k] < end[k] && packed[(j0 + k) * n_blocks + pos[k]] == x) by |= 1u << (j0 + k);
       }
-      if (pass == 0 && lane == 0) s.own[i] = at;
+      const bool own = live && (by & ((1u << i) - 1)) == 0u;  // no token before names it
+      if (live) who[i * n_blocks + e] = own ? (uint16_t)by : 0;
+      at += __popcll(__ballot(own));
     }
-    __syncthreads();
+    if (lane == 0) s.own[i] = at;
   }
+  __syncthreads();
+  for (int i = wave; i < n; i += RO_NW) {
+    int at = 0;
+    for (int j = 0; j < i; ++j) at += s.own[j];
+    for (int e0 = 0; e0 < s.count[i]; e0 += 64) {
+      const int e = e0 + lane;
+      const uint16_t by = e < s.count[i] ? who[i * n_blocks + e] : 0;
+      const uint64_t m = __ballot(by != 0);
+      if (by != 0) {
+        sel[at + __popcll(m & below)] = packed[i * n_blocks + e];
+        bits[at + __popcll(m & below)] = by;
+      }
+      at += __popcll(m);
+    }
+  }
+  __syncthreads();
+  int total = 0;
   for (int i = 0; i < n; ++i) total += s.own[i];
   return total;
 }
@@ -373,7 +391,7 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
   __shared__ __attribute__((aligned(16))) float sums_s[RO_NW * 16 * RO_PITCH];  // the tiles while wavefronts walk
   __shared__ __attribute__((aligned(16))) uint8_t q_s[NG][NB][NP][64 * 16];      // q' as column operands, by lane
   static_assert(sizeof(sums_s) >= RO_NW * NP * CA_TILE, "the tiles lie where the sums do");
-  static_assert(sizeof(sums_s) >= LIST_ALL * sizeof(int32_t), "and the packed lists before them");
+  static_assert(sizeof(sums_s) >= LIST_ALL * (sizeof(int32_t) + sizeof(uint16_t)), "and the packed lists before them");
   const PagedAttnArgs& a = p.a;
   const int kv = (int)(blockIdx.x % (unsigned)a.c.n_kv);
   const int64_t item = blockIdx.x / (unsigned)a.c.n_kv;
@@ -417,7 +435,7 @@ __global__ __launch_bounds__(RO_NT, NB == 1 && !PRECISE ? 4 : 2) void paged_rows
     } else {
       all = (1u << n_tok) - 1;
       const int n = read_lists(list, (int64_t)a.c.n_kv * p.n_blocks, p.n_blocks, n_tok, blocks, reinterpret_cast<int32_t*>(sums_s),
-                               sel_s, who_s, union_s);
+                               reinterpret_cast<uint16_t*>(sums_s + LIST_ALL), sel_s, who_s, union_s);
       int each = (n + p.n_chunks - 1) / p.n_chunks;
       each = (each + RO_NW - 1) / RO_NW * RO_NW;
       begin = chunk * each < n ? chunk * each : n;
