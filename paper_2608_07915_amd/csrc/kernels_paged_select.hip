@@ -597,11 +597,12 @@ __device__ __forceinline__ void find_step(const int32_t* count, int left, int32_
   __syncthreads();
 }
 
-// The heads' best over their chunks (values have none: theirs is taken off already).
+// The heads' best over their chunks, also of one head: what is picked from counts down from 0 (raw scores, mostly positive,
+// would all fall into one step: one token and one head to a KV head over 65k slots 306 us, so 16). Values: theirs is off already.
 template <int NT>
 __device__ __forceinline__ void best_of_heads(const PagedSelectArgs& a, int64_t t, int kv, int n_rows, float* top) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  if (n_rows == 1) {
+  if (a.by_values) {
     if (threadIdx.x == 0) top[0] = 0.0f;
     return;
   }
@@ -940,6 +941,7 @@ hipError_t launch_paged_select(const PagedSelectArgs& args, void* workspace, hip
     hipLaunchKernelGGL((paged_block_scores_kernel<1, 4, HEADS>), grid, dim3(256), 0, st, a, (int)steps);
   }
   const dim3 rows((unsigned)pairs);
+  a.by_values = many;
   const int n_rows = many ? 1 : a.n_qh;
   // (of 512 tokens and 1600 blocks in all 82 us, and 96 with 256 threads a pair)
   if (many && a.most_blocks <= 2048)

@@ -117,6 +117,7 @@ struct PagedSelectArgs {
   int32_t n_blocks, first, last;
   int32_t* blocks;
   float* scores;        // workspace: [n_new][n_q_heads][most_blocks], or the values [n_new][n_kv][most_blocks]
+  int32_t by_values;    // it holds values: the heads' best are taken off already
   float* tops;          // workspace: [n_new][n_q_heads][n_chunks], the heads' best scores
   int32_t most_blocks;  // that a sequence of max_tokens has
   int32_t n_chunks;     // of its blocks
