@@ -66,6 +66,8 @@ __device__ __forceinline__ f16x2 reduce_slots(const f16x2 (&r)[16], int lane, Op
     const uint32_t s0 = s[0], s1 = s[1];  // (a bit cast of a vector's element reads its first)
     a[i] = op(__builtin_bit_cast(f16x2, s0), __builtin_bit_cast(f16x2, s1));
   }
+  // an exchange of rows reads what was written two wait states ago or more; the compiler does not count from op's assembly
+  asm volatile("s_nop 1" : "+v"(a[0]), "+v"(a[1]), "+v"(a[2]), "+v"(a[3]), "+v"(a[4]), "+v"(a[5]), "+v"(a[6]), "+v"(a[7]));
 #pragma unroll
   for (int i = 0; i < 4; ++i) {  // rows of 16 lanes
     const auto s = __builtin_amdgcn_permlane16_swap(__builtin_bit_cast(uint32_t, a[i]), __builtin_bit_cast(uint32_t, a[i + 4]), false, false);
