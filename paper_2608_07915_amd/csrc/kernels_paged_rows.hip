@@ -1187,13 +1187,6 @@ using namespace spectra_dev;
 
 namespace {
 
-// Workgroups wanted of a CU at most (NB = 1: four are resident. More row blocks: half, as two are: 16 trees of up to 32 tokens
-// 76 us, with three 88; twice or half of all made 48 tokens over 64 blocks slower too).
-constexpr int64_t kPerCu = 4;
-
-int64_t tree_units(int32_t batch, int64_t n_new, int32_t n_qh, int rows) { return n_new * n_qh / rows + batch; }
-int64_t wanted(int32_t n_kv) { return N_CU * kPerCu / n_kv > 0 ? N_CU * kPerCu / n_kv : 1; }
-
 template <int NB, bool PRECISE, bool TREE>
 void launch_rows(const PagedRowsArgs& p, dim3 grid, hipStream_t st) {
   hipLaunchKernelGGL((paged_rows_kernel<NB, PRECISE, TREE>), grid, dim3(RO_NT), 0, st, p);
@@ -1215,50 +1208,32 @@ hipError_t launch_combine(const PagedRowsArgs& p, int rows, hipStream_t st) {
 
 }  // namespace
 
-// With 16-bit outputs sequences of more rows on a KV head are paged_chunk_kernel's, in units of 256 rows that share the
-// making of the coefficients (64 tokens of seven heads over 131k slots 191 us and 242; up to 128 rows, which leave half of
-// its wavefronts empty, 16 trees of up to 32 tokens of four heads 176 and 108).
-constexpr int64_t kFewRows = 128;
+static_assert(PART * sizeof(float) == SCAN_PART_BYTES, "workspace of a row");
 
-// The plan and the partials of any unit size, and the parts of the others' units.
 size_t paged_tree_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv, int32_t max_new, int64_t max_tokens) {
-  (void)max_tokens;
-  const int32_t n_qh = n_q_heads / n_kv;
-  const size_t lse = paged_round((size_t)n_kv * D * sizeof(float));
-  const size_t plan = paged_round((size_t)tree_units(batch, n_new, n_qh, 16) * 2 * sizeof(int32_t));
-  const size_t b = lse + plan + paged_round((size_t)((wanted(n_kv) + batch) * 64 + n_new * n_qh) * n_kv * PART * sizeof(float));
-  // (split calls have at most two parts for a CU)
-  return b + (max_new * n_qh > kFewRows ? 2 * N_CU * PAGED_PART_BYTES : 0);
+  return tree_workspace_bytes(batch, n_new, n_q_heads / n_kv, n_kv, max_new, max_tokens);
 }
 
 hipError_t launch_paged_tree(const PagedRowsArgs& args, void* workspace, hipStream_t st) {
   PagedRowsArgs p = args;
-  const int32_t n_kv = p.a.c.n_kv, batch = p.a.c.batch, n_qh = p.a.n_qh;
-  const int64_t n_new = p.a.c.n_new, few = kFewRows / n_qh;
+  const int32_t n_kv = p.a.c.n_kv;
+  const TreePlan plan = tree_plan(p.a.c.batch, p.a.c.n_new, p.a.n_qh, n_kv, p.a.max_new, p.a.max_tokens, p.a.out_f32);
   char* ws = static_cast<char*>(workspace);
   p.a.lse_u = reinterpret_cast<float*>(ws);
-  ws += paged_round((size_t)n_kv * D * sizeof(float));
-  p.plan = reinterpret_cast<int32_t*>(ws);
-  ws += paged_round((size_t)tree_units(batch, n_new, n_qh, 16) * 2 * sizeof(int32_t));
-  p.partial = reinterpret_cast<float*>(ws);
-  ws += paged_round((size_t)((wanted(n_kv) + batch) * 64 + n_new * n_qh) * n_kv * PART * sizeof(float));
-  // none of few rows where every sequence has max_new; with fp32 outputs all are
-  p.a.scan_tokens = (int32_t)(p.a.out_f32 || p.a.max_new <= few ? p.a.max_new : n_new < (int64_t)batch * p.a.max_new ? few : 0);
-  if (p.a.max_new > p.a.scan_tokens) {
-    const int64_t units = paged_units(batch, n_new, n_qh, p.a.max_new);
-    const ChunkSplit split = paged_chunk_split(units * n_kv, p.a.max_tokens);
-    p.a.part_slots = split.slots;
-    p.a.parts = split.parts;
-    p.a.partial = reinterpret_cast<float*>(ws);
+  p.plan = reinterpret_cast<int32_t*>(ws + plan.plan_at);
+  p.partial = reinterpret_cast<float*>(ws + plan.rows_at);
+  p.a.scan_tokens = plan.scan_tokens;
+  if (plan.units > 0) {
+    p.a.part_slots = plan.split.slots;
+    p.a.parts = plan.split.parts;
+    p.a.partial = reinterpret_cast<float*>(ws + plan.part_at);
     if (p.a.lse != nullptr) launch_paged_lse(p.a, st);
-    const hipError_t e = launch_paged_tree_chunks(p.a, units, st);
+    const hipError_t e = launch_paged_tree_chunks(p.a, plan.units, st);
     if (e != hipSuccess || p.a.scan_tokens == 0) return e;
   }
-  const int64_t most = (int64_t)(p.a.max_new < p.a.scan_tokens ? p.a.max_new : p.a.scan_tokens) * n_qh;
-  // (16 trees of up to 32 tokens of four heads: four blocks of rows a unit 81 us, two 91)
-  const int nb = most <= 16 ? 1 : most <= 32 || p.a.out_f32 ? 2 : 4;
-  p.want = (int32_t)(nb == 1 ? wanted(n_kv) : (wanted(n_kv) + 1) / 2);
-  p.items = (int32_t)(p.want + tree_units(batch, n_new, n_qh, 16 * nb));
+  const int nb = plan.nb;
+  p.want = plan.want;
+  p.items = plan.items;
   const dim3 grid((unsigned)((int64_t)p.items * n_kv));
   if (p.a.out_f32) {
     if (nb == 1)
@@ -1287,7 +1262,7 @@ static int32_t list_tokens(int32_t batch, int64_t n_new, int32_t n_qh, int32_t n
 
 size_t paged_sparse_bytes(int64_t n_new, int32_t n_q_heads, int32_t n_kv, int32_t n_blocks) {
   // chunks of all rows: what the card's workgroups hold, and each row's own (more where chunks are full)
-  const int64_t rows = N_CU * kPerCu * 16 + n_new * n_q_heads * (1 + ceil_div(n_blocks, LIST_CHUNK));
+  const int64_t rows = N_CU * ROWS_PER_CU * 16 + n_new * n_q_heads * (1 + ceil_div(n_blocks, LIST_CHUNK));
   return paged_round((size_t)n_kv * D * sizeof(float)) + (size_t)rows * PART * sizeof(float);
 }
 
@@ -1301,7 +1276,7 @@ hipError_t launch_paged_sparse(const PagedRowsArgs& args, void* workspace, hipSt
   // about as many workgroups as the card holds, of four entries at least
   const int64_t units = p.tokens == 1 ? p.a.c.n_new : p.a.c.n_new / p.tokens + p.a.c.batch;
   const int64_t real = std::max(ceil_div(p.a.c.n_new, p.tokens), std::min<int64_t>(p.a.c.batch, p.a.c.n_new)) * n_kv;
-  int64_t n = N_CU * kPerCu / real;
+  int64_t n = N_CU * ROWS_PER_CU / real;
   if (n < 1) n = 1;
   int64_t each = ceil_div(ceil_div(p.n_blocks, n), RO_NW) * RO_NW;
   if (p.tokens == 1 && each > LIST_CHUNK) each = LIST_CHUNK;

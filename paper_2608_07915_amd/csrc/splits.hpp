@@ -297,4 +297,74 @@ inline size_t paged_workspace_bytes(int32_t batch, int64_t n_new, int32_t n_q_he
   return b;
 }
 
+// Attention of drafted trees. With 16-bit outputs sequences of more than TREE_FEW_ROWS rows on a KV head are the chunk
+// kernel's, in units of PAGED_ROWS rows that share the making of the coefficients (64 tokens of seven heads over 131k slots
+// 191 us and 242; up to 128 rows, which leave half of its wavefronts empty, 16 trees of up to 32 tokens of four heads 176
+// and 108).
+constexpr int64_t TREE_FEW_ROWS = 128;
+// Workgroups wanted of a CU at most (NB = 1: four are resident. More row blocks: half, as two are: 16 trees of up to 32 tokens
+// 76 us, with three 88; twice or half of all made 48 tokens over 64 blocks slower too).
+constexpr int64_t ROWS_PER_CU = 4;
+struct TreePlan {
+  int32_t scan_tokens;  // sequences of at most so many new tokens are the rows kernel's (0: none)
+  int32_t nb;           // its units are of 16 nb rows
+  int32_t want, items;  // its workgroups per KV head: how many are wanted, and the most that come out
+  int64_t units;        // of PAGED_ROWS rows, for the others (0: none)
+  ChunkSplit split;
+  size_t plan_at, rows_at, part_at, bytes;  // workspace: lse terms, the plan, the rows kernel's partials, the parts
+};
+inline int64_t tree_units(int32_t batch, int64_t n_new, int32_t n_qh, int rows) { return n_new * n_qh / rows + batch; }
+inline int64_t rows_wanted(int32_t n_kv) { return N_CU * ROWS_PER_CU / n_kv > 0 ? N_CU * ROWS_PER_CU / n_kv : 1; }
+// Row blocks of a unit (16 trees of up to 32 tokens of four heads: four blocks a unit 81 us, two 91).
+inline int32_t tree_blocks(int64_t rows, bool out_f32) { return rows <= 16 ? 1 : rows <= 32 || out_f32 ? 2 : 4; }
+// The most units of 16 nb rows that sequences of at most `rows` rows come to, and workgroups wanted for them.
+inline int64_t tree_most(int32_t batch, int64_t n_new, int32_t n_qh, int64_t rows, int32_t nb) {
+  const int64_t all = tree_units(batch, n_new, n_qh, 16 * nb), most = ceil_div(rows, 16 * nb) * batch;
+  return all < most ? all : most;
+}
+inline int64_t tree_wanted(int32_t n_kv, int32_t nb) { return nb == 1 ? rows_wanted(n_kv) : (rows_wanted(n_kv) + 1) / 2; }
+inline TreePlan tree_plan(int32_t batch, int64_t n_new, int32_t n_qh, int32_t n_kv, int32_t max_new, int64_t max_tokens, bool out_f32) {
+  TreePlan p{};
+  const int32_t few = (int32_t)(TREE_FEW_ROWS / n_qh);
+  // none of few rows where every sequence has max_new; with fp32 outputs all are
+  p.scan_tokens = out_f32 || max_new <= few ? max_new : n_new < (int64_t)batch * max_new ? few : 0;
+  p.nb = tree_blocks((int64_t)p.scan_tokens * n_qh, out_f32);
+  p.want = (int32_t)tree_wanted(n_kv, p.nb);
+  p.items = (int32_t)(p.want + tree_most(batch, n_new, n_qh, (int64_t)p.scan_tokens * n_qh, p.nb));
+  p.split = ChunkSplit{max_tokens, 1};
+  if (max_new > p.scan_tokens) {
+    p.units = paged_units(batch, n_new, n_qh, max_new);
+    p.split = paged_chunk_split(p.units * n_kv, max_tokens);
+  }
+  p.plan_at = paged_round((size_t)n_kv * 128 * sizeof(float));
+  p.rows_at = p.part_at = p.plan_at;
+  if (p.scan_tokens > 0) {
+    p.rows_at += paged_round((size_t)tree_units(batch, n_new, n_qh, 16 * p.nb) * 2 * sizeof(int32_t));
+    p.part_at = p.rows_at + paged_round((size_t)p.items * n_kv * 16 * p.nb * SCAN_PART_BYTES);
+  }
+  p.bytes = p.part_at + (p.split.parts > 1 ? (size_t)(p.units * n_kv * p.split.parts) * PAGED_PART_BYTES : 0);
+  return p;
+}
+// What any call of as many heads with at most these counts needs, whatever its outputs' type.
+inline size_t tree_workspace_bytes(int32_t batch, int64_t n_new, int32_t n_qh, int32_t n_kv, int32_t max_new, int64_t max_tokens) {
+  const int64_t rows = (int64_t)max_new * n_qh, few = TREE_FEW_ROWS / n_qh * n_qh;
+  int64_t partials = 0;
+  for (int out_f32 = 0; out_f32 < 2; ++out_f32) {
+    const int64_t r = out_f32 || rows < few ? rows : few;
+    const int32_t nb = tree_blocks(r, out_f32);
+    const int64_t whole = ceil_div(r, 16 * nb) * 16 * nb * batch, loose = n_new * n_qh + (int64_t)batch * 16 * nb;
+    const int64_t n = tree_wanted(n_kv, nb) * 16 * nb + (whole < loose ? whole : loose);
+    partials = n > partials ? n : partials;
+  }
+  size_t b = paged_round((size_t)n_kv * 128 * sizeof(float)) + paged_round((size_t)tree_units(batch, n_new, n_qh, 16) * 2 * sizeof(int32_t)) +
+             paged_round((size_t)(partials * n_kv) * SCAN_PART_BYTES);
+  if (rows > TREE_FEW_ROWS) {  // (split calls have at most two parts for a CU)
+    const int64_t steps = ceil_div(max_tokens, PAGED_STEP);
+    int64_t parts = paged_units(batch, n_new, n_qh, max_new) * n_kv * (steps < 64 ? steps : 64);
+    if (parts > 2 * N_CU) parts = 2 * N_CU;
+    b += (size_t)parts * PAGED_PART_BYTES;
+  }
+  return b;
+}
+
 }  // namespace spectra
