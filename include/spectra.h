@@ -443,7 +443,7 @@ spectra_status spectra_paged_attention(const spectra_pages* m, const spectra_cod
  * as -1. A token whose own slot would lie before slot 0 sees none. At most 64 new tokens of a
  * sequence (max_new). The bounds of spectra_paged_attention's errors hold; with fp32 outputs all
  * weights are pairs of fp16 parts. Workspace: spectra_paged_tree_attention_workspace_bytes, never
- * fewer for larger counts. Asynchronous. */
+ * fewer for larger counts of as many heads. Asynchronous. */
 size_t spectra_paged_tree_attention_workspace_bytes(int32_t batch, int64_t n_new, int32_t n_q_heads, int32_t n_kv_heads,
                                                     int32_t max_new, int64_t max_tokens);
 spectra_status spectra_paged_tree_attention(const spectra_pages* m, const spectra_codec* ck, const spectra_codec* cv,
@@ -501,7 +501,7 @@ spectra_status spectra_paged_bounds(const spectra_pages* m, const spectra_codec*
  * max_tokens slots are left as they were. first, last >= 0, first + last <= n_blocks <= 4096; at most
  * 2^21 query rows and 2^18 sequences times KV heads, here and in the attentions of this part.
  * A page out of range counts as boxes of zeros. Workspace: device, 256-byte aligned,
- * spectra_paged_select_workspace_bytes, never fewer for larger counts. Asynchronous. */
+ * spectra_paged_select_workspace_bytes, never fewer for larger counts of as many heads. Asynchronous. */
 size_t spectra_paged_select_workspace_bytes(int64_t n_new, int32_t n_q_heads, int32_t n_kv_heads, int64_t max_tokens);
 spectra_status spectra_paged_select(const spectra_pages* m, const spectra_codec* ck, const uint32_t* bounds,
                                     const int32_t* rows, const int32_t* ends, const int32_t* cu_new, int32_t batch,
@@ -515,9 +515,9 @@ spectra_status spectra_paged_select(const spectra_pages* m, const spectra_codec*
  * spectra_paged_select writes them. Entries that are negative, past the blocks that the token sees, or not
  * greater than every entry before them in the list are passed over, so no block counts twice. A token
  * that sees no slot gets zeros and -inf. Sequences of any length and number of new tokens take part.
- * With fp32 outputs all weights are pairs of fp16 parts. n_blocks <= 4096, n_new * n_kv * n_blocks
- * (in whole 256s) <= 2^29. Workspace: device, 256-byte aligned, spectra_paged_sparse_attention_workspace_bytes, never fewer
- * for larger counts. Asynchronous. */
+ * With fp32 outputs all weights are pairs of fp16 parts. 1 <= n_blocks <= 4096, n_new * n_kv * n_blocks
+ * (in whole 256s) <= 2^29. Workspace: device, 256-byte aligned, spectra_paged_sparse_attention_workspace_bytes,
+ * never fewer for larger counts of as many heads. Asynchronous. */
 size_t spectra_paged_sparse_attention_workspace_bytes(int64_t n_new, int32_t n_q_heads, int32_t n_kv_heads, int32_t n_blocks);
 spectra_status spectra_paged_sparse_attention(const spectra_pages* m, const spectra_codec* ck, const spectra_codec* cv,
                                               const uint32_t* pool_k, const uint32_t* pool_v, const int32_t* rows,

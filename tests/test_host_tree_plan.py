@@ -5,6 +5,7 @@ import shutil
 import subprocess
 import tempfile
 
+import numpy as np
 import pytest
 
 import paper_2608_07915_amd as S
@@ -31,3 +32,20 @@ def test_tree_workspace_by_the_rows_there_are(batch, new, q, kv):
     unit = 16 if rows <= 16 else 32 if rows <= 32 else 64
     held = batch * kv * (-(-rows // unit) * unit) + (1024 + kv) * max(16, unit // 2) + kv * unit
     assert S.spectra_paged_tree_attention_workspace_bytes(batch, batch * new, q, kv, new, 1000) <= 136 * 4 * held + (1 << 20)
+
+
+def test_workspaces_serve_every_smaller_call_of_as_many_heads():
+    """What the header promises of the calls on trees, selections and lists: counts of tokens, sequences, slots and blocks in
+    any combination, heads as they are."""
+    rng = np.random.default_rng(0)
+    pick = lambda hi: int(np.exp(rng.uniform(0, np.log(hi + 1))))  # noqa: E731
+    for _ in range(3000):
+        kv, n_qh = pick(300), pick(16)
+        most = (1 << 21) // (kv * n_qh)
+        batch, new, max_new, tokens, blocks = pick(16384), pick(most), pick(64), pick(1 << 21), pick(4096)
+        b, n, m, t, k = pick(batch), pick(new), pick(max_new), pick(tokens), pick(blocks)
+        q = kv * n_qh
+        for call, large, small in ((S.spectra_paged_tree_attention_workspace_bytes, (batch, new, q, kv, max_new, tokens), (b, n, q, kv, m, t)),
+                                   (S.spectra_paged_select_workspace_bytes, (new, q, kv, tokens), (n, q, kv, t)),
+                                   (S.spectra_paged_sparse_attention_workspace_bytes, (new, q, kv, blocks), (n, q, kv, k))):
+            assert 0 < call(*small) <= call(*large), (call.__name__, large, small)
