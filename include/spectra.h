@@ -501,7 +501,9 @@ spectra_status spectra_paged_bounds(const spectra_pages* m, const spectra_codec*
  * max_tokens slots are left as they were. first, last >= 0, first + last <= n_blocks <= 4096; at most
  * 2^21 query rows and 2^18 sequences times KV heads, here and in the attentions of this part.
  * A page out of range counts as boxes of zeros. Workspace: device, 256-byte aligned,
- * spectra_paged_select_workspace_bytes, never fewer for larger counts of as many heads. Asynchronous. */
+ * spectra_paged_select_workspace_bytes, never fewer for larger counts of as many heads: a float for each
+ * block of max_tokens and each KV head (query head, where n_new * KV heads <= 1024) of as many new tokens
+ * at a time as 1 GiB holds, one at least. Asynchronous. */
 size_t spectra_paged_select_workspace_bytes(int64_t n_new, int32_t n_q_heads, int32_t n_kv_heads, int64_t max_tokens);
 spectra_status spectra_paged_select(const spectra_pages* m, const spectra_codec* ck, const uint32_t* bounds,
                                     const int32_t* rows, const int32_t* ends, const int32_t* cu_new, int32_t batch,

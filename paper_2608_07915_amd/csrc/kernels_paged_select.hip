@@ -176,7 +176,8 @@ __global__ __launch_bounds__(256) void paged_bounds_kernel(PagedBoundsArgs a) {
 // sign into the part against the least values and the one against the largest; the boxes are exact, so a
 // score is off by about 2^-22 of sum_j |q'_j box_j| and the sums' roundings.
 // Sequence b's units begin at first_b / TG + b: those of two sequences never meet, and a workgroup
-// finds its own without a sum over the others.
+// finds its own without a sum over the others. A launch is of the new tokens from .. to, as many as the scores' room holds:
+// to it a sequence is its tokens among those, and its end the slot of the last.
 //
 // Few tokens: HEADS writes every head's scores and the best of its chunk of blocks, the rest is
 // paged_pick_kernel's. Many: TOPS finds the heads' best alone, VALUES makes the scores again and writes
@@ -191,24 +192,33 @@ __global__ __launch_bounds__(256) void paged_bounds_kernel(PagedBoundsArgs a) {
 struct UnitScratch {
   int32_t b;
 };
+// Sequence b as this launch has it; n = 0 where it has none of its tokens, or more slots than the call allows.
+__device__ __forceinline__ PagedSeq launched(const PagedSelectArgs& a, int b) {
+  PagedSeq s = paged_seq(a.c, b);
+  const int64_t end = s.first + s.n, lo = s.first < a.from ? a.from : s.first, hi = end < a.to ? end : a.to;
+  s.n = lo < hi && s.len <= a.max_tokens ? hi - lo : 0;
+  s.first = lo;
+  s.len -= end - hi;  // (below 0: it sees nothing)
+  return s;
+}
 // The sequence of unit u and the unit's place in it; the same in every thread. b < 0: none.
 template <int NT>
-__device__ __forceinline__ int find_token_unit(const PagedCache& c, int64_t u, int tg, UnitScratch& s, int64_t& at) {
-  if (c.batch == 1) {
-    const PagedSeq q = paged_seq(c, 0);
-    at = u - q.first / tg;
+__device__ __forceinline__ int find_token_unit(const PagedSelectArgs& a, int64_t u, int tg, UnitScratch& s, int64_t& at) {
+  if (a.c.batch == 1) {
+    const PagedSeq q = launched(a, 0);
+    at = u - (q.first - a.from) / tg;
     return at >= 0 && at < (q.n + tg - 1) / tg ? 0 : -1;
   }
   if (threadIdx.x == 0) s.b = -1;
   __syncthreads();
-  for (int b = threadIdx.x; b < c.batch; b += NT) {
-    const PagedSeq q = paged_seq(c, b);
-    const int64_t base = q.first / tg + b;
+  for (int b = threadIdx.x; b < a.c.batch; b += NT) {
+    const PagedSeq q = launched(a, b);
+    const int64_t base = (q.first - a.from) / tg + b;
     if (u >= base && u < base + (q.n + tg - 1) / tg) atomicMax(&s.b, b);
   }
   __syncthreads();
   const int b = __builtin_amdgcn_readfirstlane(s.b);
-  if (b >= 0) at = u - (paged_seq(c, b).first / tg + b);
+  if (b >= 0) at = u - ((launched(a, b).first - a.from) / tg + b);
   return b;
 }
 
@@ -217,6 +227,7 @@ __device__ const u32x4 empty_box[BOX_WORDS / 4] = {};
 
 enum SelectMode { HEADS, TOPS, VALUES, BOTH };
 constexpr int PAIR = 2;  // block tiles of a wavefront's step: an operand of q' is read once for both
+static_assert(16 * PAIR == spectra::SELECT_STEP, "whole steps in a row of scores");
 
 template <int NB, int NW, SelectMode MODE>
 __global__ __launch_bounds__(64 * NW, 2) void paged_block_scores_kernel(PagedSelectArgs a, int steps) {
@@ -231,10 +242,9 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_block_scores_kernel(PagedSel
   const int tid = threadIdx.x, lane = tid & 63, col = lane & 15, quarter = lane >> 4;
   const int wave = __builtin_amdgcn_readfirstlane(tid >> 6);
   int64_t at = 0;
-  const int b = find_token_unit<NT>(a.c, blockIdx.x / (unsigned)a.c.n_kv, tg, unit_s, at);
+  const int b = find_token_unit<NT>(a, blockIdx.x / (unsigned)a.c.n_kv, tg, unit_s, at);
   if (b < 0) return;
-  const PagedSeq seq = paged_seq(a.c, b);
-  if (seq.len > a.max_tokens) return;
+  const PagedSeq seq = launched(a, b);
   const int64_t tok0 = at * tg;
   const int n_tok = (int)(seq.n - tok0 < tg ? seq.n - tok0 : tg);
   // slots that the unit's last token sees: the blocks of the others are among its
@@ -253,7 +263,8 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_block_scores_kernel(PagedSel
     head = head < a.n_qh ? head : 0;
     return live;
   };
-  auto row_of = [&](int tok, int head) { return (seq.first + tok0 + tok) * a.n_q_heads + kv * a.n_qh + head; };
+  const int64_t row0 = seq.first - a.from + tok0;  // of the unit's first token among the launch's
+  auto row_of = [&](int tok, int head) { return (row0 + tok) * a.n_q_heads + kv * a.n_qh + head; };
   if (begin >= end) {
     if constexpr (MODE == HEADS || MODE == TOPS) {  // nothing here: no best
       for (int c = tid; c < COLS; c += NT) {
@@ -419,7 +430,7 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_block_scores_kernel(PagedSel
     const bool live = column(nb, tok, head);
     out[nb] = nullptr;
     if (MODE == HEADS && live) out[nb] = a.scores + row_of(tok, head) * a.most_blocks;
-    if ((MODE == VALUES || MODE == BOTH) && live && head == 0) out[nb] = a.scores + ((seq.first + tok0 + tok) * a.c.n_kv + kv) * a.most_blocks;
+    if ((MODE == VALUES || MODE == BOTH) && live && head == 0) out[nb] = a.scores + ((row0 + tok) * a.c.n_kv + kv) * a.most_blocks;
     const int64_t l = past + tok;
     lim[nb] = l > 0 ? (int)((l + TILE - 1) / TILE) : 0;
     un[nb] = un_s[16 * nb + col];
@@ -602,14 +613,14 @@ __device__ __forceinline__ void find_step(const int32_t* count, int left, int32_
 // The heads' best over their chunks, also of one head: what is picked from counts down from 0 (raw scores, mostly positive,
 // would all fall into one step: one token and one head to a KV head over 65k slots 306 us, so 16). Values: theirs is off already.
 template <int NT>
-__device__ __forceinline__ void best_of_heads(const PagedSelectArgs& a, int64_t t, int kv, int n_rows, float* top) {
+__device__ __forceinline__ void best_of_heads(const PagedSelectArgs& a, int64_t at, int kv, int n_rows, float* top) {
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   if (a.by_values) {
     if (threadIdx.x == 0) top[0] = 0.0f;
     return;
   }
   for (int h = wave; h < n_rows; h += NT / 64) {
-    const float* tops = a.tops + (t * a.n_q_heads + kv * a.n_qh + h) * a.n_chunks;
+    const float* tops = a.tops + (at * a.n_q_heads + kv * a.n_qh + h) * a.n_chunks;
     float x = -__builtin_inff();
     for (int i = lane; i < a.n_chunks; i += 64) x = __builtin_fmaxf(x, tops[i]);
     x = wave_max(x);
@@ -623,8 +634,8 @@ __global__ __launch_bounds__(NT, NT == 128 ? 4 : 1) void paged_pick_kernel(Paged
   __shared__ PickScratch<NT> s;
   const int tid = threadIdx.x, lane = tid & 63, wave = tid >> 6;
   const int kv = (int)(blockIdx.x % (unsigned)a.c.n_kv);
-  const int64_t t = blockIdx.x / (unsigned)a.c.n_kv;
-  const float* rows = a.scores + (t * a.c.n_kv + kv) * (int64_t)n_rows * a.most_blocks;
+  const int64_t at = blockIdx.x / (unsigned)a.c.n_kv, t = a.from + at;  // the token's place among the launch's, and the call's
+  const float* rows = a.scores + (at * a.c.n_kv + kv) * (int64_t)n_rows * a.most_blocks;
   constexpr int HB = NT == 128 ? 1 : 16 / IT;  // rows at a time: 16 loads under way (values: one row)
   f32x4 x[HB][IT];
   auto load = [&](int h0) __attribute__((always_inline)) {  // (what lies behind the last block is not used)
@@ -646,7 +657,7 @@ __global__ __launch_bounds__(NT, NT == 128 ? 4 : 1) void paged_pick_kernel(Paged
   }
   for (int i = tid; i < STEPS; i += NT) s.count[i] = 0;
   if (tid == 0) s.n = 0;
-  best_of_heads<NT>(a, t, kv, n_rows, s.top);
+  best_of_heads<NT>(a, at, kv, n_rows, s.top);
   __syncthreads();
   const int b = __builtin_amdgcn_readfirstlane(s.b);
   if (b < 0) return;
@@ -814,14 +825,14 @@ __global__ __launch_bounds__(PICK) void paged_pick_long_kernel(PagedSelectArgs a
   __shared__ int32_t hist_s[256], part_s[PICK / 64], part2_s[PICK / 64], found_s[2];
   const int tid = threadIdx.x;
   const int kv = (int)(blockIdx.x % (unsigned)a.c.n_kv);
-  const int64_t t = blockIdx.x / (unsigned)a.c.n_kv;
+  const int64_t at = blockIdx.x / (unsigned)a.c.n_kv, t = a.from + at;
   if (tid == 0) b_s = -1;
   __syncthreads();
   for (int b = tid; b < a.c.batch; b += PICK) {
     const PagedSeq q = paged_seq(a.c, b);
     if (t >= q.first && t < q.first + q.n) atomicMax(&b_s, b);
   }
-  best_of_heads<PICK>(a, t, kv, n_rows, top_s);
+  best_of_heads<PICK>(a, at, kv, n_rows, top_s);
   __syncthreads();
   if (b_s < 0) return;
   const PagedSeq seq = paged_seq(a.c, b_s);
@@ -833,7 +844,7 @@ __global__ __launch_bounds__(PICK) void paged_pick_long_kernel(PagedSelectArgs a
     for (int i = tid; i < want; i += PICK) out[i] = i < have ? i : -1;
     return;
   }
-  float* rows = a.scores + (t * a.c.n_kv + kv) * (int64_t)n_rows * a.most_blocks;
+  float* rows = a.scores + (at * a.c.n_kv + kv) * (int64_t)n_rows * a.most_blocks;
   uint32_t* keys = reinterpret_cast<uint32_t*>(rows);
   for (int i = tid; i < have; i += PICK) {
     float v = -__builtin_inff();
@@ -893,69 +904,48 @@ hipError_t launch_paged_bounds(const PagedBoundsArgs& args, hipStream_t st) {
   return hipGetLastError();
 }
 
-namespace {
-
-// Tokens times KV heads up to which every head's scores are kept (one sweep over the boxes, more bytes for the pick): 8 KV
-// heads of four over 100k slots, 64 tokens 33 us and 44 by values, 128 tokens 49 and 53, 192 tokens 61 both, 512 tokens 120
-// and 82; 48 sequences' single tokens over 16k slots 22 and 44.
-constexpr int64_t kFewPairs = 1024;
-constexpr int64_t kMostChunks = 128;
-
-int64_t score_pitch(int64_t max_tokens) { return (max_tokens + 16 * PAIR * TILE - 1) / (16 * PAIR * TILE) * (16 * PAIR); }
-
-}  // namespace
-
-// Scores of all query heads of few tokens, or values of all KV heads, and the heads' best of every chunk.
 size_t paged_select_bytes(int64_t n_new, int32_t n_q_heads, int32_t n_kv, int64_t max_tokens) {
-  const int64_t few = kFewPairs / n_kv < n_new ? kFewPairs / n_kv : n_new;
-  const int64_t rows = few * n_q_heads > n_new * n_kv ? few * n_q_heads : n_new * n_kv;
-  return (size_t)(rows * score_pitch(max_tokens) + n_new * n_q_heads * kMostChunks) * sizeof(float);
+  return (size_t)select_plan(n_new, n_q_heads, n_kv, max_tokens).floats * sizeof(float);
 }
 
 hipError_t launch_paged_select(const PagedSelectArgs& args, void* workspace, hipStream_t st) {
   PagedSelectArgs a = args;
-  const int64_t n_kv = a.c.n_kv, pairs = a.c.n_new * n_kv;
-  const bool many = pairs > kFewPairs;
-  a.most_blocks = (int32_t)score_pitch(a.max_tokens);
+  const int64_t n_kv = a.c.n_kv;
+  const SelectPlan plan = select_plan(a.c.n_new, a.n_q_heads, a.c.n_kv, a.max_tokens);
+  a.by_values = plan.many;
+  a.most_blocks = (int32_t)plan.pitch;
   a.tops = static_cast<float*>(workspace);
-  a.scores = a.tops + a.c.n_new * a.n_q_heads * kMostChunks;
+  a.scores = a.tops + plan.scores_at;
   a.pitch_log2 = 0;
   while (1 << a.pitch_log2 < a.n_qh) ++a.pitch_log2;
-  const int nb = many ? 4 : 1, tg = 16 * nb >> a.pitch_log2;
-  const int64_t units = a.c.n_new / tg + a.c.batch, all = a.most_blocks / (16 * PAIR);
-  // Units for at least half of the CUs: both sweeps in one workgroup of eight wavefronts, one to a CU. Otherwise
-  // two workgroups of four on a CU (8 KV heads over 100k slots: 192 tokens 61 us and 69 by both sweeps in one, 256 tokens
-  // 69 and 69, 512 tokens 96 and 82).
-  const bool both = many && 2 * units * n_kv > N_CU;
-  const int waves = both ? 8 : 4;
-  int64_t n = both ? 1 : (2 * N_CU - 1 + units * n_kv) / (units * n_kv);
-  if (n > kMostChunks) n = kMostChunks;
-  int64_t steps = (all + n - 1) / n;
-  steps = (steps + waves - 1) / waves * waves;
-  a.n_chunks = (int32_t)((all + steps - 1) / steps);
-  const dim3 grid((unsigned)(units * n_kv), (unsigned)a.n_chunks);
-  if (both) {
-    hipLaunchKernelGGL((paged_block_scores_kernel<4, 8, BOTH>), grid, dim3(512), 0, st, a, (int)steps);
-  } else if (many) {
-    hipLaunchKernelGGL((paged_block_scores_kernel<4, 4, TOPS>), grid, dim3(256), 0, st, a, (int)steps);
-    hipLaunchKernelGGL((paged_block_scores_kernel<4, 4, VALUES>), grid, dim3(256), 0, st, a, (int)steps);
-  } else {
-    hipLaunchKernelGGL((paged_block_scores_kernel<1, 4, HEADS>), grid, dim3(256), 0, st, a, (int)steps);
+  for (a.from = 0; a.from < a.c.n_new; a.from = a.to) {
+    const int64_t left = a.c.n_new - a.from, tokens = left < plan.tokens ? left : plan.tokens;
+    a.to = a.from + (int32_t)tokens;
+    const SelectSlab slab = select_slab(plan, tokens, a.c.batch, a.c.n_kv, a.pitch_log2);
+    a.n_chunks = (int32_t)slab.chunks;
+    const dim3 grid((unsigned)(slab.units * n_kv), (unsigned)slab.chunks);
+    if (slab.both) {
+      hipLaunchKernelGGL((paged_block_scores_kernel<4, 8, BOTH>), grid, dim3(512), 0, st, a, (int)slab.steps);
+    } else if (plan.many) {
+      hipLaunchKernelGGL((paged_block_scores_kernel<4, 4, TOPS>), grid, dim3(256), 0, st, a, (int)slab.steps);
+      hipLaunchKernelGGL((paged_block_scores_kernel<4, 4, VALUES>), grid, dim3(256), 0, st, a, (int)slab.steps);
+    } else {
+      hipLaunchKernelGGL((paged_block_scores_kernel<1, 4, HEADS>), grid, dim3(256), 0, st, a, (int)slab.steps);
+    }
+    const dim3 rows((unsigned)(tokens * n_kv));
+    const int n_rows = plan.many ? 1 : a.n_qh;
+    // (of 512 tokens and 1600 blocks in all 82 us, and 96 with 256 threads a pair)
+    if (plan.many && a.most_blocks <= 2048)
+      hipLaunchKernelGGL((paged_pick_kernel<128, 4>), rows, dim3(128), 0, st, a, n_rows);
+    else if (a.most_blocks <= 1024)
+      hipLaunchKernelGGL((paged_pick_kernel<256, 1>), rows, dim3(256), 0, st, a, n_rows);
+    else if (a.most_blocks <= 4096)
+      hipLaunchKernelGGL((paged_pick_kernel<256, 4>), rows, dim3(256), 0, st, a, n_rows);
+    else if (a.most_blocks <= 16384)
+      hipLaunchKernelGGL((paged_pick_kernel<1024, 4>), rows, dim3(1024), 0, st, a, n_rows);
+    else
+      hipLaunchKernelGGL(paged_pick_long_kernel, rows, dim3(PICK), 0, st, a, n_rows);
   }
-  const dim3 rows((unsigned)pairs);
-  a.by_values = many;
-  const int n_rows = many ? 1 : a.n_qh;
-  // (of 512 tokens and 1600 blocks in all 82 us, and 96 with 256 threads a pair)
-  if (many && a.most_blocks <= 2048)
-    hipLaunchKernelGGL((paged_pick_kernel<128, 4>), rows, dim3(128), 0, st, a, n_rows);
-  else if (a.most_blocks <= 1024)
-    hipLaunchKernelGGL((paged_pick_kernel<256, 1>), rows, dim3(256), 0, st, a, n_rows);
-  else if (a.most_blocks <= 4096)
-    hipLaunchKernelGGL((paged_pick_kernel<256, 4>), rows, dim3(256), 0, st, a, n_rows);
-  else if (a.most_blocks <= 16384)
-    hipLaunchKernelGGL((paged_pick_kernel<1024, 4>), rows, dim3(1024), 0, st, a, n_rows);
-  else
-    hipLaunchKernelGGL(paged_pick_long_kernel, rows, dim3(PICK), 0, st, a, n_rows);
   return hipGetLastError();
 }
 

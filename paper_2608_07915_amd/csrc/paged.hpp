@@ -116,12 +116,13 @@ struct PagedSelectArgs {
   int64_t max_tokens;
   int32_t n_blocks, first, last;
   int32_t* blocks;
-  float* scores;        // workspace: [n_new][n_q_heads][most_blocks], or the values [n_new][n_kv][most_blocks]
+  float* scores;        // workspace, theirs: [token][n_q_heads][most_blocks], or the values [token][n_kv][most_blocks]
   int32_t by_values;    // it holds values: the heads' best are taken off already
-  float* tops;          // workspace: [n_new][n_q_heads][n_chunks], the heads' best scores
+  float* tops;          // workspace, theirs: [token][n_q_heads][n_chunks], the heads' best scores
   int32_t most_blocks;  // that a sequence of max_tokens has
   int32_t n_chunks;     // of its blocks
   int32_t pitch_log2;   // columns of a token's heads
+  int32_t from, to;     // the new tokens of this launch
 };
 
 // Attention of a few rows a sequence (drafted trees) or a token (listed blocks) over tiles.

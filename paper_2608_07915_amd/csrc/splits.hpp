@@ -367,4 +367,59 @@ inline size_t tree_workspace_bytes(int32_t batch, int64_t n_new, int32_t n_qh, i
   return b;
 }
 
+// Selection of blocks. Tokens times KV heads up to which every head's scores are kept (one sweep over the boxes, more bytes
+// for the pick): 8 KV heads of four over 100k slots, 64 tokens 33 us and 44 by values, 128 tokens 49 and 53, 192 tokens 61
+// both, 512 tokens 120 and 82; 48 sequences' single tokens over 16k slots 22 and 44.
+constexpr int64_t SELECT_FEW_PAIRS = 1024;
+constexpr int64_t SELECT_MOST_CHUNKS = 128;
+constexpr int64_t SELECT_STEP = 32;  // blocks of a wavefront's step
+// Scores, or values, are kept for as many new tokens at a time as this many floats hold, one token at least (1 GiB. With a
+// quarter of it 16384 tokens of 8 KV heads over 131k slots took 2.29 ms for 2.25 at once, 128 tokens of 128 heads over 1M
+// slots 0.93 for 0.88).
+constexpr int64_t SELECT_SCORES = (int64_t)1 << 28;
+struct SelectPlan {
+  bool many;       // values of KV heads; otherwise every head's scores
+  int64_t pitch;   // floats of a row
+  int64_t tokens;  // new tokens at a time
+  int64_t scores_at, floats;  // workspace, in floats: the heads' best of every chunk of blocks, then the scores
+};
+inline SelectPlan select_plan(int64_t n_new, int32_t n_q_heads, int32_t n_kv, int64_t max_tokens) {
+  SelectPlan p{};
+  p.many = n_new * n_kv > SELECT_FEW_PAIRS;
+  p.pitch = ceil_div(max_tokens, 64 * SELECT_STEP) * SELECT_STEP;
+  // a unit has 64 columns at most, and units enough for the card one chunk (select_slab)
+  p.scores_at = (n_new * n_q_heads + 2 * N_CU * 64 + 63) / 64 * 64;
+  const int64_t few = SELECT_FEW_PAIRS / n_kv < n_new ? SELECT_FEW_PAIRS / n_kv : n_new;  // of the calls that keep all scores
+  const int64_t rows = few * n_q_heads > n_new * n_kv ? few * n_q_heads : n_new * n_kv;
+  const int64_t floats = rows * p.pitch, least = n_q_heads * p.pitch, most = least > SELECT_SCORES ? least : SELECT_SCORES;
+  const int64_t scores = floats < most ? floats : most;
+  p.floats = p.scores_at + scores;
+  p.tokens = scores / ((p.many ? n_kv : n_q_heads) * p.pitch);
+  if (p.tokens > n_new) p.tokens = n_new;
+  return p;
+}
+// Of `tokens` new tokens: units of `columns` columns (a token's heads take 2^pitch_log2 of them), their wavefronts, and how
+// the blocks are cut.
+struct SelectSlab {
+  int columns, waves;
+  bool both;
+  int64_t units, steps, chunks;
+};
+inline SelectSlab select_slab(const SelectPlan& p, int64_t tokens, int32_t batch, int32_t n_kv, int32_t pitch_log2) {
+  SelectSlab s{};
+  s.columns = p.many ? 64 : 16;
+  s.units = tokens / (s.columns >> pitch_log2) + batch;
+  // Units for at least half of the CUs: both sweeps in one workgroup of eight wavefronts, one to a CU. Otherwise
+  // two workgroups of four on a CU (8 KV heads over 100k slots: 192 tokens 61 us and 69 by both sweeps in one, 256 tokens
+  // 69 and 69, 512 tokens 96 and 82).
+  s.both = p.many && 2 * s.units * n_kv > N_CU;
+  s.waves = s.both ? 8 : 4;
+  int64_t n = s.both ? 1 : ceil_div(2 * N_CU, s.units * n_kv);
+  if (n > SELECT_MOST_CHUNKS) n = SELECT_MOST_CHUNKS;
+  const int64_t all = p.pitch / SELECT_STEP;
+  s.steps = ceil_div(ceil_div(all, n), s.waves) * s.waves;
+  s.chunks = ceil_div(all, s.steps);
+  return s;
+}
+
 }  // namespace spectra

@@ -43,3 +43,46 @@ def test_an_infinite_score_counts_as_no_number(n, tokens, n_qh):
     for t in (0, tokens - 1):
         have = -(-(n * 64 - tokens + t + 1) // 64)
         assert np.array_equal(got[t], np.sort(np.argsort(-(np.arange(have) % 50), kind="stable")[:12])), t
+
+
+def equal_values(n, seed=0):
+    """A map of one sequence of n blocks in a shuffled order, boxes whose bounds are small whole numbers."""
+    ck, _ = codec([[4, 0, 0, 0]], 10, 1)
+    ck.basis[0] = torch.eye(D)
+    m = S.PagedCache(n, 64, 2, n)
+    rng = np.random.default_rng(seed)
+    order = rng.permutation(n)
+    m.table[0] = ints(order)
+    m.table[1] = ints(order[::-1].copy())
+    vals = rng.integers(0, 9, n)
+    box = torch.zeros((n, 1, 1, 4, 2, 32), dtype=torch.float16, device="cuda")
+    box[ints(order).long(), 0, 0, 0, 1, 0] = torch.tensor(vals, dtype=torch.float16, device="cuda")
+    return ck, m, box.view(torch.int32).view(n, -1), vals
+
+
+@pytest.mark.parametrize("n,tokens,n_qh", [(17000, 1020, 16), (17000, 17000, 1), (20000, 14000, 3), (4200, 66000, 2)])
+def test_selections_whose_scores_do_not_fit_at_once(n, tokens, n_qh):
+    """Calls that keep the scores of some of their tokens at a time: two sequences, whose new tokens meet inside one of
+    those parts, the second with a length of its own; exact values. And the workspace of exactly the size asked for."""
+    ck, m, pool, vals = equal_values(n, tokens)
+    cut, ends = tokens // 3, [n * 64, n * 32 + 17]
+    q = torch.zeros((tokens + 3, n_qh, D), device="cuda")
+    q[:, :, 0] = 1.0 + torch.arange(tokens + 3, device="cuda")[:, None] % 3
+    need = S.spectra_paged_select_workspace_bytes(tokens + 3, n_qh, 1, n * 64)
+    row = -(-n // 32) * 32
+    assert 4 * tokens * row * (n_qh if tokens <= 1024 else 1) > need  # otherwise nothing is split
+    ws = torch.full((need + 4096,), 255, dtype=torch.uint8, device="cuda")
+    out = torch.full((tokens + 3, 1, 9), 77, dtype=torch.int32, device="cuda")
+    S.spectra_paged_select(m, ck, pool, q, ints([0, cut, tokens]), 9, n * 64, first=1, last=2, ends=ints(ends), out=out, workspace=ws[:need])
+    assert (ws[need:] == 255).all() and (out[tokens:] == 77).all()
+    got = out.cpu().numpy()[:, 0]
+    for b, (lo, hi) in enumerate(((0, cut), (cut, tokens))):
+        seq = vals if b == 0 else vals[::-1]
+        for t in np.unique(np.concatenate([np.linspace(lo, hi - 1, 150).astype(int), np.arange(lo, min(hi, lo + 70)), np.arange(max(lo, hi - 70), hi)])):
+            have = -(-(ends[b] - (hi - lo) + (t - lo) + 1) // 64)
+            rest = 1 + np.argsort(-seq[1:have - 2], kind="stable")[:6]
+            assert got[t].tolist() == sorted([0, have - 2, have - 1, *rest.tolist()]), (b, t)
+    # a sequence past the call's bound is left as it was, whatever part its tokens fall into
+    out.fill_(77)
+    S.spectra_paged_select(m, ck, pool, q, ints([0, cut, tokens]), 9, n * 64 - 1, first=1, last=2, ends=ints(ends), out=out)
+    assert (out[:cut] == 77).all() and np.array_equal(out.cpu().numpy()[cut:tokens, 0], got[cut:tokens])
