@@ -406,7 +406,9 @@ spectra_status spectra_paged_encode(const spectra_pages* m, const spectra_codec*
  * out_dt fp32: factors are pairs of fp16 parts, sums fp32. With x the largest sum_j |q'_j c_j| of a
  * row and a slot (q' = scale q V_K, c a record's coefficients), a score, lse and, relative, a softmax
  * weight are off by about 2^-18 x at most; where a sequence has at most 16 new rows on a KV head (new
- * tokens times query heads) the weights are pairs of bf16 parts besides (2^-16).
+ * tokens times query heads) the weights are pairs of bf16 parts besides (2^-16). q'_j itself is off by
+ * about 2^-22 of scale sum_i |q_i V_ij| (2^-18 at most; 2^-16 with bf16 outputs), which counts where q
+ * lies mostly in directions that are not kept.
  * bf16: q', c and the weights are rounded to fp16, so a score, lse and, relative, a weight are off by
  * at most about 2^-10 x, typically 2^-12 of the root of sum_j (q'_j c_j)^2. Scores of a spread of 3
  * nats (standard deviation over the slots) leave outputs off by a third of their own rounding, of 10 by
@@ -497,7 +499,8 @@ spectra_status spectra_paged_bounds(const spectra_pages* m, const spectra_codec*
  * before slot L - n + i). blocks[(t*n_kv + kv)*n_blocks ...]: the first `first` and the last `last` blocks
  * that it sees and those of the largest value, n_blocks in all (all that it sees where they are no
  * more), ascending, -1 behind them. Equal values: the lowest index first. Values are computed to about
- * 2^-20 of sum_j |q'_j box_j|; NaN counts as the least. Rows of no sequence and of those with more than
+ * 2^-20 of sum_j |q'_j box_j|, from q'_j that are off by about 2^-22 of sum_i |q_i V_ij| (2^-18 at most: where q lies
+ * mostly in directions that are not kept, the larger share). NaN, also inf - inf, counts as the least. Rows of no sequence and of those with more than
  * max_tokens slots are left as they were. first, last >= 0, first + last <= n_blocks <= 4096; at most
  * 2^21 query rows and 2^18 sequences times KV heads, here and in the attentions of this part.
  * A page out of range counts as boxes of zeros. Workspace: device, 256-byte aligned,

@@ -4,6 +4,8 @@ import pytest
 
 import paper_2608_07915_amd as S
 from paged_ref import D, codec
+from paged_sparse_ref import B8, block_values, box_of, cache
+from test_gpu_paged_sparse import select, whole
 
 pytestmark = pytest.mark.gpu
 
@@ -86,3 +88,36 @@ def test_selections_whose_scores_do_not_fit_at_once(n, tokens, n_qh):
     out.fill_(77)
     S.spectra_paged_select(m, ck, pool, q, ints([0, cut, tokens]), 9, n * 64 - 1, first=1, last=2, ends=ints(ends), out=out)
     assert (out[:cut] == 77).all() and np.array_equal(out.cpu().numpy()[cut:tokens, 0], got[cut:tokens])
+
+
+@pytest.mark.parametrize("f32", [False, True], ids=["bf16", "f32"])
+@pytest.mark.parametrize("tokens", [5, 600])
+def test_queries_that_mostly_lie_in_dropped_directions(tokens, f32):
+    """q' of the kept directions is then a small difference of large terms and off by its rotation: three parts of 8 bits and
+    at most 24 products of 32 terms, one after the other, summed to 2^-23 each, so 2^-18 of sum_i |q_i V_ij|. No block
+    is left out whose value passes a chosen one's by more than what that and the products (2^-20 of sum |q' box|) leave of
+    two values and the bests they count from."""
+    c = cache([5000], [tokens], 4, f32=f32, seed=21)
+    box = whole(c)
+    raw, table = box.cpu().numpy(), c.cache.table.cpu().numpy()
+    rng = np.random.default_rng(tokens)
+    q = np.zeros((tokens, 8, D))
+    for h in range(2):
+        v = c.state(h)[0]
+        amount = np.where(np.arange(D) < 64, rng.standard_normal((tokens, 4, D)), 3e6 * rng.standard_normal((tokens, 4, D)))
+        q[:, 4 * h:4 * h + 4] = amount @ v.T
+    c.q = torch.from_numpy(q.astype(np.float32)).cuda()
+    c.q = c.q if f32 else c.q.bfloat16()
+    q = c.q.float().cpu().numpy().astype(np.float64)
+    got = select(c, box, 9).cpu().numpy()
+    for h in range(2):
+        v = c.state(h)[0]
+        boxed = np.stack([box_of(raw, table[0], i, 64, h, 2, B8[h])[0] for i in range(79)]) * np.repeat(np.asarray(B8[h]) > 0, 32)
+        for i in range(0, tokens, 1 + tokens // 20):
+            have = -(-(5000 - tokens + i + 1) // 64)
+            rows, mine = q[i, 4 * h:4 * h + 4], got[i, h]
+            vals, size = block_values(rows, boxed, v, np.arange(79) < have)
+            turn = (np.abs(rows) @ np.abs(v) @ np.abs(boxed[:have]).max(1).T).max()
+            taken, left = mine[1:-1], np.setdiff1d(np.arange(have), mine)
+            assert (np.diff(mine) > 0).all() and mine[0] == 0 and mine[-1] == have - 1
+            assert vals[taken].min() >= vals[left].max() - 4 * (2.0 ** -20 * size + 2.0 ** -18 * turn), (h, i)
