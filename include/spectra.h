@@ -461,7 +461,7 @@ spectra_status spectra_paged_tree_attention(const spectra_pages* m, const spectr
  * of slot L - drafted[i] + path[i * path_stride + j] move to slot L - drafted[i] + j, j < counts[i], L =
  * lens[rows[i]]; the slots behind leave the row, and its pages behind them are free once no row holds
  * them (the row's new length, ends[i]). The pools are pools of records of n_kv_heads KV heads, any
- * number of words (page_words a multiple of page_tokens * n_kv_heads); boxes (spectra_paged_bounds)
+ * number of words (page_words a multiple of page_tokens * n_kv_heads), none listed twice; boxes (spectra_paged_bounds)
  * are not: those of the kept slots' blocks are made again. ends[i] = -1 and nothing changed:
  * a row out of range or listed before, drafted[i] not in [0, min(L, 64)], counts[i] not in [0,
  * drafted[i]] or greater than path_stride, a path that does not ascend or leaves [0, drafted[i]), a

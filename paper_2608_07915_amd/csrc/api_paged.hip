@@ -346,6 +346,10 @@ spectra_status spectra_pages_accept(const spectra_pages* m, const int32_t* rows,
       return fail(SPECTRA_EINVAL, "%s: pool %d: page_words=%lld are not the records of %d slots and %d KV heads", name, i,
                   (long long)pools[i].page_words, m->page_tokens, n_kv_heads);
   if (n == 0) return SPECTRA_OK;
+  for (int i = 1; i < n_pools; ++i)  // moved twice at once, its records would be lost
+    for (int j = 0; j < i; ++j)
+      if (pools[i].page_words > 0 && pools[i].base == pools[j].base && pools[j].page_words > 0)
+        return fail(SPECTRA_EINVAL, "%s: pool %d is listed before, as pool %d", name, i, j);
   const PathList p{rows, drafted, path, counts, path_stride};
   hipError_t e = each_pools(pools, n_pools, [&](const PoolList& l) {
     return launch_pages_accept_move(map_of(m), p, n, l, n_kv_heads, (hipStream_t)stream);
