@@ -62,12 +62,14 @@ def equal_values(n, seed=0):
     return ck, m, box.view(torch.int32).view(n, -1), vals
 
 
-@pytest.mark.parametrize("n,tokens,n_qh", [(17000, 1020, 16), (17000, 17000, 1), (20000, 14000, 3), (4200, 66000, 2)])
+@pytest.mark.parametrize("n,tokens,n_qh", [(17000, 1020, 16), (17000, 17000, 1), (20000, 14000, 3), (4000, 70000, 2), (40000, 7000, 1),
+                                          (2000, 140000, 1), (10000, 30000, 1)])
 def test_selections_whose_scores_do_not_fit_at_once(n, tokens, n_qh):
     """Calls that keep the scores of some of their tokens at a time: two sequences, whose new tokens meet inside one of
     those parts, the second with a length of its own; exact values. And the workspace of exactly the size asked for."""
     ck, m, pool, vals = equal_values(n, tokens)
-    cut, ends = tokens // 3, [n * 64, n * 32 + 17]
+    cut = tokens // 3
+    ends = [n * 64, max(n * 32 + 17, tokens - cut + 1000)]
     q = torch.zeros((tokens + 3, n_qh, D), device="cuda")
     q[:, :, 0] = 1.0 + torch.arange(tokens + 3, device="cuda")[:, None] % 3
     need = S.spectra_paged_select_workspace_bytes(tokens + 3, n_qh, 1, n * 64)
