@@ -12,11 +12,12 @@
 // the unit, and multiplies them on 16 x 16 x 32 products whose columns are the rows. No barrier until
 // the wavefronts' sums are merged. The chunks' partial sums meet in the combine kernels.
 //
-// Measured (8-word records): 48 tokens of 28 heads over 64 blocks 37 us (12300 tiles of 4 KB, 1.4 TB/s), with the join
-// 39; 16 trees of up to 32 tokens of 32 heads over 8k slots 76 + 14 us; in fp32, 200 tokens over 32 blocks 87 + 12. Bound
-// by instructions and their latencies: a tile costs a wavefront about 10000 clocks of the 2000 that its instructions
-// need alone, with three on a SIMD (VALU 40 to 60% busy, matrix units 7 to 9, more than half of the wavefronts' time
-// waiting). Making the coefficients is half of a tile. With all records in the first cache 35 us for 37; with a
+// Measured (8-word records): 48 tokens of 28 heads over 64 blocks 36 us (12300 tiles of 4 KB, 1.4 TB/s), with the join
+// 39; 16 trees of up to 32 tokens of 32 heads over 8k slots 76 + 14 us; in fp32, 200 tokens over 32 blocks 85 + 12 (traced: a
+// launch then counts from the end of the one before it). No unit is near its limit: a tile costs a wavefront
+// about 10000 clocks of the 2000 that its instructions need alone, with three on a SIMD; while a CU holds work its vector unit is
+// busy 47 to 62% of the time, its matrix cores 6 to 13, and a wavefront waits for memory, LDS or a barrier 36 to 50% of its
+// time. Making the coefficients is half of a tile. With all records in the first cache 35 us for 37; with a
 // second tile in LDS, filled while the first is multiplied, 38.
 // With 16-bit outputs q', c and p are single fp16 numbers; with fp32 outputs (PRECISE) pairs of fp16 parts,
 // every product three.

@@ -36,8 +36,9 @@ __device__ __forceinline__ int sequence_of(int batch, int64_t t, Starts&& starts
 // are reduced by halving: at each of four exchanges a lane keeps half of its coefficients, the last
 // two within quads (per group 34 exchanges instead of 192). Words of HBM once, 128 bytes written
 // a group. The starts of up to BOX_STARTS sequences are searched in LDS.
-// Measured: 131072 prompt slots of 8 KV heads 25 us (38 MB, 1.5 TB/s), bound by making the coefficients and the
-// exchanges; the newest blocks of 64 sequences 10 us, by latency.
+// Measured: 131072 prompt slots of 8 KV heads 23 to 25 us (38 MB, 1.5 TB/s), by the vector unit, which making the
+// coefficients and the exchanges keep busy 85% of the time that a CU holds work; the newest blocks of 64 sequences 10 us,
+// a launch and one chain of loads.
 // ---------------------------------------------------------------------------
 // (as instructions: the compiler first makes every operand quiet, which doubles them; nothing here is NaN)
 __device__ __forceinline__ f16x2 pk_min(f16x2 a, f16x2 b) {
@@ -184,8 +185,9 @@ __global__ __launch_bounds__(256) void paged_bounds_kernel(PagedBoundsArgs a) {
 // the blocks' values, a KV head's instead of all its heads'; with units enough for the card, BOTH in turn.
 //
 // Measured, 8 KV heads of four: one token over 1M slots 17 us (34 MB of boxes, 2 TB/s; the prologue's chain and the
-// memory's latency, DEEP units under way); 512 tokens over 100k slots 67 us (27 GFLOP in both sweeps, two parts each,
-// 0.4 PFLOP/s). The latter is held by operands: without the boxes' loads 23 us less, with one of two parts 25 less; four
+// memory's latency, DEEP units under way: wavefronts wait 64% of their time, the vector unit is busy 17%); 512 tokens over
+// 100k slots 67 us (27 GFLOP in both sweeps, two parts each, 0.4 PFLOP/s; matrix cores 27% busy, vector unit 35, half of the
+// wavefronts' time waiting). The latter waits for operands: without the boxes' loads 23 us less, with one of two parts 25 less; four
 // block tiles a step, which halve the reads of q', came to 76 (fewer steps to share, spills), one sum for both
 // parts to 67.
 // ---------------------------------------------------------------------------
@@ -548,8 +550,9 @@ __global__ __launch_bounds__(64 * NW, 2) void paged_block_scores_kernel(PagedSel
 // step that holds the n-th are ranked against each other, (value, then lowest index); should they be
 // many, rounds of counts of 8 bits over value and index find the n-th instead. What stands at or before
 // it is written in ascending order.
-// Bound by latency: a dozen barriers and one pass over the scores, whose first loads are on their way while the token's
-// sequence is looked for: 14 us for 8 KV heads of four and 16384 blocks, 20 us for 4096 pairs of 1563 values.
+// A dozen barriers and one pass over the scores, whose first loads are on their way while the token's sequence is looked
+// for: 13 us for 8 KV heads of four and 16384 blocks, by latency on the eight CUs that have work; 20 us for 4096 pairs of 1563
+// values, the vector unit 65% busy.
 // ---------------------------------------------------------------------------
 __device__ __forceinline__ uint32_t order_of(float v) {
   const uint32_t u = __float_as_uint(v);
