@@ -461,8 +461,8 @@ spectra_status spectra_paged_tree_attention(const spectra_pages* m, const spectr
  * of slot L - drafted[i] + path[i * path_stride + j] move to slot L - drafted[i] + j, j < counts[i], L =
  * lens[rows[i]]; the slots behind leave the row, and its pages behind them are free once no row holds
  * them (the row's new length, ends[i]). The pools are pools of records of n_kv_heads KV heads, any
- * number of words (page_words a multiple of page_tokens * n_kv_heads), none listed twice; boxes (spectra_paged_bounds)
- * are not: those of the kept slots' blocks are made again. ends[i] = -1 and nothing changed:
+ * number of words (page_words a multiple of page_tokens * n_kv_heads), none listed twice; boxes
+ * (spectra_paged_bounds) are not: those of the kept slots' blocks are made again. ends[i] = -1 and nothing changed:
  * a row out of range or listed before, drafted[i] not in [0, min(L, 64)], counts[i] not in [0,
  * drafted[i]] or greater than path_stride, a path that does not ascend or leaves [0, drafted[i]), a
  * drafted slot whose page is out of range or has other owners (spectra_pages_extend leaves none).
@@ -499,9 +499,9 @@ spectra_status spectra_paged_bounds(const spectra_pages* m, const spectra_codec*
  * before slot L - n + i). blocks[(t*n_kv + kv)*n_blocks ...]: the first `first` and the last `last` blocks
  * that it sees and those of the largest value, n_blocks in all (all that it sees where they are no
  * more), ascending, -1 behind them. Equal values: the lowest index first. Values are computed to about
- * 2^-20 of sum_j |q'_j box_j|, from q'_j that are off by about 2^-22 of sum_i |q_i V_ij| (2^-18 at most: where q lies
- * mostly in directions that are not kept, the larger share). NaN, also inf - inf, counts as the least. Rows of no sequence and of those with more than
- * max_tokens slots are left as they were. first, last >= 0, first + last <= n_blocks <= 4096; at most
+ * 2^-20 of sum_j |q'_j box_j|, from q'_j that are off by about 2^-22 of sum_i |q_i V_ij| (2^-18 at most:
+ * the larger share where q lies mostly in directions that are not kept). NaN, also inf - inf, counts as
+ * the least. Rows of no sequence and of those with more than max_tokens slots are left as they were. first, last >= 0, first + last <= n_blocks <= 4096; at most
  * 2^21 query rows and 2^18 sequences times KV heads, here and in the attentions of this part.
  * A page out of range counts as boxes of zeros. Workspace: device, 256-byte aligned,
  * spectra_paged_select_workspace_bytes, never fewer for larger counts of as many heads: a float for each
