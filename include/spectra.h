@@ -501,8 +501,9 @@ spectra_status spectra_paged_bounds(const spectra_pages* m, const spectra_codec*
  * more), ascending, -1 behind them. Equal values: the lowest index first. Values are computed to about
  * 2^-20 of sum_j |q'_j box_j|, from q'_j that are off by about 2^-22 of sum_i |q_i V_ij| (2^-18 at most:
  * the larger share where q lies mostly in directions that are not kept). NaN, also inf - inf, counts as
- * the least. Rows of no sequence and of those with more than max_tokens slots are left as they were. first, last >= 0, first + last <= n_blocks <= 4096; at most
- * 2^21 query rows and 2^18 sequences times KV heads, here and in the attentions of this part.
+ * the least. Rows of no sequence and of those with more than max_tokens slots are left as they were.
+ * first, last >= 0, first + last <= n_blocks <= 4096; at most 2^21 query rows and 2^18 sequences times KV
+ * heads, here and in the attentions of this part.
  * A page out of range counts as boxes of zeros. Workspace: device, 256-byte aligned,
  * spectra_paged_select_workspace_bytes, never fewer for larger counts of as many heads: a float for each
  * block of max_tokens and each KV head (query head, where n_new * KV heads <= 1024) of as many new tokens
